@@ -110,6 +110,25 @@ typedef struct {
     int32_t len;
 } fvar_kv;
 
+/* Key/value cache of one block held in 4 bits, 17/64 of the room of bf16.  A block of 32 consecutive head-dim elements of
+ * one row and head shares a power of two 2^e, stored as the byte e + 127; an element is one of 0, .5, 1, 1.5, 2, 3, 4, 6
+ * with a sign (codes 0..7, 8 for the sign), element 2i in the low half of byte i.
+ *   k, v             [B][kv_heads][capacity][Dh/2] bytes
+ *   k_scale, v_scale [B][kv_heads][capacity][Dh/32] bytes
+ * All four are device memory, 16-byte aligned.  kv_heads divides the context's heads: query head h reads
+ * kv head h / (heads / kv_heads).  lens: device int32 [B], the rows that each sample holds, or NULL and every sample
+ * holds `len`.  mask: device bytes [B][capacity], 0 hides that row from the attention, or NULL and none is hidden.
+ * The calls do not change len, lens or mask (the caller advances them).  B * kv_heads <= 65535, capacity <= 2^24. */
+typedef struct {
+    void *k, *v;
+    void *k_scale, *v_scale;
+    const int32_t *lens;
+    const uint8_t *mask;
+    int32_t kv_heads;
+    int32_t capacity;
+    int32_t len;
+} fvar_kvq;
+
 typedef struct fvar_ctx fvar_ctx;
 typedef void *fvar_stream;
 
@@ -261,12 +280,56 @@ fvar_status fvar_upsample_tokens(fvar_ctx *ctx, fvar_stream stream, const void *
                                  int32_t hs, int32_t ws, int32_t c, int32_t hd, int32_t wd,
                                  void *dst);
 
+/* The 4-bit cache (fvar_kvq).  Values are quantised as rows are written and never again:
+ *   e = the smallest integer for which max |x| of the block is < 7 * 2^e, within [-124, 125];
+ *   each element becomes the nearest value of the format, ties to the even code, at most 6 * 2^e.
+ * No element is then further off than half a step of its binade (or 2^e / 4 near 0).  A block with an infinity or a NaN
+ * reads back as NaN.
+ *
+ * fvar_kvq_append writes `rows` new rows behind those that each sample holds: row j of sample b is quantised to
+ * position len + j (lens[b] + j).  k, v: element type of the context; row j of sample b starts at element (b*rows + j)*ld
+ * and holds [kv_heads][Dh]; ld = 0 stands for kv_heads*Dh (so the K and V parts of a fused projection's output are
+ * passed with its row length as ld).  ld a multiple of 8 for bf16 (of 4 for fp32).  Requires len + rows <= capacity;
+ * with lens, rows that would lie outside [0, capacity) are left out. */
+fvar_status fvar_kvq_append(fvar_ctx *ctx, fvar_stream stream, const fvar_kvq *kv, const void *k, const void *v,
+                            int32_t ld, int32_t B, int32_t rows);
+
+/* Reads rows back: k, v:[B][rows][kv_heads][Dh] of the context's element type (either may be NULL), in which every value of the
+ * cache is exact.  Row j is position first + j of its sample; first < 0 counts from the end of what each sample holds
+ * (first = -rows: the rows appended last, once len has been advanced).  Positions that a sample does not hold read as 0. */
+fvar_status fvar_kvq_read(fvar_ctx *ctx, fvar_stream stream, const fvar_kvq *kv, int32_t B, int32_t first, int32_t rows,
+                          void *k, void *v);
+
+/* Attention over the 4-bit cache, for one query per sample or many:
+ *   o[b,i,h,:] = sum_t p_t V[b,t,h',:],  p = softmax of scale * q[b,i,h,:] . K[b,t,h',:] over the visible t
+ * (t is held by the sample and its mask byte is not 0).  A sample without a visible row gives 0.  What rows that are not
+ * visible hold, NaN included, has no influence.  q: query i of sample b starts at element (b*n + i)*ld and holds
+ * [heads][Dh]; ld = 0 stands for hidden; a multiple of 8 for bf16 (of 4 for fp32).  o:[B][n][heads][Dh], must not overlap q.
+ * B*n*heads <= 2^25.  ws: at least fvar_kvq_attention_workspace_bytes(ctx,kv,B,n), which depends on kv_heads and capacity
+ * but not on the pointers, and may be 0. */
+size_t fvar_kvq_attention_workspace_bytes(const fvar_ctx *ctx, const fvar_kvq *kv, int32_t B, int32_t n);
+fvar_status fvar_kvq_attention(fvar_ctx *ctx, fvar_stream stream, const void *q, int32_t ld, const fvar_kvq *kv, int32_t B,
+                               int32_t n, void *o, void *ws, size_t ws_bytes);
+
+/* fvar_block_forward_dense / _pruned over a 4-bit cache: the new rows are quantised into it and the attention reads
+ * them from there, like all earlier ones.  kv->kv_heads must equal the context's heads; everything else as there, with
+ * ws: at least fvar_block_kvq_workspace_bytes(ctx,kv,B,rows), rows = M (dense) or k (pruned).  With lens, a sample whose
+ * rows do not fit its capacity attends over those that do. */
+size_t fvar_block_kvq_workspace_bytes(const fvar_ctx *ctx, const fvar_kvq *kv, int32_t B, int32_t rows);
+fvar_status fvar_block_forward_dense_kvq(fvar_ctx *ctx, fvar_stream stream, const fvar_block_weights *w, const void *x,
+                                         int32_t B, int32_t M, const fvar_kvq *kv, void *y, void *ws, size_t ws_bytes);
+fvar_status fvar_block_forward_pruned_kvq(fvar_ctx *ctx, fvar_stream stream, const fvar_block_weights *w, const void *x,
+                                          int32_t B, int32_t M, const int32_t *idx_keep, int32_t k, const fvar_kvq *kv,
+                                          void *y_keep, void *ws, size_t ws_bytes);
+
 /* Debug checks, off by default.  While on, fvar_block_forward_pruned, fvar_lowrank_fill and
  * fvar_cache_fill copy their index arrays to the host and verify the contract (in range,
  * strictly ascending per sample, idx_keep and idx_drop disjoint, hence a partition of [0,M));
  * a violation returns FVAR_ERR_INVALID_ARG with nothing launched.  The block calls also put a
  * 256-byte canary behind their workspace (fvar_block_workspace_bytes grows by that much while
- * the checks are on) and return FVAR_ERR_WORKSPACE if a kernel overwrote it.  Calls made with
+ * the checks are on) and return FVAR_ERR_WORKSPACE if a kernel overwrote it.  Calls with a 4-bit cache that
+ * has lens copy them to the host and return FVAR_ERR_INVALID_ARG where one is negative or where it, with the rows that
+ * the call appends, exceeds the capacity.  Calls made with
  * the checks on synchronise the stream and are not asynchronous. */
 fvar_status fvar_debug_checks(fvar_ctx *ctx, int32_t on);
 

@@ -24,6 +24,8 @@ EXPORTS = (
     "fvar_profile_enable",
     "fvar_profile_read", "fvar_debug_checks", "fvar_score_select_static",
     "fvar_fill_scored_workspace_bytes", "fvar_lowrank_fill_scored",
+    "fvar_kvq_append", "fvar_kvq_read", "fvar_kvq_attention_workspace_bytes", "fvar_kvq_attention",
+    "fvar_block_kvq_workspace_bytes", "fvar_block_forward_dense_kvq", "fvar_block_forward_pruned_kvq",
 )
 
 
@@ -48,6 +50,12 @@ class _Weights(C.Structure):
 
 class _KV(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("capacity", C.c_int32), ("len", C.c_int32)]
+
+
+class _KVQ(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("lens", C.c_void_p), ("mask", C.c_void_p), ("kv_heads", C.c_int32), ("capacity", C.c_int32),
+                ("len", C.c_int32)]
 
 
 class _ProfileEntry(C.Structure):
@@ -113,6 +121,21 @@ def load_library() -> C.CDLL:
     lib.fvar_score_select_static.restype = C.c_int
     lib.fvar_debug_checks.argtypes = [vp, i32]
     lib.fvar_debug_checks.restype = C.c_int
+    kvq = C.POINTER(_KVQ)
+    lib.fvar_kvq_append.argtypes = [vp, vp, kvq, vp, vp, i32, i32, i32]
+    lib.fvar_kvq_append.restype = C.c_int
+    lib.fvar_kvq_read.argtypes = [vp, vp, kvq, i32, i32, i32, vp, vp]
+    lib.fvar_kvq_read.restype = C.c_int
+    lib.fvar_kvq_attention_workspace_bytes.argtypes = [vp, kvq, i32, i32]
+    lib.fvar_kvq_attention_workspace_bytes.restype = sz
+    lib.fvar_kvq_attention.argtypes = [vp, vp, vp, i32, kvq, i32, i32, vp, vp, sz]
+    lib.fvar_kvq_attention.restype = C.c_int
+    lib.fvar_block_kvq_workspace_bytes.argtypes = [vp, kvq, i32, i32]
+    lib.fvar_block_kvq_workspace_bytes.restype = sz
+    lib.fvar_block_forward_dense_kvq.argtypes = [vp, vp, C.POINTER(_Weights), vp, i32, i32, kvq, vp, vp, sz]
+    lib.fvar_block_forward_dense_kvq.restype = C.c_int
+    lib.fvar_block_forward_pruned_kvq.argtypes = [vp, vp, C.POINTER(_Weights), vp, i32, i32, vp, i32, kvq, vp, vp, sz]
+    lib.fvar_block_forward_pruned_kvq.restype = C.c_int
     lib.fvar_profile_enable.argtypes = [vp, i32]
     lib.fvar_profile_enable.restype = C.c_int
     lib.fvar_profile_read.argtypes = [vp, C.POINTER(_ProfileEntry), i32]
@@ -292,6 +315,110 @@ def fvar_upsample_tokens(ctx: Context, src, B: int, hs: int, ws: int, c: int, hd
                          stream=None) -> None:
     ctx.check(ctx.lib.fvar_upsample_tokens(ctx.handle, _stream(stream), _ptr(src), B, hs, ws, c, hd,
                                            wd, _ptr(dst)))
+
+
+class KVQ:
+    """Key/value cache of one block in 4 bits: the tensors of fvar_kvq and the rows that it holds.
+
+    k, v: uint8 [B, kv_heads, capacity, head_dim / 2]; k_scale, v_scale: uint8 [B, kv_heads, capacity, head_dim / 32];
+    lens: int32 [B] on the GPU, or None where every sample holds `len` rows; mask: uint8 or bool [B, capacity], 0 hides a
+    row from the attention, or None.  `len` may be assigned to; the tensors are the caller's, who advances len or lens."""
+
+    def __init__(self, k, v, k_scale, v_scale, len: int = 0, lens=None, mask=None):
+        B, heads, capacity, codes = k.shape
+        want = {"k": (k, (B, heads, capacity, codes)), "v": (v, (B, heads, capacity, codes)),
+                "k_scale": (k_scale, (B, heads, capacity, codes // 16)),
+                "v_scale": (v_scale, (B, heads, capacity, codes // 16))}
+        if lens is not None:
+            want["lens"] = (lens, (B,))
+        if mask is not None:
+            want["mask"] = (mask, (B, capacity))
+        for name, (t, shape) in want.items():
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, {shape} is wanted")
+            kinds = ("torch.int32",) if name == "lens" else ("torch.uint8", "torch.bool") if name == "mask" else ("torch.uint8",)
+            if str(t.dtype) not in kinds:
+                raise ValueError(f"{name} is {t.dtype}, {' or '.join(kinds)} is wanted")
+        self.k, self.v, self.k_scale, self.v_scale, self.lens, self.mask = k, v, k_scale, v_scale, lens, mask
+        self.batch, self.head_dim = B, 2 * codes
+        self._c = _KVQ(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(lens), _ptr(mask), heads, capacity, len)
+
+    kv_heads = property(lambda self: self._c.kv_heads)
+    capacity = property(lambda self: self._c.capacity)
+
+    @property
+    def len(self) -> int:
+        return self._c.len
+
+    @len.setter
+    def len(self, value: int) -> None:
+        self._c.len = value
+
+    def _for(self, ctx: Context, B: int):
+        if self.head_dim != ctx.head_dim or B > self.batch:
+            raise ValueError(f"a cache of {self.batch} samples with head_dim {self.head_dim} does not serve {B} samples "
+                             f"with head_dim {ctx.head_dim}")
+        return C.byref(self._c)
+
+
+def _rows(t, B: int, rows: int, width: int):
+    """Pointer and row pitch of t:[B, rows, ...], whose rows of `width` elements are contiguous; they may lie apart, as
+    the parts of a fused projection's output do."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError("tensors handed to fvar must be GPU tensors")
+    if t.is_contiguous():
+        if t.numel() < B * rows * width:
+            raise ValueError(f"{B} x {rows} rows of {width} elements are wanted, got a tensor of shape {tuple(t.shape)}")
+        return t.data_ptr(), 0
+    if t.dim() < 3 or t.shape[0] != B or t.shape[1] != rows or t[0, 0].numel() != width or not t[0, 0].is_contiguous():
+        raise ValueError(f"[{B}, {rows}, ...] with contiguous rows of {width} elements is wanted, got shape "
+                         f"{tuple(t.shape)} with strides {t.stride()}")
+    ld = t.stride(1) if rows > 1 else t.stride(0)
+    if B > 1 and t.stride(0) != rows * ld:
+        raise ValueError("the rows of all samples have to be equally far apart")
+    return t.data_ptr(), ld
+
+
+def fvar_kvq_append(ctx: Context, kv: KVQ, k, v, B: int, rows: int, stream=None) -> None:
+    width = kv.kv_heads * ctx.head_dim
+    (kp, ldk), (vp, ldv) = _rows(k, B, rows, width), _rows(v, B, rows, width)
+    if (ldk or width) != (ldv or width):
+        raise ValueError("k and v have different distances between rows")
+    ctx.check(ctx.lib.fvar_kvq_append(ctx.handle, _stream(stream), kv._for(ctx, B), kp, vp, ldk, B, rows))
+
+
+def fvar_kvq_read(ctx: Context, kv: KVQ, B: int, first: int, rows: int, k=None, v=None, stream=None) -> None:
+    ctx.check(ctx.lib.fvar_kvq_read(ctx.handle, _stream(stream), kv._for(ctx, B), B, first, rows, _ptr(k), _ptr(v)))
+
+
+def fvar_kvq_attention_workspace_bytes(ctx: Context, kv: KVQ, B: int, n: int) -> int:
+    return ctx.lib.fvar_kvq_attention_workspace_bytes(ctx.handle, kv._for(ctx, B), B, n)
+
+
+def fvar_kvq_attention(ctx: Context, q, kv: KVQ, B: int, n: int, o, ws=None, stream=None) -> None:
+    qp, ld = _rows(q, B, n, ctx.hidden)
+    ctx.check(ctx.lib.fvar_kvq_attention(ctx.handle, _stream(stream), qp, ld, kv._for(ctx, B), B, n, _ptr(o), _ptr(ws),
+                                         _nbytes(ws)))
+
+
+def fvar_block_kvq_workspace_bytes(ctx: Context, kv: KVQ, B: int, rows: int) -> int:
+    return ctx.lib.fvar_block_kvq_workspace_bytes(ctx.handle, kv._for(ctx, B), B, rows)
+
+
+def fvar_block_forward_dense_kvq(ctx: Context, w: dict, x, B: int, M: int, kv: KVQ, y, ws, stream=None) -> None:
+    ws_ = _weights(w)
+    ctx.check(ctx.lib.fvar_block_forward_dense_kvq(ctx.handle, _stream(stream), C.byref(ws_), _ptr(x), B, M,
+                                                   kv._for(ctx, B), _ptr(y), _ptr(ws), _nbytes(ws)))
+
+
+def fvar_block_forward_pruned_kvq(ctx: Context, w: dict, x, B: int, M: int, idx_keep, k: int, kv: KVQ, y_keep, ws,
+                                  stream=None) -> None:
+    ws_ = _weights(w)
+    ctx.check(ctx.lib.fvar_block_forward_pruned_kvq(ctx.handle, _stream(stream), C.byref(ws_), _ptr(x), B, M,
+                                                    _ptr(idx_keep), k, kv._for(ctx, B), _ptr(y_keep), _ptr(ws),
+                                                    _nbytes(ws)))
 
 
 def fvar_profile_enable(ctx: Context, on: bool) -> None:

@@ -147,12 +147,14 @@ fvar_status validate_indices(fvar_ctx *c, hipStream_t st, const int32_t *idx_kee
 
 struct BlockWs {
     char *x_keep, *u, *q, *att, *h1, *hid;
+    char *k_new, *v_new;                      // new K / V rows on their way into a 4-bit cache
     float *part;                              // partial results of the attention and of each linear layer in turn
     fvar::GemmPlan qkv, o, fc1, fc2;          // how each linear layer runs at this row count
     size_t total;
 };
 
-BlockWs carve(const fvar_ctx *c, void *ws, int B, int rows)
+// q: null, or the 4-bit cache that the block runs over
+BlockWs carve(const fvar_ctx *c, void *ws, int B, int rows, const fvar_kvq *q = nullptr)
 {
     const size_t es = esize(c), R = (size_t)B * rows, d = c->cfg.hidden, F = c->cfg.ffn_hidden;
     BlockWs w;
@@ -168,18 +170,83 @@ BlockWs carve(const fvar_ctx *c, void *ws, int B, int rows)
     const fvar::BlockPlan plan = fvar::block_plan(dtype(c), B, rows, c->cfg.hidden, c->cfg.heads, c->cfg.head_dim,
                                                   c->cfg.ffn_hidden);
     w.qkv = plan.layer[0]; w.o = plan.layer[1]; w.fc1 = plan.layer[2]; w.fc2 = plan.layer[3];
-    const size_t part = plan.floats;
+    size_t part = plan.floats;
+    w.k_new = w.v_new = nullptr;
+    if (q) {
+        w.k_new = w.att;                      // both are read before their buffers are written
+        w.v_new = w.h1;
+        const size_t att = fvar::kvq_attention_scratch_floats(dtype(c), B, rows, c->cfg.heads, q->kv_heads, c->cfg.head_dim,
+                                                              q->capacity);
+        if (att > part) part = att;
+    }
     w.part = part ? reinterpret_cast<float *>(take(part * sizeof(float))) : nullptr;
     w.total = off;
     return w;
 }
 
-// The block on `rows` rows per sample.  idx == nullptr: rows are x's own rows (rows == M).
+// A 4-bit cache that a call with `rows` new rows per sample can work on (0: none are written).
+fvar_status check_kvq(fvar_ctx *c, hipStream_t st, const fvar_kvq *kv, int B, int rows, const char *who)
+{
+    if (!kv) return fail(c, FVAR_ERR_INVALID_ARG, "%s: null cache", who);
+    if (B < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need B>=1 (B=%d)", who, B);
+    if (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: a pointer of the cache is NULL", who);
+    if (!aligned16(kv->k) || !aligned16(kv->v) || !aligned16(kv->k_scale) || !aligned16(kv->v_scale) ||
+        (reinterpret_cast<uintptr_t>(kv->lens) & 3))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer of the cache not aligned (16 bytes; lens 4)", who);
+    if (kv->kv_heads < 1 || c->cfg.heads % kv->kv_heads)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: kv_heads=%d does not divide heads=%d", who, kv->kv_heads, c->cfg.heads);
+    if (kv->capacity < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: capacity=%d", who, kv->capacity);
+    if (kv->capacity > (1 << 24) || (int64_t)B * kv->kv_heads > 65535)
+        return fail(c, FVAR_ERR_UNSUPPORTED, "%s: capacity exceeds 2^24 or B*kv_heads 65535", who);
+    if (!kv->lens && (kv->len < 0 || (int64_t)kv->len + rows > (int64_t)kv->capacity))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: cache too small (len=%d + rows=%d > capacity=%d)", who, kv->len, rows,
+                    kv->capacity);
+    if (!kv->lens || !c->debug_checks) return FVAR_OK;
+    std::vector<int32_t> lens((size_t)B);
+    if (hipStreamSynchronize(st) != hipSuccess ||
+        hipMemcpy(lens.data(), kv->lens, lens.size() * sizeof(int32_t), hipMemcpyDeviceToHost) != hipSuccess)
+        return fail(c, FVAR_ERR_HIP, "%s: cannot read lens", who);
+    for (int b = 0; b < B; ++b)
+        if (lens[b] < 0 || (int64_t)lens[b] + rows > (int64_t)kv->capacity)
+            return fail(c, FVAR_ERR_INVALID_ARG, "%s: lens[%d] = %d with rows=%d is outside [0,%d]", who, b, lens[b], rows,
+                        kv->capacity);
+    return FVAR_OK;
+}
+
+fvar::KvqCache kvq_cache(const fvar_kvq *kv)
+{
+    return {(uint8_t *)kv->k, (uint8_t *)kv->v, (uint8_t *)kv->k_scale, (uint8_t *)kv->v_scale, kv->lens, kv->mask,
+            kv->kv_heads, kv->capacity, kv->len};
+}
+
+// Elements from one row to the next: `ld`, or the row itself where it is 0; -1 where it is not one that can be read.
+int row_pitch(const fvar_ctx *c, int ld, int row)
+{
+    const int chunk = c->cfg.dtype == FVAR_BF16 ? 8 : 4;
+    if (ld == 0) return row;
+    return ld < row || ld % chunk ? -1 : ld;
+}
+
+// Whether the sizes of a cache are some that workspace can be computed for.
+bool kvq_sizes(const fvar_ctx *c, const fvar_kvq *kv, int B)
+{
+    return kv && B >= 1 && kv->kv_heads >= 1 && c->cfg.heads % kv->kv_heads == 0 && kv->capacity >= 1;
+}
+
+size_t kvq_attention_ws(const fvar_ctx *c, const fvar_kvq *kv, int B, int n)
+{
+    return align256(fvar::kvq_attention_scratch_floats(dtype(c), B, n, c->cfg.heads, kv->kv_heads, c->cfg.head_dim,
+                                                       kv->capacity) * sizeof(float));
+}
+
+// The block on `rows` rows per sample, over one of two kinds of cache (the other is null).
+// idx == nullptr: rows are x's own rows (rows == M).
 fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights *w, const void *x,
-                          int B, int M, const int32_t *idx, int rows, const fvar_kv *kv, void *y,
+                          int B, int M, const int32_t *idx, int rows, const fvar_kv *kv, const fvar_kvq *kvq, void *y,
                           void *ws, size_t ws_bytes, const char *who)
 {
-    if (!w || !x || !kv || !y) return fail(c, FVAR_ERR_INVALID_ARG, "%s: null argument", who);
+    if (!w || !x || (!kv && !kvq) || !y) return fail(c, FVAR_ERR_INVALID_ARG, "%s: null argument", who);
     if (B < 1 || M < 1 || rows < 1 || rows > M)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: need B>=1 and 1<=rows<=M (B=%d M=%d rows=%d)", who, B,
                     M, rows);
@@ -187,11 +254,19 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: idx_keep may be NULL only when k == M", who);
     if (!w->w_qkv || !w->w_o || !w->w_fc1 || !w->w_fc2)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: weight matrix pointer is NULL", who);
-    if (!kv->k || !kv->v || kv->len < 0 || kv->capacity < 1 ||
+    if (kvq) {
+        const fvar_status ks = check_kvq(c, st, kvq, B, rows, who);
+        if (ks != FVAR_OK) return ks;
+        if (kvq->kv_heads != c->cfg.heads)
+            return fail(c, FVAR_ERR_UNSUPPORTED, "%s: kv_heads=%d, and the block has %d heads of keys", who, kvq->kv_heads,
+                        c->cfg.heads);
+        if ((int64_t)B * rows * c->cfg.heads > (1 << 25))
+            return fail(c, FVAR_ERR_UNSUPPORTED, "%s: B*rows*heads exceeds 2^25", who);
+    } else if (!kv->k || !kv->v || kv->len < 0 || kv->capacity < 1 ||
         (int64_t)kv->len + rows > (int64_t)kv->capacity)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: KV cache too small (len=%d + rows=%d > capacity=%d)",
                     who, kv->len, rows, kv->capacity);
-    const void *ptrs[] = {x, y, kv->k, kv->v, w->w_qkv, w->w_o, w->w_fc1, w->w_fc2, w->ln1_g, w->ln1_b,
+    const void *ptrs[] = {x, y, kv ? kv->k : nullptr, kv ? kv->v : nullptr, w->w_qkv, w->w_o, w->w_fc1, w->w_fc2, w->ln1_g, w->ln1_b,
                           w->ln2_g, w->ln2_b, w->b_qkv, w->b_o, w->b_fc1, w->b_fc2, ws};
     for (const void *p : ptrs)
         if (!aligned16(p)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
@@ -211,7 +286,7 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
         if ((int64_t)B * 8 > 65535 || c->cfg.heads > 65535)
             return fail(c, FVAR_ERR_UNSUPPORTED, "%s: B or heads exceeds the launch grid limits", who);
     }
-    BlockWs s = carve(c, ws, B, rows);
+    BlockWs s = carve(c, ws, B, rows, kvq);
     const size_t ws_need = s.total + (c->debug_checks ? kCanaryBytes : 0);
     if (!ws || ws_bytes < ws_need)
         return fail(c, FVAR_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, ws_need,
@@ -228,7 +303,7 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
 
     const DType dt = dtype(c);
     const int d = c->cfg.hidden, H = c->cfg.heads, Dh = c->cfg.head_dim, F = c->cfg.ffn_hidden;
-    const int R = B * rows, L = kv->len + rows;
+    const int R = B * rows;
 
     bool launched = true;
 
@@ -238,18 +313,28 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
         fvar::launch_gather_ln(dt, x, idx, B, M, rows, d, w->ln1_g, w->ln1_b, c->eps,
                                idx ? s.x_keep : nullptr, s.u, st);
     });
-    // QKV projection; K and V rows land in the cache behind the valid prefix
+    // QKV projection; K and V rows land in the cache behind the valid prefix, or in the workspace to be quantised
     timed(c, st, "gemm_qkv", [&] {
         fvar::GemmEpilogue e;
         e.bias = w->b_qkv; e.out0 = s.q; e.ld0 = d; e.split = d;
-        e.kcache = kv->k; e.vcache = kv->v; e.hd = d; e.cap = kv->capacity; e.len = kv->len;
+        e.kcache = kvq ? s.k_new : kv->k; e.vcache = kvq ? s.v_new : kv->v; e.hd = d;
+        e.cap = kvq ? rows : kv->capacity; e.len = kvq ? 0 : kv->len;
         e.rows_per_sample = rows;
         launched &= fvar::launch_gemm(dt, s.u, w->w_qkv, R, 3 * d, d, e, s.qkv, s.part, st);
     });
-    timed(c, st, "attention", [&] {
-        fvar::launch_attention(dt, s.q, kv->k, kv->v, B, rows, L, kv->capacity, H, Dh, c->scale, s.att,
-                               s.part, st);
-    });
+    if (kvq) {
+        timed(c, st, "kvq_append", [&] {
+            fvar::launch_kvq_append(dt, s.k_new, s.v_new, d, kvq_cache(kvq), B, rows, Dh, st);
+        });
+        timed(c, st, "kvq_attention", [&] {
+            fvar::launch_kvq_attention(dt, s.q, d, kvq_cache(kvq), rows, B, rows, H, Dh, c->scale, s.att, s.part, st);
+        });
+    } else {
+        timed(c, st, "attention", [&] {
+            fvar::launch_attention(dt, s.q, kv->k, kv->v, B, rows, kv->len + rows, kv->capacity, H, Dh, c->scale, s.att,
+                                   s.part, st);
+        });
+    }
     timed(c, st, "gemm_o", [&] {
         fvar::GemmEpilogue e;
         e.bias = w->b_o; e.residual = resid; e.out0 = s.h1; e.ld0 = d; e.split = d;
@@ -457,7 +542,7 @@ fvar_status fvar_block_forward_dense(fvar_ctx *c, fvar_stream stream, const fvar
                                      void *ws, size_t ws_bytes)
 {
     if (!c) return FVAR_ERR_INVALID_ARG;
-    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, nullptr, M, kv, y, ws,
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, nullptr, M, kv, nullptr, y, ws,
                          ws_bytes, "fvar_block_forward_dense");
 }
 
@@ -467,8 +552,104 @@ fvar_status fvar_block_forward_pruned(fvar_ctx *c, fvar_stream stream, const fva
                                       size_t ws_bytes)
 {
     if (!c) return FVAR_ERR_INVALID_ARG;
-    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, idx_keep, k, kv, y_keep, ws,
-                         ws_bytes, "fvar_block_forward_pruned");
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, idx_keep, k, kv, nullptr, y_keep,
+                         ws, ws_bytes, "fvar_block_forward_pruned");
+}
+
+fvar_status fvar_block_forward_dense_kvq(fvar_ctx *c, fvar_stream stream, const fvar_block_weights *w, const void *x,
+                                         int32_t B, int32_t M, const fvar_kvq *kv, void *y, void *ws, size_t ws_bytes)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, nullptr, M, nullptr, kv, y, ws, ws_bytes,
+                         "fvar_block_forward_dense_kvq");
+}
+
+fvar_status fvar_block_forward_pruned_kvq(fvar_ctx *c, fvar_stream stream, const fvar_block_weights *w, const void *x,
+                                          int32_t B, int32_t M, const int32_t *idx_keep, int32_t k, const fvar_kvq *kv,
+                                          void *y_keep, void *ws, size_t ws_bytes)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, idx_keep, k, nullptr, kv, y_keep, ws, ws_bytes,
+                         "fvar_block_forward_pruned_kvq");
+}
+
+size_t fvar_block_kvq_workspace_bytes(const fvar_ctx *c, const fvar_kvq *kv, int32_t B, int32_t rows)
+{
+    if (!c || !kvq_sizes(c, kv, B) || rows < 1) return 0;
+    return carve(c, nullptr, B, rows, kv).total + (c->debug_checks ? kCanaryBytes : 0);
+}
+
+fvar_status fvar_kvq_append(fvar_ctx *c, fvar_stream stream, const fvar_kvq *kv, const void *k, const void *v, int32_t ld,
+                            int32_t B, int32_t rows)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    const char *who = "fvar_kvq_append";
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rows < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need rows>=1 (rows=%d)", who, rows);
+    const fvar_status ks = check_kvq(c, st, kv, B, rows, who);
+    if (ks != FVAR_OK) return ks;
+    if (!k || !v) return fail(c, FVAR_ERR_INVALID_ARG, "%s: k or v is NULL", who);
+    if (!aligned16(k) || !aligned16(v)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
+    if (rows > kv->capacity) return fail(c, FVAR_ERR_INVALID_ARG, "%s: rows=%d > capacity=%d", who, rows, kv->capacity);
+    const int pitch = row_pitch(c, ld, kv->kv_heads * c->cfg.head_dim);
+    if (pitch < 0)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: ld=%d is shorter than a row or no multiple of 16 bytes", who, ld);
+    timed(c, st, "kvq_append", [&] {
+        fvar::launch_kvq_append(dtype(c), k, v, pitch, kvq_cache(kv), B, rows, c->cfg.head_dim, st);
+    });
+    return launch_status(c, who);
+}
+
+fvar_status fvar_kvq_read(fvar_ctx *c, fvar_stream stream, const fvar_kvq *kv, int32_t B, int32_t first, int32_t rows,
+                          void *k, void *v)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    const char *who = "fvar_kvq_read";
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const fvar_status ks = check_kvq(c, st, kv, B, 0, who);
+    if (ks != FVAR_OK) return ks;
+    if (!k && !v) return fail(c, FVAR_ERR_INVALID_ARG, "%s: k and v both NULL", who);
+    if (!aligned16(k) || !aligned16(v)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
+    if (rows < 1 || rows > kv->capacity || first < -kv->capacity || (int64_t)first + (first < 0 ? 0 : rows) > kv->capacity)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: rows [%d,+%d) are outside the capacity of %d", who, first, rows,
+                    kv->capacity);
+    timed(c, st, "kvq_read", [&] {
+        fvar::launch_kvq_read(dtype(c), kvq_cache(kv), B, first, rows, c->cfg.head_dim, k, v, st);
+    });
+    return launch_status(c, who);
+}
+
+size_t fvar_kvq_attention_workspace_bytes(const fvar_ctx *c, const fvar_kvq *kv, int32_t B, int32_t n)
+{
+    if (!c || !kvq_sizes(c, kv, B) || n < 1) return 0;
+    return kvq_attention_ws(c, kv, B, n);
+}
+
+fvar_status fvar_kvq_attention(fvar_ctx *c, fvar_stream stream, const void *q, int32_t ld, const fvar_kvq *kv, int32_t B,
+                               int32_t n, void *o, void *ws, size_t ws_bytes)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    const char *who = "fvar_kvq_attention";
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (n < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need n>=1 (n=%d)", who, n);
+    const fvar_status ks = check_kvq(c, st, kv, B, 0, who);
+    if (ks != FVAR_OK) return ks;
+    if (!q || !o) return fail(c, FVAR_ERR_INVALID_ARG, "%s: q or o is NULL", who);
+    if (!aligned16(q) || !aligned16(o) || !aligned16(ws))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
+    const int pitch = row_pitch(c, ld, c->cfg.hidden);
+    if (pitch < 0)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: ld=%d is shorter than a row or no multiple of 16 bytes", who, ld);
+    if ((int64_t)B * n * c->cfg.heads > (1 << 25))
+        return fail(c, FVAR_ERR_UNSUPPORTED, "%s: B*n*heads exceeds 2^25", who);
+    const size_t need = kvq_attention_ws(c, kv, B, n);
+    if (need && (!ws || ws_bytes < need))
+        return fail(c, FVAR_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, ws_bytes);
+    timed(c, st, "kvq_attention", [&] {
+        fvar::launch_kvq_attention(dtype(c), q, pitch, kvq_cache(kv), 0, B, n, c->cfg.heads, c->cfg.head_dim, c->scale, o,
+                                   (float *)ws, st);
+    });
+    return launch_status(c, who);
 }
 
 static fvar_status lowrank_fill(fvar_ctx *c, fvar_stream stream, const void *y_keep,

@@ -178,6 +178,32 @@ int attention_ways(int B, int n, int L, int H, int Dh);   // bf16: 100 * wavefro
 void launch_attention(DType dt, const void *q, const void *K, const void *V, int B, int n, int L,
                       int cap, int H, int Dh, float scale, void *o, float *part, hipStream_t st);
 
+// A cache held in 4 bits, see kvq.hip: codes [B][heads][capacity][Dh/2], scales [B][heads][capacity][Dh/32].
+// lens: rows of each sample, or null and `len` for all; mask: [B][capacity], 0 hides a row from the attention, or null.
+struct KvqCache {
+    uint8_t *k, *v, *k_scale, *v_scale;
+    const int32_t *lens;
+    const uint8_t *mask;
+    int heads, capacity, len;
+};
+// rows of sample b, `extra` more than the cache says, within its capacity
+__device__ __forceinline__ int kvq_length(const KvqCache &c, int b, int extra)
+{
+    const long l = (long)(c.lens ? c.lens[b] : c.len) + extra;
+    return (int)(l < 0 ? 0 : l > c.capacity ? c.capacity : l);
+}
+// rows k, v:[B,rows,heads,Dh] (ld elements from one to the next) quantised to the cache behind each sample's rows; rows
+// past the capacity are left out
+void launch_kvq_append(DType dt, const void *k, const void *v, int ld, const KvqCache &c, int B, int rows, int Dh,
+                       hipStream_t st);
+// k, v:[B,rows,heads,Dh] or null: rows first.. of the cache (first < 0: from the end of each sample's); 0 outside them
+void launch_kvq_read(DType dt, const KvqCache &c, int B, int first, int rows, int Dh, void *k, void *v, hipStream_t st);
+// attention over the cache's rows and `extra` more, see kvq_attention.hip; q:[B,n,H,Dh], ld elements from one query to
+// the next; o:[B,n,H,Dh]; part: kvq_attention_scratch_floats() floats
+size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity);
+void launch_kvq_attention(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, int Dh,
+                          float scale, void *o, float *part, hipStream_t st);
+
 // y[b,idx_keep[b,j],:] = y_keep[b,j,:];  y[b,i,:] = w_c[b,i,:] g_c[b] for i in idx_drop[b,:]
 // parts / scores_out: null, or scratch of B*M*fill_score_parts() doubles and a [B*M] fp32 array that
 // receives the energy (sum of squares of the stored elements) of every row of y

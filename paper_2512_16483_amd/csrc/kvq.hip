@@ -1,0 +1,144 @@
+// A key/value cache held in 4 bits: quantising new rows into it, and reading rows back.
+//
+// Format, per block of 32 consecutive head-dim elements of one token and head: a power of two 2^e stored as the byte
+// e + 127, and elements in E2M1 (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign), element 2i in the low half of byte i.  It is
+// the block format that gfx950 converts and multiplies in hardware.  e is the smallest integer with max|x| < 7 * 2^e:
+// values up to 7 * 2^e round to at most 6 * 2^e with an error of half a step of their binade, as all smaller ones do.
+// It is held to [-124, 125], so that every value of the cache is 0 or a normal number of bf16 and fp32.  A block with an
+// infinity or a NaN has the byte 255 and reads as NaN.
+//
+// Layout: codes [B][heads][capacity][DH/2], scales [B][heads][capacity][DH/32]: a head's rows are consecutive, as the
+// attention streams them.
+#include "common.h"
+
+namespace fvar {
+
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+
+// Byte of the scale from the bits of the block's largest magnitude: exponent field less 2, one more from a mantissa of
+// .75 on (1.75 * 4 = 7).  MB: mantissa bits of the type.
+template <int MB> __device__ __forceinline__ uint32_t scale_byte(uint32_t top)
+{
+    const int e = (int)((top + (1u << (MB - 2))) >> MB) - 2;
+    return top >= (255u << MB) ? 255u : (uint32_t)min(max(e, 3), 252);
+}
+
+__device__ __forceinline__ uint32_t quad_max(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));    // quad_perm 1,0,3,2
+    return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true)); // quad_perm 2,3,0,1
+}
+
+// Eight elements per thread, four threads per block of 32: their maximum is two steps in registers.
+// grid: (chunks of a head's new rows, B * heads, K or V).  Memory-bound: rows are read as whole lines of one head, and
+// written as one run per head.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kvq_append_kernel(const T *__restrict__ k, const T *__restrict__ v, int ld,
+                                                         KvqCache c, int rows)
+{
+    constexpr int CH = DH / 8;                               // threads of a row
+    const int item = blockIdx.x * 256 + threadIdx.x, j = item / CH, ch = item % CH;
+    const int b = blockIdx.y / c.heads, h = blockIdx.y % c.heads;
+    const long pos = (long)(c.lens ? c.lens[b] : c.len) + j;
+    if (j >= rows || pos < 0 || pos >= c.capacity) return;   // whole rows: the threads of a block go together
+    const T *src = (blockIdx.z ? v : k) + ((size_t)b * rows + j) * ld + (size_t)h * DH + ch * 8;
+    uint32_t top, word = 0, byte;
+    if constexpr (sizeof(T) == 2) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(src);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t hi = 0, lo = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { hi = max(hi, w[i] & 0x7fff0000u); lo = max(lo, w[i] & 0x7fffu); }
+        top = quad_max(max(hi >> 16, lo));
+        byte = scale_byte<7>(top);
+        const float scale = __uint_as_float(byte << 23);
+#define FVAR_PAIR(i) word = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(word, __builtin_bit_cast(bf16x2v, w[i]), scale, i)
+        FVAR_PAIR(0); FVAR_PAIR(1); FVAR_PAIR(2); FVAR_PAIR(3);
+#undef FVAR_PAIR
+    } else {
+        const float4 x = *reinterpret_cast<const float4 *>(src), y = *reinterpret_cast<const float4 *>(src + 4);
+        const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+        top = quad_max(top);
+        byte = scale_byte<23>(top);
+        const float scale = __uint_as_float(byte << 23);
+#define FVAR_PAIR(i) word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, f[2 * i], f[2 * i + 1], scale, i)
+        FVAR_PAIR(0); FVAR_PAIR(1); FVAR_PAIR(2); FVAR_PAIR(3);
+#undef FVAR_PAIR
+    }
+    if (byte == 255) word = 0;
+    const size_t row = (size_t)blockIdx.y * c.capacity + pos;
+    reinterpret_cast<uint32_t *>(blockIdx.z ? c.v : c.k)[row * CH + ch] = word;
+    if (ch % 4 == 0) (blockIdx.z ? c.v_scale : c.k_scale)[row * (DH / 32) + ch / 4] = (uint8_t)byte;
+}
+
+// Eight elements per thread.  Every value of the format is exact in bf16 and fp32.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kvq_read_kernel(KvqCache c, int first, int rows, T *__restrict__ k,
+                                                       T *__restrict__ v, int only_v)
+{
+    constexpr int CH = DH / 8;
+    const int item = blockIdx.x * 256 + threadIdx.x, j = item / CH, ch = item % CH;
+    if (j >= rows) return;
+    const int b = blockIdx.y / c.heads, h = blockIdx.y % c.heads;
+    const bool is_v = only_v || blockIdx.z;
+    const int len = kvq_length(c, b, 0);
+    const long pos = (long)(first < 0 ? len : 0) + first + j;
+    uint32_t word = 0, byte = 127;
+    if (pos >= 0 && pos < len) {
+        const size_t row = (size_t)blockIdx.y * c.capacity + pos;
+        word = reinterpret_cast<const uint32_t *>(is_v ? c.v : c.k)[row * CH + ch];
+        byte = (is_v ? c.v_scale : c.k_scale)[row * (DH / 32) + ch / 4];
+    }
+    const float scale = __uint_as_float(byte << 23);         // 255: infinity, which the conversion turns into NaN
+    T *dst = (is_v ? v : k) + (((size_t)b * rows + j) * c.heads + h) * DH + ch * 8;
+    if constexpr (sizeof(T) == 2) {
+        uint4 x;
+        x.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
+        x.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
+        x.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
+        x.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
+        *reinterpret_cast<uint4 *>(dst) = x;
+    } else {
+        const floatx2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 0);
+        const floatx2_t p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 1);
+        const floatx2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 2);
+        const floatx2_t p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 3);
+        *reinterpret_cast<float4 *>(dst) = make_float4(p0[0], p0[1], p1[0], p1[1]);
+        *reinterpret_cast<float4 *>(dst + 4) = make_float4(p2[0], p2[1], p3[0], p3[1]);
+    }
+}
+
+void launch_kvq_append(DType dt, const void *k, const void *v, int ld, const KvqCache &c, int B, int rows, int Dh,
+                       hipStream_t st)
+{
+    const dim3 grid((unsigned)(((long)rows * (Dh / 8) + 255) / 256), (unsigned)(B * c.heads), 2);
+#define FVAR_APPEND(T, DH) launch(kvq_append_kernel<T, DH>, grid, dim3(256), 0, st, (const T *)k, (const T *)v, ld, c, rows)
+    if (dt == DType::BF16) {
+        if (Dh == 64) FVAR_APPEND(uint16_t, 64);
+        else FVAR_APPEND(uint16_t, 128);
+    } else {
+        if (Dh == 64) FVAR_APPEND(float, 64);
+        else FVAR_APPEND(float, 128);
+    }
+#undef FVAR_APPEND
+}
+
+void launch_kvq_read(DType dt, const KvqCache &c, int B, int first, int rows, int Dh, void *k, void *v, hipStream_t st)
+{
+    const dim3 grid((unsigned)(((long)rows * (Dh / 8) + 255) / 256), (unsigned)(B * c.heads), k && v ? 2 : 1);
+    const int only_v = !k;
+#define FVAR_READ(T, DH) launch(kvq_read_kernel<T, DH>, grid, dim3(256), 0, st, c, first, rows, (T *)k, (T *)v, only_v)
+    if (dt == DType::BF16) {
+        if (Dh == 64) FVAR_READ(uint16_t, 64);
+        else FVAR_READ(uint16_t, 128);
+    } else {
+        if (Dh == 64) FVAR_READ(float, 64);
+        else FVAR_READ(float, 128);
+    }
+#undef FVAR_READ
+}
+
+}  // namespace fvar

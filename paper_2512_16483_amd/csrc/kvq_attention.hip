@@ -1,106 +1,431 @@
 // Attention over a key/value cache held in 4 bits (format and layout: kvq.hip).
 //   o[b,i,h,:] = sum_t p_t V[b,t,h',:],  p = softmax over the visible t of scale * q[b,i,h,:] . K[b,t,h',:],
 //   h' = h / (H / heads); t is visible when t < length of sample b and mask[b][t] != 0; o = 0 where nothing is visible.
+//
+// The query heads of one kv head are further rows of the same problem: row r of a (sample, kv head) is query r / G of
+// query head h' * G + r % G, G = H / heads.
 #include "common.h"
 
 namespace fvar {
 
-// One wavefront per query and head, a lane per key for the scores, a lane per one or two head-dim elements for the sum
-// over the values; running maximum and sum in fp32.
-template <typename T, int DH>
-__global__ __launch_bounds__(64) void kvq_attn_kernel(const T *__restrict__ q, int ld, KvqCache c, int extra, int n, int H,
-                                                      float c_log2, T *__restrict__ o)
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef short shortx4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) shortx4_t lds_shortx4_t;
+
+// Values as fp16 operands.  An fp16 number holds an element of the format times 2^-25 to 2^13, so a value goes in as
+// value * 2^(kTop - E), E the largest scale byte seen so far and two more: sums are rescaled when a byte exceeds E, which is
+// seldom, and blocks 2^-36 and less of the largest vanish.  Weights go in as p * 2^8, with a reference that may be up to
+// 2^7 below the true maximum.  Next to bf16 operands (any exponent, 8 bits) the weights keep 11 bits, so that the
+// output's own rounding is the only one of note: 1.7e-3 against 2.4e-3 of the result.
+constexpr int kTop = 13, kRoom = 2;
+constexpr float kShift = 8.f, kLag = 7.f;
+
+__device__ __forceinline__ float half_scale(uint32_t byte, int E, bool seen)
 {
-    constexpr int NB = DH / 32, DV = DH / 64;
-    __shared__ float qs[DH];
-    const int lane = threadIdx.x;
-    const int h = blockIdx.x % H;
-    const long bi = blockIdx.x / H;
-    const int b = (int)(bi / n), hk = h / (H / c.heads);
-    const T *src = q + (size_t)bi * ld + (size_t)h * DH;
-#pragma unroll
-    for (int e = 0; e < DV; ++e) qs[lane * DV + e] = Elem<T>::load(src + lane * DV + e);
-    __syncthreads();
-    const int len = kvq_length(c, b, extra);
-    const size_t head = ((size_t)b * c.heads + hk) * c.capacity;
-    const uint4 *Kc = reinterpret_cast<const uint4 *>(c.k) + head * NB;
-    const uint8_t *Ks = c.k_scale + head * NB, *Vs = c.v_scale + head * NB, *Vc = c.v + head * (DH / 2);
-    float m = -INFINITY, l = 0.f, acc[DV] = {};
-    for (int t0 = 0; t0 < len; t0 += 64) {
-        const int t = t0 + lane;
-        const bool seen = t < len && (!c.mask || c.mask[(size_t)b * c.capacity + t]);
-        float s = -INFINITY;
-        if (seen) {
-            s = 0.f;
-#pragma unroll
-            for (int k = 0; k < NB; ++k) {
-                const uint4 x = Kc[(size_t)t * NB + k];
-                const float scale = __uint_as_float((uint32_t)Ks[(size_t)t * NB + k] << 23);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                float part = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const floatx2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 0);
-                    const floatx2_t p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 1);
-                    const floatx2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 2);
-                    const floatx2_t p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 3);
-                    const float *qk = qs + 32 * k + 8 * i;
-                    part = fmaf(p0[0], qk[0], part); part = fmaf(p0[1], qk[1], part);
-                    part = fmaf(p1[0], qk[2], part); part = fmaf(p1[1], qk[3], part);
-                    part = fmaf(p2[0], qk[4], part); part = fmaf(p2[1], qk[5], part);
-                    part = fmaf(p3[0], qk[6], part); part = fmaf(p3[1], qk[7], part);
-                }
-                s += part;
-            }
-        }
-        float mx = fmaxf(m, s);
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-        const float base = fmaxf(mx, -1e30f);                // nothing finite yet: weights of 0
-        const float alpha = __builtin_amdgcn_exp2f((m - base) * c_log2);
-        const float p = __builtin_amdgcn_exp2f((s - base) * c_log2);
-        m = mx;
-        l = l * alpha + wave_sum(p);
-#pragma unroll
-        for (int e = 0; e < DV; ++e) acc[e] *= alpha;
-        unsigned long long vis = __ballot(seen);
-        while (vis) {
-            const int kk = __builtin_ctzll(vis);
-            vis &= vis - 1;
-            const float w = __shfl(p, kk);
-            const int d0 = lane * DV;
-            const float scale = __uint_as_float((uint32_t)Vs[(size_t)(t0 + kk) * NB + d0 / 32] << 23);
-            const floatx2_t x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(Vc[(size_t)(t0 + kk) * (DH / 2) + d0 / 2], scale, 0);
-            if constexpr (DV == 2) {
-                acc[0] = fmaf(w, x[0], acc[0]);
-                acc[1] = fmaf(w, x[1], acc[1]);
-            } else {
-                acc[0] = fmaf(w, lane & 1 ? x[1] : x[0], acc[0]);
-            }
-        }
-    }
-    T *dst = o + (size_t)bi * H * DH + (size_t)h * DH + lane * DV;
-#pragma unroll
-    for (int e = 0; e < DV; ++e) Elem<T>::store(dst + e, l == 0.f ? 0.f : acc[e] / l);
+    const int e = (int)byte - E + kTop + 127;
+    return seen ? __uint_as_float(byte == 255 ? 0x7f800000u : (uint32_t)max(e, 0) << 23) : 0.f;
 }
 
-size_t kvq_attention_scratch_floats(DType, int, int, int, int, int, int) { return 0; }
+template <int W> __device__ __forceinline__ uint32_t half_pair(uint32_t word, float scale)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale, W));
+}
+template <int W> __device__ __forceinline__ uint32_t bf16_pair(uint32_t word, float scale)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, W));
+}
+__device__ __forceinline__ uint4 half_eight(uint32_t w, float s)
+{
+    return make_uint4(half_pair<0>(w, s), half_pair<1>(w, s), half_pair<2>(w, s), half_pair<3>(w, s));
+}
+__device__ __forceinline__ uint4 bf16_eight(uint32_t w, float s)
+{
+    return make_uint4(bf16_pair<0>(w, s), bf16_pair<1>(w, s), bf16_pair<2>(w, s), bf16_pair<3>(w, s));
+}
+
+// the same value in the lanes of a column group: 16 and 32 lanes apart
+__device__ __forceinline__ float column_max(float v)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float column_sum(float v)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// Three bf16 numbers that add up to an fp32 one: its bits from the top (no rounding, so no overflow either).
+__device__ __forceinline__ void three_pieces(const float *x, bf16x8_t *out)
+{
+    uint32_t w[3][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const uint32_t ha = __float_as_uint(a) & 0xffff0000u, hb = __float_as_uint(b) & 0xffff0000u;
+            w[p][i] = (ha >> 16) | hb;
+            a -= __uint_as_float(ha);
+            b -= __uint_as_float(hb);
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) out[p] = __builtin_bit_cast(bf16x8_t, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
+}
+
+template <typename T> struct Quad;                           // four consecutive results
+template <> struct Quad<uint16_t> {
+    __device__ static __forceinline__ void store(uint16_t *p, float4 v)
+    {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    }
+};
+template <> struct Quad<float> {
+    __device__ static __forceinline__ void store(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
+};
+
+// Sixteen rows per workgroup, whose wavefronts take every NW-th tile of 32 keys of the workgroup's share [t0, t1) of the
+// key axis, each with a softmax of its own, and meet in LDS at the end.  For the rows of one query or a few, where the
+// cache's way from memory is what counts (each wavefront fetches a tile ahead, no barrier in the loop), and for fp32, where the
+// three products that make up one of 24 bits are.
+//   S^T = K Q^T by 16x16x32 MFMAs: a lane holds 32 (16) elements of one key as they lie in memory, a block or half of one,
+//     converts them to bf16 (exact) and multiplies them eight at a time; Q follows that order.
+//   O^T = V^T P^T: a lane takes whole blocks of values as they lie in memory, converts them and leaves them in LDS row by
+//     row, from where the transposing load brings eight keys of one head-dim element; P is in that order already.
+// fp32: Q and P go in as three bf16 numbers each, K and V are exact in one.
+template <typename T, int DH, int NW>
+__global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restrict__ q, int ld, KvqCache c, int extra,
+                                                                int n, int H, float c_log2, T *__restrict__ o,
+                                                                int nrb, int splits, float *__restrict__ part_o,
+                                                                float *__restrict__ part_ml)
+{
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int NP = F32 ? 3 : 1;
+    constexpr int KS = DH / 32, DB = DH / 16, NB = DH / 32;  // steps of S, 16-row blocks of O^T, scale blocks of a row
+    constexpr int KW = DH / 32;                              // words of a key per lane
+    constexpr int VL = DH / 64;                              // blocks of values per lane
+    __shared__ uint4 vlds[NW][32 * DH / 8];                  // a tile of values; at the end the partial results
+    __shared__ float2 ml[NW][16];
+
+    const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int unit = xcd_contiguous(blockIdx.x, gridDim.x);        // the row blocks of a head share an L2
+    const int rb = unit % nrb;
+    unit /= nrb;
+    const int split = unit % splits;
+    unit /= splits;
+    const int hk = unit % c.heads, b = unit / c.heads;
+    const int G = H / c.heads, R = n * G;
+    const int len = kvq_length(c, b, extra);
+    const int tiles = (len + 31) / 32;
+    const int t0 = (int)((long)tiles * split / splits), t1 = (int)((long)tiles * (split + 1) / splits);
+
+    // ---- Q: lane = row, the elements of the lane's part of a key
+    const int row = min(rb * 16 + c16, R - 1);
+    const T *qsrc = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g4 * (DH / 4);
+    bf16x8_t qf[KS][NP];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        if constexpr (F32) {
+            float x[8];
+            *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(qsrc + 8 * s);
+            *reinterpret_cast<float4 *>(x + 4) = *reinterpret_cast<const float4 *>(qsrc + 8 * s + 4);
+            three_pieces(x, qf[s]);
+        } else {
+            qf[s][0] = *reinterpret_cast<const bf16x8_t *>(qsrc + 8 * s);
+        }
+    }
+
+    const size_t head = (size_t)(b * c.heads + hk) * c.capacity;
+    const uint8_t *Kc = c.k + head * (DH / 2), *Vc = c.v + head * (DH / 2), *Ks = c.k_scale + head * NB, *Vs = c.v_scale + head * NB;
+    const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
+
+    struct Tile {
+        uint32_t k[2][KW];
+        uint4 v[VL];
+        uint32_t ks[2], vs[VL], seen;
+    };
+    auto fetch = [&](int t, Tile &x) {
+        const int base = t * 32;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t key = (uint32_t)min(base + 16 * u + c16, len - 1);
+            if constexpr (KW == 4) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(Kc + key * (DH / 2) + g4 * 16);
+                x.k[u][0] = w.x; x.k[u][1] = w.y; x.k[u][2] = w.z; x.k[u][3] = w.w;
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2 *>(Kc + key * (DH / 2) + g4 * 8);
+                x.k[u][0] = w.x; x.k[u][1] = w.y;
+            }
+            x.ks[u] = Ks[key * NB + g4 * NB / 4];
+        }
+#pragma unroll
+        for (int j = 0; j < VL; ++j) {
+            const uint32_t key = (uint32_t)min(base + (64 * j + lane) / NB, len - 1), blk = lane % NB;
+            x.v[j] = *reinterpret_cast<const uint4 *>(Vc + key * (DH / 2) + blk * 16);
+            x.vs[j] = Vs[key * NB + blk];
+        }
+        const int key = base + (lane & 31);
+        x.seen = key < len;
+        if (mask) x.seen = x.seen && mask[min(key, len - 1)];
+    };
+
+    // ---- LDS: 32-byte pieces of a row are turned by its number, so that eight rows' pieces of one column lie in different banks
+    uint16_t *vl = reinterpret_cast<uint16_t *>(vlds[wave]);
+    auto turn = [](int key) { return DH == 128 ? key & 7 : (key >> 1) & 3; };
+    const int rrow = 4 * g4 + ((lane >> 2) & 3);             // transposing load: the lane's row and four elements of it
+    const int rturn = turn(rrow), rbase = rrow * DH + (lane & 3) * 4;
+
+    floatx4_t acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = floatx4_t{0};
+    float m_ref = -INFINITY, l_run = 0.f;
+    const float lag = kLag / c_log2;
+    int E = 0;
+
+    Tile cur, nxt;
+    if (t0 + wave < t1) fetch(t0 + wave, cur);
+    for (int t = t0 + wave; t < t1; t += NW) {
+        const bool more = t + NW < t1;
+        if (more) fetch(t + NW, nxt);
+        const uint32_t vis = (uint32_t)__ballot(cur.seen != 0);
+        if (vis) {
+            // ---- S^T: lane (c16, g4) gets the keys 4 g4 .. + 3 and 16 more of row c16
+            float s[8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                floatx4_t a = {0};
+                const float scale = __uint_as_float(cur.ks[u] << 23);
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, bf16_eight(cur.k[u][i], scale));
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p)
+                        a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][p], a, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * u + i] = a[i];
+            }
+            // ---- values to LDS
+            if constexpr (!F32) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int j = 0; j < VL; ++j) {
+                    const bool seen = (vis >> ((64 * j + lane) / NB)) & 1;
+                    if (seen && cur.vs[j] != 255) top = max(top, cur.vs[j]);
+                }
+                if (__any((int)top > E)) {                   // uniform: the largest block so far
+                    const int now = (int)wave_max(top) + kRoom;
+                    const float down = __builtin_amdgcn_ldexpf(1.f, max(E - now, -200));
+                    E = now;
+#pragma unroll
+                    for (int i = 0; i < DB; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][e] *= down;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < VL; ++j) {
+                const int key = (64 * j + lane) / NB, blk = lane % NB;
+                const bool seen = (vis >> key) & 1;
+                const uint32_t w[4] = {cur.v[j].x, cur.v[j].y, cur.v[j].z, cur.v[j].w};
+                const float scale = F32 ? (seen ? __uint_as_float(cur.vs[j] << 23) : 0.f) : half_scale(cur.vs[j], E, seen);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int piece = (2 * blk + (i >> 1)) ^ turn(key);
+                    *reinterpret_cast<uint4 *>(vl + key * DH + piece * 16 + (i & 1) * 8) = F32 ? bf16_eight(w[i], scale) : half_eight(w[i], scale);
+                }
+            }
+            // ---- softmax
+            if (vis != ~0u) {
+                const uint32_t mine = vis >> (4 * g4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!(mine >> i & 1)) s[i] = -INFINITY;
+                    if (!(mine >> (16 + i) & 1)) s[4 + i] = -INFINITY;
+                }
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i]);
+            if (__any(mx > m_ref + lag)) {
+                const float now = column_max(fmaxf(m_ref, mx));
+                const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
+                m_ref = now;
+                l_run *= alpha;
+#pragma unroll
+                for (int i = 0; i < DB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][e] *= alpha;
+            }
+            const float fin = fmaxf(m_ref, -1e30f), base = fmaf(-fin, c_log2, kShift);
+            float p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // fp32: the difference first, so that a row's only key weighs exactly 1
+                p[i] = __builtin_amdgcn_exp2f(F32 ? (s[i] - fin) * c_log2 : fmaf(s[i], c_log2, base));
+                l_run += p[i];
+            }
+            // ---- O^T += V^T P^T
+            bf16x8_t pf[NP];
+            f16x8_t ph;
+            if constexpr (F32) {
+                three_pieces(p, pf);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ph[i] = (_Float16)p[i];
+            }
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                const uint16_t *src = vl + rbase + ((i ^ rturn) << 4);
+                const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)src);
+                const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(src + 16 * DH));
+                const auto v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                if constexpr (F32) {
+#pragma unroll
+                    for (int k = NP - 1; k >= 0; --k)
+                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v), pf[k], acc[i], 0, 0, 0);
+                } else {
+                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, v), ph, acc[i], 0, 0, 0);
+                }
+            }
+            asm volatile("" ::: "memory");
+        }
+        cur = nxt;
+    }
+
+    // ---- the wavefronts' results: each as the mean of the values it saw, with its weight l at the reference m
+    l_run = column_sum(l_run);
+    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+    float4 *slots = reinterpret_cast<float4 *>(vlds[wave]);
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+        float4 v = make_float4(acc[i][0] * inv, acc[i][1] * inv, acc[i][2] * inv, acc[i][3] * inv);
+        if constexpr (!F32) {                                // |mean| <= 6 * 2^kTop: back to its size, which may be any
+            v.x = __builtin_amdgcn_ldexpf(v.x, E - kTop - 127); v.y = __builtin_amdgcn_ldexpf(v.y, E - kTop - 127);
+            v.z = __builtin_amdgcn_ldexpf(v.z, E - kTop - 127); v.w = __builtin_amdgcn_ldexpf(v.w, E - kTop - 127);
+        }
+        slots[i * 64 + lane] = v;
+    }
+    if (g4 == 0) ml[wave][c16] = make_float2(m_ref, l_run);
+    __syncthreads();
+    float m = ml[0][c16].x;
+#pragma unroll
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, ml[w][c16].x);
+    const float fin = fmaxf(m, -1e30f);
+    float wgt[NW], sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        wgt[w] = ml[w][c16].y * __builtin_amdgcn_exp2f((ml[w][c16].x - fin) * c_log2);
+        sum += wgt[w];
+    }
+    const float each = sum == 0.f ? 0.f : 1.0f / sum;
+    if (rb * 16 + c16 >= R) return;
+    const size_t prow = ((size_t)(b * c.heads + hk) * R + row) * splits + split;
+    T *dst = o + (size_t)(b * (long)n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH;
+    for (int i = wave; i < DB; i += NW) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float4 x = reinterpret_cast<const float4 *>(vlds[w])[i * 64 + lane];
+            const float k = wgt[w] * each;
+            v.x = fmaf(x.x, k, v.x); v.y = fmaf(x.y, k, v.y); v.z = fmaf(x.z, k, v.z); v.w = fmaf(x.w, k, v.w);
+        }
+        if (splits > 1) *reinterpret_cast<float4 *>(part_o + prow * DH + 16 * i + 4 * g4) = v;
+        else Quad<T>::store(dst + 16 * i + 4 * g4, v);
+    }
+    if (splits > 1 && wave == 0 && g4 == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m, sum);
+}
+
+// The shares of a row joined: each is a mean and its weight.  One thread per four head-dim elements of a row.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
+                                                             int n, int H, int heads, int splits, float c_log2, long total,
+                                                             T *__restrict__ o)
+{
+    const long idx = (long)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= total) return;
+    const int d = (int)(idx % (DH / 4)) * 4;
+    const long prow = idx / (DH / 4);                        // (sample, kv head, row)
+    const int G = H / heads, R = n * G;
+    const int row = (int)(prow % R);
+    const long bh = prow / R, b = bh / heads, hk = bh % heads;
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + prow * splits;
+    float m = -INFINITY;
+    for (int s = 0; s < splits; ++s) m = fmaxf(m, ml[s].x);
+    const float fin = fmaxf(m, -1e30f);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+    for (int s = 0; s < splits; ++s) {
+        const float w = ml[s].y * __builtin_amdgcn_exp2f((ml[s].x - fin) * c_log2);
+        const float4 v = *reinterpret_cast<const float4 *>(part_o + (prow * splits + s) * DH + d);
+        acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y);
+        acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
+        sum += w;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    Quad<T>::store(o + (size_t)(b * n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH + d,
+                   make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+}
+
+constexpr int kRowWaves = 4;
+
+// Shares of the key axis for `length` keys: enough workgroups for four on every CU, each with two tiles per wavefront at least.
+// Never falls as length grows.
+static int kvq_splits(int B, int n, int H, int heads, int length)
+{
+    const long units = (long)B * heads * ((n * (H / heads) + 15) / 16);
+    const long want = (1024 + units - 1) / units, most = ((length + 31) / 32) / (2 * kRowWaves);
+    return (int)(want < most ? want : most > 0 ? most : 1);
+}
+
+size_t kvq_attention_scratch_floats(DType, int B, int n, int H, int heads, int Dh, int capacity)
+{
+    const int splits = kvq_splits(B, n, H, heads, capacity);
+    return splits > 1 ? (size_t)B * n * H * splits * (Dh + 2) : 0;
+}
+
+template <typename T, int DH>
+static void launch_rows(const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, float c_log2, void *o,
+                        float *part, hipStream_t st)
+{
+    const int nrb = (n * (H / c.heads) + 15) / 16;
+    const int splits = kvq_splits(B, n, H, c.heads, c.lens ? c.capacity : c.len + extra);
+    const size_t rows = (size_t)B * n * H;
+    float *part_ml = part + rows * splits * DH;
+    launch(kvq_attn_rows_kernel<T, DH, kRowWaves>, dim3((unsigned)((long)B * c.heads * splits * nrb)), dim3(64 * kRowWaves), 0, st,
+           (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, nrb, splits, part, part_ml);
+    if (splits > 1) {
+        const long total = (long)rows * (DH / 4);
+        launch(kvq_attn_merge_kernel<T, DH>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, (const float *)part,
+               (const float *)part_ml, n, H, c.heads, splits, c_log2, total, (T *)o);
+    }
+}
 
 void launch_kvq_attention(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, int Dh,
-                          float scale, void *o, float *, hipStream_t st)
+                          float scale, void *o, float *part, hipStream_t st)
 {
-    const dim3 grid((unsigned)((long)B * n * H));
     const float c_log2 = scale * 1.4426950408889634f;
-#define FVAR_KVQ(T, DH) \
-    launch(kvq_attn_kernel<T, DH>, grid, dim3(64), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, (T *)o)
     if (dt == DType::BF16) {
-        if (Dh == 64) FVAR_KVQ(uint16_t, 64);
-        else FVAR_KVQ(uint16_t, 128);
+        if (Dh == 64) launch_rows<uint16_t, 64>(q, ld, c, extra, B, n, H, c_log2, o, part, st);
+        else launch_rows<uint16_t, 128>(q, ld, c, extra, B, n, H, c_log2, o, part, st);
     } else {
-        if (Dh == 64) FVAR_KVQ(float, 64);
-        else FVAR_KVQ(float, 128);
+        if (Dh == 64) launch_rows<float, 64>(q, ld, c, extra, B, n, H, c_log2, o, part, st);
+        else launch_rows<float, 128>(q, ld, c, extra, B, n, H, c_log2, o, part, st);
     }
-#undef FVAR_KVQ
 }
 
 }  // namespace fvar

@@ -11,6 +11,9 @@ namespace fvar {
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef short shortx4_t __attribute__((ext_vector_type(4)));
+typedef int intx8_t __attribute__((ext_vector_type(8)));
+typedef unsigned uintx6_t __attribute__((ext_vector_type(6)));
+typedef float floatx32_t __attribute__((ext_vector_type(32)));
 typedef __attribute__((address_space(3))) shortx4_t lds_shortx4_t;
 
 // Values as fp16 operands.  An fp16 number holds an element of the format times 2^-25 to 2^13, so a value goes in as
@@ -334,7 +337,7 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
     }
     const float each = sum == 0.f ? 0.f : 1.0f / sum;
     if (rb * 16 + c16 >= R) return;
-    const size_t prow = ((size_t)(b * c.heads + hk) * R + row) * splits + split;
+    const size_t prow = ((size_t)((b * c.heads + hk) * nrb + rb) * splits + split) * 16 + c16;
     T *dst = o + (size_t)(b * (long)n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH;
     for (int i = wave; i < DB; i += NW) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -350,28 +353,298 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
     if (splits > 1 && wave == 0 && g4 == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m, sum);
 }
 
-// The shares of a row joined: each is a mean and its weight.  One thread per four head-dim elements of a row.
+// 128 rows per workgroup, 32 per wavefront, over tiles of 64 keys; bf16.  For the rows of a whole scale, where the matrix cores and the
+// softmax bound the time.
+//   S^T = K Q^T by the 32x32x64 block-scaled MFMA: it takes keys in 4 bits with their scale bytes as they lie in memory, so K is
+//     neither converted nor staged, and at four times the rate of bf16 where the other operand has 6 bits.  Q goes in as three E2M3
+//     numbers per element (sign, 2 bits of exponent, 3 of mantissa, a shared 2^e per 32), each for what the one before leaves and 2^-5
+//     smaller: off by at most 2^-13 of the block's largest element.  (Two leave 2^-8 of it, which scores of 20 and more, a
+//     few times the usual, show in the output.)
+//   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into one of two LDS stages.
+// In the 32x32 accumulator layout a lane owns a query column, so maximum and sum are lane-local, and P is in the order in which the
+// second product takes it, as in attention.hip.
+template <int DH>
+__global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
+                                                                int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,
+                                                                int full_units, int shares, float *__restrict__ part_o,
+                                                                float *__restrict__ part_ml)
+{
+    constexpr int KS = DH / 64, DB = DH / 32, NB = DH / 32;  // k64 steps of S, 32-row blocks of O^T, scale blocks of a row
+    constexpr int VW = DH / 32;                              // words of values per thread
+    __shared__ uint4 vlds[2][64 * DH / 8];
+
+    const int tid = threadIdx.x, lane = tid & 63, rl = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int unit = blockIdx.x, share = 0, ranges = 1;
+    if (unit < full_units) {
+        unit = xcd_contiguous(unit, full_units);
+    } else {
+        const int t = xcd_contiguous(unit - full_units, (int)gridDim.x - full_units);
+        unit = full_units + t / shares;
+        share = t % shares;
+        ranges = shares;
+    }
+    const int rb = unit % nrb, hk = unit / nrb % c.heads, b = unit / (nrb * c.heads);
+    const int G = H / c.heads, R = n * G;
+    const int len = kvq_length(c, b, extra);
+    const int tiles = (len + 63) / 64;
+    const int t0 = (int)((long)tiles * share / ranges), t1 = (int)((long)tiles * (share + 1) / ranges);
+    const int r0 = rb * 128 + wave * 32, row = min(r0 + rl, R - 1);
+    const bool active = __builtin_amdgcn_readfirstlane(r0 < R ? 1 : 0) != 0;
+
+    // ---- Q in three pieces of 6 bits: lane = row, block 2 s + g of its elements
+    intx8_t qf[KS][3];
+    int qs[KS][3];
+    {
+        const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(w + 4 * i) = *reinterpret_cast<const uint4 *>(src + 64 * s + 8 * i);
+            uint32_t top = 0;
+            floatx16_t even, odd;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+                even[i] = bf16_lo(w[i]);
+                odd[i] = bf16_hi(w[i]);
+            }
+            // the smallest 2^e with all elements below 7.75 * 2^e, which round to at most 7.5; 255 makes NaN of what is not finite
+            const int e = min(max((int)((top + 8) >> 7) - 2, 13), 252);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                const float size = __uint_as_float((uint32_t)(e - 5 * p) << 23);
+                const uintx6_t x = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, size);
+                const floatx32_t back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(x, size);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) { even[i] -= back[2 * i]; odd[i] -= back[2 * i + 1]; }
+                qf[s][p] = intx8_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+                qs[s][p] = top >= 0x7f80u ? 255 : e - 5 * p;
+            }
+        }
+    }
+
+    const size_t head = (size_t)(b * c.heads + hk) * c.capacity;
+    const uint8_t *Kc = c.k + head * (DH / 2), *Vc = c.v + head * (DH / 2), *Ks = c.k_scale + head * NB, *Vs = c.v_scale + head * NB;
+    const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
+
+    // A tile of keys: every wavefront its own operands.  A tile of values: thread `tid` a quarter of a row, its scale byte; besides, every
+    // wavefront all scale bytes (lane = row), so that all of them see the same largest one.
+    struct Keys { uint4 k[2][KS]; uint32_t ks[2]; };
+    struct Values { uint32_t v[VW], vs, all, seen; };
+    // rows of a wavefront's sixteen in an order in which neighbouring quads' chunks lie in different banks (128-wide rows)
+    const int vkey = DH == 128 ? wave * 16 + ((lane >> 4) & 3) + (lane >> 2 & 3) * 4 : tid >> 2, vpart = tid & 3;
+    auto fetch_keys = [&](int t, Keys &x) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t key = (uint32_t)min(t * 64 + 32 * u + rl, len - 1);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) x.k[u][s] = *reinterpret_cast<const uint4 *>(Kc + key * (DH / 2) + (2 * s + g) * 16);
+            x.ks[u] = NB == 4 ? *reinterpret_cast<const uint32_t *>(Ks + key * NB) : *reinterpret_cast<const uint16_t *>(Ks + key * NB);
+        }
+    };
+    auto fetch_values = [&](int t, Values &x) {
+        const uint32_t key = (uint32_t)min(t * 64 + vkey, len - 1);
+        if constexpr (VW == 4) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(Vc + key * (DH / 2) + vpart * 16);
+            x.v[0] = w.x; x.v[1] = w.y; x.v[2] = w.z; x.v[3] = w.w;
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2 *>(Vc + key * (DH / 2) + vpart * 8);
+            x.v[0] = w.x; x.v[1] = w.y;
+        }
+        x.vs = Vs[key * NB + vpart * NB / 4];
+        const int mine = t * 64 + lane;
+        const uint32_t held = (uint32_t)min(mine, len - 1);
+        x.all = NB == 4 ? *reinterpret_cast<const uint32_t *>(Vs + held * NB) : *reinterpret_cast<const uint16_t *>(Vs + held * NB);
+        x.seen = mine < len;
+        if (mask) x.seen = x.seen && mask[held];
+    };
+
+    // ---- LDS: 16-byte chunks of a row are turned so that four rows' 64-byte quarters lie in different banks when they are read
+    // (transposing load, as in attention.hip), and the chunks of neighbouring quads of lanes when they are written
+    auto turn = [](int key) { return DH == 128 ? ((key & 3) << 2) | ((key >> 2) & 3) : ((key >> 1) & 1) << 2; };
+    const int tG = lane >> 4, tj = (lane >> 2) & 3, ta = lane & 3;
+    const int vrow = 4 * (tG >> 1) + tj;
+    // chunk 4 db + 2 (tG & 1) + (ta >> 1) of row vrow + 16 u + 8 h: `turn` of the row in two parts, h and u only in the low bits
+    auto chunk_at = [&](int db, int step8) {
+        const int key = vrow + 8 * step8;
+        return key * DH + (((4 * db + 2 * (tG & 1) + (ta >> 1)) ^ turn(key)) << 3) + (ta & 1) * 4;
+    };
+
+    floatx16_t acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = floatx16_t{0};
+    float m_ref = -INFINITY, l_run = 0.f;
+    const float lag = kLag / c_log2;
+    int E = 0;
+
+    // the values of a tile, converted, into a stage; the rows that can be seen
+    auto stage_values = [&](int t, const Values &x) -> unsigned long long {
+        const unsigned long long vis = __ballot(x.seen != 0);
+        uint32_t top = 0;
+        if (x.seen) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const uint32_t byte = x.all >> (8 * i) & 255;
+                if (byte != 255) top = max(top, byte);
+            }
+        }
+        if (__any((int)top > E)) {                           // the same in all wavefronts: the largest block so far
+            const int now = (int)wave_max(top) + kRoom;
+            const float down = __builtin_amdgcn_ldexpf(1.f, max(E - now, -200));
+            E = now;
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][e] *= down;
+        }
+        const float scale = half_scale(x.vs, E, (vis >> vkey) & 1);
+        uint16_t *dst = reinterpret_cast<uint16_t *>(vlds[t & 1]) + vkey * DH;
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
+            *reinterpret_cast<uint4 *>(dst + (((vpart * VW + i) ^ turn(vkey)) << 3)) = half_eight(x.v[i], scale);
+        return vis;
+    };
+
+    Keys keys;
+    Values values;
+    unsigned long long vis = 0;
+    if (t0 < t1) {
+        fetch_keys(t0, keys);
+        fetch_values(t0, values);
+        vis = stage_values(t0, values);
+        if (t0 + 1 < t1) fetch_values(t0 + 1, values);
+    }
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        // ---- S^T
+        floatx16_t s[2];
+        if (active) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                s[u] = floatx16_t{0};
+                const int sc = (int)(keys.ks[u] >> (8 * g));
+#pragma unroll
+                for (int p = 2; p >= 0; --p) {
+                    const intx8_t k0 = {(int)keys.k[u][0].x, (int)keys.k[u][0].y, (int)keys.k[u][0].z, (int)keys.k[u][0].w, 0, 0, 0, 0};
+                    s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k0, qf[0][p], s[u], 4, 2, 0, sc, 0, qs[0][p]);
+                    if constexpr (KS == 2) {
+                        const intx8_t k1 = {(int)keys.k[u][KS - 1].x, (int)keys.k[u][KS - 1].y, (int)keys.k[u][KS - 1].z, (int)keys.k[u][KS - 1].w, 0, 0, 0, 0};
+                        s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k1, qf[KS - 1][p], s[u], 4, 2, 2, sc, 0, qs[KS - 1][p]);
+                    }
+                }
+            }
+        }
+        if (t + 1 < t1) fetch_keys(t + 1, keys);
+        if (active && vis) {
+            // ---- softmax
+            if (vis != ~0ull) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t mine = (uint32_t)(vis >> (32 * u)) >> (4 * g);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[u][i] = -INFINITY;
+                }
+            }
+            float mx = s[0][0];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
+            if (__any(mx > m_ref + lag)) {
+                mx = fmaxf(m_ref, mx);
+                const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                const float now = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+                const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
+                m_ref = now;
+                l_run *= alpha;
+#pragma unroll
+                for (int i = 0; i < DB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][e] *= alpha;
+            }
+            const float base = fmaf(-fmaxf(m_ref, -1e30f), c_log2, kShift);
+            f16x8_t pf[4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float p[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], c_log2, base));
+                    l_run += p[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pf[2 * u + (i >> 3)][i & 7] = (_Float16)p[i];
+            }
+            // ---- O^T += V^T P^T
+            const uint16_t *vt = reinterpret_cast<const uint16_t *>(vlds[t & 1]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < DB; ++i) {
+                    const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + chunk_at(i, 2 * u)));
+                    const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + chunk_at(i, 2 * u + 1)));
+                    const auto v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, v), pf[u], acc[i], 0, 0, 0);
+                }
+        }
+        if (t + 1 < t1) {
+            vis = stage_values(t + 1, values);
+            if (t + 2 < t1) fetch_values(t + 2, values);
+        }
+        __syncthreads();
+    }
+
+    // ---- means, back at their size (see half_scale), which is stored or left with its weight for the merge
+    {
+        const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+        l_run = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+    }
+    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+    if (r0 + rl >= R) return;
+    const size_t prow = ((size_t)(unit - full_units) * shares + share) * 128 + wave * 32 + rl;
+    uint16_t *dst = o + (size_t)(b * (long)n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const int d = 32 * i + 8 * (e >> 2) + 4 * g;
+            const float4 v = make_float4(__builtin_amdgcn_ldexpf(acc[i][e] * inv, E - kTop - 127),
+                                         __builtin_amdgcn_ldexpf(acc[i][e + 1] * inv, E - kTop - 127),
+                                         __builtin_amdgcn_ldexpf(acc[i][e + 2] * inv, E - kTop - 127),
+                                         __builtin_amdgcn_ldexpf(acc[i][e + 3] * inv, E - kTop - 127));
+            if (ranges > 1) *reinterpret_cast<float4 *>(part_o + prow * DH + d) = v;
+            else Quad<uint16_t>::store(dst + d, v);
+        }
+    if (ranges > 1 && g == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m_ref, l_run);
+}
+
+// The shares of rows joined: each is a mean and its weight.  A unit is a block of BR rows of one (sample, kv head); the shares
+// of unit first + u lie at [u][share][row].  One thread per four head-dim elements of a row.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                                                             int n, int H, int heads, int splits, float c_log2, long total,
-                                                             T *__restrict__ o)
+                                                             int n, int H, int heads, int nrb, int BR, int first, int shares,
+                                                             float c_log2, long total, T *__restrict__ o)
 {
     const long idx = (long)blockIdx.x * 256 + threadIdx.x;
     if (idx >= total) return;
     const int d = (int)(idx % (DH / 4)) * 4;
-    const long prow = idx / (DH / 4);                        // (sample, kv head, row)
-    const int G = H / heads, R = n * G;
-    const int row = (int)(prow % R);
-    const long bh = prow / R, b = bh / heads, hk = bh % heads;
-    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + prow * splits;
+    const int r = (int)(idx / (DH / 4) % BR), u = (int)(idx / (DH / 4) / BR), unit = first + u;
+    const int G = H / heads, row = unit % nrb * BR + r, hk = unit / nrb % heads;
+    const long b = unit / nrb / heads;
+    if (row >= n * G) return;
+    const size_t prow = (size_t)u * shares * BR + r;
     float m = -INFINITY;
-    for (int s = 0; s < splits; ++s) m = fmaxf(m, ml[s].x);
+    for (int s = 0; s < shares; ++s) m = fmaxf(m, part_ml[(prow + (size_t)s * BR) * 2]);
     const float fin = fmaxf(m, -1e30f);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
-    for (int s = 0; s < splits; ++s) {
-        const float w = ml[s].y * __builtin_amdgcn_exp2f((ml[s].x - fin) * c_log2);
-        const float4 v = *reinterpret_cast<const float4 *>(part_o + (prow * splits + s) * DH + d);
+    for (int s = 0; s < shares; ++s) {
+        const float2 ml = *reinterpret_cast<const float2 *>(part_ml + (prow + (size_t)s * BR) * 2);
+        const float w = ml.y * __builtin_amdgcn_exp2f((ml.x - fin) * c_log2);
+        const float4 v = *reinterpret_cast<const float4 *>(part_o + (prow + (size_t)s * BR) * DH + d);
         acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y);
         acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
         sum += w;
@@ -383,35 +656,59 @@ __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__rest
 
 constexpr int kRowWaves = 4;
 
-// Shares of the key axis for `length` keys: enough workgroups for four on every CU, each with two tiles per wavefront at least.
-// Never falls as length grows.
-static int kvq_splits(int B, int n, int H, int heads, int length)
+// How an attention is run: by blocks of 16 rows (kvq_attn_rows_kernel) or of 128 (kvq_attn_tiles_kernel); nrb blocks per
+// (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
+struct KvqRun { int block, nrb, units, full, shares; };
+static KvqRun kvq_run(DType dt, int B, int n, int H, int heads, int length)
 {
-    const long units = (long)B * heads * ((n * (H / heads) + 15) / 16);
-    const long want = (1024 + units - 1) / units, most = ((length + 31) / 32) / (2 * kRowWaves);
-    return (int)(want < most ? want : most > 0 ? most : 1);
+    const int rows = n * (H / heads);
+    KvqRun run;
+    run.block = dt == DType::BF16 && rows > 64 ? 128 : 16;
+    run.nrb = (rows + run.block - 1) / run.block;
+    run.units = B * heads * run.nrb;
+    if (run.block == 16) {
+        // enough workgroups for four on every CU, each with two tiles per wavefront at least
+        const int want = (1024 + run.units - 1) / run.units, most = (length + 31) / 32 / (2 * kRowWaves);
+        run.shares = want < most ? want : most > 0 ? most : 1;
+        run.full = run.shares > 1 ? 0 : run.units;
+        return run;
+    }
+    // two workgroups on every CU; those beyond the last full round are divided, into pieces of four tiles at least
+    const int slots = 512, rest = run.units % slots, most = (length + 63) / 64 / 4;
+    run.full = run.units - rest;
+    int want = rest ? slots / rest : 1;
+    if (want > 8) want = 8;
+    run.shares = want < most ? want : most > 0 ? most : 1;
+    if (run.shares == 1) run.full = run.units;
+    return run;
 }
 
-size_t kvq_attention_scratch_floats(DType, int B, int n, int H, int heads, int Dh, int capacity)
+size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity)
 {
-    const int splits = kvq_splits(B, n, H, heads, capacity);
-    return splits > 1 ? (size_t)B * n * H * splits * (Dh + 2) : 0;
+    // shares never fall as the length grows: what the capacity needs is enough for every length
+    const KvqRun run = kvq_run(dt, B, n, H, heads, capacity);
+    return (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
 }
 
 template <typename T, int DH>
-static void launch_rows(const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, float c_log2, void *o,
-                        float *part, hipStream_t st)
+static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, float c_log2,
+                       void *o, float *part, hipStream_t st)
 {
-    const int nrb = (n * (H / c.heads) + 15) / 16;
-    const int splits = kvq_splits(B, n, H, c.heads, c.lens ? c.capacity : c.len + extra);
-    const size_t rows = (size_t)B * n * H;
-    float *part_ml = part + rows * splits * DH;
-    launch(kvq_attn_rows_kernel<T, DH, kRowWaves>, dim3((unsigned)((long)B * c.heads * splits * nrb)), dim3(64 * kRowWaves), 0, st,
-           (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, nrb, splits, part, part_ml);
-    if (splits > 1) {
-        const long total = (long)rows * (DH / 4);
+    const KvqRun run = kvq_run(dt, B, n, H, c.heads, c.lens ? c.capacity : c.len + extra);
+    const int divided = run.units - run.full;
+    float *part_ml = part + (size_t)divided * run.shares * run.block * DH;
+    const unsigned wgs = (unsigned)(run.full + divided * run.shares);
+    if (run.block == 16) {
+        launch(kvq_attn_rows_kernel<T, DH, kRowWaves>, dim3(wgs), dim3(64 * kRowWaves), 0, st, (const T *)q, ld, c, extra, n, H,
+               c_log2, (T *)o, run.nrb, run.shares, part, part_ml);
+    } else if constexpr (sizeof(T) == 2) {
+        launch(kvq_attn_tiles_kernel<DH>, dim3(wgs), dim3(256), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, run.nrb,
+               run.full, run.shares, part, part_ml);
+    }
+    if (divided) {
+        const long total = (long)divided * run.block * (DH / 4);
         launch(kvq_attn_merge_kernel<T, DH>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, (const float *)part,
-               (const float *)part_ml, n, H, c.heads, splits, c_log2, total, (T *)o);
+               (const float *)part_ml, n, H, c.heads, run.nrb, run.block, run.full, run.shares, c_log2, total, (T *)o);
     }
 }
 
@@ -420,11 +717,11 @@ void launch_kvq_attention(DType dt, const void *q, int ld, const KvqCache &c, in
 {
     const float c_log2 = scale * 1.4426950408889634f;
     if (dt == DType::BF16) {
-        if (Dh == 64) launch_rows<uint16_t, 64>(q, ld, c, extra, B, n, H, c_log2, o, part, st);
-        else launch_rows<uint16_t, 128>(q, ld, c, extra, B, n, H, c_log2, o, part, st);
+        if (Dh == 64) launch_kvq<uint16_t, 64>(dt, q, ld, c, extra, B, n, H, c_log2, o, part, st);
+        else launch_kvq<uint16_t, 128>(dt, q, ld, c, extra, B, n, H, c_log2, o, part, st);
     } else {
-        if (Dh == 64) launch_rows<float, 64>(q, ld, c, extra, B, n, H, c_log2, o, part, st);
-        else launch_rows<float, 128>(q, ld, c, extra, B, n, H, c_log2, o, part, st);
+        if (Dh == 64) launch_kvq<float, 64>(dt, q, ld, c, extra, B, n, H, c_log2, o, part, st);
+        else launch_kvq<float, 128>(dt, q, ld, c, extra, B, n, H, c_log2, o, part, st);
     }
 }
 

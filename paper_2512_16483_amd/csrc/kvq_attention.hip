@@ -229,7 +229,7 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
                     const bool seen = (vis >> ((64 * j + lane) / NB)) & 1;
                     if (seen && cur.vs[j] != 255) top = max(top, cur.vs[j]);
                 }
-                if (__any((int)top > E)) {                   // uniform: the largest block so far
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) {   // uniform: the largest block so far
                     const int now = (int)wave_max(top) + kRoom;
                     const float down = __builtin_amdgcn_ldexpf(1.f, max(E - now, -200));
                     E = now;
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
             float mx = s[0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i]);
-            if (__any(mx > m_ref + lag)) {
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_ref + lag) != 0, 0)) {
                 const float now = column_max(fmaxf(m_ref, mx));
                 const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
                 m_ref = now;
@@ -388,13 +388,15 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     const int G = H / c.heads, R = n * G;
     const int len = kvq_length(c, b, extra);
     const int tiles = (len + 63) / 64;
-    const int t0 = (int)((long)tiles * share / ranges), t1 = (int)((long)tiles * (share + 1) / ranges);
+    // tiles [t0, t1], one at least: where there is none, one in which nothing is seen
+    const int t0 = (int)((long)tiles * share / ranges), end = (int)((long)tiles * (share + 1) / ranges);
+    const int t1 = max(end - 1, t0), seen_end = min(len, end * 64), last_row = max(len - 1, 0);
     const int r0 = rb * 128 + wave * 32, row = min(r0 + rl, R - 1);
     const bool active = __builtin_amdgcn_readfirstlane(r0 < R ? 1 : 0) != 0;
 
     // ---- Q in three pieces of 6 bits: lane = row, block 2 s + g of its elements
     intx8_t qf[KS][3];
-    int qs[KS][3];
+    int qs[KS];                                              // scale bytes of the pieces, in byte 0, 1, 2
     {
         const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
 #pragma unroll
@@ -420,8 +422,8 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
 #pragma unroll
                 for (int i = 0; i < 16; ++i) { even[i] -= back[2 * i]; odd[i] -= back[2 * i + 1]; }
                 qf[s][p] = intx8_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
-                qs[s][p] = top >= 0x7f80u ? 255 : e - 5 * p;
             }
+            qs[s] = top >= 0x7f80u ? 0xffffff : e | (e - 5) << 8 | (e - 10) << 16;
         }
     }
 
@@ -438,14 +440,14 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     auto fetch_keys = [&](int t, Keys &x) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint32_t key = (uint32_t)min(t * 64 + 32 * u + rl, len - 1);
+            const uint32_t key = (uint32_t)min(t * 64 + 32 * u + rl, last_row);
 #pragma unroll
             for (int s = 0; s < KS; ++s) x.k[u][s] = *reinterpret_cast<const uint4 *>(Kc + key * (DH / 2) + (2 * s + g) * 16);
             x.ks[u] = NB == 4 ? *reinterpret_cast<const uint32_t *>(Ks + key * NB) : *reinterpret_cast<const uint16_t *>(Ks + key * NB);
         }
     };
     auto fetch_values = [&](int t, Values &x) {
-        const uint32_t key = (uint32_t)min(t * 64 + vkey, len - 1);
+        const uint32_t key = (uint32_t)min(t * 64 + vkey, last_row);
         if constexpr (VW == 4) {
             const uint4 w = *reinterpret_cast<const uint4 *>(Vc + key * (DH / 2) + vpart * 16);
             x.v[0] = w.x; x.v[1] = w.y; x.v[2] = w.z; x.v[3] = w.w;
@@ -455,9 +457,9 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
         }
         x.vs = Vs[key * NB + vpart * NB / 4];
         const int mine = t * 64 + lane;
-        const uint32_t held = (uint32_t)min(mine, len - 1);
+        const uint32_t held = (uint32_t)min(mine, last_row);
         x.all = NB == 4 ? *reinterpret_cast<const uint32_t *>(Vs + held * NB) : *reinterpret_cast<const uint16_t *>(Vs + held * NB);
-        x.seen = mine < len;
+        x.seen = mine < seen_end;
         if (mask) x.seen = x.seen && mask[held];
     };
 
@@ -477,10 +479,10 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     for (int i = 0; i < DB; ++i) acc[i] = floatx16_t{0};
     float m_ref = -INFINITY, l_run = 0.f;
     const float lag = kLag / c_log2;
-    int E = 0;
+    int E = 0, acc_E = 0;                                    // of the stage, of the sums
 
     // the values of a tile, converted, into a stage; the rows that can be seen
-    auto stage_values = [&](int t, const Values &x) -> unsigned long long {
+    auto stage_values = [&](int stage, const Values &x) -> unsigned long long {
         const unsigned long long vis = __ballot(x.seen != 0);
         uint32_t top = 0;
         if (x.seen) {
@@ -490,17 +492,9 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
                 if (byte != 255) top = max(top, byte);
             }
         }
-        if (__any((int)top > E)) {                           // the same in all wavefronts: the largest block so far
-            const int now = (int)wave_max(top) + kRoom;
-            const float down = __builtin_amdgcn_ldexpf(1.f, max(E - now, -200));
-            E = now;
-#pragma unroll
-            for (int i = 0; i < DB; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][e] *= down;
-        }
+        if (__any((int)top > E)) E = (int)wave_max(top) + kRoom;   // the same in all wavefronts: the largest block so far
         const float scale = half_scale(x.vs, E, (vis >> vkey) & 1);
-        uint16_t *dst = reinterpret_cast<uint16_t *>(vlds[t & 1]) + vkey * DH;
+        uint16_t *dst = reinterpret_cast<uint16_t *>(vlds[stage & 1]) + vkey * DH;
 #pragma unroll
         for (int i = 0; i < VW; ++i)
             *reinterpret_cast<uint4 *>(dst + (((vpart * VW + i) ^ turn(vkey)) << 3)) = half_eight(x.v[i], scale);
@@ -509,93 +503,111 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
 
     Keys keys;
     Values values;
-    unsigned long long vis = 0;
-    if (t0 < t1) {
-        fetch_keys(t0, keys);
-        fetch_values(t0, values);
-        vis = stage_values(t0, values);
-        if (t0 + 1 < t1) fetch_values(t0 + 1, values);
-    }
+    unsigned long long vis;
+    fetch_keys(t0, keys);
+    fetch_values(t0, values);
+    vis = stage_values(t0, values);
+    fetch_values(min(t0 + 1, t1), values);
     __syncthreads();
-    for (int t = t0; t < t1; ++t) {
+    if (!active) {                                           // rows past the end: only helps with the values
+        for (int t = t0; t <= t1; ++t) {
+            stage_values(t + 1, values);
+            fetch_values(min(t + 2, t1), values);
+            __syncthreads();
+        }
+        return;
+    }
+    // What is fetched for past the end is the last tile again, and what is staged then is not used: the loop has one way round.
+    int t = t0;
+    do {
         // ---- S^T
         floatx16_t s[2];
-        if (active) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            s[u] = floatx16_t{0};
+            const int sc = (int)(keys.ks[u] >> (8 * g));
+#define FVAR_S(ks, p)                                                                                                    \
+    s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(                                                              \
+        intx8_t{(int)keys.k[u][ks].x, (int)keys.k[u][ks].y, (int)keys.k[u][ks].z, (int)keys.k[u][ks].w, 0, 0, 0, 0},      \
+        qf[ks][p], s[u], 4, 2, 2 * (ks), sc, p, qs[ks])
+            FVAR_S(0, 2); FVAR_S(0, 1); FVAR_S(0, 0);
+            if constexpr (KS == 2) { FVAR_S(KS - 1, 2); FVAR_S(KS - 1, 1); FVAR_S(KS - 1, 0); }
+#undef FVAR_S
+        }
+        // ---- values of a step of 16 keys, fetched one step ahead of the products that use them
+        const uint16_t *vt = reinterpret_cast<const uint16_t *>(vlds[t & 1]);
+        f16x8_t vf[2][DB];
+        auto load_v = [&](int u, f16x8_t *x) {
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + chunk_at(i, 2 * u)));
+                const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + chunk_at(i, 2 * u + 1)));
+                x[i] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        };
+        load_v(0, vf[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        // ---- softmax
+        if (vis != ~0ull) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                s[u] = floatx16_t{0};
-                const int sc = (int)(keys.ks[u] >> (8 * g));
+                const uint32_t mine = (uint32_t)(vis >> (32 * u)) >> (4 * g);
 #pragma unroll
-                for (int p = 2; p >= 0; --p) {
-                    const intx8_t k0 = {(int)keys.k[u][0].x, (int)keys.k[u][0].y, (int)keys.k[u][0].z, (int)keys.k[u][0].w, 0, 0, 0, 0};
-                    s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k0, qf[0][p], s[u], 4, 2, 0, sc, 0, qs[0][p]);
-                    if constexpr (KS == 2) {
-                        const intx8_t k1 = {(int)keys.k[u][KS - 1].x, (int)keys.k[u][KS - 1].y, (int)keys.k[u][KS - 1].z, (int)keys.k[u][KS - 1].w, 0, 0, 0, 0};
-                        s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k1, qf[KS - 1][p], s[u], 4, 2, 2, sc, 0, qs[KS - 1][p]);
-                    }
-                }
+                for (int i = 0; i < 16; ++i)
+                    if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[u][i] = -INFINITY;
             }
         }
-        if (t + 1 < t1) fetch_keys(t + 1, keys);
-        if (active && vis) {
-            // ---- softmax
-            if (vis != ~0ull) {
+        float mx = s[0][0];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t mine = (uint32_t)(vis >> (32 * u)) >> (4 * g);
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[u][i] = -INFINITY;
-                }
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
+        const bool lags = __builtin_amdgcn_ballot_w64(mx > m_ref + lag) != 0 || E != acc_E;
+        if (__builtin_expect(lags, 0)) {
+            mx = fmaxf(m_ref, mx);
+            const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            const float now = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+            const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
+            const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E, -200));
+            m_ref = now;
+            acc_E = E;
+            l_run *= alpha;
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                acc[i] *= down;
+                asm volatile("" : "+v"(acc[i]));
             }
-            float mx = s[0][0];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
-            if (__any(mx > m_ref + lag)) {
-                mx = fmaxf(m_ref, mx);
-                const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                const float now = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-                const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
-                m_ref = now;
-                l_run *= alpha;
-#pragma unroll
-                for (int i = 0; i < DB; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[i][e] *= alpha;
-            }
-            const float base = fmaf(-fmaxf(m_ref, -1e30f), c_log2, kShift);
-            f16x8_t pf[4];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float p[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], c_log2, base));
-                    l_run += p[i];
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) pf[2 * u + (i >> 3)][i & 7] = (_Float16)p[i];
-            }
-            // ---- O^T += V^T P^T
-            const uint16_t *vt = reinterpret_cast<const uint16_t *>(vlds[t & 1]);
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < DB; ++i) {
-                    const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + chunk_at(i, 2 * u)));
-                    const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + chunk_at(i, 2 * u + 1)));
-                    const auto v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, v), pf[u], acc[i], 0, 0, 0);
-                }
         }
-        if (t + 1 < t1) {
-            vis = stage_values(t + 1, values);
-            if (t + 2 < t1) fetch_values(t + 2, values);
+        const float base = fmaf(-fmaxf(m_ref, -1e30f), c_log2, kShift);
+        f16x8_t pf[4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], c_log2, base));
+                l_run += p[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pf[2 * u + (i >> 3)][i & 7] = (_Float16)p[i];
+            asm volatile("" : "+v"(l_run));                  // added here: the weights are not kept until the loop's end
         }
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_keys(min(t + 1, t1), keys);                    // not before: the scores' registers are free only now
+        // ---- O^T += V^T P^T
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (u + 1 < 4) load_v(u + 1, vf[(u + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[u & 1][i], pf[u], acc[i], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        vis = stage_values(t + 1, values);
+        fetch_values(min(t + 2, t1), values);
         __syncthreads();
-    }
+    } while (++t <= t1);
 
     // ---- means, back at their size (see half_scale), which is stored or left with its weight for the merge
     {

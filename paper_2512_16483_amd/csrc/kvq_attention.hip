@@ -22,7 +22,7 @@ typedef __attribute__((address_space(3))) shortx4_t lds_shortx4_t;
 // 2^7 below the true maximum.  Next to bf16 operands (any exponent, 8 bits) the weights keep 11 bits, so that the
 // output's own rounding is the only one of note: 1.7e-3 against 2.4e-3 of the result.
 constexpr int kTop = 13, kRoom = 2;
-constexpr float kShift = 8.f, kLag = 7.f;
+constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
 
 __device__ __forceinline__ float half_scale(uint32_t byte, int E, bool seen)
 {
@@ -408,12 +408,12 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
             floatx16_t even, odd;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
-                even[i] = bf16_lo(w[i]);
-                odd[i] = bf16_hi(w[i]);
+                even[i] = bf16_lo(w[i]) * c_log2;
+                odd[i] = bf16_hi(w[i]) * c_log2;
+                top = max(top, max(__float_as_uint(even[i]) & 0x7fffffffu, __float_as_uint(odd[i]) & 0x7fffffffu));
             }
             // the smallest 2^e with all elements below 7.75 * 2^e, which round to at most 7.5; 255 makes NaN of what is not finite
-            const int e = min(max((int)((top + 8) >> 7) - 2, 13), 252);
+            const int e = min(max((int)((top + (1u << 19)) >> 23) - 2, 13), 252);
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
                 const float size = __uint_as_float((uint32_t)(e - 5 * p) << 23);
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
                 for (int i = 0; i < 16; ++i) { even[i] -= back[2 * i]; odd[i] -= back[2 * i + 1]; }
                 qf[s][p] = intx8_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
             }
-            qs[s] = top >= 0x7f80u ? 0xffffff : e | (e - 5) << 8 | (e - 10) << 16;
+            qs[s] = top >= 0x7f800000u ? 0xffffff : e | (e - 5) << 8 | (e - 10) << 16;
         }
     }
 
@@ -477,8 +477,11 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     floatx16_t acc[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = floatx16_t{0};
-    float m_ref = -INFINITY, l_run = 0.f;
-    const float lag = kLag / c_log2;
+    // Scores come in units of log2, with the reference subtracted: Q is scaled by c_log2 and the MFMAs start from -reference + kShift.
+    floatx16_t base;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) base[i] = kShift;
+    float m_ref = -INFINITY, l_run = 0.f, most = -1.f;       // most: the sum of a tile's weights from which on a reference is looked for
     int E = 0, acc_E = 0;                                    // of the stage, of the sums
 
     // the values of a tile, converted, into a stage; the rows that can be seen
@@ -520,21 +523,48 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     // What is fetched for past the end is the last tile again, and what is staged then is not used: the loop has one way round.
     int t = t0;
     do {
-        // ---- S^T
+        // ---- S^T, on top of `from`
         floatx16_t s[2];
+        auto scores = [&](const floatx16_t &from) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            s[u] = floatx16_t{0};
-            const int sc = (int)(keys.ks[u] >> (8 * g));
-#define FVAR_S(ks, p)                                                                                                    \
+            for (int u = 0; u < 2; ++u) {
+                const int sc = (int)(keys.ks[u] >> (8 * g));
+#define FVAR_S(ks, p, on)                                                                                                \
     s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(                                                              \
         intx8_t{(int)keys.k[u][ks].x, (int)keys.k[u][ks].y, (int)keys.k[u][ks].z, (int)keys.k[u][ks].w, 0, 0, 0, 0},      \
-        qf[ks][p], s[u], 4, 2, 2 * (ks), sc, p, qs[ks])
-            FVAR_S(0, 2); FVAR_S(0, 1); FVAR_S(0, 0);
-            if constexpr (KS == 2) { FVAR_S(KS - 1, 2); FVAR_S(KS - 1, 1); FVAR_S(KS - 1, 0); }
+        qf[ks][p], on, 4, 2, 2 * (ks), sc, p, qs[ks])
+                FVAR_S(0, 2, from); FVAR_S(0, 1, s[u]); FVAR_S(0, 0, s[u]);
+                if constexpr (KS == 2) { FVAR_S(KS - 1, 2, s[u]); FVAR_S(KS - 1, 1, s[u]); FVAR_S(KS - 1, 0, s[u]); }
 #undef FVAR_S
-        }
-        // ---- values of a step of 16 keys, fetched one step ahead of the products that use them
+            }
+            if (vis != ~0ull) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t mine = (uint32_t)(vis >> (32 * u)) >> (4 * g);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[u][i] = -INFINITY;
+                }
+            }
+        };
+        // ---- weights and their sum
+        f16x8_t pf[4];
+        float sum;
+        auto weigh = [&]() {
+            sum = 0.f;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const f16x2_t p = __builtin_convertvector(
+                        (floatx2_t{__builtin_amdgcn_exp2f(s[u][i]), __builtin_amdgcn_exp2f(s[u][i + 1])}), f16x2_t);
+                    sum = __builtin_amdgcn_fdot2(p, f16x2_t{(_Float16)1.f, (_Float16)1.f}, sum, false);
+                    pf[2 * u + (i >> 3)][i & 7] = p[0];
+                    pf[2 * u + (i >> 3)][(i & 7) + 1] = p[1];
+                }
+        };
+        scores(base);
+        // values of a step of 16 keys are fetched one step ahead of the products that use them
         const uint16_t *vt = reinterpret_cast<const uint16_t *>(vlds[t & 1]);
         f16x8_t vf[2][DB];
         auto load_v = [&](int u, f16x8_t *x) {
@@ -547,29 +577,25 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
         };
         load_v(0, vf[0]);
         __builtin_amdgcn_sched_barrier(0);
-        // ---- softmax
-        if (vis != ~0ull) {
+        weigh();
+        // The reference is not the running maximum but one that was it; the weights tell when it no longer serves.  A sum of NaN
+        // does not ask for another: it stays NaN.
+        const bool anew = (__builtin_amdgcn_ballot_w64(sum > most) != 0 && vis != 0) || E != acc_E;
+        if (__builtin_expect(anew, 0)) {
+            scores(floatx16_t{0});
+            float mx = s[0][0];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t mine = (uint32_t)(vis >> (32 * u)) >> (4 * g);
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[u][i] = -INFINITY;
-            }
-        }
-        float mx = s[0][0];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
-        const bool lags = __builtin_amdgcn_ballot_w64(mx > m_ref + lag) != 0 || E != acc_E;
-        if (__builtin_expect(lags, 0)) {
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
             mx = fmaxf(m_ref, mx);
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
             const float now = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-            const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
+            const bool none = now == -INFINITY;              // nothing finite yet
+            const float alpha = none ? 0.f : __builtin_amdgcn_exp2f(m_ref - now);
             const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E, -200));
             m_ref = now;
+            most = none ? -1.f : kMost;
             acc_E = E;
             l_run *= alpha;
 #pragma unroll
@@ -577,21 +603,13 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
                 acc[i] *= down;
                 asm volatile("" : "+v"(acc[i]));
             }
+            const float from = none ? kShift : kShift - now;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) base[i] = from;
+            scores(base);
+            weigh();
         }
-        const float base = fmaf(-fmaxf(m_ref, -1e30f), c_log2, kShift);
-        f16x8_t pf[4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            float p[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], c_log2, base));
-                l_run += p[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) pf[2 * u + (i >> 3)][i & 7] = (_Float16)p[i];
-            asm volatile("" : "+v"(l_run));                  // added here: the weights are not kept until the loop's end
-        }
+        l_run += sum;
         __builtin_amdgcn_sched_barrier(0);
         fetch_keys(min(t + 1, t1), keys);                    // not before: the scores' registers are free only now
         // ---- O^T += V^T P^T
@@ -630,7 +648,7 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
             if (ranges > 1) *reinterpret_cast<float4 *>(part_o + prow * DH + d) = v;
             else Quad<uint16_t>::store(dst + d, v);
         }
-    if (ranges > 1 && g == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m_ref, l_run);
+    if (ranges > 1 && g == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m_ref / c_log2, l_run);
 }
 
 // The shares of rows joined: each is a mean and its weight.  A unit is a block of BR rows of one (sample, kv head); the shares

@@ -4,6 +4,8 @@
 //
 // The query heads of one kv head are further rows of the same problem: row r of a (sample, kv head) is query r / G of
 // query head h' * G + r % G, G = H / heads.
+#include <type_traits>
+
 #include "common.h"
 
 namespace fvar {
@@ -12,9 +14,12 @@ typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef short shortx4_t __attribute__((ext_vector_type(4)));
 typedef int intx8_t __attribute__((ext_vector_type(8)));
+typedef unsigned uintx4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) const uintx4_t lds_uintx4_t;
 typedef unsigned uintx6_t __attribute__((ext_vector_type(6)));
 typedef float floatx32_t __attribute__((ext_vector_type(32)));
 typedef __attribute__((address_space(3))) shortx4_t lds_shortx4_t;
+typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 
 // Values as fp16 operands.  An fp16 number holds an element of the format times 2^-25 to 2^13, so a value goes in as
 // value * 2^(kTop - E), E the largest scale byte seen so far and two more: sums are rescaled when a byte exceeds E, which is
@@ -353,16 +358,28 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
     if (splits > 1 && wave == 0 && g4 == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m, sum);
 }
 
+// 16 bytes per lane global -> LDS; the wavefront fills 1 KiB starting at `lds_addr` in lane order.  The compiler does not see the
+// load: it is waited for by hand before a barrier.
+__device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_off, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(lds_addr), "v"(byte_off), "s"(base) : "memory", "m0");
+}
+
 // 128 rows per workgroup, 32 per wavefront, over tiles of 64 keys; bf16.  For the rows of a whole scale, where the matrix cores and the
 // softmax bound the time.
 //   S^T = K Q^T by the 32x32x64 block-scaled MFMA: it takes keys in 4 bits with their scale bytes as they lie in memory, so K is
-//     neither converted nor staged, and at four times the rate of bf16 where the other operand has 6 bits.  Q goes in as three E2M3
-//     numbers per element (sign, 2 bits of exponent, 3 of mantissa, a shared 2^e per 32), each for what the one before leaves and 2^-5
-//     smaller: off by at most 2^-13 of the block's largest element.  (Two leave 2^-8 of it, which scores of 20 and more, a
-//     few times the usual, show in the output.)
-//   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into one of two LDS stages.
-// In the 32x32 accumulator layout a lane owns a query column, so maximum and sum are lane-local, and P is in the order in which the
-// second product takes it, as in attention.hip.
+//     not converted, and at four times the rate of bf16 where the other operand has 6 bits.  Q, scaled so that scores come in units of
+//     log2, goes in as three E2M3 numbers per element (sign, 2 bits of exponent, 3 of mantissa, a shared 2^e per 32), each for
+//     what the one before leaves and 2^-5 smaller: off by at most 2^-13 of the block's largest element.  (Two leave 2^-8 of it,
+//     which scores of 20 and more, a few times the usual, show in the output.)
+//   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
+// In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
+// product takes it, as in attention.hip.
+// Tiles come by DMA two ahead, into one of three stages of LDS that hold a tile's codes, scales and converted values.
+// The loop goes by halves of a tile: beside the softmax of one stand the scores of the next and the products of the one before, in turn.
+// Matrix cores and vector unit overlap only for instructions that do not wait for each other and stand next to each other, and a
+// product that adds to the one right before it waits (a pair of weights 38 cycles, a product 40, both 58, 66 where they add on).
 template <int DH>
 __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
                                                                 int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,
@@ -371,7 +388,9 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
 {
     constexpr int KS = DH / 64, DB = DH / 32, NB = DH / 32;  // k64 steps of S, 32-row blocks of O^T, scale blocks of a row
     constexpr int VW = DH / 32;                              // words of values per thread
-    __shared__ uint4 vlds[2][64 * DH / 8];
+    constexpr int RAW = 64 * DH / 2;                         // bytes of a tile's codes
+    constexpr int KOFF = 64 * DH * 2, VOFF = KOFF + RAW, SOFF = VOFF + RAW, STAGE = SOFF + 2 * 64 * NB;
+    __shared__ uint4 lds[3 * STAGE / 16];                    // [stage][values fp16 | codes of K | of V | scales of K | of V]
 
     const int tid = threadIdx.x, lane = tid & 63, rl = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -430,202 +449,320 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     const size_t head = (size_t)(b * c.heads + hk) * c.capacity;
     const uint8_t *Kc = c.k + head * (DH / 2), *Vc = c.v + head * (DH / 2), *Ks = c.k_scale + head * NB, *Vs = c.v_scale + head * NB;
     const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
+    uint8_t *lds8 = reinterpret_cast<uint8_t *>(lds);
+    const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
 
-    // A tile of keys: every wavefront its own operands.  A tile of values: thread `tid` a quarter of a row, its scale byte; besides, every
-    // wavefront all scale bytes (lane = row), so that all of them see the same largest one.
-    struct Keys { uint4 k[2][KS]; uint32_t ks[2]; };
-    struct Values { uint32_t v[VW], vs, all, seen; };
-    // rows of a wavefront's sixteen in an order in which neighbouring quads' chunks lie in different banks (128-wide rows)
+    // ---- A tile by DMA.  K: 16-byte chunks of a row are turned by its number, so that the rows of sixteen lanes that read one chunk
+    // lie in all banks.  V: the order in which the threads convert it: a quarter of a row each, neighbouring quads four rows apart
+    // (128-wide rows) so that their writes lie in different banks.  A row past the last is the last again.
     const int vkey = DH == 128 ? wave * 16 + ((lane >> 4) & 3) + (lane >> 2 & 3) * 4 : tid >> 2, vpart = tid & 3;
-    auto fetch_keys = [&](int t, Keys &x) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint32_t key = (uint32_t)min(t * 64 + 32 * u + rl, last_row);
-#pragma unroll
-            for (int s = 0; s < KS; ++s) x.k[u][s] = *reinterpret_cast<const uint4 *>(Kc + key * (DH / 2) + (2 * s + g) * 16);
-            x.ks[u] = NB == 4 ? *reinterpret_cast<const uint32_t *>(Ks + key * NB) : *reinterpret_cast<const uint16_t *>(Ks + key * NB);
+    const int dwave = DH == 128 ? wave : wave & 1;           // 64-wide rows: two wavefronts fetch V, two K
+    const int krow = DH == 128 ? dwave * 16 + (lane >> 2) : dwave * 32 + (lane >> 1);
+    const int kchunk = DH == 128 ? (lane & 3) ^ ((krow >> 2) & 3) : (lane & 1) ^ ((krow >> 3) & 1);
+    const int vrow_d = DH == 128 ? vkey : krow, vchunk = DH == 128 ? vpart : lane & 1;
+    struct Next { uint32_t scale, seen; };                   // scales of the tile on their way to LDS (wavefront 0: K, 1: V); mask bytes
+    auto fetch = [&](int t, int stage, Next &x) {
+        const int first = t * 64;
+        uint32_t kr = (uint32_t)(first + krow), vr = (uint32_t)(first + vrow_d), sr = (uint32_t)(first + lane);
+        if (first + 64 > len) {                              // uniform: the last tile
+            kr = min(kr, (uint32_t)last_row);
+            vr = min(vr, (uint32_t)last_row);
+            sr = min(sr, (uint32_t)last_row);
+        }
+        const uint32_t at = lds_base + stage * STAGE + dwave * 1024;
+        if (DH == 128 || wave >= 2) tile_dma_b128(Kc, kr * (DH / 2) + kchunk * 16, at + KOFF);
+        if (DH == 128 || wave < 2) tile_dma_b128(Vc, vr * (DH / 2) + vchunk * 16, at + VOFF);
+        if (wave < 2) {
+            const uint8_t *src = wave ? Vs : Ks;
+            x.scale = NB == 4 ? *reinterpret_cast<const uint32_t *>(src + sr * NB) : *reinterpret_cast<const uint16_t *>(src + sr * NB);
+        }
+        if (mask) x.seen = mask[sr];
+    };
+    auto put_scales = [&](int stage, const Next &x) {
+        if (wave < 2) {
+            uint8_t *dst = lds8 + stage * STAGE + SOFF + wave * (64 * NB) + lane * NB;
+            if (NB == 4) *reinterpret_cast<uint32_t *>(dst) = x.scale;
+            else *reinterpret_cast<uint16_t *>(dst) = (uint16_t)x.scale;
         }
     };
-    auto fetch_values = [&](int t, Values &x) {
-        const uint32_t key = (uint32_t)min(t * 64 + vkey, last_row);
-        if constexpr (VW == 4) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(Vc + key * (DH / 2) + vpart * 16);
-            x.v[0] = w.x; x.v[1] = w.y; x.v[2] = w.z; x.v[3] = w.w;
-        } else {
-            const uint2 w = *reinterpret_cast<const uint2 *>(Vc + key * (DH / 2) + vpart * 8);
-            x.v[0] = w.x; x.v[1] = w.y;
-        }
-        x.vs = Vs[key * NB + vpart * NB / 4];
-        const int mine = t * 64 + lane;
-        const uint32_t held = (uint32_t)min(mine, last_row);
-        x.all = NB == 4 ? *reinterpret_cast<const uint32_t *>(Vs + held * NB) : *reinterpret_cast<const uint16_t *>(Vs + held * NB);
-        x.seen = mine < seen_end;
-        if (mask) x.seen = x.seen && mask[held];
+    // everything on its way to LDS is there, for all wavefronts
+    auto meet = [&]() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
     };
 
-    // ---- LDS: 16-byte chunks of a row are turned so that four rows' 64-byte quarters lie in different banks when they are read
+    // ---- values: chunks of a row are turned so that four rows' 64-byte quarters lie in different banks when they are read
     // (transposing load, as in attention.hip), and the chunks of neighbouring quads of lanes when they are written
     auto turn = [](int key) { return DH == 128 ? ((key & 3) << 2) | ((key >> 2) & 3) : ((key >> 1) & 1) << 2; };
     const int tG = lane >> 4, tj = (lane >> 2) & 3, ta = lane & 3;
     const int vrow = 4 * (tG >> 1) + tj;
-    // chunk 4 db + 2 (tG & 1) + (ta >> 1) of row vrow + 16 u + 8 h: `turn` of the row in two parts, h and u only in the low bits
+    // chunk 4 db + 2 (tG & 1) + (ta >> 1) of row vrow + 8 step8, in bytes
     auto chunk_at = [&](int db, int step8) {
         const int key = vrow + 8 * step8;
-        return key * DH + (((4 * db + 2 * (tG & 1) + (ta >> 1)) ^ turn(key)) << 3) + (ta & 1) * 4;
+        return (key * DH + (((4 * db + 2 * (tG & 1) + (ta >> 1)) ^ turn(key)) << 3) + (ta & 1) * 4) * 2;
     };
 
     floatx16_t acc[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = floatx16_t{0};
-    // Scores come in units of log2, with the reference subtracted: Q is scaled by c_log2 and the MFMAs start from -reference + kShift.
-    floatx16_t base;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) base[i] = kShift;
-    float m_ref = -INFINITY, l_run = 0.f, most = -1.f;       // most: the sum of a tile's weights from which on a reference is looked for
-    int E = 0, acc_E = 0;                                    // of the stage, of the sums
+    float m_ref = -INFINITY, l_run = 0.f, most = -1.f;       // most: the sum of weights from which on a reference is looked for
+    float base = kShift;                                     // - reference + kShift, in units of log2 as the scores
+    int E = 0, E_now = 0, acc_E = 0;                         // of the values converted last, of the tile at work, of the sums
 
-    // the values of a tile, converted, into a stage; the rows that can be seen
-    auto stage_values = [&](int stage, const Values &x) -> unsigned long long {
-        const unsigned long long vis = __ballot(x.seen != 0);
+    // A thread's values as they came, and their scale byte; all scale bytes of the lane's row.  The rows that can be seen, and the
+    // size of the values: E is the same in all wavefronts, each of which sees all bytes.
+    struct Raw { uint32_t v[VW], vs, all; };
+    auto read_raw = [&](int stage, Raw &x) {
+        const uint8_t *src = lds8 + stage * STAGE;
+        if constexpr (VW == 4) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(src + VOFF + tid * 16);
+            x.v[0] = w.x; x.v[1] = w.y; x.v[2] = w.z; x.v[3] = w.w;
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2 *>(src + VOFF + tid * 8);
+            x.v[0] = w.x; x.v[1] = w.y;
+        }
+        const uint8_t *sc = src + SOFF + 64 * NB;
+        x.vs = sc[vkey * NB + vpart * NB / 4];
+        x.all = NB == 4 ? *reinterpret_cast<const uint32_t *>(sc + lane * NB) : *reinterpret_cast<const uint16_t *>(sc + lane * NB);
+    };
+    float scale;
+    auto look = [&](int t, const Raw &x, const Next &f) -> unsigned long long {
+        const bool seen = t * 64 + lane < seen_end && (!mask || f.seen);
+        const unsigned long long vis = __ballot(seen);
         uint32_t top = 0;
-        if (x.seen) {
+        if (seen) {
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 const uint32_t byte = x.all >> (8 * i) & 255;
                 if (byte != 255) top = max(top, byte);
             }
         }
-        if (__any((int)top > E)) E = (int)wave_max(top) + kRoom;   // the same in all wavefronts: the largest block so far
-        const float scale = half_scale(x.vs, E, (vis >> vkey) & 1);
-        uint16_t *dst = reinterpret_cast<uint16_t *>(vlds[stage & 1]) + vkey * DH;
-#pragma unroll
-        for (int i = 0; i < VW; ++i)
-            *reinterpret_cast<uint4 *>(dst + (((vpart * VW + i) ^ turn(vkey)) << 3)) = half_eight(x.v[i], scale);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) E = (int)wave_max(top) + kRoom;
+        scale = half_scale(x.vs, E, (vis >> vkey) & 1);
         return vis;
     };
+    int vdst[VW];                                            // where the thread's words go, in bytes
+#pragma unroll
+    for (int i = 0; i < VW; ++i) vdst[i] = (vkey * DH + (((vpart * VW + i) ^ turn(vkey)) << 3)) * 2;
+    auto convert = [&](int stage, const Raw &x, int i) {
+        *reinterpret_cast<uint4 *>(lds8 + stage * STAGE + vdst[i]) = half_eight(x.v[i], scale);
+    };
 
-    Keys keys;
-    Values values;
-    unsigned long long vis;
-    fetch_keys(t0, keys);
-    fetch_values(t0, values);
-    vis = stage_values(t0, values);
-    fetch_values(min(t0 + 1, t1), values);
-    __syncthreads();
-    if (!active) {                                           // rows past the end: only helps with the values
+    Next next;
+    Raw raw;
+    fetch(t0, 0, next);
+    put_scales(0, next);
+    meet();
+    read_raw(0, raw);
+    unsigned long long vis = look(t0, raw, next), vis_next;
+#pragma unroll
+    for (int i = 0; i < VW; ++i) convert(0, raw, i);
+    fetch(min(t0 + 1, t1), 1, next);
+    put_scales(1, next);
+    meet();
+    int stage = 0;                                           // of the tile at work
+    auto after = [](int s) { return s == 2 ? 0 : s + 1; };
+    Next later;
+    if (!active) {                                           // rows past the end: only helps with the tiles
         for (int t = t0; t <= t1; ++t) {
-            stage_values(t + 1, values);
-            fetch_values(min(t + 2, t1), values);
-            __syncthreads();
+            const int s1 = after(stage);
+            fetch(min(t + 2, t1), after(s1), later);
+            read_raw(s1, raw);
+            look(min(t + 1, t1), raw, next);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) convert(s1, raw, i);
+            put_scales(after(s1), later);
+            next = later;
+            stage = s1;
+            meet();
         }
         return;
     }
-    // What is fetched for past the end is the last tile again, and what is staged then is not used: the loop has one way round.
-    int t = t0;
-    do {
-        // ---- S^T, on top of `from`
-        floatx16_t s[2];
-        auto scores = [&](const floatx16_t &from) {
+
+    // Where the lane reads values of the first 16 keys of a tile, and the first 32 keys; further on by constants.
+    lds_byte_t *vp[DB][2], *kp[KS], *sp;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int sc = (int)(keys.ks[u] >> (8 * g));
-#define FVAR_S(ks, p, on)                                                                                                \
-    s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(                                                              \
-        intx8_t{(int)keys.k[u][ks].x, (int)keys.k[u][ks].y, (int)keys.k[u][ks].z, (int)keys.k[u][ks].w, 0, 0, 0, 0},      \
-        qf[ks][p], on, 4, 2, 2 * (ks), sc, p, qs[ks])
-                FVAR_S(0, 2, from); FVAR_S(0, 1, s[u]); FVAR_S(0, 0, s[u]);
-                if constexpr (KS == 2) { FVAR_S(KS - 1, 2, s[u]); FVAR_S(KS - 1, 1, s[u]); FVAR_S(KS - 1, 0, s[u]); }
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) vp[i][h] = (lds_byte_t *)(lds8 + chunk_at(i, h));
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+        kp[s] = (lds_byte_t *)(lds8 + KOFF + rl * (DH / 2) + ((2 * s + g) ^ (DH == 128 ? (rl >> 2) & 3 : (rl >> 3) & 1)) * 16);
+    sp = (lds_byte_t *)(lds8 + SOFF + rl * NB);
+
+    floatx16_t s[2];                                         // scores of the two halves of a tile
+    f16x8_t pf[2][2];                                        // their weights, by steps of 16 keys
+    float sum;
+    pf[1][0] = pf[1][1] = f16x8_t{0};
+    auto load_keys = [&](int half, uintx4_t *k) -> int {
+#pragma unroll
+        for (int x = 0; x < KS; ++x) k[x] = *(lds_uintx4_t *)(kp[x] + half * (RAW / 2));
+        const uint32_t w = NB == 4 ? *(__attribute__((address_space(3))) const uint32_t *)(sp + half * 32 * NB)
+                                   : *(__attribute__((address_space(3))) const uint16_t *)(sp + half * 32 * NB);
+        return (int)(w >> (8 * g));
+    };
+#define FVAR_S(half, ks, p, on)                                                                                          \
+    s[half] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(                                                           \
+        intx8_t{(int)k[ks][0], (int)k[ks][1], (int)k[ks][2], (int)k[ks][3], 0, 0, 0, 0}, qf[ks][p], on, 4, 2, 2 * (ks), sc, p, qs[ks])
+    // product number i of a half's scores: smallest pieces first
+    auto score = [&](int half, int i, const uintx4_t *k, int sc) {
+        if (i == 0) FVAR_S(half, 0, 2, floatx16_t{0});
+        if (i == 1) FVAR_S(half, KS - 1, KS == 2 ? 2 : 1, s[half]);
+        if (i == 2) FVAR_S(half, 0, KS == 2 ? 1 : 0, s[half]);
+        if constexpr (KS == 2) {
+            if (i == 3) FVAR_S(half, 1, 1, s[half]);
+            if (i == 4) FVAR_S(half, 0, 0, s[half]);
+            if (i == 5) FVAR_S(half, 1, 0, s[half]);
+        }
+    };
 #undef FVAR_S
-            }
-            if (vis != ~0ull) {
+    auto load_v = [&](int i, int rows) -> f16x8_t {
+        const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vp[i][0] + rows * DH * 2));
+        const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vp[i][1] + rows * DH * 2));
+        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // One half's softmax beside the scores of the other (of the next tile where that is the first) and the products of the other's
+    // weights (of the tile before where that is the second).  A step: a product, the weights of a pair or two in three stages.
+    auto region = [&](auto which, int s1) {
+        constexpr int half = decltype(which)::value, other = 1 - half;
+        constexpr int NS = 3 * KS, NPV = 2 * DB, STEPS = NS + NPV, PP = DH == 128 ? 1 : 2;     // PP: pairs of weights per step
+        uintx4_t k[KS];
+        f16x8_t vf[DB];
+        const int sc = load_keys(other, k);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t mine = (uint32_t)(vis >> (32 * u)) >> (4 * g);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[u][i] = -INFINITY;
-                }
-            }
-        };
-        // ---- weights and their sum
-        f16x8_t pf[4];
-        float sum;
-        auto weigh = [&]() {
-            sum = 0.f;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const f16x2_t p = __builtin_convertvector(
-                        (floatx2_t{__builtin_amdgcn_exp2f(s[u][i]), __builtin_amdgcn_exp2f(s[u][i + 1])}), f16x2_t);
-                    sum = __builtin_amdgcn_fdot2(p, f16x2_t{(_Float16)1.f, (_Float16)1.f}, sum, false);
-                    pf[2 * u + (i >> 3)][i & 7] = p[0];
-                    pf[2 * u + (i >> 3)][(i & 7) + 1] = p[1];
-                }
-        };
-        scores(base);
-        // values of a step of 16 keys are fetched one step ahead of the products that use them
-        const uint16_t *vt = reinterpret_cast<const uint16_t *>(vlds[t & 1]);
-        f16x8_t vf[2][DB];
-        auto load_v = [&](int u, f16x8_t *x) {
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + chunk_at(i, 2 * u)));
-                const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + chunk_at(i, 2 * u + 1)));
-                x[i] = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
-        };
-        load_v(0, vf[0]);
+        for (int i = 0; i < DB; ++i) vf[i] = load_v(i, other * 32);
+        if constexpr (half == 0) read_raw(s1, raw);
         __builtin_amdgcn_sched_barrier(0);
-        weigh();
+        float x[16], a = 0.f, bsum = 0.f;
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step) {
+            const int before = min((step + 1) / 2, NS);      // scores' products up to here, this one included if it is one
+            if ((step & 1) && step / 2 < NS) {
+                score(other, step / 2, k, sc);
+            } else {
+                const int i = step - before;
+                acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i % DB], pf[other][i / DB], acc[i % DB], 0, 0, 0);
+                if (i < DB) vf[i] = load_v(i, other * 32 + 16);
+            }
+#pragma unroll
+            for (int w = 0; w < PP; ++w) {
+                const int p2 = (step - 2) * PP + w, p1 = (step - 1) * PP + w, p0 = step * PP + w;
+                if (p1 >= 0 && p1 < 8) {
+                    x[2 * p1] = __builtin_amdgcn_exp2f(x[2 * p1]);
+                    x[2 * p1 + 1] = __builtin_amdgcn_exp2f(x[2 * p1 + 1]);
+                }
+                if (p0 < 8) {
+                    x[2 * p0] = s[half][2 * p0] + base;
+                    x[2 * p0 + 1] = s[half][2 * p0 + 1] + base;
+                }
+                if (p2 >= 0 && p2 < 8) {
+                    a += x[2 * p2];
+                    bsum += x[2 * p2 + 1];
+                    const f16x2_t p = __builtin_convertvector((floatx2_t{x[2 * p2], x[2 * p2 + 1]}), f16x2_t);
+                    pf[half][p2 >> 2][(2 * p2) & 7] = p[0];
+                    pf[half][p2 >> 2][(2 * p2 + 1) & 7] = p[1];
+                }
+            }
+            if constexpr (half == 1) {
+                constexpr int from = DH == 128 ? 8 : 4;
+                if (step >= from && step - from < VW) convert(s1, raw, step - from);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum = a + bsum;
+        // the region's results are made in it
+        asm volatile("" : "+v"(pf[half][0]), "+v"(pf[half][1]), "+v"(sum));
+        asm volatile("" : "+v"(s[other]));
+#pragma unroll
+        for (int i = 0; i < DB; ++i) asm volatile("" : "+v"(acc[i]));
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto hide = [&](int half) {
+        const uint32_t part = (uint32_t)(vis >> (32 * half));
+        if (__builtin_expect(part != ~0u, 0)) {
+            const uint32_t mine = part >> (4 * g);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[half][i] = -INFINITY;
+        }
+    };
+    auto settle = [&](int half) {
         // The reference is not the running maximum but one that was it; the weights tell when it no longer serves.  A sum of NaN
         // does not ask for another: it stays NaN.
-        const bool anew = (__builtin_amdgcn_ballot_w64(sum > most) != 0 && vis != 0) || E != acc_E;
+        const bool anew = (__builtin_amdgcn_ballot_w64(sum > most) != 0 && (uint32_t)(vis >> (32 * half)) != 0) || E_now != acc_E;
         if (__builtin_expect(anew, 0)) {
-            scores(floatx16_t{0});
-            float mx = s[0][0];
+            float mx = s[half][0];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
             mx = fmaxf(m_ref, mx);
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
             const float now = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
             const bool none = now == -INFINITY;              // nothing finite yet
             const float alpha = none ? 0.f : __builtin_amdgcn_exp2f(m_ref - now);
-            const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E, -200));
+            const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E_now, -200));
             m_ref = now;
             most = none ? -1.f : kMost;
-            acc_E = E;
+            acc_E = E_now;
+            base = none ? kShift : kShift - now;
             l_run *= alpha;
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
                 acc[i] *= down;
                 asm volatile("" : "+v"(acc[i]));
             }
-            const float from = none ? kShift : kShift - now;
+            sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) base[i] = from;
-            scores(base);
-            weigh();
+            for (int i = 0; i < 16; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(s[half][i] + base), y = __builtin_amdgcn_exp2f(s[half][i + 1] + base);
+                sum += x + y;
+                const f16x2_t p = __builtin_convertvector((floatx2_t{x, y}), f16x2_t);
+                pf[half][i >> 3][i & 7] = p[0];
+                pf[half][i >> 3][(i & 7) + 1] = p[1];
+            }
         }
         l_run += sum;
-        __builtin_amdgcn_sched_barrier(0);
-        fetch_keys(min(t + 1, t1), keys);                    // not before: the scores' registers are free only now
-        // ---- O^T += V^T P^T
+    };
+
+    {
+        uintx4_t k[KS];
+        const int sc = load_keys(0, k);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (u + 1 < 4) load_v(u + 1, vf[(u + 1) & 1]);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < 3 * KS; ++i) score(0, i, k, sc);
+    }
+    E_now = E;
+    int t = t0;
+    do {
+        const int s1 = after(stage), s2 = after(s1);
+        fetch(min(t + 2, t1), s2, later);
+        hide(0);
+        region(std::integral_constant<int, 0>{}, s1);
+        settle(0);
+        {
+            // values go on to this tile's stage, keys to the next's
+            const int by = (stage == 0 ? -2 : 1) * STAGE, k_by = (s1 == 0 ? -2 : 1) * STAGE, v_by = t == t0 ? 0 : by;
 #pragma unroll
-            for (int i = 0; i < DB; ++i)
-                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[u & 1][i], pf[u], acc[i], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < DB; ++i) { vp[i][0] += v_by; vp[i][1] += v_by; }
+#pragma unroll
+            for (int i = 0; i < KS; ++i) kp[i] += k_by;
+            sp += k_by;
         }
-        vis = stage_values(t + 1, values);
-        fetch_values(min(t + 2, t1), values);
-        __syncthreads();
+        hide(1);
+        vis_next = look(min(t + 1, t1), raw, next);
+        region(std::integral_constant<int, 1>{}, s1);
+        settle(1);
+        put_scales(s2, later);
+        next = later;
+        vis = vis_next;
+        stage = s1;
+        E_now = E;
+        meet();
     } while (++t <= t1);
+    // the last half's products
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(load_v(i, 32 + 16 * u), pf[1][u], acc[i], 0, 0, 0);
 
     // ---- means, back at their size (see half_scale), which is stored or left with its weight for the merge
     {
@@ -641,10 +778,10 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             const int d = 32 * i + 8 * (e >> 2) + 4 * g;
-            const float4 v = make_float4(__builtin_amdgcn_ldexpf(acc[i][e] * inv, E - kTop - 127),
-                                         __builtin_amdgcn_ldexpf(acc[i][e + 1] * inv, E - kTop - 127),
-                                         __builtin_amdgcn_ldexpf(acc[i][e + 2] * inv, E - kTop - 127),
-                                         __builtin_amdgcn_ldexpf(acc[i][e + 3] * inv, E - kTop - 127));
+            const float4 v = make_float4(__builtin_amdgcn_ldexpf(acc[i][e] * inv, acc_E - kTop - 127),
+                                         __builtin_amdgcn_ldexpf(acc[i][e + 1] * inv, acc_E - kTop - 127),
+                                         __builtin_amdgcn_ldexpf(acc[i][e + 2] * inv, acc_E - kTop - 127),
+                                         __builtin_amdgcn_ldexpf(acc[i][e + 3] * inv, acc_E - kTop - 127));
             if (ranges > 1) *reinterpret_cast<float4 *>(part_o + prow * DH + d) = v;
             else Quad<uint16_t>::store(dst + d, v);
         }

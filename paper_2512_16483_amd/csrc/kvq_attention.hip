@@ -104,6 +104,17 @@ template <> struct Quad<float> {
     __device__ static __forceinline__ void store(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
 };
 
+// Workgroup `id` -> one of `groups` groups of `size`: the workgroups of a group on one XCD (id % 8), whose L2 they share, and neighbouring
+// groups on different ones, so that long samples next to each other do not meet on one.  (Contiguous shares of the numbering for
+// each XCD: 79 us instead of 60 for 32 samples of 1 to 16921 keys.)
+__device__ __forceinline__ int xcd_grouped(int id, int groups, int size)
+{
+    const int even = groups & ~7;                            // the last few groups stay as they are numbered
+    if (id >= even * size) return id;
+    const int pos = id >> 3;
+    return (pos / size * 8 + (id & 7)) * size + pos % size;
+}
+
 // Sixteen rows per workgroup, whose wavefronts take every NW-th tile of 32 keys of the workgroup's share [t0, t1) of the
 // key axis, each with a softmax of its own, and meet in LDS at the end.  For the rows of one query or a few, where the
 // cache's way from memory is what counts (each wavefront fetches a tile ahead, no barrier in the loop), and for fp32, where the
@@ -114,7 +125,7 @@ template <> struct Quad<float> {
 //     row, from where the transposing load brings eight keys of one head-dim element; P is in that order already.
 // fp32: Q and P go in as three bf16 numbers each, K and V are exact in one.
 template <typename T, int DH, int NW>
-__global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restrict__ q, int ld, KvqCache c, int extra,
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows_kernel(const T *__restrict__ q, int ld, KvqCache c, int extra,
                                                                 int n, int H, float c_log2, T *__restrict__ o,
                                                                 int nrb, int splits, float *__restrict__ part_o,
                                                                 float *__restrict__ part_ml)
@@ -129,7 +140,7 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
 
     const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int unit = xcd_contiguous(blockIdx.x, gridDim.x);        // the row blocks of a head share an L2
+    int unit = xcd_grouped(blockIdx.x, (int)(gridDim.x / nrb), nrb);
     const int rb = unit % nrb;
     unit /= nrb;
     const int split = unit % splits;
@@ -139,6 +150,7 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
     const int len = kvq_length(c, b, extra);
     const int tiles = (len + 31) / 32;
     const int t0 = (int)((long)tiles * split / splits), t1 = (int)((long)tiles * (split + 1) / splits);
+    const int last = max(tiles - 1, 0), last_row = max(len - 1, 0);
 
     // ---- Q: lane = row, the elements of the lane's part of a key
     const int row = min(rb * 16 + c16, R - 1);
@@ -169,7 +181,7 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
         const int base = t * 32;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint32_t key = (uint32_t)min(base + 16 * u + c16, len - 1);
+            const uint32_t key = (uint32_t)min(base + 16 * u + c16, last_row);
             if constexpr (KW == 4) {
                 const uint4 w = *reinterpret_cast<const uint4 *>(Kc + key * (DH / 2) + g4 * 16);
                 x.k[u][0] = w.x; x.k[u][1] = w.y; x.k[u][2] = w.z; x.k[u][3] = w.w;
@@ -181,13 +193,13 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
         }
 #pragma unroll
         for (int j = 0; j < VL; ++j) {
-            const uint32_t key = (uint32_t)min(base + (64 * j + lane) / NB, len - 1), blk = lane % NB;
+            const uint32_t key = (uint32_t)min(base + (64 * j + lane) / NB, last_row), blk = lane % NB;
             x.v[j] = *reinterpret_cast<const uint4 *>(Vc + key * (DH / 2) + blk * 16);
             x.vs[j] = Vs[key * NB + blk];
         }
         const int key = base + (lane & 31);
         x.seen = key < len;
-        if (mask) x.seen = x.seen && mask[min(key, len - 1)];
+        if (mask) x.seen = x.seen && mask[min(key, last_row)];
     };
 
     // ---- LDS: 32-byte pieces of a row are turned by its number, so that eight rows' pieces of one column lie in different banks
@@ -201,119 +213,115 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
     for (int i = 0; i < DB; ++i) acc[i] = floatx4_t{0};
     float m_ref = -INFINITY, l_run = 0.f;
     const float lag = kLag / c_log2;
-    int E = 0;
+    int E = 0, acc_E = 0;                                    // of the values, of the sums
 
-    Tile cur, nxt;
-    if (t0 + wave < t1) fetch(t0 + wave, cur);
-    for (int t = t0 + wave; t < t1; t += NW) {
-        const bool more = t + NW < t1;
-        if (more) fetch(t + NW, nxt);
-        const uint32_t vis = (uint32_t)__ballot(cur.seen != 0);
-        if (vis) {
-            // ---- S^T: lane (c16, g4) gets the keys 4 g4 .. + 3 and 16 more of row c16
-            float s[8];
+    // A tile's keys and values are converted first; the next one's are then fetched into the same registers, under the softmax and the
+    // products.  A wavefront without a tile looks at one in which it sees nothing.
+    Tile x;
+    int t = t0 + wave;
+    fetch(min(t, last), x);
+    do {
+        const uint32_t vis = (uint32_t)__ballot(x.seen != 0 && t < t1);
+        // ---- S^T: lane (c16, g4) gets the keys 4 g4 .. + 3 and 16 more of row c16
+        floatx4_t s[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                floatx4_t a = {0};
-                const float scale = __uint_as_float(cur.ks[u] << 23);
+        for (int u = 0; u < 2; ++u) {
+            s[u] = floatx4_t{0};
+            const float scale = __uint_as_float(x.ks[u] << 23);
 #pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, bf16_eight(cur.k[u][i], scale));
+            for (int i = 0; i < KS; ++i) {
+                const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, bf16_eight(x.k[u][i], scale));
 #pragma unroll
-                    for (int p = NP - 1; p >= 0; --p)
-                        a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][p], a, 0, 0, 0);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[4 * u + i] = a[i];
+                for (int p = NP - 1; p >= 0; --p)
+                    s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][p], s[u], 0, 0, 0);
             }
-            // ---- values to LDS
-            if constexpr (!F32) {
-                uint32_t top = 0;
-#pragma unroll
-                for (int j = 0; j < VL; ++j) {
-                    const bool seen = (vis >> ((64 * j + lane) / NB)) & 1;
-                    if (seen && cur.vs[j] != 255) top = max(top, cur.vs[j]);
-                }
-                if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) {   // uniform: the largest block so far
-                    const int now = (int)wave_max(top) + kRoom;
-                    const float down = __builtin_amdgcn_ldexpf(1.f, max(E - now, -200));
-                    E = now;
-#pragma unroll
-                    for (int i = 0; i < DB; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][e] *= down;
-                }
-            }
+        }
+        // ---- values to LDS
+        if constexpr (!F32) {
+            uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < VL; ++j) {
-                const int key = (64 * j + lane) / NB, blk = lane % NB;
-                const bool seen = (vis >> key) & 1;
-                const uint32_t w[4] = {cur.v[j].x, cur.v[j].y, cur.v[j].z, cur.v[j].w};
-                const float scale = F32 ? (seen ? __uint_as_float(cur.vs[j] << 23) : 0.f) : half_scale(cur.vs[j], E, seen);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int piece = (2 * blk + (i >> 1)) ^ turn(key);
-                    *reinterpret_cast<uint4 *>(vl + key * DH + piece * 16 + (i & 1) * 8) = F32 ? bf16_eight(w[i], scale) : half_eight(w[i], scale);
-                }
+                const bool seen = (vis >> ((64 * j + lane) / NB)) & 1;
+                if (seen && x.vs[j] != 255) top = max(top, x.vs[j]);
             }
-            // ---- softmax
-            if (vis != ~0u) {
-                const uint32_t mine = vis >> (4 * g4);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) E = (int)wave_max(top) + kRoom;
+        }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (!(mine >> i & 1)) s[i] = -INFINITY;
-                    if (!(mine >> (16 + i) & 1)) s[4 + i] = -INFINITY;
-                }
+        for (int j = 0; j < VL; ++j) {
+            const int key = (64 * j + lane) / NB, blk = lane % NB;
+            const bool seen = (vis >> key) & 1;
+            const uint32_t w[4] = {x.v[j].x, x.v[j].y, x.v[j].z, x.v[j].w};
+            const float scale = F32 ? (seen ? __uint_as_float(x.vs[j] << 23) : 0.f) : half_scale(x.vs[j], E, seen);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int piece = (2 * blk + (i >> 1)) ^ turn(key);
+                *reinterpret_cast<uint4 *>(vl + key * DH + piece * 16 + (i & 1) * 8) = F32 ? bf16_eight(w[i], scale) : half_eight(w[i], scale);
             }
-            float mx = s[0];
+        }
+        t += NW;
+        fetch(min(t, last), x);
+        // ---- softmax
+        if (__builtin_expect(vis != ~0u, 0)) {
+            const uint32_t mine = vis >> (4 * g4);
 #pragma unroll
-            for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i]);
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_ref + lag) != 0, 0)) {
-                const float now = column_max(fmaxf(m_ref, mx));
-                const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
-                m_ref = now;
-                l_run *= alpha;
-#pragma unroll
-                for (int i = 0; i < DB; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][e] *= alpha;
+            for (int i = 0; i < 4; ++i) {
+                if (!(mine >> i & 1)) s[0][i] = -INFINITY;
+                if (!(mine >> (16 + i) & 1)) s[1][i] = -INFINITY;
             }
-            const float fin = fmaxf(m_ref, -1e30f), base = fmaf(-fin, c_log2, kShift);
-            float p[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                // fp32: the difference first, so that a row's only key weighs exactly 1
-                p[i] = __builtin_amdgcn_exp2f(F32 ? (s[i] - fin) * c_log2 : fmaf(s[i], c_log2, base));
-                l_run += p[i];
-            }
-            // ---- O^T += V^T P^T
-            bf16x8_t pf[NP];
-            f16x8_t ph;
-            if constexpr (F32) {
-                three_pieces(p, pf);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ph[i] = (_Float16)p[i];
-            }
-            asm volatile("" ::: "memory");
+        }
+        const float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        const bool lags = __builtin_amdgcn_ballot_w64(mx > m_ref + lag) != 0 || E != acc_E;
+        if (__builtin_expect(lags, 0)) {
+            const float now = column_max(fmaxf(m_ref, mx));
+            const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
+            const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E, -200));
+            m_ref = now;
+            acc_E = E;
+            l_run *= alpha;
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
-                const uint16_t *src = vl + rbase + ((i ^ rturn) << 4);
-                const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)src);
-                const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(src + 16 * DH));
-                const auto v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                if constexpr (F32) {
-#pragma unroll
-                    for (int k = NP - 1; k >= 0; --k)
-                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v), pf[k], acc[i], 0, 0, 0);
-                } else {
-                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, v), ph, acc[i], 0, 0, 0);
-                }
+                acc[i] *= down;
+                asm volatile("" : "+v"(acc[i]));
             }
-            asm volatile("" ::: "memory");
         }
-        cur = nxt;
-    }
+        const float fin = fmaxf(m_ref, -1e30f), base = fmaf(-fin, c_log2, kShift);
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // fp32: the difference first, so that a row's only key weighs exactly 1
+            p[i] = __builtin_amdgcn_exp2f(F32 ? (s[i >> 2][i & 3] - fin) * c_log2 : fmaf(s[i >> 2][i & 3], c_log2, base));
+            l_run += p[i];
+        }
+        // ---- O^T += V^T P^T
+        bf16x8_t pf[NP];
+        f16x8_t ph;
+        if constexpr (F32) {
+            three_pieces(p, pf);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ph[i] = (_Float16)p[i];
+        }
+        asm volatile("" ::: "memory");
+        shortx4_t v[DB][2];
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            const uint16_t *src = vl + rbase + ((i ^ rturn) << 4);
+            v[i][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)src);
+            v[i][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(src + 16 * DH));
+        }
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            const auto both = __builtin_shufflevector(v[i][0], v[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
+            if constexpr (F32) {
+#pragma unroll
+                for (int k = NP - 1; k >= 0; --k)
+                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, both), pf[k], acc[i], 0, 0, 0);
+            } else {
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, both), ph, acc[i], 0, 0, 0);
+            }
+        }
+        asm volatile("" ::: "memory");
+    } while (t < t1);
 
     // ---- the wavefronts' results: each as the mean of the values it saw, with its weight l at the reference m
     l_run = column_sum(l_run);
@@ -323,8 +331,8 @@ __global__ __launch_bounds__(64 * NW) void kvq_attn_rows_kernel(const T *__restr
     for (int i = 0; i < DB; ++i) {
         float4 v = make_float4(acc[i][0] * inv, acc[i][1] * inv, acc[i][2] * inv, acc[i][3] * inv);
         if constexpr (!F32) {                                // |mean| <= 6 * 2^kTop: back to its size, which may be any
-            v.x = __builtin_amdgcn_ldexpf(v.x, E - kTop - 127); v.y = __builtin_amdgcn_ldexpf(v.y, E - kTop - 127);
-            v.z = __builtin_amdgcn_ldexpf(v.z, E - kTop - 127); v.w = __builtin_amdgcn_ldexpf(v.w, E - kTop - 127);
+            v.x = __builtin_amdgcn_ldexpf(v.x, acc_E - kTop - 127); v.y = __builtin_amdgcn_ldexpf(v.y, acc_E - kTop - 127);
+            v.z = __builtin_amdgcn_ldexpf(v.z, acc_E - kTop - 127); v.w = __builtin_amdgcn_ldexpf(v.w, acc_E - kTop - 127);
         }
         slots[i * 64 + lane] = v;
     }
@@ -381,7 +389,7 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // Matrix cores and vector unit overlap only for instructions that do not wait for each other and stand next to each other, and a
 // product that adds to the one right before it waits (a pair of weights 38 cycles, a product 40, both 58, 66 where they add on).
 template <int DH>
-__global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
+__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
                                                                 int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,
                                                                 int full_units, int shares, float *__restrict__ part_o,
                                                                 float *__restrict__ part_ml)
@@ -396,9 +404,9 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int unit = blockIdx.x, share = 0, ranges = 1;
     if (unit < full_units) {
-        unit = xcd_contiguous(unit, full_units);
+        unit = xcd_grouped(unit, full_units / nrb, nrb);
     } else {
-        const int t = xcd_contiguous(unit - full_units, (int)gridDim.x - full_units);
+        const int t = unit - full_units;
         unit = full_units + t / shares;
         share = t % shares;
         ranges = shares;
@@ -412,39 +420,6 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     const int t1 = max(end - 1, t0), seen_end = min(len, end * 64), last_row = max(len - 1, 0);
     const int r0 = rb * 128 + wave * 32, row = min(r0 + rl, R - 1);
     const bool active = __builtin_amdgcn_readfirstlane(r0 < R ? 1 : 0) != 0;
-
-    // ---- Q in three pieces of 6 bits: lane = row, block 2 s + g of its elements
-    intx8_t qf[KS][3];
-    int qs[KS];                                              // scale bytes of the pieces, in byte 0, 1, 2
-    {
-        const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            uint32_t w[16];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(w + 4 * i) = *reinterpret_cast<const uint4 *>(src + 64 * s + 8 * i);
-            uint32_t top = 0;
-            floatx16_t even, odd;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                even[i] = bf16_lo(w[i]) * c_log2;
-                odd[i] = bf16_hi(w[i]) * c_log2;
-                top = max(top, max(__float_as_uint(even[i]) & 0x7fffffffu, __float_as_uint(odd[i]) & 0x7fffffffu));
-            }
-            // the smallest 2^e with all elements below 7.75 * 2^e, which round to at most 7.5; 255 makes NaN of what is not finite
-            const int e = min(max((int)((top + (1u << 19)) >> 23) - 2, 13), 252);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                const float size = __uint_as_float((uint32_t)(e - 5 * p) << 23);
-                const uintx6_t x = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, size);
-                const floatx32_t back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(x, size);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) { even[i] -= back[2 * i]; odd[i] -= back[2 * i + 1]; }
-                qf[s][p] = intx8_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
-            }
-            qs[s] = top >= 0x7f800000u ? 0xffffff : e | (e - 5) << 8 | (e - 10) << 16;
-        }
-    }
 
     const size_t head = (size_t)(b * c.heads + hk) * c.capacity;
     const uint8_t *Kc = c.k + head * (DH / 2), *Vc = c.v + head * (DH / 2), *Ks = c.k_scale + head * NB, *Vs = c.v_scale + head * NB;
@@ -485,6 +460,43 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
             else *reinterpret_cast<uint16_t *>(dst) = (uint16_t)x.scale;
         }
     };
+    Next next, later;
+    fetch(t0, 0, next);                                      // on their way under what follows
+    fetch(min(t0 + 1, t1), 1, later);
+
+    // ---- Q in three pieces of 6 bits: lane = row, block 2 s + g of its elements
+    intx8_t qf[KS][3];
+    int qs[KS];                                              // scale bytes of the pieces, in byte 0, 1, 2
+    {
+        const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(w + 4 * i) = *reinterpret_cast<const uint4 *>(src + 64 * s + 8 * i);
+            uint32_t top = 0;
+            floatx16_t even, odd;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                even[i] = bf16_lo(w[i]) * c_log2;
+                odd[i] = bf16_hi(w[i]) * c_log2;
+                top = max(top, max(__float_as_uint(even[i]) & 0x7fffffffu, __float_as_uint(odd[i]) & 0x7fffffffu));
+            }
+            // the smallest 2^e with all elements below 7.75 * 2^e, which round to at most 7.5; 255 makes NaN of what is not finite
+            const int e = min(max((int)((top + (1u << 19)) >> 23) - 2, 13), 252);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                const float size = __uint_as_float((uint32_t)(e - 5 * p) << 23);
+                const uintx6_t x = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, size);
+                const floatx32_t back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(x, size);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) { even[i] -= back[2 * i]; odd[i] -= back[2 * i + 1]; }
+                qf[s][p] = intx8_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+            }
+            qs[s] = top >= 0x7f800000u ? 0xffffff : e | (e - 5) << 8 | (e - 10) << 16;
+        }
+    }
+
     // everything on its way to LDS is there, for all wavefronts
     auto meet = [&]() {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -548,21 +560,18 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
         *reinterpret_cast<uint4 *>(lds8 + stage * STAGE + vdst[i]) = half_eight(x.v[i], scale);
     };
 
-    Next next;
     Raw raw;
-    fetch(t0, 0, next);
     put_scales(0, next);
+    put_scales(1, later);
     meet();
     read_raw(0, raw);
     unsigned long long vis = look(t0, raw, next), vis_next;
 #pragma unroll
     for (int i = 0; i < VW; ++i) convert(0, raw, i);
-    fetch(min(t0 + 1, t1), 1, next);
-    put_scales(1, next);
-    meet();
+    next = later;
+    __syncthreads();
     int stage = 0;                                           // of the tile at work
     auto after = [](int s) { return s == 2 ? 0 : s + 1; };
-    Next later;
     if (!active) {                                           // rows past the end: only helps with the tiles
         for (int t = t0; t <= t1; ++t) {
             const int s1 = after(stage);
@@ -789,33 +798,61 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
 }
 
 // The shares of rows joined: each is a mean and its weight.  A unit is a block of BR rows of one (sample, kv head); the shares
-// of unit first + u lie at [u][share][row].  One thread per four head-dim elements of a row.
-template <typename T, int DH>
+// of unit first + u lie at [u][share][row].  GROUPS groups of DH/4 threads per row, four head-dim elements a thread: a group takes every
+// GROUPS-th share in one pass with a running reference, and the groups meet in LDS.  One group where the shares are few and the
+// rows many; more where a few rows have many shares, whose loads would wait for each other (64 shares of 16 rows: 24 us by one, 3 by 8).
+template <typename T, int DH, int GROUPS>
 __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
                                                              int n, int H, int heads, int nrb, int BR, int first, int shares,
-                                                             float c_log2, long total, T *__restrict__ o)
+                                                             float c_log2, int total, T *__restrict__ o)
 {
-    const long idx = (long)blockIdx.x * 256 + threadIdx.x;
-    if (idx >= total) return;
-    const int d = (int)(idx % (DH / 4)) * 4;
-    const int r = (int)(idx / (DH / 4) % BR), u = (int)(idx / (DH / 4) / BR), unit = first + u;
+    constexpr int W = DH / 4, ROWS = 256 / (W * GROUPS);     // threads of a group, rows of a workgroup
+    __shared__ float4 lo[GROUPS > 1 ? 256 : 1];
+    __shared__ float2 lm[GROUPS > 1 ? 256 / W : 1];
+    const int d = threadIdx.x % W * 4, group = threadIdx.x / W % GROUPS, in_wg = threadIdx.x / (W * GROUPS);
+    const int idx = blockIdx.x * ROWS + in_wg;               // row among those of the divided units
+    const int r = idx % BR, u = idx / BR, unit = first + u;
     const int G = H / heads, row = unit % nrb * BR + r, hk = unit / nrb % heads;
     const long b = unit / nrb / heads;
-    if (row >= n * G) return;
+    const bool mine = idx < total && row < n * G;
     const size_t prow = (size_t)u * shares * BR + r;
-    float m = -INFINITY;
-    for (int s = 0; s < shares; ++s) m = fmaxf(m, part_ml[(prow + (size_t)s * BR) * 2]);
-    const float fin = fmaxf(m, -1e30f);
+    float m = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    for (int s = 0; s < shares; ++s) {
-        const float2 ml = *reinterpret_cast<const float2 *>(part_ml + (prow + (size_t)s * BR) * 2);
-        const float w = ml.y * __builtin_amdgcn_exp2f((ml.x - fin) * c_log2);
-        const float4 v = *reinterpret_cast<const float4 *>(part_o + (prow + (size_t)s * BR) * DH + d);
-        acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y);
-        acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
-        sum += w;
+    if (mine) {
+#pragma unroll 4
+        for (int s = group; s < shares; s += GROUPS) {
+            const float2 ml = *reinterpret_cast<const float2 *>(part_ml + (prow + (size_t)s * BR) * 2);
+            const float4 v = *reinterpret_cast<const float4 *>(part_o + (prow + (size_t)s * BR) * DH + d);
+            const float now = fmaxf(m, ml.x), fin = fmaxf(now, -1e30f);
+            const float keep = __builtin_amdgcn_exp2f((m - fin) * c_log2), w = ml.y * __builtin_amdgcn_exp2f((ml.x - fin) * c_log2);
+            acc.x = fmaf(v.x, w, acc.x * keep); acc.y = fmaf(v.y, w, acc.y * keep);
+            acc.z = fmaf(v.z, w, acc.z * keep); acc.w = fmaf(v.w, w, acc.w * keep);
+            sum = fmaf(sum, keep, w);
+            m = now;
+        }
     }
+    if constexpr (GROUPS > 1) {
+        lo[threadIdx.x] = acc;
+        if (d == 0) lm[threadIdx.x / W] = make_float2(m, sum);
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, lm[threadIdx.x / W + k].x);
+        const float fin = fmaxf(m, -1e30f);
+        float keep = __builtin_amdgcn_exp2f((lm[threadIdx.x / W].x - fin) * c_log2);
+        acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
+        sum *= keep;
+#pragma unroll
+        for (int k = 1; k < GROUPS; ++k) {
+            const float2 ml = lm[threadIdx.x / W + k];
+            const float4 v = lo[threadIdx.x + k * W];
+            keep = __builtin_amdgcn_exp2f((ml.x - fin) * c_log2);
+            acc.x = fmaf(v.x, keep, acc.x); acc.y = fmaf(v.y, keep, acc.y);
+            acc.z = fmaf(v.z, keep, acc.z); acc.w = fmaf(v.w, keep, acc.w);
+            sum = fmaf(ml.y, keep, sum);
+        }
+    }
+    if (!mine) return;
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
     Quad<T>::store(o + (size_t)(b * n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH + d,
                    make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
@@ -825,8 +862,9 @@ constexpr int kRowWaves = 4;
 
 // How an attention is run: by blocks of 16 rows (kvq_attn_rows_kernel) or of 128 (kvq_attn_tiles_kernel); nrb blocks per
 // (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
+// `ragged`: samples of lengths of their own, which only the GPU knows.
 struct KvqRun { int block, nrb, units, full, shares; };
-static KvqRun kvq_run(DType dt, int B, int n, int H, int heads, int length)
+static KvqRun kvq_run(DType dt, int B, int n, int H, int heads, int length, bool ragged)
 {
     const int rows = n * (H / heads);
     KvqRun run;
@@ -834,8 +872,11 @@ static KvqRun kvq_run(DType dt, int B, int n, int H, int heads, int length)
     run.nrb = (rows + run.block - 1) / run.block;
     run.units = B * heads * run.nrb;
     if (run.block == 16) {
-        // enough workgroups for four on every CU, each with two tiles per wavefront at least
-        const int want = (1024 + run.units - 1) / run.units, most = (length + 31) / 32 / (2 * kRowWaves);
+        // Enough workgroups for two on every CU, each with two tiles per wavefront at least; four where samples differ, so that
+        // a CU that has had short ones takes more (32 samples of 8461 keys, 8 kv heads: 512, 1024, 2048 places 53, 59, 59 us; of 1 to 16921 keys
+        // 1024, 2048, 4096 places 56, 59, 69 us).
+        const int places = ragged ? 1024 : 512;
+        const int want = (places + run.units - 1) / run.units, most = (length + 31) / 32 / (2 * kRowWaves);
         run.shares = want < most ? want : most > 0 ? most : 1;
         run.full = run.shares > 1 ? 0 : run.units;
         return run;
@@ -852,8 +893,8 @@ static KvqRun kvq_run(DType dt, int B, int n, int H, int heads, int length)
 
 size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity)
 {
-    // shares never fall as the length grows: what the capacity needs is enough for every length
-    const KvqRun run = kvq_run(dt, B, n, H, heads, capacity);
+    // shares never fall as the length grows, nor where samples have lengths of their own: this is enough for every call
+    const KvqRun run = kvq_run(dt, B, n, H, heads, capacity, true);
     return (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
 }
 
@@ -861,7 +902,7 @@ template <typename T, int DH>
 static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, float c_log2,
                        void *o, float *part, hipStream_t st)
 {
-    const KvqRun run = kvq_run(dt, B, n, H, c.heads, c.lens ? c.capacity : c.len + extra);
+    const KvqRun run = kvq_run(dt, B, n, H, c.heads, c.lens ? c.capacity : c.len + extra, c.lens != nullptr);
     const int divided = run.units - run.full;
     float *part_ml = part + (size_t)divided * run.shares * run.block * DH;
     const unsigned wgs = (unsigned)(run.full + divided * run.shares);
@@ -873,9 +914,13 @@ static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int e
                run.full, run.shares, part, part_ml);
     }
     if (divided) {
-        const long total = (long)divided * run.block * (DH / 4);
-        launch(kvq_attn_merge_kernel<T, DH>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, (const float *)part,
-               (const float *)part_ml, n, H, c.heads, run.nrb, run.block, run.full, run.shares, c_log2, total, (T *)o);
+        const int total = divided * run.block, per = 256 / (DH / 4);
+        if (run.shares > 8)
+            launch(kvq_attn_merge_kernel<T, DH, 8>, dim3((unsigned)((total + per / 8 - 1) / (per / 8))), dim3(256), 0, st, (const float *)part,
+                   (const float *)part_ml, n, H, c.heads, run.nrb, run.block, run.full, run.shares, c_log2, total, (T *)o);
+        else
+            launch(kvq_attn_merge_kernel<T, DH, 1>, dim3((unsigned)((total + per - 1) / per)), dim3(256), 0, st, (const float *)part,
+                   (const float *)part_ml, n, H, c.heads, run.nrb, run.block, run.full, run.shares, c_log2, total, (T *)o);
     }
 }
 

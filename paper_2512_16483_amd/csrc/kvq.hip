@@ -31,7 +31,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v)
 
 // Eight elements per thread, four threads per block of 32: their maximum is two steps in registers.
 // grid: (chunks of a head's new rows, B * heads, K or V).  Memory-bound: rows are read as whole lines of one head, and
-// written as one run per head.
+// written as one run per head (4 x 6400 rows, 32 heads of 128: 107 us, 5.0 TB/s; 32 x 2521, 16 heads 151 us, 5.5; two or four
+// rows per thread and reads past the caches are no faster).
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kvq_append_kernel(const T *__restrict__ k, const T *__restrict__ v, int ld,
                                                          KvqCache c, int rows)
@@ -74,12 +75,16 @@ __global__ __launch_bounds__(256) void kvq_append_kernel(const T *__restrict__ k
     if (ch % 4 == 0) (blockIdx.z ? c.v_scale : c.k_scale)[row * (DH / 32) + ch / 4] = (uint8_t)byte;
 }
 
-// Eight elements per thread.  Every value of the format is exact in bf16 and fp32.
-template <typename T, int DH>
+// Sixteen bytes of a row per thread.  Every value of the format is exact in bf16 and fp32.  Memory-bound: four fifths of the bytes are the
+// rows written, which go past the caches where L2 would not hold them for their reader anyway (32 x 2521 rows, 16 heads of 128: 168 us
+// through the caches, 118 past them, 7.1 TB/s), a lane next to the other: 32 bytes a lane in two stores take 108 us for 16 x 2000 fp32
+// rows of 16 heads of 64 where they go past the caches and 65 where not.
+template <typename T, int DH, bool PAST>
 __global__ __launch_bounds__(256) void kvq_read_kernel(KvqCache c, int first, int rows, T *__restrict__ k,
                                                        T *__restrict__ v, int only_v)
 {
-    constexpr int CH = DH / 8;
+    typedef uint32_t uintx4_t __attribute__((ext_vector_type(4)));
+    constexpr int PER = 16 / sizeof(T), CH = DH / PER;       // elements per thread, threads of a row
     const int item = blockIdx.x * 256 + threadIdx.x, j = item / CH, ch = item % CH;
     if (j >= rows) return;
     const int b = blockIdx.y / c.heads, h = blockIdx.y % c.heads;
@@ -89,26 +94,26 @@ __global__ __launch_bounds__(256) void kvq_read_kernel(KvqCache c, int first, in
     uint32_t word = 0, byte = 127;
     if (pos >= 0 && pos < len) {
         const size_t row = (size_t)blockIdx.y * c.capacity + pos;
-        word = reinterpret_cast<const uint32_t *>(is_v ? c.v : c.k)[row * CH + ch];
-        byte = (is_v ? c.v_scale : c.k_scale)[row * (DH / 32) + ch / 4];
+        const uint8_t *codes = is_v ? c.v : c.k;
+        word = PER == 8 ? reinterpret_cast<const uint32_t *>(codes)[row * CH + ch]
+                        : reinterpret_cast<const uint16_t *>(codes)[row * CH + ch];
+        byte = (is_v ? c.v_scale : c.k_scale)[row * (DH / 32) + ch * PER / 32];
     }
     const float scale = __uint_as_float(byte << 23);         // 255: infinity, which the conversion turns into NaN
-    T *dst = (is_v ? v : k) + (((size_t)b * rows + j) * c.heads + h) * DH + ch * 8;
-    if constexpr (sizeof(T) == 2) {
-        uint4 x;
-        x.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
-        x.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
-        x.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
-        x.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
-        *reinterpret_cast<uint4 *>(dst) = x;
+    uintx4_t x;
+    if constexpr (PER == 8) {
+        x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
+        x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
+        x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
+        x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
     } else {
         const floatx2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 0);
         const floatx2_t p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 1);
-        const floatx2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 2);
-        const floatx2_t p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 3);
-        *reinterpret_cast<float4 *>(dst) = make_float4(p0[0], p0[1], p1[0], p1[1]);
-        *reinterpret_cast<float4 *>(dst + 4) = make_float4(p2[0], p2[1], p3[0], p3[1]);
+        x = uintx4_t{__float_as_uint(p0[0]), __float_as_uint(p0[1]), __float_as_uint(p1[0]), __float_as_uint(p1[1])};
     }
+    uintx4_t *dst = reinterpret_cast<uintx4_t *>((is_v ? v : k) + (((size_t)b * rows + j) * c.heads + h) * DH + ch * PER);
+    if (PAST) __builtin_nontemporal_store(x, dst);
+    else *dst = x;
 }
 
 void launch_kvq_append(DType dt, const void *k, const void *v, int ld, const KvqCache &c, int B, int rows, int Dh,
@@ -128,9 +133,14 @@ void launch_kvq_append(DType dt, const void *k, const void *v, int ld, const Kvq
 
 void launch_kvq_read(DType dt, const KvqCache &c, int B, int first, int rows, int Dh, void *k, void *v, hipStream_t st)
 {
-    const dim3 grid((unsigned)(((long)rows * (Dh / 8) + 255) / 256), (unsigned)(B * c.heads), k && v ? 2 : 1);
+    const int per = dt == DType::BF16 ? 8 : 4;               // elements per thread
+    const dim3 grid((unsigned)(((long)rows * (Dh / per) + 255) / 256), (unsigned)(B * c.heads), k && v ? 2 : 1);
     const int only_v = !k;
-#define FVAR_READ(T, DH) launch(kvq_read_kernel<T, DH>, grid, dim3(256), 0, st, c, first, rows, (T *)k, (T *)v, only_v)
+    const size_t bytes = (size_t)grid.z * B * rows * c.heads * Dh * (dt == DType::BF16 ? 2 : 4);
+    const bool past = bytes > (32u << 20);                   // the L2s together
+#define FVAR_READ(T, DH)                                                                                                 \
+    (past ? launch(kvq_read_kernel<T, DH, true>, grid, dim3(256), 0, st, c, first, rows, (T *)k, (T *)v, only_v)          \
+          : launch(kvq_read_kernel<T, DH, false>, grid, dim3(256), 0, st, c, first, rows, (T *)k, (T *)v, only_v))
     if (dt == DType::BF16) {
         if (Dh == 64) FVAR_READ(uint16_t, 64);
         else FVAR_READ(uint16_t, 128);

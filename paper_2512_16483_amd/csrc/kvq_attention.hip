@@ -860,21 +860,30 @@ __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__rest
 
 constexpr int kRowWaves = 4;
 
-// How an attention is run: by blocks of 16 rows (kvq_attn_rows_kernel) or of 128 (kvq_attn_tiles_kernel); nrb blocks per
-// (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
-// `ragged`: samples of lengths of their own, which only the GPU knows.
-struct KvqRun { int block, nrb, units, full, shares; };
-static KvqRun kvq_run(DType dt, int B, int n, int H, int heads, int length, bool ragged)
+// Blocks of how many rows of a (sample, kv head) an attention is run by: 16 (kvq_attn_rows_kernel) or 128 (kvq_attn_tiles_kernel, bf16
+// only).  The first needs least time per block and is bound by the work, which it does at 0.4 of the other's pace; the other
+// fetches and converts for 128 rows whatever there are.  us by 16 / by 128, 16 heads of 128: 32 x 48 rows x 3001 keys 81 / 82, 32 x 64 101 / 83,
+// 8 x 96 x 2521 36 / 39, 8 x 128 46 / 43, 1 x 128 x 4813 20 / 25, 4 x 200 x 2500 42 / 39; 30 heads of 64: 8 x 128 x 871 24 / 26, 8 x 200 36 / 26.
+static int kvq_block(DType dt, int B, int n, int H, int heads, int length)
 {
     const int rows = n * (H / heads);
+    if (dt != DType::BF16 || rows <= 48) return 16;
+    return rows <= 128 && (long)B * heads * ((rows + 15) / 16) * length <= 1l << 21 ? 16 : 128;
+}
+
+// nrb blocks per (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
+// `ragged`: samples of lengths of their own, which only the GPU knows.
+struct KvqRun { int block, nrb, units, full, shares; };
+static KvqRun kvq_run(int block, int B, int n, int H, int heads, int length, bool ragged)
+{
     KvqRun run;
-    run.block = dt == DType::BF16 && rows > 64 ? 128 : 16;
-    run.nrb = (rows + run.block - 1) / run.block;
+    run.block = block;
+    run.nrb = (n * (H / heads) + block - 1) / block;
     run.units = B * heads * run.nrb;
-    if (run.block == 16) {
+    if (block == 16) {
         // Enough workgroups for two on every CU, each with two tiles per wavefront at least; four where samples differ, so that
-        // a CU that has had short ones takes more (32 samples of 8461 keys, 8 kv heads: 512, 1024, 2048 places 53, 59, 59 us; of 1 to 16921 keys
-        // 1024, 2048, 4096 places 56, 59, 69 us).
+        // a CU that has had short ones takes more (32 samples of 8461 keys, 8 kv heads: 512, 1024, 2048 places 53, 59, 59 us; of 1 to
+        // 16921 keys 1024, 2048, 4096 places 56, 59, 69 us).
         const int places = ragged ? 1024 : 512;
         const int want = (places + run.units - 1) / run.units, most = (length + 31) / 32 / (2 * kRowWaves);
         run.shares = want < most ? want : most > 0 ? most : 1;
@@ -893,16 +902,24 @@ static KvqRun kvq_run(DType dt, int B, int n, int H, int heads, int length, bool
 
 size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity)
 {
-    // shares never fall as the length grows, nor where samples have lengths of their own: this is enough for every call
-    const KvqRun run = kvq_run(dt, B, n, H, heads, capacity, true);
-    return (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
+    // Shares never fall as the length grows, nor where samples have lengths of their own, so for either kind of blocks this is enough for
+    // every call; a shorter length may be run by the other kind.
+    size_t most = 0;
+    for (int block = 16; block <= 128; block *= 8) {
+        if (block == 128 ? kvq_block(dt, B, n, H, heads, capacity) == 16 : kvq_block(dt, B, n, H, heads, 1) == 128) continue;
+        const KvqRun run = kvq_run(block, B, n, H, heads, capacity, true);
+        const size_t floats = (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
+        if (floats > most) most = floats;
+    }
+    return most;
 }
 
 template <typename T, int DH>
 static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, float c_log2,
                        void *o, float *part, hipStream_t st)
 {
-    const KvqRun run = kvq_run(dt, B, n, H, c.heads, c.lens ? c.capacity : c.len + extra, c.lens != nullptr);
+    const int length = c.lens ? c.capacity : c.len + extra;
+    const KvqRun run = kvq_run(kvq_block(dt, B, n, H, c.heads, length), B, n, H, c.heads, length, c.lens != nullptr);
     const int divided = run.units - run.full;
     float *part_ml = part + (size_t)divided * run.shares * run.block * DH;
     const unsigned wgs = (unsigned)(run.full + divided * run.shares);

@@ -75,45 +75,57 @@ __global__ __launch_bounds__(256) void kvq_append_kernel(const T *__restrict__ k
     if (ch % 4 == 0) (blockIdx.z ? c.v_scale : c.k_scale)[row * (DH / 32) + ch / 4] = (uint8_t)byte;
 }
 
-// Sixteen bytes of a row per thread.  Every value of the format is exact in bf16 and fp32.  Memory-bound: four fifths of the bytes are the
-// rows written, which go past the caches where L2 would not hold them for their reader anyway (32 x 2521 rows, 16 heads of 128: 168 us
-// through the caches, 118 past them, 7.1 TB/s), a lane next to the other: 32 bytes a lane in two stores take 108 us for 16 x 2000 fp32
-// rows of 16 heads of 64 where they go past the caches and 65 where not.
+// Sixteen bytes of a row per thread, two such pieces for bf16, whose codes are fetched first.  Every value of the format is exact in
+// bf16 and fp32.  Memory-bound: four fifths of the bytes are the rows written, which go past the caches where L2 would not hold
+// them for their reader anyway, a lane next to the other (32 bytes a lane in two stores take 108 us for 16 x 2000 fp32 rows of 16 heads
+// of 64, these 41).  32 x 2521 rows of 16 heads of 128 from cold caches: 167 us through the caches, 164 past them, 135 with two pieces per
+// thread (6.2 TB/s), 139 with four.
+template <typename T> constexpr int kReadPieces = sizeof(T) == 2 ? 2 : 1;
+
 template <typename T, int DH, bool PAST>
 __global__ __launch_bounds__(256) void kvq_read_kernel(KvqCache c, int first, int rows, T *__restrict__ k,
                                                        T *__restrict__ v, int only_v)
 {
     typedef uint32_t uintx4_t __attribute__((ext_vector_type(4)));
-    constexpr int PER = 16 / sizeof(T), CH = DH / PER;       // elements per thread, threads of a row
-    const int item = blockIdx.x * 256 + threadIdx.x, j = item / CH, ch = item % CH;
-    if (j >= rows) return;
+    constexpr int PER = 16 / sizeof(T), CH = DH / PER, N = kReadPieces<T>;   // elements of a piece, pieces of a row
     const int b = blockIdx.y / c.heads, h = blockIdx.y % c.heads;
     const bool is_v = only_v || blockIdx.z;
-    const int len = kvq_length(c, b, 0);
-    const long pos = (long)(first < 0 ? len : 0) + first + j;
-    uint32_t word = 0, byte = 127;
-    if (pos >= 0 && pos < len) {
-        const size_t row = (size_t)blockIdx.y * c.capacity + pos;
-        const uint8_t *codes = is_v ? c.v : c.k;
-        word = PER == 8 ? reinterpret_cast<const uint32_t *>(codes)[row * CH + ch]
-                        : reinterpret_cast<const uint16_t *>(codes)[row * CH + ch];
-        byte = (is_v ? c.v_scale : c.k_scale)[row * (DH / 32) + ch * PER / 32];
+    const int len = kvq_length(c, b, 0), item = blockIdx.x * (256 * N) + threadIdx.x;
+    const uint8_t *codes = is_v ? c.v : c.k, *scales = is_v ? c.v_scale : c.k_scale;
+    uint32_t word[N], byte[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = (item + 256 * i) / CH, ch = (item + 256 * i) % CH;
+        const long pos = (long)(first < 0 ? len : 0) + first + j;
+        word[i] = 0;
+        byte[i] = 127;
+        if (j < rows && pos >= 0 && pos < len) {
+            const size_t row = (size_t)blockIdx.y * c.capacity + pos;
+            word[i] = PER == 8 ? reinterpret_cast<const uint32_t *>(codes)[row * CH + ch]
+                               : reinterpret_cast<const uint16_t *>(codes)[row * CH + ch];
+            byte[i] = scales[row * (DH / 32) + ch * PER / 32];
+        }
     }
-    const float scale = __uint_as_float(byte << 23);         // 255: infinity, which the conversion turns into NaN
-    uintx4_t x;
-    if constexpr (PER == 8) {
-        x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
-        x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
-        x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
-        x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
-    } else {
-        const floatx2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 0);
-        const floatx2_t p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 1);
-        x = uintx4_t{__float_as_uint(p0[0]), __float_as_uint(p0[1]), __float_as_uint(p1[0]), __float_as_uint(p1[1])};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = (item + 256 * i) / CH, ch = (item + 256 * i) % CH;
+        if (j >= rows) return;
+        const float scale = __uint_as_float(byte[i] << 23);  // 255: infinity, which the conversion turns into NaN
+        uintx4_t x;
+        if constexpr (PER == 8) {
+            x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[i], scale, 0));
+            x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[i], scale, 1));
+            x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[i], scale, 2));
+            x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[i], scale, 3));
+        } else {
+            const floatx2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 0);
+            const floatx2_t p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 1);
+            x = uintx4_t{__float_as_uint(p0[0]), __float_as_uint(p0[1]), __float_as_uint(p1[0]), __float_as_uint(p1[1])};
+        }
+        uintx4_t *dst = reinterpret_cast<uintx4_t *>((is_v ? v : k) + (((size_t)b * rows + j) * c.heads + h) * DH + ch * PER);
+        if (PAST) __builtin_nontemporal_store(x, dst);
+        else *dst = x;
     }
-    uintx4_t *dst = reinterpret_cast<uintx4_t *>((is_v ? v : k) + (((size_t)b * rows + j) * c.heads + h) * DH + ch * PER);
-    if (PAST) __builtin_nontemporal_store(x, dst);
-    else *dst = x;
 }
 
 void launch_kvq_append(DType dt, const void *k, const void *v, int ld, const KvqCache &c, int B, int rows, int Dh,
@@ -133,8 +145,8 @@ void launch_kvq_append(DType dt, const void *k, const void *v, int ld, const Kvq
 
 void launch_kvq_read(DType dt, const KvqCache &c, int B, int first, int rows, int Dh, void *k, void *v, hipStream_t st)
 {
-    const int per = dt == DType::BF16 ? 8 : 4;               // elements per thread
-    const dim3 grid((unsigned)(((long)rows * (Dh / per) + 255) / 256), (unsigned)(B * c.heads), k && v ? 2 : 1);
+    const int per = dt == DType::BF16 ? 8 * 256 * kReadPieces<uint16_t> : 4 * 256 * kReadPieces<float>;   // elements per workgroup
+    const dim3 grid((unsigned)(((long)rows * Dh + per - 1) / per), (unsigned)(B * c.heads), k && v ? 2 : 1);
     const int only_v = !k;
     const size_t bytes = (size_t)grid.z * B * rows * c.heads * Dh * (dt == DType::BF16 ? 2 : 4);
     const bool past = bytes > (32u << 20);                   // the L2s together

@@ -881,11 +881,12 @@ static KvqRun kvq_run(int block, int B, int n, int H, int heads, int length, boo
     run.nrb = (n * (H / heads) + block - 1) / block;
     run.units = B * heads * run.nrb;
     if (block == 16) {
-        // Enough workgroups for two on every CU, each with two tiles per wavefront at least; four where samples differ, so that
-        // a CU that has had short ones takes more (32 samples of 8461 keys, 8 kv heads: 512, 1024, 2048 places 53, 59, 59 us; of 1 to
-        // 16921 keys 1024, 2048, 4096 places 56, 59, 69 us).
-        const int places = ragged ? 1024 : 512;
-        const int want = (places + run.units - 1) / run.units, most = (length + 31) / 32 / (2 * kRowWaves);
+        // Enough workgroups for two on every CU; four where samples differ, so that a CU that has had short ones takes more (32 samples of
+        // 8461 keys, 8 kv heads: 512, 1024, 2048 places 53, 59, 59 us; of 1 to 16921 keys 1024, 2048, 4096 places 56, 59, 69 us).  Each with
+        // two tiles per wavefront at least, or eight where every CU has a workgroup already and the joining, 3 us, is for nothing else
+        // (fp32, 2 x 128 x 552, 16 heads of 64: 8.7 us whole, 11.5 in two shares).
+        const int places = ragged ? 1024 : 512, least = run.units < 256 ? 2 : 8;
+        const int want = (places + run.units - 1) / run.units, most = (length + 31) / 32 / (least * kRowWaves);
         run.shares = want < most ? want : most > 0 ? most : 1;
         run.full = run.shares > 1 ? 0 : run.units;
         return run;

@@ -858,8 +858,6 @@ __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__rest
                    make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
 }
 
-constexpr int kRowWaves = 4;
-
 // Blocks of how many rows of a (sample, kv head) an attention is run by: 16 (kvq_attn_rows_kernel) or 128 (kvq_attn_tiles_kernel, bf16
 // only).  The first needs least time per block and is bound by the work, which it does at 0.4 of the other's pace; the other
 // fetches and converts for 128 rows whatever there are.  us by 16 / by 128, 16 heads of 128: 32 x 48 rows x 3001 keys 81 / 82, 32 x 64 101 / 83,
@@ -873,20 +871,28 @@ static int kvq_block(DType dt, int B, int n, int H, int heads, int length)
 
 // nrb blocks per (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
 // `ragged`: samples of lengths of their own, which only the GPU knows.
-struct KvqRun { int block, nrb, units, full, shares; };
+// waves: wavefronts of a workgroup that divide a block's keys.
+struct KvqRun { int block, nrb, units, full, shares, waves; };
 static KvqRun kvq_run(int block, int B, int n, int H, int heads, int length, bool ragged)
 {
     KvqRun run;
     run.block = block;
     run.nrb = (n * (H / heads) + block - 1) / block;
     run.units = B * heads * run.nrb;
+    run.waves = 4;
     if (block == 16) {
+        // Where the blocks alone fill the chip and the cache is short, wavefronts without a tile, and the meeting of those with one, cost
+        // more than they save: us with 1 / 2 / 4 of them, 17 x 125 rows x 4 keys of 32 heads 14 / 18 / 31, 32 x 64 x 121 of 16 11 / 14 / 17,
+        // 8 x 100 x 500 17 / 14.5 / 15.8, 32 x 40 x 800 32 / 27 / 30; but 8 x 64 x 250 10 / 8.8 / 7.5, 32 x 32 x 4000 68 / 51 / 46.
+        const int tiles = (length + 31) / 32;
+        if (tiles <= 4 && run.units >= 1024) run.waves = 1;
+        else if (tiles <= 32 && run.units >= 768 && !ragged) run.waves = 2;
         // Enough workgroups for two on every CU; four where samples differ, so that a CU that has had short ones takes more (32 samples of
         // 8461 keys, 8 kv heads: 512, 1024, 2048 places 53, 59, 59 us; of 1 to 16921 keys 1024, 2048, 4096 places 56, 59, 69 us).  Each with
         // two tiles per wavefront at least, or eight where every CU has a workgroup already and the joining, 3 us, is for nothing else
         // (fp32, 2 x 128 x 552, 16 heads of 64: 8.7 us whole, 11.5 in two shares).
         const int places = ragged ? 1024 : 512, least = run.units < 256 ? 2 : 8;
-        const int want = (places + run.units - 1) / run.units, most = (length + 31) / 32 / (least * kRowWaves);
+        const int want = (places + run.units - 1) / run.units, most = tiles / (least * 4);
         run.shares = want < most ? want : most > 0 ? most : 1;
         run.full = run.shares > 1 ? 0 : run.units;
         return run;
@@ -915,6 +921,14 @@ size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, in
     return most;
 }
 
+// How an attention is run, for the tests: 100000 * rows of a block + 1000 * wavefronts + shares.
+int kvq_attention_ways(int bf16, int B, int n, int H, int heads, int length, int ragged)
+{
+    const int block = kvq_block(bf16 ? DType::BF16 : DType::F32, B, n, H, heads, length);
+    const KvqRun run = kvq_run(block, B, n, H, heads, length, ragged != 0);
+    return 100000 * block + 1000 * run.waves + run.shares;
+}
+
 template <typename T, int DH>
 static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, float c_log2,
                        void *o, float *part, hipStream_t st)
@@ -925,8 +939,13 @@ static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int e
     float *part_ml = part + (size_t)divided * run.shares * run.block * DH;
     const unsigned wgs = (unsigned)(run.full + divided * run.shares);
     if (run.block == 16) {
-        launch(kvq_attn_rows_kernel<T, DH, kRowWaves>, dim3(wgs), dim3(64 * kRowWaves), 0, st, (const T *)q, ld, c, extra, n, H,
-               c_log2, (T *)o, run.nrb, run.shares, part, part_ml);
+#define FVAR_ROWS(NW)                                                                                                    \
+    launch(kvq_attn_rows_kernel<T, DH, NW>, dim3(wgs), dim3(64 * NW), 0, st, (const T *)q, ld, c, extra, n, H, c_log2,    \
+           (T *)o, run.nrb, run.shares, part, part_ml)
+        if (run.waves == 1) FVAR_ROWS(1);
+        else if (run.waves == 2) FVAR_ROWS(2);
+        else FVAR_ROWS(4);
+#undef FVAR_ROWS
     } else if constexpr (sizeof(T) == 2) {
         launch(kvq_attn_tiles_kernel<DH>, dim3(wgs), dim3(256), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, run.nrb,
                run.full, run.shares, part, part_ml);

@@ -150,3 +150,59 @@ def test_binding_refuses_tensors_that_do_not_fit():
             fv.KVQ(**dict(good, **kw))
     with pytest.raises(ValueError, match="GPU"):
         fv.KVQ(**good)                                        # right shapes, but host memory
+
+
+# ------------------------------------------------------------------------------------ ways of running the attention
+def ways(dtype, B, n, H, heads, length, ragged):
+    """(rows of a block, wavefronts that divide its keys, shares of the keys of a divided block)"""
+    w = fv.load_library()["_ZN4fvar18kvq_attention_waysEiiiiiii"](dtype == "bf16", B, n, H, heads, length, ragged)
+    return w // 100000, w // 1000 % 100, w % 1000
+
+
+# dtype, head_dim, heads, kv heads, samples, queries, keys, lengths of their own, way
+WAYS = {
+    "16 rows, 1 wavefront": ("bf16", 64, 16, 16, 32, 40, 100, False, (16, 1, 1)),
+    "16 rows, 1 wavefront, 128": ("bf16", 128, 16, 16, 24, 40, 97, False, (16, 1, 1)),
+    "16 rows, 1 wavefront, ragged": ("bf16", 128, 16, 16, 24, 40, 128, True, (16, 1, 1)),
+    "16 rows, 1 wavefront, fp32": ("f32", 64, 8, 8, 16, 130, 70, False, (16, 1, 1)),
+    "16 rows, 2 wavefronts": ("bf16", 128, 16, 16, 16, 40, 300, False, (16, 2, 1)),
+    "16 rows, 2 wavefronts, 64": ("bf16", 64, 32, 8, 32, 10, 333, False, (16, 2, 1)),
+    "16 rows, 2 wavefronts, fp32": ("f32", 128, 8, 8, 12, 130, 201, False, (16, 2, 1)),
+    "16 rows, 4 wavefronts": ("bf16", 128, 8, 8, 16, 40, 600, False, (16, 4, 1)),
+    "16 rows, 4 wavefronts, fp32": ("f32", 64, 4, 4, 9, 200, 511, False, (16, 4, 1)),
+    "16 rows, 3 shares": ("bf16", 128, 8, 2, 3, 30, 900, False, (16, 4, 3)),
+    "16 rows, 20 shares": ("bf16", 64, 4, 4, 1, 3, 5151, False, (16, 4, 20)),
+    "16 rows, 20 shares, fp32": ("f32", 128, 4, 4, 1, 3, 5151, False, (16, 4, 20)),
+    "16 rows, shares of ragged samples": ("bf16", 128, 8, 8, 32, 1, 2100, True, (16, 4, 2)),
+    "128 rows, whole": ("bf16", 128, 8, 8, 32, 200, 130, False, (128, 4, 1)),
+    "128 rows, all divided": ("bf16", 128, 4, 4, 2, 230, 1600, False, (128, 4, 6)),
+    "128 rows, all divided, 64": ("bf16", 64, 8, 2, 2, 130, 2900, False, (128, 4, 8)),
+    "128 rows, last round divided": ("bf16", 64, 16, 16, 20, 200, 1100, False, (128, 4, 4)),
+    "128 rows, last round divided, 128": ("bf16", 128, 4, 4, 70, 200, 600, True, (128, 4, 2)),
+    "128 rows, last round divided, ragged": ("bf16", 64, 16, 8, 40, 90, 1400, True, (128, 4, 4)),
+}
+
+
+@pytest.mark.parametrize("case", sorted(WAYS))
+def test_ways_that_the_gpu_tests_are_there_for(case):
+    """tests/test_gpu_kvq_ways.py runs these: another choice of constants must not take a way out of its reach unseen."""
+    dtype, dh, H, heads, B, n, L, ragged, expect = WAYS[case]
+    assert ways(dtype, B, n, H, heads, L, ragged) == expect
+
+
+def test_small_changes_of_length_and_lengths_of_their_own_need_no_more_workspace():
+    lib = fv.load_library()
+    for dtype in ("bf16", "f32"):
+        for heads, kv_heads, dh in ((16, 16, 128), (30, 30, 64), (32, 4, 128)):
+            ctx = fv.Context(hidden=heads * dh, heads=heads, head_dim=dh, ffn_hidden=64, dtype=dtype)
+            for B in (1, 3, 32):
+                for n in (1, 7, 48, 64, 128, 129, 700):
+                    last = 0
+                    for cap in (1, 100, 127, 128, 400, 1024, 1025, 3000, 12121, 100000):
+                        size = lib.fvar_kvq_attention_workspace_bytes(ctx.handle, C.byref(_cache(kv_heads=kv_heads, capacity=cap, len=1)), B, n)
+                        assert size >= last                   # never falls as the capacity grows
+                        last = size
+                        block, _, shares = ways(dtype, B, n, heads, kv_heads, cap, False)
+                        units = B * kv_heads * -(-(n * heads // kv_heads) // block)
+                        if shares > 1 and units < 256:        # every unit divided
+                            assert size >= 4 * units * shares * block * (dh + 2)

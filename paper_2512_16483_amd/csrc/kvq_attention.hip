@@ -149,7 +149,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
     const int G = H / c.heads, R = n * G;
     const int len = kvq_length(c, b, extra);
     const int tiles = (len + 31) / 32;
-    const int t0 = (int)((long)tiles * split / splits), t1 = (int)((long)tiles * (split + 1) / splits);
+    // (products below 2^30: at most 2^19 tiles and 1024 shares)
+    const int t0 = tiles * split / splits, t1 = tiles * (split + 1) / splits;
     const int last = max(tiles - 1, 0), last_row = max(len - 1, 0);
 
     // ---- Q: lane = row, the elements of the lane's part of a key
@@ -389,7 +390,7 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // Matrix cores and vector unit overlap only for instructions that do not wait for each other and stand next to each other, and a
 // product that adds to the one right before it waits (a pair of weights 38 cycles, a product 40, both 58, 66 where they add on).
 template <int DH>
-__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
+__global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
                                                                 int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,
                                                                 int full_units, int shares, float *__restrict__ part_o,
                                                                 float *__restrict__ part_ml)
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void kvq_attn_tiles_kernel(c
     const int len = kvq_length(c, b, extra);
     const int tiles = (len + 63) / 64;
     // tiles [t0, t1], one at least: where there is none, one in which nothing is seen
-    const int t0 = (int)((long)tiles * share / ranges), end = (int)((long)tiles * (share + 1) / ranges);
+    const int t0 = tiles * share / ranges, end = tiles * (share + 1) / ranges;       // (at most 2^18 tiles and 8 shares)
     const int t1 = max(end - 1, t0), seen_end = min(len, end * 64), last_row = max(len - 1, 0);
     const int r0 = rb * 128 + wave * 32, row = min(r0 + rl, R - 1);
     const bool active = __builtin_amdgcn_readfirstlane(r0 < R ? 1 : 0) != 0;

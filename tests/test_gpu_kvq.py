@@ -492,3 +492,29 @@ def test_block_over_the_cache(dtype, d, H, B, M, keep, Lp, ragged):
     att = kvq.attention(qn, *held, dh ** -0.5, [n + keep for n in lens]).reshape(B, keep, d)
     xk = np.stack([x[b, idx[b]] for b in range(B)])
     _check(f"block {dtype} {B}x{keep}", y, xk + att, dtype)
+
+
+def test_example_of_scales_over_the_cache():
+    """The example's chain: the 4-bit cache changes a scale's output by the error of the values it holds, about a tenth of the attention's
+    part of a row whose residual it is added to."""
+    import workloads
+    from examples.kvq_scales import run
+
+    W = workloads.Workload("small", 256, 4, 64, 512, (1, 2, 4, 9, 12), (9, 12), 2, 5, 16, 2, 2, "bf16")
+    lines = []
+    far = run(W, W.scales, 2, 2, out=lines.append)
+    assert sorted(far) == [1, 2, 4, 9, 12] and all(0 < x < 0.1 for x in far.values()), far
+    assert len(lines) == 7 and "read back" in lines[-1]
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 1), ("bf16", 140), ("f32", 3)])
+def test_lengths_outside_the_cache_are_held_to_it(dtype, n):
+    B, H, dh, cap = 4, 2, 64, 90
+    lens = [-7, 2 ** 31 - 1, cap + 1, 40]
+    ctx = _ctx(H, dh, dtype)
+    kv = _empty_cache(B, H, cap, dh, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    kk, vv = _load(kv, _rows(110, B, cap, H, dh, dtype), _rows(111, B, cap, H, dh, dtype))
+    q = _rows(112, B, n, H, dh, dtype, spread=0.2)
+    o = _attend(ctx, to_dev(q, dtype), kv, dtype, B, n)
+    assert not to_np(o[0]).any()
+    _check(f"held to the cache {dtype} {n}", o, kvq.attention(q, kk, vv, dh ** -0.5, [0, cap, cap, 40]), dtype)

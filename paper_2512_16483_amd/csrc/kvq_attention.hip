@@ -379,9 +379,10 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // softmax bound the time.
 //   S^T = K Q^T by the 32x32x64 block-scaled MFMA: it takes keys in 4 bits with their scale bytes as they lie in memory, so K is
 //     not converted, and at four times the rate of bf16 where the other operand has 6 bits.  Q, scaled so that scores come in units of
-//     log2, goes in as three E2M3 numbers per element (sign, 2 bits of exponent, 3 of mantissa, a shared 2^e per 32), each for
-//     what the one before leaves and 2^-5 smaller: off by at most 2^-13 of the block's largest element.  (Two leave 2^-8 of it,
-//     which scores of 20 and more, a few times the usual, show in the output.)
+//     log2, goes in as three E2M3 numbers per element (sign, 2 bits of exponent, 3 of mantissa, a shared 2^e, 2^(e-4), 2^(e-9) per 32),
+//     each for what the one before leaves.  That is at most 2^-2 of its unit, then 2^-3, which the next one's units hold whole
+//     (2^-5 after the first would be 8, past the largest, 7.5); what the last leaves is at most 2^(e-12), 2^-13 of the block's largest
+//     element.  (Two leave 2^-9 of it, which scores of 20 and more, a few times the usual, show in the output.)
 //   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
 // In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
 // product takes it, as in attention.hip.
@@ -487,14 +488,14 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
             const int e = min(max((int)((top + (1u << 19)) >> 23) - 2, 13), 252);
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-                const float size = __uint_as_float((uint32_t)(e - 5 * p) << 23);
+                const float size = __uint_as_float((uint32_t)(p ? e + 1 - 5 * p : e) << 23);
                 const uintx6_t x = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, size);
                 const floatx32_t back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(x, size);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) { even[i] -= back[2 * i]; odd[i] -= back[2 * i + 1]; }
                 qf[s][p] = intx8_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
             }
-            qs[s] = top >= 0x7f800000u ? 0xffffff : e | (e - 5) << 8 | (e - 10) << 16;
+            qs[s] = top >= 0x7f800000u ? 0xffffff : e | (e - 4) << 8 | (e - 9) << 16;
         }
     }
 

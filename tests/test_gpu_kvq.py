@@ -341,6 +341,26 @@ def test_attention_of_equal_scores_is_the_mean():
         assert (np.abs(o - want) <= lim).all()
 
 
+@pytest.mark.parametrize("dtype,dh,n", [("bf16", 64, 600), ("bf16", 128, 600), ("bf16", 128, 20), ("f32", 64, 20)])
+def test_queries_half_way_between_numbers_of_few_bits(dtype, dh, n):
+    """Queries whose elements, in units of log2, lie half-way between two numbers with three bits of mantissa, over one key, and on such
+    numbers over another, of the same score: what is left of the queries, added over a row, must not show in the weights."""
+    B, H, L, quarter = 8, 8, 440, dh // 4
+    ctx = _ctx(H, dh, dtype, attn_scale=float(np.log(2)))
+    sign = np.random.default_rng(20).choice([-1.0, 1.0], dh)
+    ties = [4.25, 4.75, 5.25, 5.75, 6.25, 6.75, 7.25]
+    q, k, v = np.zeros((B, n, H, dh), np.float32), np.zeros((B, L, H, dh), np.float32), _rows(21, B, L, H, dh, dtype)
+    for r in range(n):
+        t = ties[r % len(ties)]
+        q[:, r] = np.repeat([t, t, 4.0, t - 4.0], quarter) * sign
+    k[:, 3, :, :quarter] = sign[:quarter]                    # scores of quarter * t, both
+    k[:, 300, :, 2 * quarter:] = sign[2 * quarter:]
+    kv = _empty_cache(B, H, L, dh, len=L)
+    kk, vv = _load(kv, k, v)
+    _check(f"half-way {dtype} {dh} n {n}", _attend(ctx, to_dev(q, dtype), kv, dtype, B, n),
+           kvq.attention(q, kk, vv, np.log(2), [L] * B), dtype)
+
+
 def test_attention_scale_of_the_context():
     H, dh, n, L = 2, 64, 5, 90
     k, v, q = _rows(70, 1, L, H, dh, "f32"), _rows(71, 1, L, H, dh, "f32"), _rows(72, 1, n, H, dh, "f32")

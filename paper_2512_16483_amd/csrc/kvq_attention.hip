@@ -390,8 +390,10 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // The loop goes by halves of a tile: beside the softmax of one stand the scores of the next and the products of the one before, in turn.
 // Matrix cores and vector unit overlap only for instructions that do not wait for each other and stand next to each other, and a
 // product that adds to the one right before it waits (a pair of weights 38 cycles, a product 40, both 58, 66 where they add on).
-template <int DH>
-__global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
+// KG = 2: two groups of four wavefronts on the same rows, each with half of the keys and stages of its own, which meet in LDS at the end:
+// as full a CU as two workgroups make, without partial results in memory.
+template <int DH, int KG>
+__global__ __launch_bounds__(256 * KG, KG == 1 && DH == 64 ? 3 : 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
                                                                 int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,
                                                                 int full_units, int shares, float *__restrict__ part_o,
                                                                 float *__restrict__ part_ml)
@@ -400,10 +402,11 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     constexpr int VW = DH / 32;                              // words of values per thread
     constexpr int RAW = 64 * DH / 2;                         // bytes of a tile's codes
     constexpr int KOFF = 64 * DH * 2, VOFF = KOFF + RAW, SOFF = VOFF + RAW, STAGE = SOFF + 2 * 64 * NB;
-    __shared__ uint4 lds[3 * STAGE / 16];                    // [stage][values fp16 | codes of K | of V | scales of K | of V]
+    __shared__ uint4 lds[KG * 3 * STAGE / 16];               // [group][stage][values fp16 | codes of K | of V | scales of K | of V]
 
-    const int tid = threadIdx.x, lane = tid & 63, rl = lane & 31, g = lane >> 5;
+    const int tid = threadIdx.x & 255, lane = tid & 63, rl = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = KG > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8) : 0;
     int unit = blockIdx.x, share = 0, ranges = 1;
     if (unit < full_units) {
         unit = xcd_grouped(unit, full_units / nrb, nrb);
@@ -417,17 +420,18 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
     const int G = H / c.heads, R = n * G;
     const int len = kvq_length(c, b, extra);
     const int tiles = (len + 63) / 64;
-    // tiles [t0, t1], one at least: where there is none, one in which nothing is seen
-    const int t0 = tiles * share / ranges, end = tiles * (share + 1) / ranges;       // (at most 2^18 tiles and 8 shares)
-    const int t1 = max(end - 1, t0), seen_end = min(len, end * 64), last_row = max(len - 1, 0);
+    // the group's tiles [t0, t1], one at least and as many as the other's: where there is none, one in which nothing is seen
+    const int first_tile = tiles * share / ranges, end = tiles * (share + 1) / ranges;   // (at most 2^18 tiles and 16 shares)
+    const int trips = max((end - first_tile + KG - 1) / KG, 1), t0 = first_tile + kg * trips, t1 = t0 + trips - 1;
+    const int seen_end = min(len, min(end, t1 + 1) * 64), last_row = max(len - 1, 0);
     const int r0 = rb * 128 + wave * 32, row = min(r0 + rl, R - 1);
     const bool active = __builtin_amdgcn_readfirstlane(r0 < R ? 1 : 0) != 0;
 
     const size_t head = (size_t)(b * c.heads + hk) * c.capacity;
     const uint8_t *Kc = c.k + head * (DH / 2), *Vc = c.v + head * (DH / 2), *Ks = c.k_scale + head * NB, *Vs = c.v_scale + head * NB;
     const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
-    uint8_t *lds8 = reinterpret_cast<uint8_t *>(lds);
-    const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
+    uint8_t *lds8 = reinterpret_cast<uint8_t *>(lds) + kg * 3 * STAGE;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)lds + kg * 3 * STAGE;
 
     // ---- A tile by DMA.  K: 16-byte chunks of a row are turned by its number, so that the rows of sixteen lanes that read one chunk
     // lie in all banks.  V: the order in which the threads convert it: a quarter of a row each, neighbouring quads four rows apart
@@ -586,6 +590,10 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
             next = later;
             stage = s1;
             meet();
+        }
+        if (KG > 1) {                                        // (the meeting of the groups)
+            __syncthreads();
+            __syncthreads();
         }
         return;
     }
@@ -775,28 +783,66 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_tiles_kernel(const uint16_t *
         for (int i = 0; i < DB; ++i)
             acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(load_v(i, 32 + 16 * u), pf[1][u], acc[i], 0, 0, 0);
 
-    // ---- means, back at their size (see half_scale), which is stored or left with its weight for the merge
+    // ---- means, back at their size (see half_scale)
     {
         const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
         l_run = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
     }
     const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
-    if (r0 + rl >= R) return;
+    auto mean = [&](float x) { return __builtin_amdgcn_ldexpf(x * inv, acc_E - kTop - 127); };
     const size_t prow = ((size_t)(unit - full_units) * shares + share) * 128 + wave * 32 + rl;
     uint16_t *dst = o + (size_t)(b * (long)n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH;
+    // results, or a share's with their weight for the merge
+    auto put = [&](int d, float4 v) {
+        if (ranges > 1) *reinterpret_cast<float4 *>(part_o + prow * DH + d) = v;
+        else Quad<uint16_t>::store(dst + d, v);
+    };
+    auto put_weight = [&](float m, float l) {
+        if (ranges > 1 && g == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m / c_log2, l);
+    };
+    if constexpr (KG == 1) {
+        if (r0 + rl >= R) return;
 #pragma unroll
-    for (int i = 0; i < DB; ++i)
+        for (int i = 0; i < DB; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            const int d = 32 * i + 8 * (e >> 2) + 4 * g;
-            const float4 v = make_float4(__builtin_amdgcn_ldexpf(acc[i][e] * inv, acc_E - kTop - 127),
-                                         __builtin_amdgcn_ldexpf(acc[i][e + 1] * inv, acc_E - kTop - 127),
-                                         __builtin_amdgcn_ldexpf(acc[i][e + 2] * inv, acc_E - kTop - 127),
-                                         __builtin_amdgcn_ldexpf(acc[i][e + 3] * inv, acc_E - kTop - 127));
-            if (ranges > 1) *reinterpret_cast<float4 *>(part_o + prow * DH + d) = v;
-            else Quad<uint16_t>::store(dst + d, v);
-        }
-    if (ranges > 1 && g == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m_ref / c_log2, l_run);
+            for (int e = 0; e < 16; e += 4)
+                put(32 * i + 8 * (e >> 2) + 4 * g, make_float4(mean(acc[i][e]), mean(acc[i][e + 1]), mean(acc[i][e + 2]), mean(acc[i][e + 3])));
+        put_weight(m_ref, l_run);
+    } else {
+        // each group leaves half of its means, its reference and weight where the other finds them, and takes the other half to the end
+        constexpr int HB = DB / 2;
+        float4 *xo = reinterpret_cast<float4 *>(lds);        // [group][wave][block, quad][lane]
+        float2 *xm = reinterpret_cast<float2 *>(xo + 8 * HB * 4 * 64);   // [group][wave][lane]
+        __syncthreads();                                     // the stages have been read
+#pragma unroll
+        for (int i = 0; i < HB; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                xo[((kg * 4 + wave) * HB * 4 + i * 4 + e / 4) * 64 + lane] =
+                    make_float4(mean(kg ? acc[i][e] : acc[HB + i][e]), mean(kg ? acc[i][e + 1] : acc[HB + i][e + 1]),
+                                mean(kg ? acc[i][e + 2] : acc[HB + i][e + 2]), mean(kg ? acc[i][e + 3] : acc[HB + i][e + 3]));
+        xm[(kg * 4 + wave) * 64 + lane] = make_float2(m_ref, l_run);
+        __syncthreads();
+        if (r0 + rl >= R) return;
+        const float2 other = xm[((1 - kg) * 4 + wave) * 64 + lane];
+        const float m = fmaxf(m_ref, other.x), fin = fmaxf(m, -1e30f);
+        float own = l_run * __builtin_amdgcn_exp2f(m_ref - fin), theirs = other.y * __builtin_amdgcn_exp2f(other.x - fin);
+        const float all = own + theirs, each = all == 0.f ? 0.f : 1.0f / all;
+        own *= each;
+        theirs *= each;
+#pragma unroll
+        for (int i = 0; i < HB; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                float a[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a[k] = mean(kg ? acc[HB + i][e + k] : acc[i][e + k]);
+                const float4 x = xo[(((1 - kg) * 4 + wave) * HB * 4 + i * 4 + e / 4) * 64 + lane];
+                put(32 * (kg * HB + i) + 8 * (e >> 2) + 4 * g, make_float4(fmaf(x.x, theirs, a[0] * own), fmaf(x.y, theirs, a[1] * own),
+                                                                          fmaf(x.z, theirs, a[2] * own), fmaf(x.w, theirs, a[3] * own)));
+            }
+        if (!kg) put_weight(m, all);
+    }
 }
 
 // The shares of rows joined: each is a mean and its weight.  A unit is a block of BR rows of one (sample, kv head); the shares
@@ -861,21 +907,23 @@ __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__rest
 }
 
 // Blocks of how many rows of a (sample, kv head) an attention is run by: 16 (kvq_attn_rows_kernel) or 128 (kvq_attn_tiles_kernel, bf16
-// only).  The first needs least time per block and is bound by the work, which it does at 0.4 of the other's pace; the other
-// fetches and converts for 128 rows whatever there are.  us by 16 / by 128, 16 heads of 128: 32 x 48 rows x 3001 keys 81 / 82, 32 x 64 101 / 83,
-// 8 x 96 x 2521 36 / 39, 8 x 128 46 / 43, 1 x 128 x 4813 20 / 25, 4 x 200 x 2500 42 / 39; 30 heads of 64: 8 x 128 x 871 24 / 26, 8 x 200 36 / 26.
+// only).  The first starts and ends soonest and is bound by the work, which it does at less than half the other's pace; the other fetches
+// and converts for 128 rows whatever there are, and joins groups and shares.  So the work decides, and at half a block and less twice as
+// much of it is still by 16.  us by 16 / by 128, 16 heads of 128: 1 x 144 rows x 265 keys 6.3 / 16, 1 x 400 x 921 13 / 24, 1 x 576 x 1497
+// 24 / 27, 1 x 200 x 4813 29 / 27, 2 x 128 x 5000 30 / 28, 16 x 100 x 1000 40 / 28, 8 x 64 x 2521 27 / 32, 16 x 64 x 3000 55 / 50,
+// 32 x 48 x 3001 81 / 82; 30 heads of 64: 1 x 324 x 640 9.6 / 13, 2 x 231 x 871 14 / 16, 8 x 169 x 316 17 / 15, 8 x 100 x 871 23 / 17.
 static int kvq_block(DType dt, int B, int n, int H, int heads, int length)
 {
     const int rows = n * (H / heads);
     if (dt != DType::BF16 || rows <= 48) return 16;
-    return rows <= 128 && (long)B * heads * ((rows + 15) / 16) * length <= 1l << 21 ? 16 : 128;
+    return (long)B * heads * ((rows + 15) / 16) * length <= (rows <= 64 ? 1l << 21 : 1l << 20) ? 16 : 128;
 }
 
 // nrb blocks per (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
 // `ragged`: samples of lengths of their own, which only the GPU knows.
-// waves: wavefronts of a workgroup that divide a block's keys.
+// waves: wavefronts of a workgroup, which divide a block's keys (16 rows), or its rows and, if there are 8, keys (128 rows).
 struct KvqRun { int block, nrb, units, full, shares, waves; };
-static KvqRun kvq_run(int block, int B, int n, int H, int heads, int length, bool ragged)
+static KvqRun kvq_run(int block, int B, int n, int H, int heads, int Dh, int length, bool ragged)
 {
     KvqRun run;
     run.block = block;
@@ -899,11 +947,19 @@ static KvqRun kvq_run(int block, int B, int n, int H, int heads, int length, boo
         run.full = run.shares > 1 ? 0 : run.units;
         return run;
     }
-    // two workgroups on every CU; those beyond the last full round are divided, into pieces of four tiles at least
-    const int slots = 512, rest = run.units % slots, most = (length + 63) / 64 / 4;
+    // Up to a workgroup on every CU: two groups of wavefronts in each, and shares where there are half as many or fewer (4 x 300 x 2500 keys
+    // of 16 heads 44 us, 52 by one group; 2 x 130 x 2000 24, 25; 1 x 1664 x 6000 88, 99).  Otherwise, and over long caches where shares of
+    // one group leave fewer CUs idle (1 x 1152 x 6000, 144 blocks, 76 us, 85 by two groups; 30 heads of 64, 640 x 6000, 150 blocks, 49, 64;
+    // but 1 x 1152 x 2500 46, 43), two workgroups on every CU, three of 64-wide rows; those beyond the last full round are divided.
+    // Pieces have four tiles at least for each group.
+    const int two = Dh == 64 ? 768 : 512;
+    bool groups = run.units <= 256;
+    if (groups && length >= 4096) groups = (two / run.units) * 256 * 8 <= (256 / run.units) * two * 9;
+    const int slots = groups ? 256 : two, rest = run.units % slots, most = (length + 63) / 64 / (groups ? 8 : 4);
+    run.waves = groups ? 8 : 4;
     run.full = run.units - rest;
     int want = rest ? slots / rest : 1;
-    if (want > 8) want = 8;
+    if (want > 16) want = 16;
     run.shares = want < most ? want : most > 0 ? most : 1;
     if (run.shares == 1) run.full = run.units;
     return run;
@@ -916,7 +972,7 @@ size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, in
     size_t most = 0;
     for (int block = 16; block <= 128; block *= 8) {
         if (block == 128 ? kvq_block(dt, B, n, H, heads, capacity) == 16 : kvq_block(dt, B, n, H, heads, 1) == 128) continue;
-        const KvqRun run = kvq_run(block, B, n, H, heads, capacity, true);
+        const KvqRun run = kvq_run(block, B, n, H, heads, Dh, capacity, true);
         const size_t floats = (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
         if (floats > most) most = floats;
     }
@@ -924,10 +980,10 @@ size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, in
 }
 
 // How an attention is run, for the tests: 100000 * rows of a block + 1000 * wavefronts + shares.
-int kvq_attention_ways(int bf16, int B, int n, int H, int heads, int length, int ragged)
+int kvq_attention_ways(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged)
 {
     const int block = kvq_block(bf16 ? DType::BF16 : DType::F32, B, n, H, heads, length);
-    const KvqRun run = kvq_run(block, B, n, H, heads, length, ragged != 0);
+    const KvqRun run = kvq_run(block, B, n, H, heads, Dh, length, ragged != 0);
     return 100000 * block + 1000 * run.waves + run.shares;
 }
 
@@ -936,7 +992,7 @@ static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int e
                        void *o, float *part, hipStream_t st)
 {
     const int length = c.lens ? c.capacity : c.len + extra;
-    const KvqRun run = kvq_run(kvq_block(dt, B, n, H, c.heads, length), B, n, H, c.heads, length, c.lens != nullptr);
+    const KvqRun run = kvq_run(kvq_block(dt, B, n, H, c.heads, length), B, n, H, c.heads, DH, length, c.lens != nullptr);
     const int divided = run.units - run.full;
     float *part_ml = part + (size_t)divided * run.shares * run.block * DH;
     const unsigned wgs = (unsigned)(run.full + divided * run.shares);
@@ -949,8 +1005,12 @@ static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int e
         else FVAR_ROWS(4);
 #undef FVAR_ROWS
     } else if constexpr (sizeof(T) == 2) {
-        launch(kvq_attn_tiles_kernel<DH>, dim3(wgs), dim3(256), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, run.nrb,
-               run.full, run.shares, part, part_ml);
+        if (run.waves == 8)
+            launch(kvq_attn_tiles_kernel<DH, 2>, dim3(wgs), dim3(512), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, run.nrb,
+                   run.full, run.shares, part, part_ml);
+        else
+            launch(kvq_attn_tiles_kernel<DH, 1>, dim3(wgs), dim3(256), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, run.nrb,
+                   run.full, run.shares, part, part_ml);
     }
     if (divided) {
         const int total = divided * run.block, per = 256 / (DH / 4);

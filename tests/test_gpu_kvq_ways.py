@@ -18,7 +18,7 @@ from test_kvq_host import WAYS, ways  # noqa: E402
 @pytest.mark.parametrize("case", sorted(WAYS))
 def test_attention_in_every_way(case):
     dtype, dh, H, heads, B, n, L, ragged, expect = WAYS[case]
-    assert ways(dtype, B, n, H, heads, L, ragged) == expect
+    assert ways(dtype, B, n, H, heads, dh, L, ragged) == expect
     k, v, q = _rows(1, B, L, heads, dh, dtype), _rows(2, B, L, heads, dh, dtype), _rows(3, B, n, H, dh, dtype, spread=0.2)
     lens = [(L * (b + 1) // B + 7 * b) % (L + 1) if ragged else L for b in range(B)]
     ctx = _ctx(H, dh, dtype)

@@ -153,9 +153,9 @@ def test_binding_refuses_tensors_that_do_not_fit():
 
 
 # ------------------------------------------------------------------------------------ ways of running the attention
-def ways(dtype, B, n, H, heads, length, ragged):
-    """(rows of a block, wavefronts that divide its keys, shares of the keys of a divided block)"""
-    w = fv.load_library()["_ZN4fvar18kvq_attention_waysEiiiiiii"](dtype == "bf16", B, n, H, heads, length, ragged)
+def ways(dtype, B, n, H, heads, dh, length, ragged):
+    """(rows of a block, wavefronts of its workgroup, shares of the keys of a divided block)"""
+    w = fv.load_library()["_ZN4fvar18kvq_attention_waysEiiiiiiii"](dtype == "bf16", B, n, H, heads, dh, length, ragged)
     return w // 100000, w // 1000 % 100, w % 1000
 
 
@@ -174,12 +174,17 @@ WAYS = {
     "16 rows, 20 shares": ("bf16", 64, 4, 4, 1, 3, 5151, False, (16, 4, 20)),
     "16 rows, 20 shares, fp32": ("f32", 128, 4, 4, 1, 3, 5151, False, (16, 4, 20)),
     "16 rows, shares of ragged samples": ("bf16", 128, 8, 8, 32, 1, 2100, True, (16, 4, 2)),
-    "128 rows, whole": ("bf16", 128, 8, 8, 32, 200, 130, False, (128, 4, 1)),
-    "128 rows, all divided": ("bf16", 128, 4, 4, 2, 230, 1600, False, (128, 4, 6)),
-    "128 rows, all divided, 64": ("bf16", 64, 8, 2, 2, 130, 2900, False, (128, 4, 8)),
-    "128 rows, last round divided": ("bf16", 64, 16, 16, 20, 200, 1100, False, (128, 4, 4)),
+    "128 rows, whole": ("bf16", 128, 8, 8, 32, 200, 330, False, (128, 4, 1)),
+    "128 rows, two groups": ("bf16", 128, 4, 4, 20, 230, 900, False, (128, 8, 1)),
+    "128 rows, two groups, 64": ("bf16", 64, 4, 2, 32, 130, 1000, False, (128, 8, 1)),
+    "128 rows, two groups, ragged": ("bf16", 64, 8, 8, 14, 240, 1000, True, (128, 8, 1)),
+    "128 rows, two groups, divided": ("bf16", 128, 8, 8, 4, 230, 3600, False, (128, 8, 4)),
+    "128 rows, two groups, many shares": ("bf16", 64, 8, 2, 1, 130, 16000, False, (128, 8, 16)),
+    "128 rows, two groups, ragged shares": ("bf16", 128, 4, 4, 9, 200, 2300, True, (128, 8, 3)),
+    "128 rows, one group, divided": ("bf16", 128, 4, 4, 18, 129, 4100, False, (128, 4, 3)),
+    "128 rows, last round divided": ("bf16", 64, 16, 16, 31, 200, 1100, False, (128, 4, 3)),
     "128 rows, last round divided, 128": ("bf16", 128, 4, 4, 70, 200, 600, True, (128, 4, 2)),
-    "128 rows, last round divided, ragged": ("bf16", 64, 16, 8, 40, 90, 1400, True, (128, 4, 4)),
+    "128 rows, last round divided, ragged": ("bf16", 128, 16, 8, 40, 90, 1400, True, (128, 4, 4)),
 }
 
 
@@ -187,7 +192,7 @@ WAYS = {
 def test_ways_that_the_gpu_tests_are_there_for(case):
     """tests/test_gpu_kvq_ways.py runs these: another choice of constants must not take a way out of its reach unseen."""
     dtype, dh, H, heads, B, n, L, ragged, expect = WAYS[case]
-    assert ways(dtype, B, n, H, heads, L, ragged) == expect
+    assert ways(dtype, B, n, H, heads, dh, L, ragged) == expect
 
 
 def test_small_changes_of_length_and_lengths_of_their_own_need_no_more_workspace():
@@ -202,7 +207,7 @@ def test_small_changes_of_length_and_lengths_of_their_own_need_no_more_workspace
                         size = lib.fvar_kvq_attention_workspace_bytes(ctx.handle, C.byref(_cache(kv_heads=kv_heads, capacity=cap, len=1)), B, n)
                         assert size >= last                   # never falls as the capacity grows
                         last = size
-                        block, _, shares = ways(dtype, B, n, heads, kv_heads, cap, False)
+                        block, _, shares = ways(dtype, B, n, heads, kv_heads, dh, cap, False)
                         units = B * kv_heads * -(-(n * heads // kv_heads) // block)
                         if shares > 1 and units < 256:        # every unit divided
                             assert size >= 4 * units * shares * block * (dh + 2)

@@ -392,8 +392,11 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // product that adds to the one right before it waits (a pair of weights 38 cycles, a product 40, both 58, 66 where they add on).
 // KG = 2: two groups of four wavefronts on the same rows, each with half of the keys and stages of its own, which meet in LDS at the end:
 // as full a CU as two workgroups make, without partial results in memory.
-template <int DH, int KG>
-__global__ __launch_bounds__(256 * KG, KG == 1 && DH == 64 ? 3 : 2) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
+// WAVES, of a SIMD: 3 with 64-wide rows where there are more than two workgroups for every CU (30 heads, 8 x 410 x 1281 keys 66 us, 69 with
+// 2); with 2 there are registers for products that start from the reference, an addition less per weight (32 x 480 x 3001, 16 heads of 128,
+// 396 to 386 us; 30 of 64, 8 x 231 x 871, 25.2 to 23.9).
+template <int DH, int KG, int WAVES>
+__global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
                                                                 int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,
                                                                 int full_units, int shares, float *__restrict__ part_o,
                                                                 float *__restrict__ part_ml)
@@ -524,7 +527,18 @@ __global__ __launch_bounds__(256 * KG, KG == 1 && DH == 64 ? 3 : 2) void kvq_att
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = floatx16_t{0};
     float m_ref = -INFINITY, l_run = 0.f, most = -1.f;       // most: the sum of weights from which on a reference is looked for
-    float base = kShift;                                     // - reference + kShift, in units of log2 as the scores
+    // - reference + kShift, in units of log2 as the scores; where registers allow, the products that make scores start from it
+    constexpr bool FROM = WAVES == 2;
+    float base = kShift;
+    floatx16_t bases;
+    auto set_base = [&](float x) {
+        base = x;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bases[i] = FROM ? x : 0.f;
+        if constexpr (FROM) asm volatile("" : "+v"(bases));
+    };
+    set_base(kShift);
+    auto with_base = [&](float score) { return FROM ? score : score + base; };
     int E = 0, E_now = 0, acc_E = 0;                         // of the values converted last, of the tile at work, of the sums
 
     // A thread's values as they came, and their scale byte; all scale bytes of the lane's row.  The rows that can be seen, and the
@@ -625,7 +639,7 @@ __global__ __launch_bounds__(256 * KG, KG == 1 && DH == 64 ? 3 : 2) void kvq_att
         intx8_t{(int)k[ks][0], (int)k[ks][1], (int)k[ks][2], (int)k[ks][3], 0, 0, 0, 0}, qf[ks][p], on, 4, 2, 2 * (ks), sc, p, qs[ks])
     // product number i of a half's scores: smallest pieces first
     auto score = [&](int half, int i, const uintx4_t *k, int sc) {
-        if (i == 0) FVAR_S(half, 0, 2, floatx16_t{0});
+        if (i == 0) FVAR_S(half, 0, 2, bases);
         if (i == 1) FVAR_S(half, KS - 1, KS == 2 ? 2 : 1, s[half]);
         if (i == 2) FVAR_S(half, 0, KS == 2 ? 1 : 0, s[half]);
         if constexpr (KS == 2) {
@@ -671,8 +685,8 @@ __global__ __launch_bounds__(256 * KG, KG == 1 && DH == 64 ? 3 : 2) void kvq_att
                     x[2 * p1 + 1] = __builtin_amdgcn_exp2f(x[2 * p1 + 1]);
                 }
                 if (p0 < 8) {
-                    x[2 * p0] = s[half][2 * p0] + base;
-                    x[2 * p0 + 1] = s[half][2 * p0 + 1] + base;
+                    x[2 * p0] = with_base(s[half][2 * p0]);
+                    x[2 * p0 + 1] = with_base(s[half][2 * p0 + 1]);
                 }
                 if (p2 >= 0 && p2 < 8) {
                     a += x[2 * p2];
@@ -713,6 +727,7 @@ __global__ __launch_bounds__(256 * KG, KG == 1 && DH == 64 ? 3 : 2) void kvq_att
             float mx = s[half][0];
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
+            if constexpr (FROM) mx -= base;
             mx = fmaxf(m_ref, mx);
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
             const float now = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
@@ -722,7 +737,12 @@ __global__ __launch_bounds__(256 * KG, KG == 1 && DH == 64 ? 3 : 2) void kvq_att
             m_ref = now;
             most = none ? -1.f : kMost;
             acc_E = E_now;
-            base = none ? kShift : kShift - now;
+            const float before = base;
+            set_base(none ? kShift : kShift - now);
+            if constexpr (FROM) {
+                s[0] += base - before;
+                s[1] += base - before;
+            }
             l_run *= alpha;
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
@@ -732,7 +752,7 @@ __global__ __launch_bounds__(256 * KG, KG == 1 && DH == 64 ? 3 : 2) void kvq_att
             sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(s[half][i] + base), y = __builtin_amdgcn_exp2f(s[half][i + 1] + base);
+                const float x = __builtin_amdgcn_exp2f(with_base(s[half][i])), y = __builtin_amdgcn_exp2f(with_base(s[half][i + 1]));
                 sum += x + y;
                 const f16x2_t p = __builtin_convertvector((floatx2_t{x, y}), f16x2_t);
                 pf[half][i >> 3][i & 7] = p[0];
@@ -1005,12 +1025,13 @@ static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int e
         else FVAR_ROWS(4);
 #undef FVAR_ROWS
     } else if constexpr (sizeof(T) == 2) {
-        if (run.waves == 8)
-            launch(kvq_attn_tiles_kernel<DH, 2>, dim3(wgs), dim3(512), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, run.nrb,
-                   run.full, run.shares, part, part_ml);
-        else
-            launch(kvq_attn_tiles_kernel<DH, 1>, dim3(wgs), dim3(256), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, (T *)o, run.nrb,
-                   run.full, run.shares, part, part_ml);
+#define FVAR_TILES(KG, WAVES)                                                                                            \
+    launch(kvq_attn_tiles_kernel<DH, KG, WAVES>, dim3(wgs), dim3(256 * KG), 0, st, (const T *)q, ld, c, extra, n, H,      \
+           c_log2, (T *)o, run.nrb, run.full, run.shares, part, part_ml)
+        if (run.waves == 8) FVAR_TILES(2, 2);
+        else if (DH == 128 || wgs <= 512) FVAR_TILES(1, 2);
+        else if constexpr (DH == 64) FVAR_TILES(1, 3);
+#undef FVAR_TILES
     }
     if (divided) {
         const int total = divided * run.block, per = 256 / (DH / 4);

@@ -175,6 +175,7 @@ WAYS = {
     "16 rows, 20 shares, fp32": ("f32", 128, 4, 4, 1, 3, 5151, False, (16, 4, 20)),
     "16 rows, shares of ragged samples": ("bf16", 128, 8, 8, 32, 1, 2100, True, (16, 4, 2)),
     "128 rows, whole": ("bf16", 128, 8, 8, 32, 200, 330, False, (128, 4, 1)),
+    "128 rows, whole, 64": ("bf16", 64, 8, 8, 32, 200, 330, False, (128, 4, 1)),
     "128 rows, two groups": ("bf16", 128, 4, 4, 20, 230, 900, False, (128, 8, 1)),
     "128 rows, two groups, 64": ("bf16", 64, 4, 2, 32, 130, 1000, False, (128, 8, 1)),
     "128 rows, two groups, ragged": ("bf16", 64, 8, 8, 14, 240, 1000, True, (128, 8, 1)),

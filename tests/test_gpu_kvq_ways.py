@@ -30,6 +30,33 @@ def test_attention_in_every_way(case):
     assert torch.equal(o, _attend(ctx, qd, kv, dtype, B, n))
 
 
+@pytest.mark.parametrize("case", sorted(WAYS))
+def test_hidden_rows_in_every_way(case):
+    """A third of the rows hidden, a stretch of 70, the first and the last of all samples but one, whose rows are all hidden; what they
+    hold is not a number."""
+    dtype, dh, H, heads, B, n, L, ragged, expect = WAYS[case]
+    if n * B * heads * L > 5e7:
+        n = max(1, int(5e7 / (B * heads * L)))               # (the same blocks and waves, or others: all are run somewhere)
+    g = np.random.default_rng(4)
+    k, v, q = _rows(1, B, L, heads, dh, dtype), _rows(2, B, L, heads, dh, dtype), _rows(3, B, n, H, dh, dtype, spread=0.2)
+    lens = [(L * (b + 1) // B + 7 * b) % (L + 1) if ragged else L for b in range(B)]
+    mask = (g.random((B, L)) < 0.67).astype(np.uint8)
+    mask[:, L // 3:L // 3 + 70] = 0
+    mask[:, 0] = mask[:, -1] = 0
+    if B > 1:
+        mask[B // 2] = 0
+    kv = _empty_cache(B, heads, L, dh, len=L, lens=torch.tensor(lens, dtype=torch.int32, device="cuda") if ragged else None,
+                      mask=torch.from_numpy(mask).cuda())
+    kk, vv = _load(kv, k, v)
+    hidden = torch.from_numpy(mask == 0).cuda()[:, None, :, None]
+    for t in (kv.k, kv.v, kv.k_scale, kv.v_scale):
+        t.masked_fill_(hidden, 255)
+    o = _attend(_ctx(H, dh, dtype), to_dev(q, dtype), kv, dtype, B, n)
+    _check(f"hidden, {case}", o, kvq.attention(q, kk, vv, dh ** -0.5, lens, mask), dtype)
+    if B > 1:
+        assert not to_np(o)[B // 2].any()
+
+
 @pytest.mark.parametrize("dtype,n", [("bf16", 1), ("bf16", 100), ("bf16", 128), ("bf16", 200), ("f32", 20)])
 def test_one_workspace_serves_every_length(dtype, n):
     """The workspace of the capacity is enough for any number of rows held, whichever way that is run, and its contents do not matter."""

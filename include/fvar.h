@@ -21,6 +21,10 @@
  * fvar_upsample_tokens brings a cached token map (or the thin factor W_c of its
  * rank-r form) from the previous scale's grid to the current one.
  *
+ * fvar_kvq_append, fvar_kvq_read and fvar_kvq_attention write, read back and attend
+ * over a key/value cache held in 4 bits (fvar_kvq), and fvar_block_forward_*_kvq
+ * run the block over one.
+ *
  * Conventions common to every call
  *  - Every tensor pointer is DEVICE memory owned by the caller, row-major,
  *    contiguous, 16-byte aligned, of element type `fvar_config.dtype`

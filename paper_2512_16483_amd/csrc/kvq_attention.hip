@@ -676,7 +676,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         for (int i = 0; i < DB; ++i) vf[i] = load_v(i, other * 32);
         if constexpr (half == 0) read_raw(s1, raw);
         __builtin_amdgcn_sched_barrier(0);
-        float x[16], a = 0.f, bsum = 0.f;
+        float x[16], a, bsum;
 #pragma unroll
         for (int step = 0; step < STEPS; ++step) {
             const int before = min((step + 1) / 2, NS);      // scores' products up to here, this one included if it is one
@@ -699,8 +699,9 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
                     x[2 * p0 + 1] = with_base(s[half][2 * p0 + 1]);
                 }
                 if (p2 >= 0 && p2 < 8) {
-                    a += x[2 * p2];
-                    bsum += x[2 * p2 + 1];
+                    a = p2 ? a + x[2 * p2] : x[0];
+                    bsum = p2 ? bsum + x[2 * p2 + 1] : x[1];
+                    asm volatile("" : "+v"(a), "+v"(bsum));  // here, not after the region with all of x alive until then
                     const f16x2_t p = __builtin_convertvector((floatx2_t{x[2 * p2], x[2 * p2 + 1]}), f16x2_t);
                     pf[half][p2 >> 2][(2 * p2) & 7] = p[0];
                     pf[half][p2 >> 2][(2 * p2 + 1) & 7] = p[1];

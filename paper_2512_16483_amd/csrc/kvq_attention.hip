@@ -823,35 +823,49 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
     auto mean = [&](float x) { return __builtin_amdgcn_ldexpf(x * inv, acc_E - kTop - 127); };
     const size_t prow = ((size_t)(unit - full_units) * shares + share) * 128 + wave * 32 + rl;
     uint16_t *dst = o + (size_t)(b * (long)n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH;
-    // results, or a share's with their weight for the merge
-    auto put = [&](int d, float4 v) {
-        if (ranges > 1) *reinterpret_cast<float4 *>(part_o + prow * DH + d) = v;
-        else Quad<uint16_t>::store(dst + d, v);
+    // Two quads of results that lie eight apart in the lane's row: four more stand in the lane 32 further, which changes one of its
+    // quads for one of these, so that each stores 16 bytes (30 heads of 64: 8 x 231 x 871 25.0 to 24.1 us, 8 x 410 x 1281 69 to 64).  A share's,
+    // with its weight, go as they are to the merge.
+    auto put = [&](auto divided, int d, float4 x, float4 y) {
+        if constexpr (decltype(divided)::value) {
+            float *to = part_o + prow * DH + d + 4 * g;
+            *reinterpret_cast<float4 *>(to) = x;
+            *reinterpret_cast<float4 *>(to + 8) = y;
+        } else {
+            const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16x2(x.x, x.y), pack_bf16x2(y.x, y.y), false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16x2(x.z, x.w), pack_bf16x2(y.z, y.w), false, false);
+            *reinterpret_cast<uint4 *>(dst + d + 8 * g) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+        }
     };
     auto put_weight = [&](float m, float l) {
         if (ranges > 1 && g == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m / c_log2, l);
     };
+    auto quad_mean = [&](const floatx16_t &x, int e) { return make_float4(mean(x[e]), mean(x[e + 1]), mean(x[e + 2]), mean(x[e + 3])); };
     if constexpr (KG == 1) {
         if (r0 + rl >= R) return;
+        auto finish = [&](auto divided) {
 #pragma unroll
-        for (int i = 0; i < DB; ++i)
+            for (int i = 0; i < DB; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                put(32 * i + 8 * (e >> 2) + 4 * g, make_float4(mean(acc[i][e]), mean(acc[i][e + 1]), mean(acc[i][e + 2]), mean(acc[i][e + 3])));
+                for (int e = 0; e < 16; e += 8) put(divided, 32 * i + 2 * e, quad_mean(acc[i], e), quad_mean(acc[i], e + 4));
+        };
+        if (ranges > 1) finish(std::true_type{});
+        else finish(std::false_type{});
         put_weight(m_ref, l_run);
     } else {
         // each group leaves half of its means, its reference and weight where the other finds them, and takes the other half to the end
         constexpr int HB = DB / 2;
         float4 *xo = reinterpret_cast<float4 *>(lds);        // [group][wave][block, quad][lane]
         float2 *xm = reinterpret_cast<float2 *>(xo + 8 * HB * 4 * 64);   // [group][wave][lane]
+        auto leave = [&](const floatx16_t *x) {
+#pragma unroll
+            for (int i = 0; i < HB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) xo[((kg * 4 + wave) * HB * 4 + i * 4 + e / 4) * 64 + lane] = quad_mean(x[i], e);
+        };
         __syncthreads();                                     // the stages have been read
-#pragma unroll
-        for (int i = 0; i < HB; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                xo[((kg * 4 + wave) * HB * 4 + i * 4 + e / 4) * 64 + lane] =
-                    make_float4(mean(kg ? acc[i][e] : acc[HB + i][e]), mean(kg ? acc[i][e + 1] : acc[HB + i][e + 1]),
-                                mean(kg ? acc[i][e + 2] : acc[HB + i][e + 2]), mean(kg ? acc[i][e + 3] : acc[HB + i][e + 3]));
+        if (kg) leave(acc);
+        else leave(acc + HB);
         xm[(kg * 4 + wave) * 64 + lane] = make_float2(m_ref, l_run);
         __syncthreads();
         if (r0 + rl >= R) return;
@@ -861,17 +875,24 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         const float all = own + theirs, each = all == 0.f ? 0.f : 1.0f / all;
         own *= each;
         theirs *= each;
+        auto finish = [&](auto divided, const floatx16_t *x) {
+            auto joined = [&](int i, int e) {
+                const float4 a = quad_mean(x[i], e), b = xo[(((1 - kg) * 4 + wave) * HB * 4 + i * 4 + e / 4) * 64 + lane];
+                return make_float4(fmaf(b.x, theirs, a.x * own), fmaf(b.y, theirs, a.y * own), fmaf(b.z, theirs, a.z * own),
+                                   fmaf(b.w, theirs, a.w * own));
+            };
 #pragma unroll
-        for (int i = 0; i < HB; ++i)
+            for (int i = 0; i < HB; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                float a[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] = mean(kg ? acc[HB + i][e + k] : acc[i][e + k]);
-                const float4 x = xo[(((1 - kg) * 4 + wave) * HB * 4 + i * 4 + e / 4) * 64 + lane];
-                put(32 * (kg * HB + i) + 8 * (e >> 2) + 4 * g, make_float4(fmaf(x.x, theirs, a[0] * own), fmaf(x.y, theirs, a[1] * own),
-                                                                          fmaf(x.z, theirs, a[2] * own), fmaf(x.w, theirs, a[3] * own)));
-            }
+                for (int e = 0; e < 16; e += 8) put(divided, 32 * (kg * HB + i) + 2 * e, joined(i, e), joined(i, e + 4));
+        };
+        if (ranges > 1) {
+            if (kg) finish(std::true_type{}, acc + HB);
+            else finish(std::true_type{}, acc);
+        } else {
+            if (kg) finish(std::false_type{}, acc + HB);
+            else finish(std::false_type{}, acc);
+        }
         if (!kg) put_weight(m, all);
     }
 }

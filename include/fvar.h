@@ -310,7 +310,7 @@ fvar_status fvar_kvq_read(fvar_ctx *ctx, fvar_stream stream, const fvar_kvq *kv,
  * visible hold, NaN included, has no influence.  q: query i of sample b starts at element (b*n + i)*ld and holds
  * [heads][Dh]; ld = 0 stands for hidden; a multiple of 8 for bf16 (of 4 for fp32).  o:[B][n][heads][Dh], must not overlap q.
  * B*n*heads <= 2^25.  ws: at least fvar_kvq_attention_workspace_bytes(ctx,kv,B,n), which depends on kv_heads and capacity
- * but not on the pointers, and may be 0. */
+ * but not on the pointers, and may be 0 (as it is for sizes that the call refuses). */
 size_t fvar_kvq_attention_workspace_bytes(const fvar_ctx *ctx, const fvar_kvq *kv, int32_t B, int32_t n);
 fvar_status fvar_kvq_attention(fvar_ctx *ctx, fvar_stream stream, const void *q, int32_t ld, const fvar_kvq *kv, int32_t B,
                                int32_t n, void *o, void *ws, size_t ws_bytes);

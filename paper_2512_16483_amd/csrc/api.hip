@@ -228,10 +228,11 @@ int row_pitch(const fvar_ctx *c, int ld, int row)
     return ld < row || ld % chunk ? -1 : ld;
 }
 
-// Whether the sizes of a cache are some that workspace can be computed for.
-bool kvq_sizes(const fvar_ctx *c, const fvar_kvq *kv, int B)
+// Whether the sizes are some that workspace can be computed for: those that the calls accept.
+bool kvq_sizes(const fvar_ctx *c, const fvar_kvq *kv, int B, int n)
 {
-    return kv && B >= 1 && kv->kv_heads >= 1 && c->cfg.heads % kv->kv_heads == 0 && kv->capacity >= 1;
+    return kv && B >= 1 && n >= 1 && kv->kv_heads >= 1 && c->cfg.heads % kv->kv_heads == 0 && kv->capacity >= 1 &&
+           kv->capacity <= 1 << 24 && (int64_t)B * kv->kv_heads <= 65535 && (int64_t)B * n <= (1 << 25) / c->cfg.heads;
 }
 
 size_t kvq_attention_ws(const fvar_ctx *c, const fvar_kvq *kv, int B, int n)
@@ -575,7 +576,7 @@ fvar_status fvar_block_forward_pruned_kvq(fvar_ctx *c, fvar_stream stream, const
 
 size_t fvar_block_kvq_workspace_bytes(const fvar_ctx *c, const fvar_kvq *kv, int32_t B, int32_t rows)
 {
-    if (!c || !kvq_sizes(c, kv, B) || rows < 1) return 0;
+    if (!c || !kvq_sizes(c, kv, B, rows)) return 0;
     return carve(c, nullptr, B, rows, kv).total + (c->debug_checks ? kCanaryBytes : 0);
 }
 
@@ -621,7 +622,7 @@ fvar_status fvar_kvq_read(fvar_ctx *c, fvar_stream stream, const fvar_kvq *kv, i
 
 size_t fvar_kvq_attention_workspace_bytes(const fvar_ctx *c, const fvar_kvq *kv, int32_t B, int32_t n)
 {
-    if (!c || !kvq_sizes(c, kv, B) || n < 1) return 0;
+    if (!c || !kvq_sizes(c, kv, B, n)) return 0;
     return kvq_attention_ws(c, kv, B, n);
 }
 

@@ -992,7 +992,7 @@ static KvqRun kvq_run(int block, int B, int n, int H, int heads, int Dh, int len
         // Enough workgroups for two on every CU; four where samples differ, so that a CU that has had short ones takes more (32 samples of
         // 8461 keys, 8 kv heads: 512, 1024, 2048 places 53, 59, 59 us; of 1 to 16921 keys 1024, 2048, 4096 places 56, 59, 69 us).  Each with
         // two tiles per wavefront at least, or eight where every CU has a workgroup already and the joining, 3 us, is for nothing else
-        // (fp32, 2 x 128 x 552, 16 heads of 64: 8.7 us whole, 11.5 in two shares).
+        // (fp32, 2 x 128 x 552, 16 heads of 64: 6.9 us whole, 10.6 in two shares).
         const int places = ragged ? 1024 : 512, least = run.units < 256 ? 2 : 8;
         const int want = (places + run.units - 1) / run.units, most = tiles / (least * 4);
         run.shares = want < most ? want : most > 0 ? most : 1;

@@ -140,6 +140,18 @@ def test_workspace_sizes_do_not_read_the_pointers():
     assert lib.fvar_block_kvq_workspace_bytes(h, C.byref(_cache(kv_heads=4)), 2, 30) >= lib.fvar_block_workspace_bytes(h, 2, 30)
 
 
+def test_sizes_that_the_calls_refuse_need_no_workspace():
+    lib = fv.load_library()
+    ctx = fv.Context(hidden=256, heads=4, head_dim=64, ffn_hidden=256)
+    for fn in (lib.fvar_kvq_attention_workspace_bytes, lib.fvar_block_kvq_workspace_bytes):
+        size = lambda B, n, **kw: fn(ctx.handle, C.byref(_cache(kv_heads=4, **kw)), B, n)
+        assert size(1, 10, capacity=1 << 24) > 0 and size(1, 10, capacity=(1 << 24) + 1) == 0
+        assert size(16384, 1, capacity=1 << 24) == 0                              # B * kv_heads
+        assert size(1, (1 << 23) + 1) == 0 and size(1, 2 ** 31 - 1) == 0 and size(2 ** 31 - 1, 2 ** 31 - 1) == 0
+        if fn is lib.fvar_block_kvq_workspace_bytes:                              # (the attention by itself may need none)
+            assert size(16383, 512) > 0 and size(1, 1 << 23) > 0
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     u8 = lambda *s: torch.zeros(s, dtype=torch.uint8)
     good = dict(k=u8(2, 4, 10, 32), v=u8(2, 4, 10, 32), k_scale=u8(2, 4, 10, 2), v_scale=u8(2, 4, 10, 2))

@@ -982,6 +982,7 @@ static int kvq_block(DType dt, int B, int n, int H, int heads, int length)
 // `ragged`: samples of lengths of their own, which only the GPU knows.
 // waves: wavefronts of a workgroup, which divide a block's keys (16 rows), or its rows and, if there are 8, keys (128 rows).
 struct KvqRun { int block, nrb, units, full, shares, waves; };
+constexpr int kGroupsFrom = 2048, kGroupsTo = 4096;          // lengths at which the choice between one and two groups changes
 static KvqRun kvq_run(int block, int B, int n, int H, int heads, int Dh, int length, bool ragged)
 {
     KvqRun run;
@@ -1010,10 +1011,12 @@ static KvqRun kvq_run(int block, int B, int n, int H, int heads, int Dh, int len
     // of 16 heads 44 us, 52 by one group; 2 x 130 x 2000 24, 25; 1 x 1664 x 6000 88, 99).  Otherwise, and over long caches where shares of
     // one group leave fewer CUs idle (1 x 1152 x 6000, 144 blocks, 76 us, 85 by two groups; 30 heads of 64, 640 x 6000, 150 blocks, 49, 64;
     // but 1 x 1152 x 2500 46, 43), two workgroups on every CU, three of 64-wide rows; those beyond the last full round are divided.
-    // Pieces have four tiles at least for each group.
+    // Pieces have four tiles at least for each group.  A quarter of a round more than one by two groups, divided, is also soonest done
+    // so, if there is enough to divide (272 blocks, 1 x 2176 x 6000 keys of 16 heads 127 us, 159 by one group, x 2500 71, 78, but x 1000 47, 39;
+    // 320 blocks, x 6000 139, 159, x 2500 75, 74; 384 blocks, x 2500 83, 77; 30 heads of 64, 270 blocks, 1 x 1152 x 6000 79, 92).
     const int two = Dh == 64 ? 768 : 512;
-    bool groups = run.units <= 256;
-    if (groups && length >= 4096) groups = (two / run.units) * 256 * 8 <= (256 / run.units) * two * 9;
+    bool groups = run.units <= 256 || (run.units <= 320 && length >= kGroupsFrom);
+    if (run.units <= 256 && length >= kGroupsTo) groups = (two / run.units) * 256 * 8 <= (256 / run.units) * two * 9;
     const int slots = groups ? 256 : two, rest = run.units % slots, most = (length + 63) / 64 / (groups ? 8 : 4);
     run.waves = groups ? 8 : 4;
     run.full = run.units - rest;
@@ -1026,14 +1029,17 @@ static KvqRun kvq_run(int block, int B, int n, int H, int heads, int Dh, int len
 
 size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity)
 {
-    // Shares never fall as the length grows, nor where samples have lengths of their own, so for either kind of blocks this is enough for
-    // every call; a shorter length may be run by the other kind.
+    // Between those lengths shares never fall as the length grows, nor where samples have lengths of their own, so for either kind of
+    // blocks the longest length of each stretch is enough for every call; a shorter length may be run by the other kind.
     size_t most = 0;
-    for (int block = 16; block <= 128; block *= 8) {
-        if (block == 128 ? kvq_block(dt, B, n, H, heads, capacity) == 16 : kvq_block(dt, B, n, H, heads, 1) == 128) continue;
-        const KvqRun run = kvq_run(block, B, n, H, heads, Dh, capacity, true);
-        const size_t floats = (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
-        if (floats > most) most = floats;
+    for (int length : {capacity, kGroupsTo - 1, kGroupsFrom - 1}) {
+        if (length > capacity) continue;
+        for (int block = 16; block <= 128; block *= 8) {
+            if (block == 128 ? kvq_block(dt, B, n, H, heads, length) == 16 : kvq_block(dt, B, n, H, heads, 1) == 128) continue;
+            const KvqRun run = kvq_run(block, B, n, H, heads, Dh, length, true);
+            const size_t floats = (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
+            if (floats > most) most = floats;
+        }
     }
     return most;
 }

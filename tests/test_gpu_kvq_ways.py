@@ -83,3 +83,22 @@ def test_one_workspace_serves_every_length(dtype, n):
                 assert not to_np(o).any()
             else:
                 _check(f"workspace {dtype} n {n} length {length} ragged {ragged}", o, want, dtype)
+
+
+def test_one_workspace_serves_lengths_run_by_one_group_and_by_two():
+    """288 blocks of 64-wide rows: in two shares each where the cache is short, 256 whole by two groups and the rest divided where it is long."""
+    B, H, dh, cap, n = 8, 4, 64, 2300, 1100
+    assert ways("bf16", B, n, H, H, dh, 1000, False) == (128, 4, 2) and ways("bf16", B, n, H, H, dh, cap, False) == (128, 8, 4)
+    ctx, kv = _ctx(H, dh, "bf16"), _empty_cache(B, H, cap, dh)
+    kk, vv = _load(kv, _rows(13, B, cap, H, dh, "bf16"), _rows(14, B, cap, H, dh, "bf16"))
+    q = _rows(15, B, n, H, dh, "bf16", spread=0.2)
+    size, guard = fv.fvar_kvq_attention_workspace_bytes(ctx, kv, B, n), 4096
+    room = torch.empty(size + guard, dtype=torch.uint8, device="cuda")
+    o = torch.empty((B, n, H, dh), dtype=torch.bfloat16, device="cuda")
+    for length in (1000, 2047, 2048, cap):
+        room.fill_(255)
+        o.fill_(float("nan"))
+        fv.fvar_kvq_attention(ctx, to_dev(q, "bf16"), fv.KVQ(kv.k, kv.v, kv.k_scale, kv.v_scale, len=length), B, n, o, room[:size])
+        torch.cuda.synchronize()
+        assert (room[size:] == 255).all()
+        _check(f"groups, length {length}", o, kvq.attention(q, kk, vv, dh ** -0.5, [length] * B), "bf16")

@@ -194,6 +194,8 @@ WAYS = {
     "128 rows, two groups, divided": ("bf16", 128, 8, 8, 4, 230, 3600, False, (128, 8, 4)),
     "128 rows, two groups, many shares": ("bf16", 64, 8, 2, 1, 130, 16000, False, (128, 8, 16)),
     "128 rows, two groups, ragged shares": ("bf16", 128, 4, 4, 9, 200, 2300, True, (128, 8, 3)),
+    "128 rows, two groups, the rest divided": ("bf16", 128, 11, 11, 12, 200, 2100, False, (128, 8, 4)),
+    "128 rows, two groups, the rest divided, ragged": ("bf16", 64, 10, 5, 13, 200, 2050, True, (128, 8, 4)),
     "128 rows, one group, divided": ("bf16", 128, 4, 4, 18, 129, 4100, False, (128, 4, 3)),
     "128 rows, last round divided": ("bf16", 64, 16, 16, 31, 200, 1100, False, (128, 4, 3)),
     "128 rows, last round divided, 128": ("bf16", 128, 4, 4, 70, 200, 600, True, (128, 4, 2)),
@@ -224,3 +226,15 @@ def test_small_changes_of_length_and_lengths_of_their_own_need_no_more_workspace
                         units = B * kv_heads * -(-(n * heads // kv_heads) // block)
                         if shares > 1 and units < 256:        # every unit divided
                             assert size >= 4 * units * shares * block * (dh + 2)
+
+
+def test_workspace_never_falls_where_the_choice_of_groups_changes():
+    """What a length takes is in the size of a cache of that capacity; a longer one has to be enough for it, on both sides of every change."""
+    lib = fv.load_library()
+    caps = [1000, 1500, 2040, 2047, 2048, 2049, 2500, 4000, 4095, 4096, 4097, 5000, 9000]
+    for heads, dh in ((16, 128), (30, 64), (8, 64), (12, 128)):
+        ctx = fv.Context(hidden=heads * dh, heads=heads, head_dim=dh, ffn_hidden=64, dtype="bf16")
+        for B in (1, 3, 8):
+            for n in range(100, 4600, 257):
+                size = [lib.fvar_kvq_attention_workspace_bytes(ctx.handle, C.byref(_cache(kv_heads=heads, capacity=c, len=1)), B, n) for c in caps]
+                assert size == sorted(size), (heads, dh, B, n, size)

@@ -379,6 +379,8 @@ def _rows(t, B: int, rows: int, width: int):
         raise ValueError(f"[{B}, {rows}, ...] with contiguous rows of {width} elements is wanted, got shape "
                          f"{tuple(t.shape)} with strides {t.stride()}")
     ld = t.stride(1) if rows > 1 else t.stride(0)
+    if ld < width:                                            # rows that share memory, or one broadcast over them: 0 would mean packed
+        raise ValueError(f"rows of {width} elements cannot be {ld} elements apart: a copy of the tensor is wanted")
     if B > 1 and t.stride(0) != rows * ld:
         raise ValueError("the rows of all samples have to be equally far apart")
     return t.data_ptr(), ld

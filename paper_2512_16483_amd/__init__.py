@@ -364,17 +364,33 @@ class KVQ:
         return C.byref(self._c)
 
 
-def _rows(t, B: int, rows: int, width: int):
-    """Pointer and row pitch of t:[B, rows, ...], whose rows of `width` elements are contiguous; they may lie apart, as
-    the parts of a fused projection's output do."""
+_ELEMENT = {"bf16": "torch.bfloat16", "f32": "torch.float32"}
+
+
+def _packed(t, kind: str, B: int, rows: int, width: int) -> Optional[int]:
+    """Pointer of contiguous t whose first B * rows * width elements are [B, rows, width] (None passes NULL).  A tensor with room for
+    more is taken where those are its first elements: a flat one, rows of `width`, more samples, or more rows of the only one."""
     if t is None:
-        return None, 0
-    if not t.is_cuda:
-        raise ValueError("tensors handed to fvar must be GPU tensors")
-    if t.is_contiguous():
-        if t.numel() < B * rows * width:
-            raise ValueError(f"{B} x {rows} rows of {width} elements are wanted, got a tensor of shape {tuple(t.shape)}")
-        return t.data_ptr(), 0
+        return None
+    if str(t.dtype) != kind:
+        raise ValueError(f"a tensor of {kind} is wanted, got {t.dtype}")
+    n, s = t.numel(), t.shape if width > 1 else (*t.shape, 1)
+    if n != B * rows * width:
+        fits = n > B * rows * width and (len(s) == 1 or s[-1] == width and len(s) == 2 or
+                                         len(s) > 2 and s[0] * s[1] * width == n and (s[1] == rows or B == 1))
+        if not fits:
+            raise ValueError(f"{B} x {rows} rows of {width} elements are wanted, got a tensor of shape {tuple(s)}")
+    return _ptr(t)
+
+
+def _rows(ctx: Context, t, B: int, rows: int, width: int):
+    """Pointer and row pitch of t:[B, rows, ...] of the context's type, whose rows of `width` elements are contiguous; they may lie apart,
+    as the parts of a fused projection's output do."""
+    kind = _ELEMENT[ctx.dtype]
+    if t is None or t.is_contiguous():
+        return _packed(t, kind, B, rows, width), 0
+    if not t.is_cuda or str(t.dtype) != kind:
+        raise ValueError(f"tensors handed to fvar must be GPU tensors, here of {kind}")
     if t.dim() < 3 or t.shape[0] != B or t.shape[1] != rows or t[0, 0].numel() != width or not t[0, 0].is_contiguous():
         raise ValueError(f"[{B}, {rows}, ...] with contiguous rows of {width} elements is wanted, got shape "
                          f"{tuple(t.shape)} with strides {t.stride()}")
@@ -388,14 +404,15 @@ def _rows(t, B: int, rows: int, width: int):
 
 def fvar_kvq_append(ctx: Context, kv: KVQ, k, v, B: int, rows: int, stream=None) -> None:
     width = kv.kv_heads * ctx.head_dim
-    (kp, ldk), (vp, ldv) = _rows(k, B, rows, width), _rows(v, B, rows, width)
+    (kp, ldk), (vp, ldv) = _rows(ctx, k, B, rows, width), _rows(ctx, v, B, rows, width)
     if (ldk or width) != (ldv or width):
         raise ValueError("k and v have different distances between rows")
     ctx.check(ctx.lib.fvar_kvq_append(ctx.handle, _stream(stream), kv._for(ctx, B), kp, vp, ldk, B, rows))
 
 
 def fvar_kvq_read(ctx: Context, kv: KVQ, B: int, first: int, rows: int, k=None, v=None, stream=None) -> None:
-    ctx.check(ctx.lib.fvar_kvq_read(ctx.handle, _stream(stream), kv._for(ctx, B), B, first, rows, _ptr(k), _ptr(v)))
+    kp, vp = (_packed(t, _ELEMENT[ctx.dtype], B, rows, kv.kv_heads * ctx.head_dim) for t in (k, v))
+    ctx.check(ctx.lib.fvar_kvq_read(ctx.handle, _stream(stream), kv._for(ctx, B), B, first, rows, kp, vp))
 
 
 def fvar_kvq_attention_workspace_bytes(ctx: Context, kv: KVQ, B: int, n: int) -> int:
@@ -403,9 +420,9 @@ def fvar_kvq_attention_workspace_bytes(ctx: Context, kv: KVQ, B: int, n: int) ->
 
 
 def fvar_kvq_attention(ctx: Context, q, kv: KVQ, B: int, n: int, o, ws=None, stream=None) -> None:
-    qp, ld = _rows(q, B, n, ctx.hidden)
-    ctx.check(ctx.lib.fvar_kvq_attention(ctx.handle, _stream(stream), qp, ld, kv._for(ctx, B), B, n, _ptr(o), _ptr(ws),
-                                         _nbytes(ws)))
+    qp, ld = _rows(ctx, q, B, n, ctx.hidden)
+    op = _packed(o, _ELEMENT[ctx.dtype], B, n, ctx.hidden)
+    ctx.check(ctx.lib.fvar_kvq_attention(ctx.handle, _stream(stream), qp, ld, kv._for(ctx, B), B, n, op, _ptr(ws), _nbytes(ws)))
 
 
 def fvar_block_kvq_workspace_bytes(ctx: Context, kv: KVQ, B: int, rows: int) -> int:
@@ -413,16 +430,17 @@ def fvar_block_kvq_workspace_bytes(ctx: Context, kv: KVQ, B: int, rows: int) -> 
 
 
 def fvar_block_forward_dense_kvq(ctx: Context, w: dict, x, B: int, M: int, kv: KVQ, y, ws, stream=None) -> None:
-    ws_ = _weights(w)
-    ctx.check(ctx.lib.fvar_block_forward_dense_kvq(ctx.handle, _stream(stream), C.byref(ws_), _ptr(x), B, M,
-                                                   kv._for(ctx, B), _ptr(y), _ptr(ws), _nbytes(ws)))
+    ws_, xy = _weights(w), [_packed(t, _ELEMENT[ctx.dtype], B, M, ctx.hidden) for t in (x, y)]
+    ctx.check(ctx.lib.fvar_block_forward_dense_kvq(ctx.handle, _stream(stream), C.byref(ws_), xy[0], B, M, kv._for(ctx, B), xy[1],
+                                                   _ptr(ws), _nbytes(ws)))
 
 
 def fvar_block_forward_pruned_kvq(ctx: Context, w: dict, x, B: int, M: int, idx_keep, k: int, kv: KVQ, y_keep, ws,
                                   stream=None) -> None:
-    ws_ = _weights(w)
-    ctx.check(ctx.lib.fvar_block_forward_pruned_kvq(ctx.handle, _stream(stream), C.byref(ws_), _ptr(x), B, M,
-                                                    _ptr(idx_keep), k, kv._for(ctx, B), _ptr(y_keep), _ptr(ws),
+    ws_, kind = _weights(w), _ELEMENT[ctx.dtype]
+    xp, yp = _packed(x, kind, B, M, ctx.hidden), _packed(y_keep, kind, B, k, ctx.hidden)
+    ctx.check(ctx.lib.fvar_block_forward_pruned_kvq(ctx.handle, _stream(stream), C.byref(ws_), xp, B, M,
+                                                    _packed(idx_keep, "torch.int32", B, k, 1), k, kv._for(ctx, B), yp, _ptr(ws),
                                                     _nbytes(ws)))
 
 

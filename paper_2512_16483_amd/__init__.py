@@ -325,29 +325,42 @@ class KVQ:
 
     k, v: uint8 [B, kv_heads, capacity, head_dim / 2]; k_scale, v_scale: uint8 [B, kv_heads, capacity, head_dim / 32];
     lens: int32 [B] on the GPU, or None where every sample holds `len` rows; mask: uint8 or bool [B, capacity], 0 hides a
-    row from the attention, or None.  `len` may be assigned to; the tensors are the caller's, who advances len or lens."""
+    row from the attention, or None.  The tensors and `len` may be assigned to, tensors of the same shape; they are the caller's,
+    who advances len or lens."""
 
     def __init__(self, k, v, k_scale, v_scale, len: int = 0, lens=None, mask=None):
         B, heads, capacity, codes = k.shape
-        want = {"k": (k, (B, heads, capacity, codes)), "v": (v, (B, heads, capacity, codes)),
-                "k_scale": (k_scale, (B, heads, capacity, codes // 16)),
-                "v_scale": (v_scale, (B, heads, capacity, codes // 16))}
-        if lens is not None:
-            want["lens"] = (lens, (B,))
-        if mask is not None:
-            want["mask"] = (mask, (B, capacity))
-        for name, (t, shape) in want.items():
-            if tuple(t.shape) != shape:
-                raise ValueError(f"{name} has shape {tuple(t.shape)}, {shape} is wanted")
+        self._shapes = {"k": (B, heads, capacity, codes), "v": (B, heads, capacity, codes),
+                        "k_scale": (B, heads, capacity, codes // 16), "v_scale": (B, heads, capacity, codes // 16),
+                        "lens": (B,), "mask": (B, capacity)}
+        self._tensors = {}
+        self._c = _KVQ(kv_heads=heads, capacity=capacity, len=len)
+        for name, t in (("k", k), ("v", v), ("k_scale", k_scale), ("v_scale", v_scale), ("lens", lens), ("mask", mask)):
+            self._hold(name, t)
+
+    def _hold(self, name: str, t) -> None:
+        """Tensor and pointer change together: the calls read what the attribute shows, and it lives as long."""
+        if t is not None:
+            if tuple(t.shape) != self._shapes[name]:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, {self._shapes[name]} is wanted")
             kinds = ("torch.int32",) if name == "lens" else ("torch.uint8", "torch.bool") if name == "mask" else ("torch.uint8",)
             if str(t.dtype) not in kinds:
                 raise ValueError(f"{name} is {t.dtype}, {' or '.join(kinds)} is wanted")
-        self.k, self.v, self.k_scale, self.v_scale, self.lens, self.mask = k, v, k_scale, v_scale, lens, mask
-        self.batch, self.head_dim = B, 2 * codes
-        self._c = _KVQ(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(lens), _ptr(mask), heads, capacity, len)
+        elif name not in ("lens", "mask"):
+            raise ValueError(f"{name} is None")
+        setattr(self._c, name, _ptr(t))
+        self._tensors[name] = t
 
+    k = property(lambda self: self._tensors["k"], lambda self, t: self._hold("k", t))
+    v = property(lambda self: self._tensors["v"], lambda self, t: self._hold("v", t))
+    k_scale = property(lambda self: self._tensors["k_scale"], lambda self, t: self._hold("k_scale", t))
+    v_scale = property(lambda self: self._tensors["v_scale"], lambda self, t: self._hold("v_scale", t))
+    lens = property(lambda self: self._tensors["lens"], lambda self, t: self._hold("lens", t))
+    mask = property(lambda self: self._tensors["mask"], lambda self, t: self._hold("mask", t))
     kv_heads = property(lambda self: self._c.kv_heads)
     capacity = property(lambda self: self._c.capacity)
+    batch = property(lambda self: self._shapes["k"][0])
+    head_dim = property(lambda self: 2 * self._shapes["k"][3])
 
     @property
     def len(self) -> int:

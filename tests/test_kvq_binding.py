@@ -165,3 +165,42 @@ def test_room_for_more_rows_is_taken_only_where_the_rows_are_where_the_calls_loo
     with pytest.raises(ValueError):
         pruned(idx(2, 6), 2)
     assert len(ctx.lib.calls) == 8
+
+
+# ------------------------------------------------------------------------------------ the cache's tensors
+@pytest.mark.parametrize("name,shape,dtype", [
+    ("k", (2, 4, 10, 32), torch.uint8), ("v", (2, 4, 10, 32), torch.uint8), ("k_scale", (2, 4, 10, 2), torch.uint8),
+    ("v_scale", (2, 4, 10, 2), torch.uint8), ("lens", (2,), torch.int32), ("mask", (2, 10), torch.uint8), ("mask", (2, 10), torch.bool)])
+def test_a_tensor_assigned_to_a_cache_is_the_one_that_the_calls_read(ctx, name, shape, dtype):
+    """Neither the tensor of before, which its caller may have let go, nor one that does not fit."""
+    for kv in (cache(), cache(lens=zeros(2, dtype=torch.int32), mask=zeros(2, 10, dtype=torch.uint8))):
+        new = zeros(*shape, dtype=dtype)
+        setattr(kv, name, new)
+        assert getattr(kv, name) is new and getattr(kv._c, name) == new.data_ptr()
+        fv.fvar_kvq_append(ctx, kv, zeros(2, 5, 256), zeros(2, 5, 256), 2, 5, stream=1)
+        passed = C.cast(ctx.lib.calls[-1][1][2], C.POINTER(fv._KVQ)).contents
+        assert getattr(passed, name) == new.data_ptr()
+        for bad in (zeros(*shape, dtype=torch.float32), zeros(*shape[:-1], shape[-1] + 1, dtype=dtype), torch.zeros(shape, dtype=dtype),
+                    zeros(*shape, 2, dtype=dtype)[..., 0]):
+            with pytest.raises(ValueError):
+                setattr(kv, name, bad)
+            assert getattr(kv, name) is new and getattr(kv._c, name) == new.data_ptr()
+
+
+def test_lengths_and_masks_come_and_go():
+    kv = cache(len=3)
+    lens, mask = zeros(2, dtype=torch.int32), zeros(2, 10, dtype=torch.bool)
+    kv.lens, kv.mask = lens, mask
+    kv.lens = kv.lens + 1                                     # another tensor
+    assert kv._c.lens == kv.lens.data_ptr() != lens.data_ptr() and kv._c.mask == mask.data_ptr()
+    at = kv.lens
+    kv.lens += 1                                              # the same one
+    assert kv.lens is at and kv._c.lens == at.data_ptr() and at.tolist() == [2, 2]
+    kv.lens = kv.mask = None
+    assert kv._c.lens is None and kv._c.mask is None and kv.len == kv._c.len == 3
+    for name in ("k", "v", "k_scale", "v_scale"):
+        with pytest.raises(ValueError):
+            setattr(kv, name, None)
+    for name in ("kv_heads", "capacity", "batch", "head_dim"):
+        with pytest.raises(AttributeError):
+            setattr(kv, name, 1)

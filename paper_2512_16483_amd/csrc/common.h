@@ -202,6 +202,7 @@ void launch_kvq_read(DType dt, const KvqCache &c, int B, int first, int rows, in
 // the next; o:[B,n,H,Dh]; part: kvq_attention_scratch_floats() floats
 size_t kvq_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity);
 int kvq_attention_ways(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged);
+int kvq_attention_waves_per_simd(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged);
 void launch_kvq_attention(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, int Dh,
                           float scale, void *o, float *part, hipStream_t st);
 

@@ -1052,6 +1052,21 @@ int kvq_attention_ways(int bf16, int B, int n, int H, int heads, int Dh, int len
     return 100000 * block + 1000 * run.waves + run.shares;
 }
 
+// Wavefronts of a SIMD that the kernel is built for (see kvq_attn_tiles_kernel); wgs: workgroups of the launch.
+static int kvq_waves(DType dt, int Dh, const KvqRun &run, int wgs)
+{
+    if (run.block == 16) return dt == DType::F32 ? 2 : 3;
+    return Dh == 64 && run.waves == 4 && wgs > 512 ? 3 : 2;
+}
+
+// The same for the tests.
+int kvq_attention_waves_per_simd(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged)
+{
+    const DType dt = bf16 ? DType::BF16 : DType::F32;
+    const KvqRun run = kvq_run(kvq_block(dt, B, n, H, heads, length), B, n, H, heads, Dh, length, ragged != 0);
+    return kvq_waves(dt, Dh, run, run.full + (run.units - run.full) * run.shares);
+}
+
 template <typename T, int DH>
 static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, float c_log2,
                        void *o, float *part, hipStream_t st)
@@ -1074,7 +1089,7 @@ static void launch_kvq(DType dt, const void *q, int ld, const KvqCache &c, int e
     launch(kvq_attn_tiles_kernel<DH, KG, WAVES>, dim3(wgs), dim3(256 * KG), 0, st, (const T *)q, ld, c, extra, n, H,      \
            c_log2, (T *)o, run.nrb, run.full, run.shares, part, part_ml)
         if (run.waves == 8) FVAR_TILES(2, 2);
-        else if (DH == 128 || wgs <= 512) FVAR_TILES(1, 2);
+        else if (kvq_waves(dt, DH, run, (int)wgs) == 2) FVAR_TILES(1, 2);
         else if constexpr (DH == 64) FVAR_TILES(1, 3);
 #undef FVAR_TILES
     }

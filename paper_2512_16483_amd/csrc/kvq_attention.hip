@@ -67,6 +67,21 @@ __device__ __forceinline__ float column_sum(float v)
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+// the smaller of two 16-bit numbers each; of 32 lanes' numbers, in each of them
+__device__ __forceinline__ uint32_t pair_min(uint32_t a, uint32_t b)
+{
+    typedef uint16_t uint16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(uint16x2_t, a), __builtin_bit_cast(uint16x2_t, b)));
+}
+__device__ __forceinline__ uint32_t half_min(uint32_t v)
+{
+    v = pair_min(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));       // quad_perm 1,0,3,2
+    v = pair_min(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));       // quad_perm 2,3,0,1
+    v = pair_min(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true));      // row_half_mirror
+    v = pair_min(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true));      // row_mirror
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return pair_min(a[0], a[1]);
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
 #pragma unroll
@@ -398,8 +413,13 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 //     not converted, and at four times the rate of bf16 where the other operand has 6 bits.  Q, scaled so that scores come in units of
 //     log2, goes in as three E2M3 numbers per element (sign, 2 bits of exponent, 3 of mantissa, a shared 2^e, 2^(e-4), 2^(e-9) per 32),
 //     each for what the one before leaves.  That is at most 2^-2 of its unit, then 2^-3, which the next one's units hold whole
-//     (2^-5 after the first would be 8, past the largest, 7.5); what the last leaves is at most 2^(e-12), 2^-13 of the block's largest
-//     element.  (Two leave 2^-9 of it, which scores of 20 and more, a few times the usual, show in the output.)
+//     (2^-5 after the first would be 8, past the largest, 7.5); what the last leaves is at most 2^(e-12).
+//     What is left is the same for an element of any size, so it is held against the keys: a block of 32 adds at most 6 * 2^k (a key's
+//     largest value) times the sum of what is left to a score's error.  While that is below 2^-5 over a row for all rows of a wavefront and
+//     the keys of a tile, the pieces serve (queries and keys of normal numbers: 2^-7.5 at most, 2^-14 rms).  From the first tile on for
+//     which it is not (scores of 15 and more, or a few elements far larger than the others), a wavefront takes its queries as they came, in bf16, and
+//     converts the keys: exact, four products of 16 elements for three of 64 and 32 conversions per half a tile more, 10 to 17 % slower (4 x 1600
+//     x 12121, 32 heads of 128: 1240 us, 1100 with pieces; 8 x 231 x 871, 30 of 64, 25.4, 23.0; 4 x 300 x 2500, 16 of 128, 46.9, 40.7).
 //   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
 // In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
 // product takes it, as in attention.hip.
@@ -493,6 +513,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
     // ---- Q in three pieces of 6 bits: lane = row, block 2 s + g of its elements
     intx8_t qf[KS][3];
     int qs[KS];                                              // scale bytes of the pieces, in byte 0, 1, 2
+    uint32_t limit = 0;                                      // largest scale bytes of keys for them, of block g in the low half, 2 + g above
     {
         const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
 #pragma unroll
@@ -508,7 +529,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
                 odd[i] = bf16_hi(w[i]) * c_log2;
                 top = max(top, max(__float_as_uint(even[i]) & 0x7fffffffu, __float_as_uint(odd[i]) & 0x7fffffffu));
             }
-            // the smallest 2^e with all elements below 7.75 * 2^e, which round to at most 7.5; 255 makes NaN of what is not finite
+            // the smallest 2^e with all elements below 7.75 * 2^e, which round to at most 7.5
             const int e = min(max((int)((top + (1u << 19)) >> 23) - 2, 13), 252);
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
@@ -519,9 +540,18 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
                 for (int i = 0; i < 16; ++i) { even[i] -= back[2 * i]; odd[i] -= back[2 * i + 1]; }
                 qf[s][p] = intx8_t{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
             }
-            qs[s] = top >= 0x7f800000u ? 0xffffff : e | (e - 4) << 8 | (e - 9) << 16;
+            qs[s] = e | (e - 4) << 8 | (e - 9) << 16;
+            // A block of a key adds at most 6 * 2^k * rest to a score's error: the largest k for which that is below 2^-5 / NB; none for
+            // what is not finite.
+            float rest = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) rest += fabsf(even[i]) + fabsf(odd[i]);
+            const int most_k = 127 - 6 - (DH == 128) - ((int)(__float_as_uint(6.f * rest) >> 23) - 126);
+            limit |= (uint32_t)(top >= 0x7f800000u ? 0 : rest == 0.f ? 254 : min(max(most_k, 0), 254)) << (16 * s);
         }
     }
+    limit = half_min(limit);                                 // of the wavefront's rows: blocks 0 and 2, 1 and 3
+    const uint32_t limit_even = __builtin_amdgcn_readlane(limit, 0) + 0x1000100, limit_odd = __builtin_amdgcn_readlane(limit, 32) + 0x1000100;
 
     // everything on its way to LDS is there, for all wavefronts
     auto meet = [&]() {
@@ -558,9 +588,9 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
     auto with_base = [&](float score) { return FROM ? score : score + base; };
     int E = 0, E_now = 0, acc_E = 0;                         // of the values converted last, of the tile at work, of the sums
 
-    // A thread's values as they came, and their scale byte; all scale bytes of the lane's row.  The rows that can be seen, and the
-    // size of the values: E is the same in all wavefronts, each of which sees all bytes.
-    struct Raw { uint32_t v[VW], vs, all; };
+    // A thread's values as they came, and their scale byte; all scale bytes of the lane's row, of values and of keys.  The rows that can be
+    // seen, and the size of the values: E is the same in all wavefronts, each of which sees all bytes.
+    struct Raw { uint32_t v[VW], vs, all, keys; };
     auto read_raw = [&](int stage, Raw &x) {
         const uint8_t *src = lds8 + stage * STAGE;
         if constexpr (VW == 4) {
@@ -573,6 +603,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         const uint8_t *sc = src + SOFF + 64 * NB;
         x.vs = sc[vkey * NB + vpart * NB / 4];
         x.all = NB == 4 ? *reinterpret_cast<const uint32_t *>(sc + lane * NB) : *reinterpret_cast<const uint16_t *>(sc + lane * NB);
+        sc = src + SOFF;
+        x.keys = NB == 4 ? *reinterpret_cast<const uint32_t *>(sc + lane * NB) : *reinterpret_cast<const uint16_t *>(sc + lane * NB);
     };
     float scale;
     auto look = [&](int t, const Raw &x, const Next &f) -> unsigned long long {
@@ -590,6 +622,11 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         scale = half_scale(x.vs, E, (vis >> vkey) & 1);
         return vis;
     };
+    // whether a key that is seen is too large for queries in pieces (256 + limit - byte, of two blocks at a time)
+    auto too_large = [&](const Raw &x, unsigned long long vis) {
+        const uint32_t fits = (limit_even - (x.keys & 0xff00ff)) & (limit_odd - (x.keys >> 8 & 0xff00ff)) & 0x1000100;
+        return (__builtin_amdgcn_ballot_w64(fits != 0x1000100) & vis) != 0;
+    };
     int vdst[VW];                                            // where the thread's words go, in bytes
 #pragma unroll
     for (int i = 0; i < VW; ++i) vdst[i] = (vkey * DH + (((vpart * VW + i) ^ turn(vkey)) << 3)) * 2;
@@ -603,6 +640,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
     meet();
     read_raw(0, raw);
     unsigned long long vis = look(t0, raw, next), vis_next;
+    bool far = too_large(raw, vis);                          // of the tile at work
 #pragma unroll
     for (int i = 0; i < VW; ++i) convert(0, raw, i);
     next = later;
@@ -666,6 +704,13 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         }
     };
 #undef FVAR_S
+    // The same with queries as they came: eight elements of a key at a time as bf16.
+    bf16x8_t whole[4 * KS];
+    auto score_whole = [&](int half, int i, const uintx4_t *k, int sc) {
+        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, bf16_eight(k[i / 4][i % 4], __uint_as_float((uint32_t)(sc >> (16 * (i / 4)) & 255) << 23)));
+        const floatx16_t none = {0};
+        s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, whole[i], i ? s[half] : none, 0, 0, 0);
+    };
     auto load_v = [&](int i, int rows) -> f16x8_t {
         const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vp[i][0] + rows * DH * 2));
         const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vp[i][1] + rows * DH * 2));
@@ -673,9 +718,10 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
     };
     // One half's softmax beside the scores of the other (of the next tile where that is the first) and the products of the other's
     // weights (of the tile before where that is the second).  A step: a product, the weights of a pair or two in three stages.
-    auto region = [&](auto which, int s1) {
+    auto region = [&](auto which, auto as_came, int s1) {
         constexpr int half = decltype(which)::value, other = 1 - half;
-        constexpr int NS = 3 * KS, NPV = 2 * DB, STEPS = NS + NPV, PP = DH == 128 ? 1 : 2;     // PP: pairs of weights per step
+        constexpr bool WHOLE = decltype(as_came)::value;
+        constexpr int NS = WHOLE ? 4 * KS : 3 * KS, NPV = 2 * DB, STEPS = NS + NPV, PP = DH == 128 ? 1 : 2;     // PP: pairs of weights per step
         uintx4_t k[KS];
         f16x8_t vf[DB];
         const int sc = load_keys(other, k);
@@ -688,7 +734,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         for (int step = 0; step < STEPS; ++step) {
             const int before = min((step + 1) / 2, NS);      // scores' products up to here, this one included if it is one
             if ((step & 1) && step / 2 < NS) {
-                score(other, step / 2, k, sc);
+                if constexpr (WHOLE) score_whole(other, step / 2, k, sc);
+                else score(other, step / 2, k, sc);
             } else {
                 const int i = step - before;
                 acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i % DB], pf[other][i / DB], acc[i % DB], 0, 0, 0);
@@ -702,8 +749,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
                     x[2 * p1 + 1] = __builtin_amdgcn_exp2f(x[2 * p1 + 1]);
                 }
                 if (p0 < 8) {
-                    x[2 * p0] = with_base(s[half][2 * p0]);
-                    x[2 * p0 + 1] = with_base(s[half][2 * p0 + 1]);
+                    x[2 * p0] = WHOLE ? fmaf(s[half][2 * p0], c_log2, base) : with_base(s[half][2 * p0]);
+                    x[2 * p0 + 1] = WHOLE ? fmaf(s[half][2 * p0 + 1], c_log2, base) : with_base(s[half][2 * p0 + 1]);
                 }
                 if (p2 >= 0 && p2 < 8) {
                     a = p2 ? a + x[2 * p2] : x[0];
@@ -737,7 +784,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
                 if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[half][i] = -INFINITY;
         }
     };
-    auto settle = [&](int half) {
+    auto settle = [&](int half, auto as_came) {
+        constexpr bool WHOLE = decltype(as_came)::value;     // scores: not yet in units of log2, and without the base
         // The reference is not the running maximum but one that was it; the weights tell when it no longer serves.  A sum of NaN
         // does not ask for another: it stays NaN.
         const bool anew = (__builtin_amdgcn_ballot_w64(sum > most) != 0 && (uint32_t)(vis >> (32 * half)) != 0) || E_now != acc_E;
@@ -745,7 +793,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
             float mx = s[half][0];
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
-            if constexpr (FROM) mx -= base;
+            if constexpr (WHOLE) mx *= c_log2;
+            else if constexpr (FROM) mx -= base;
             mx = fmaxf(m_ref, mx);
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
             const float now = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
@@ -757,7 +806,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
             acc_E = E_now;
             const float before = base;
             set_base(none ? kShift : kShift - now);
-            if constexpr (FROM) {
+            if constexpr (FROM && !WHOLE) {
                 s[0] += base - before;
                 s[1] += base - before;
             }
@@ -770,7 +819,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
             sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(with_base(s[half][i])), y = __builtin_amdgcn_exp2f(with_base(s[half][i + 1]));
+                const float x = __builtin_amdgcn_exp2f(WHOLE ? fmaf(s[half][i], c_log2, base) : with_base(s[half][i]));
+                const float y = __builtin_amdgcn_exp2f(WHOLE ? fmaf(s[half][i + 1], c_log2, base) : with_base(s[half][i + 1]));
                 sum += x + y;
                 const f16x2_t p = __builtin_convertvector((floatx2_t{x, y}), f16x2_t);
                 pf[half][i >> 3][i & 7] = p[0];
@@ -780,20 +830,14 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         l_run += sum;
     };
 
-    {
-        uintx4_t k[KS];
-        const int sc = load_keys(0, k);
-#pragma unroll
-        for (int i = 0; i < 3 * KS; ++i) score(0, i, k, sc);
-    }
     E_now = E;
     int t = t0;
-    do {
+    auto tile = [&](auto as_came) {
         const int s1 = after(stage), s2 = after(s1);
         fetch(min(t + 2, t1), s2, later);
         hide(0);
-        region(std::integral_constant<int, 0>{}, s1);
-        settle(0);
+        region(std::integral_constant<int, 0>{}, as_came, s1);
+        settle(0, as_came);
         {
             // values go on to this tile's stage, keys to the next's
             const int by = (stage == 0 ? -2 : 1) * STAGE, k_by = (s1 == 0 ? -2 : 1) * STAGE, v_by = t == t0 ? 0 : by;
@@ -805,15 +849,45 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         }
         hide(1);
         vis_next = look(min(t + 1, t1), raw, next);
-        region(std::integral_constant<int, 1>{}, s1);
-        settle(1);
+        if constexpr (!decltype(as_came)::value) far = too_large(raw, vis_next);
+        region(std::integral_constant<int, 1>{}, as_came, s1);
+        settle(1, as_came);
         put_scales(s2, later);
         next = later;
         vis = vis_next;
         stage = s1;
         E_now = E;
         meet();
-    } while (++t <= t1);
+        ++t;
+    };
+    // Queries in pieces as long as the keys allow it, then as they came.
+    if (!far) {
+        uintx4_t k[KS];
+        const int sc = load_keys(0, k);
+#pragma unroll
+        for (int i = 0; i < 3 * KS; ++i) score(0, i, k, sc);
+        do tile(std::false_type{});
+        while (t <= t1 && !far);
+    }
+    if (t <= t1) {
+        const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 4 * KS; ++i) {
+            const uintx4_t w = *reinterpret_cast<const uintx4_t *>(src + 64 * (i / 4) + 8 * (i % 4));
+            whole[i] = __builtin_bit_cast(bf16x8_t, w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, max(w[j] << 16 & 0x7fff0000u, w[j] & 0x7fff0000u));
+        }
+        // (an infinity makes scores that are not numbers, not some that are all -inf)
+        if (top >= 0x7f800000u) whole[0] = __builtin_bit_cast(bf16x8_t, uintx4_t{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u});
+        uintx4_t k[KS];
+        const int sc = load_keys(0, k);
+#pragma unroll
+        for (int i = 0; i < 4 * KS; ++i) score_whole(0, i, k, sc);
+        do tile(std::true_type{});
+        while (t <= t1);
+    }
     // the last half's products
 #pragma unroll
     for (int u = 0; u < 2; ++u)

@@ -153,7 +153,7 @@ def test_what_is_not_a_number_is_passed_on(name):
 
 # ------------------------------------------------------------------------------------ sizes
 @pytest.mark.parametrize("name", BOTH)
-@pytest.mark.parametrize("case", ["sharp", "rising", "falling", "steps", "steps down"])
+@pytest.mark.parametrize("case", ["sharp", "rising", "falling", "steps", "steps down", "queries of every size", "some large queries"])
 def test_references_that_move(name, case):
     """Scores of several hundred, which rise or fall along the rows, a little at every row or much at some: the running reference has to be
     found anew again and again, in rows of a block at different places."""
@@ -162,6 +162,11 @@ def test_references_that_move(name, case):
     t = np.arange(way.L)
     if case == "sharp":
         q = q * 8
+    elif case == "queries of every size":                     # rows of a block whose references lie far apart
+        q = q * 2.0 ** np.random.default_rng(55).integers(-12, 5, (1, way.n, way.few, 1))
+    elif case == "some large queries":                        # those of one wavefront, with keys that grow
+        q = q * np.where(np.arange(way.n) // 32 % 4 == 1, 30.0, 1.0)[None, :, None, None]
+        k = k * 2.0 ** (t // 150 % 3 - 1.0)[None, :, None, None]
     else:
         up = {"rising": 2.0 ** np.linspace(-10, 4, way.L), "steps": 2.0 ** (t // 97 % 7 - 3.0)}.get(case.split(" down")[0], None)
         if case == "falling":
@@ -207,6 +212,31 @@ def test_equal_scores_are_the_mean(name):
     o, want = to_np(way.attend(np.zeros_like(q), kv)[:2]).reshape(2, way.n, -1, way.two, way.few // way.two, way.dh), held[1].mean(2)[0][:, None]
     lim = 2.0 ** -8 * np.abs(want) + way.L * 2.0 ** -24 * np.abs(held[1]).mean(2)[0][:, None]
     assert (np.abs(o - want) <= lim).all()
+
+
+# ------------------------------------------------------------------------------------ queries with elements of very different sizes
+@pytest.mark.parametrize("name", BOTH)
+@pytest.mark.parametrize("case", ["x 30", "x 200", "x 1000", "x 1e5", "half of them", "one to a block", "a ladder"])
+def test_queries_with_elements_far_larger_than_the_others(name, case):
+    """Scores of about 15 that come from a query's small elements, where the keys of its largest are 0 or small: each element counts with all
+    bits that it was given with."""
+    way = Way(name)
+    k, v, q = way.kqv(80)
+    g = np.random.default_rng(83)
+    q = q * 4
+    lift = np.ones(way.dh)
+    if case.startswith("x"):
+        lift[g.integers(0, way.dh)] = float(case[2:])
+    elif case == "half of them":
+        lift[g.permutation(way.dh)[:way.dh // 2]] = 2000.0
+    elif case == "one to a block":
+        lift[5::32] = 700.0
+    else:
+        lift = 2.0 ** (np.arange(way.dh) % 32 / 2)            # 1 to 2^15 in every block
+    q, k = way.round((q * lift).astype(np.float32), (k / lift).astype(np.float32))
+    kv, held = way.cache(k, v)
+    o, want = way.attend(q, kv), way.want(q, held)
+    way.check(case, o, want, min(_off(way, q, *held, want), 2e-3))
 
 
 # ------------------------------------------------------------------------------------ a graph

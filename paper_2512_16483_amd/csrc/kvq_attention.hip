@@ -980,7 +980,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
 
 // The shares of rows joined: each is a mean and its weight.  A unit is a block of BR rows of one (sample, kv head); the shares
 // of unit first + u lie at [u][share][row].  GROUPS groups of DH/4 threads per row, four head-dim elements a thread: a group takes every
-// GROUPS-th share in one pass with a running reference, and the groups meet in LDS.  One group where the shares are few and the
+// GROUPS-th share, four at a time, with a running reference and mean (not the sum: a mean times its weight need not be a number that fp32
+// holds), and the groups meet in LDS.  One group where the shares are few and the
 // rows many; more where a few rows have many shares, whose loads would wait for each other (64 shares of 16 rows: 24 us by one, 3 by 8).
 template <typename T, int DH, int GROUPS>
 __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
@@ -997,18 +998,35 @@ __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__rest
     const long b = unit / nrb / heads;
     const bool mine = idx < total && row < n * G;
     const size_t prow = (size_t)u * shares * BR + r;
+    auto weight = [&](float2 ml, float m) { return ml.y * __builtin_amdgcn_exp2f((ml.x - fmaxf(m, -1e30f)) * c_log2); };
     float m = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float4 v, float w) {
+        acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y); acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
+    };
     if (mine) {
-#pragma unroll 4
-        for (int s = group; s < shares; s += GROUPS) {
-            const float2 ml = *reinterpret_cast<const float2 *>(part_ml + (prow + (size_t)s * BR) * 2);
-            const float4 v = *reinterpret_cast<const float4 *>(part_o + (prow + (size_t)s * BR) * DH + d);
-            const float now = fmaxf(m, ml.x), fin = fmaxf(now, -1e30f);
-            const float keep = __builtin_amdgcn_exp2f((m - fin) * c_log2), w = ml.y * __builtin_amdgcn_exp2f((ml.x - fin) * c_log2);
-            acc.x = fmaf(v.x, w, acc.x * keep); acc.y = fmaf(v.y, w, acc.y * keep);
-            acc.z = fmaf(v.z, w, acc.z * keep); acc.w = fmaf(v.w, w, acc.w * keep);
-            sum = fmaf(sum, keep, w);
+        for (int s = group; s < shares; s += 4 * GROUPS) {
+            float2 ml[4];
+            float4 v[4];
+            float now = m, w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool there = s + i * GROUPS < shares;  // (instead of one that is not, the first with a weight of 0)
+                const size_t at = prow + (size_t)(there ? s + i * GROUPS : s) * BR;
+                ml[i] = *reinterpret_cast<const float2 *>(part_ml + at * 2);
+                v[i] = *reinterpret_cast<const float4 *>(part_o + at * DH + d);
+                if (!there) ml[i].y = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) now = fmaxf(now, ml[i].x);
+            const float before = weight(make_float2(m, sum), now);
+            sum = before;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += w[i] = weight(ml[i], now);
+            const float each = sum == 0.f ? 0.f : 1.0f / sum, keep = before * each;
+            acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add(v[i], w[i] * each);
             m = now;
         }
     }
@@ -1019,24 +1037,15 @@ __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__rest
         if (group) return;
 #pragma unroll
         for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, lm[threadIdx.x / W + k].x);
-        const float fin = fmaxf(m, -1e30f);
-        float keep = __builtin_amdgcn_exp2f((lm[threadIdx.x / W].x - fin) * c_log2);
-        acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
-        sum *= keep;
+        sum = 0.f;
 #pragma unroll
-        for (int k = 1; k < GROUPS; ++k) {
-            const float2 ml = lm[threadIdx.x / W + k];
-            const float4 v = lo[threadIdx.x + k * W];
-            keep = __builtin_amdgcn_exp2f((ml.x - fin) * c_log2);
-            acc.x = fmaf(v.x, keep, acc.x); acc.y = fmaf(v.y, keep, acc.y);
-            acc.z = fmaf(v.z, keep, acc.z); acc.w = fmaf(v.w, keep, acc.w);
-            sum = fmaf(ml.y, keep, sum);
-        }
+        for (int k = 0; k < GROUPS; ++k) sum += weight(lm[threadIdx.x / W + k], m);
+        const float each = sum == 0.f ? 0.f : 1.0f / sum;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) add(lo[threadIdx.x + k * W], weight(lm[threadIdx.x / W + k], m) * each);
     }
-    if (!mine) return;
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    Quad<T>::store(o + (size_t)(b * n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH + d,
-                   make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+    if (mine) Quad<T>::store(o + (size_t)(b * n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH + d, acc);
 }
 
 // Blocks of how many rows of a (sample, kv head) an attention is run by: 16 (kvq_attn_rows_kernel) or 128 (kvq_attn_tiles_kernel, bf16

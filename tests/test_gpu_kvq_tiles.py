@@ -181,13 +181,16 @@ def test_references_that_move(name, case):
 
 
 @pytest.mark.parametrize("name", BOTH)
-@pytest.mark.parametrize("case", ["tiny values", "mixed values", "rising values", "tiny queries", "huge queries", "huge keys"])
+@pytest.mark.parametrize("case", ["tiny values", "huge values", "mixed values", "rising values", "tiny queries", "huge queries",
+                                  "huge keys"])
 def test_values_queries_and_keys_of_every_size(name, case):
     way = Way(name)
     k, v, q = way.kqv(60)
     g = np.random.default_rng(63)
     if case == "tiny values":
         v = v * 2.0 ** -110
+    elif case == "huge values":
+        v = v * 2.0 ** 115
     elif case == "mixed values":                              # sizes from 2^-30 to 1, in no order
         v = v * 2.0 ** -g.integers(0, 31, (1, way.L, way.two, 1))
     elif case == "rising values":                             # each tile's larger than the one's before

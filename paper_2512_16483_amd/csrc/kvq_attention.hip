@@ -26,12 +26,14 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 // seldom, and blocks 2^-36 and less of the largest vanish.  Weights go in as p * 2^8, with a reference that may be up to
 // 2^7 below the true maximum.  Next to bf16 operands (any exponent, 8 bits) the weights keep 11 bits, so that the
 // output's own rounding is the only one of note: 1.7e-3 against 2.4e-3 of the result.
-constexpr int kTop = 13, kRoom = 2;
+// fp32 takes them as they are in bf16 up to blocks of 2^64, and at 2^64 over E from there on: a sum of weights up to 2^7 each stays finite.
+constexpr int kTop = 13, kRoom = 2, kLarge = 127 + 64;
 constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
 
-__device__ __forceinline__ float half_scale(uint32_t byte, int E, bool seen)
+// (scale with which a block is converted that goes in at 2^(byte - E) of 2^top, top with the exponent's bias)
+__device__ __forceinline__ float value_scale(uint32_t byte, int E, int top, bool seen)
 {
-    const int e = (int)byte - E + kTop + 127;
+    const int e = (int)byte - E + top;
     return seen ? __uint_as_float(byte == 255 ? 0x7f800000u : (uint32_t)max(e, 0) << 23) : 0.f;
 }
 
@@ -238,7 +240,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
     for (int i = 0; i < DB; ++i) acc[i] = floatx4_t{0};
     float m_ref = -INFINITY, l_run = 0.f;
     const float lag = kLag / c_log2;
-    int E = 0, acc_E = 0;                                    // of the values, of the sums
+    constexpr int TOP = F32 ? kLarge : kTop + 127;
+    int E = F32 ? kLarge : 0, acc_E = E;                     // of the values, of the sums
 
     // A tile's keys and values are converted first; the next one's are then fetched into the same registers, under the softmax and the
     // products.  A wavefront without a tile looks at one in which it sees nothing.
@@ -267,21 +270,19 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
                 }
             }
             // ---- values to LDS
-            if constexpr (!F32) {
-                uint32_t top = 0;
+            uint32_t top = 0;
 #pragma unroll
-                for (int j = 0; j < VL; ++j) {
-                    const bool seen = (vis >> ((64 * j + lane) / NB)) & 1;
-                    if (seen && x.vs[j] != 255) top = max(top, x.vs[j]);
-                }
-                if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) E = (int)wave_max(top) + kRoom;
+            for (int j = 0; j < VL; ++j) {
+                const bool seen = (vis >> ((64 * j + lane) / NB)) & 1;
+                if (seen && x.vs[j] != 255) top = max(top, x.vs[j]);
             }
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) E = (int)wave_max(top) + kRoom;
 #pragma unroll
             for (int j = 0; j < VL; ++j) {
                 const int key = (64 * j + lane) / NB, blk = lane % NB;
                 const bool seen = (vis >> key) & 1;
                 const uint32_t w[4] = {x.v[j].x, x.v[j].y, x.v[j].z, x.v[j].w};
-                const float scale = F32 ? (seen ? __uint_as_float(x.vs[j] << 23) : 0.f) : half_scale(x.vs[j], E, seen);
+                const float scale = value_scale(x.vs[j], E, TOP, seen);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int piece = (2 * blk + (i >> 1)) ^ turn(key);
@@ -363,10 +364,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
 #pragma unroll
     for (int i = 0; i < DB; ++i) {
         float4 v = make_float4(acc[i][0] * inv, acc[i][1] * inv, acc[i][2] * inv, acc[i][3] * inv);
-        if constexpr (!F32) {                                // |mean| <= 6 * 2^kTop: back to its size, which may be any
-            v.x = __builtin_amdgcn_ldexpf(v.x, acc_E - kTop - 127); v.y = __builtin_amdgcn_ldexpf(v.y, acc_E - kTop - 127);
-            v.z = __builtin_amdgcn_ldexpf(v.z, acc_E - kTop - 127); v.w = __builtin_amdgcn_ldexpf(v.w, acc_E - kTop - 127);
-        }
+        // back to its size, which may be any
+        v.x = __builtin_amdgcn_ldexpf(v.x, acc_E - TOP); v.y = __builtin_amdgcn_ldexpf(v.y, acc_E - TOP);
+        v.z = __builtin_amdgcn_ldexpf(v.z, acc_E - TOP); v.w = __builtin_amdgcn_ldexpf(v.w, acc_E - TOP);
         slots[i * 64 + lane] = v;
     }
     if (g4 == 0) ml[wave][c16] = make_float2(m_ref, l_run);
@@ -619,7 +619,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
             }
         }
         if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) E = (int)wave_max(top) + kRoom;
-        scale = half_scale(x.vs, E, (vis >> vkey) & 1);
+        scale = value_scale(x.vs, E, kTop + 127, (vis >> vkey) & 1);
         return vis;
     };
     // whether a key that is seen is too large for queries in pieces (256 + limit - byte, of two blocks at a time)
@@ -895,7 +895,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         for (int i = 0; i < DB; ++i)
             acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(load_v(i, 32 + 16 * u), pf[1][u], acc[i], 0, 0, 0);
 
-    // ---- means, back at their size (see half_scale)
+    // ---- means, back at their size (see value_scale)
     {
         const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
         l_run = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);

@@ -181,7 +181,7 @@ def test_references_that_move(name, case):
 
 
 @pytest.mark.parametrize("name", BOTH)
-@pytest.mark.parametrize("case", ["tiny values", "huge values", "mixed values", "rising values", "tiny queries", "huge queries",
+@pytest.mark.parametrize("case", ["tiny values", "huge values", "largest values", "mixed values", "rising values", "tiny queries", "huge queries",
                                   "huge keys"])
 def test_values_queries_and_keys_of_every_size(name, case):
     way = Way(name)
@@ -191,6 +191,8 @@ def test_values_queries_and_keys_of_every_size(name, case):
         v = v * 2.0 ** -110
     elif case == "huge values":
         v = v * 2.0 ** 115
+    elif case == "largest values":                            # a mean of some that are near the largest number is not past it
+        v = np.sign(v) * 3e38 * (1 - 0.2 * g.random(v.shape))
     elif case == "mixed values":                              # sizes from 2^-30 to 1, in no order
         v = v * 2.0 ** -g.integers(0, 31, (1, way.L, way.two, 1))
     elif case == "rising values":                             # each tile's larger than the one's before

@@ -84,6 +84,9 @@ __device__ __forceinline__ uint32_t half_min(uint32_t v)
     const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
     return pair_min(a[0], a[1]);
 }
+// What is taken off scores whose largest is m: m, or 0 where nothing finite has been seen and all scores are -inf
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
+
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
 #pragma unroll
@@ -303,10 +306,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
                 }
             }
             const float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            const bool lags = __builtin_amdgcn_ballot_w64(mx > m_ref + lag) != 0 || E != acc_E;
+            const bool lags = __builtin_amdgcn_ballot_w64(mx - m_ref > lag) != 0 || E != acc_E;
             if (__builtin_expect(lags, 0)) {
                 const float now = column_max(fmaxf(m_ref, mx));
-                const float alpha = __builtin_amdgcn_exp2f((m_ref - fmaxf(now, -1e30f)) * c_log2);
+                const float alpha = __builtin_amdgcn_exp2f((m_ref - reference(now)) * c_log2);
                 const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E, -200));
                 m_ref = now;
                 acc_E = E;
@@ -317,12 +320,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
                     asm volatile("" : "+v"(acc[i]));
                 }
             }
-            const float fin = fmaxf(m_ref, -1e30f), base = fmaf(-fin, c_log2, kShift);
+            const float fin = reference(m_ref);
             float p[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                // fp32: the difference first, so that a row's only key weighs exactly 1
-                p[i] = __builtin_amdgcn_exp2f(F32 ? (s[i >> 2][i & 3] - fin) * c_log2 : fmaf(s[i >> 2][i & 3], c_log2, base));
+                // the difference first: exact near the reference, however large the scores
+                const float x = s[i >> 2][i & 3] - fin;
+                p[i] = __builtin_amdgcn_exp2f(F32 ? x * c_log2 : fmaf(x, c_log2, kShift));
                 l_run += p[i];
             }
             // ---- O^T += V^T P^T
@@ -374,7 +378,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
     float m = ml[0][c16].x;
 #pragma unroll
     for (int w = 1; w < NW; ++w) m = fmaxf(m, ml[w][c16].x);
-    const float fin = fmaxf(m, -1e30f);
+    const float fin = reference(m);
     float wgt[NW], sum = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
@@ -573,8 +577,9 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
     floatx16_t acc[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = floatx16_t{0};
-    float m_ref = -INFINITY, l_run = 0.f, most = -1.f;       // most: the sum of weights from which on a reference is looked for
-    // - reference + kShift, in units of log2 as the scores; where registers allow, the products that make scores start from it
+    float l_run = 0.f, most = -1.f;                          // most: the sum of weights from which on a reference is looked for; < 0: no reference yet
+    // Queries in pieces: - reference + kShift, in units of log2 as the scores; where registers allow, the products that make scores start
+    // from it.
     constexpr bool FROM = WAVES == 2;
     float base = kShift;
     floatx16_t bases;
@@ -586,6 +591,9 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
     };
     set_base(kShift);
     auto with_base = [&](float score) { return FROM ? score : score + base; };
+    // Queries as they came: the reference, in units of the scores (which are not yet those of log2).
+    float m_ref = -INFINITY;
+    auto from_ref = [&](float score) { return fmaf(score - reference(m_ref), c_log2, kShift); };
     int E = 0, E_now = 0, acc_E = 0;                         // of the values converted last, of the tile at work, of the sums
 
     // A thread's values as they came, and their scale byte; all scale bytes of the lane's row, of values and of keys.  The rows that can be
@@ -749,8 +757,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
                     x[2 * p1 + 1] = __builtin_amdgcn_exp2f(x[2 * p1 + 1]);
                 }
                 if (p0 < 8) {
-                    x[2 * p0] = WHOLE ? fmaf(s[half][2 * p0], c_log2, base) : with_base(s[half][2 * p0]);
-                    x[2 * p0 + 1] = WHOLE ? fmaf(s[half][2 * p0 + 1], c_log2, base) : with_base(s[half][2 * p0 + 1]);
+                    x[2 * p0] = WHOLE ? from_ref(s[half][2 * p0]) : with_base(s[half][2 * p0]);
+                    x[2 * p0 + 1] = WHOLE ? from_ref(s[half][2 * p0 + 1]) : with_base(s[half][2 * p0 + 1]);
                 }
                 if (p2 >= 0 && p2 < 8) {
                     a = p2 ? a + x[2 * p2] : x[0];
@@ -785,7 +793,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         }
     };
     auto settle = [&](int half, auto as_came) {
-        constexpr bool WHOLE = decltype(as_came)::value;     // scores: not yet in units of log2, and without the base
+        constexpr bool WHOLE = decltype(as_came)::value;
         // The reference is not the running maximum but one that was it; the weights tell when it no longer serves.  A sum of NaN
         // does not ask for another: it stays NaN.
         const bool anew = (__builtin_amdgcn_ballot_w64(sum > most) != 0 && (uint32_t)(vis >> (32 * half)) != 0) || E_now != acc_E;
@@ -793,23 +801,31 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
             float mx = s[half][0];
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
-            if constexpr (WHOLE) mx *= c_log2;
-            else if constexpr (FROM) mx -= base;
-            mx = fmaxf(m_ref, mx);
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-            const float now = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-            const bool none = now == -INFINITY;              // nothing finite yet
-            const float alpha = none ? 0.f : __builtin_amdgcn_exp2f(m_ref - now);
+            mx = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+            const bool had = most >= 0.f, none = !had && mx == -INFINITY;
+            float alpha = 1.f;
+            if constexpr (WHOLE) {
+                const float now = fmaxf(m_ref, mx);
+                alpha = __builtin_amdgcn_exp2f((m_ref - reference(now)) * c_log2);
+                m_ref = now;
+            } else {
+                // the largest score to kShift, or to 0 where its neighbours are too far apart for kShift to count
+                const float before = base, over = FROM ? mx : mx + base;
+                if (!none && (!had || over > kShift)) {
+                    const float by = fabsf(mx) >= 0x1p24f ? mx : mx - kShift;
+                    if constexpr (FROM) {
+                        s[0] -= by;
+                        s[1] -= by;
+                    }
+                    set_base(FROM ? base - by : -by);
+                }
+                alpha = __builtin_amdgcn_exp2f(base - before);
+            }
+            if (!had) alpha = 0.f;
             const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E_now, -200));
-            m_ref = now;
             most = none ? -1.f : kMost;
             acc_E = E_now;
-            const float before = base;
-            set_base(none ? kShift : kShift - now);
-            if constexpr (FROM && !WHOLE) {
-                s[0] += base - before;
-                s[1] += base - before;
-            }
             l_run *= alpha;
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
@@ -819,8 +835,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
             sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(WHOLE ? fmaf(s[half][i], c_log2, base) : with_base(s[half][i]));
-                const float y = __builtin_amdgcn_exp2f(WHOLE ? fmaf(s[half][i + 1], c_log2, base) : with_base(s[half][i + 1]));
+                const float x = __builtin_amdgcn_exp2f(WHOLE ? from_ref(s[half][i]) : with_base(s[half][i]));
+                const float y = __builtin_amdgcn_exp2f(WHOLE ? from_ref(s[half][i + 1]) : with_base(s[half][i + 1]));
                 sum += x + y;
                 const f16x2_t p = __builtin_convertvector((floatx2_t{x, y}), f16x2_t);
                 pf[half][i >> 3][i & 7] = p[0];
@@ -869,6 +885,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         do tile(std::false_type{});
         while (t <= t1 && !far);
     }
+    m_ref = most < 0.f ? -INFINITY : (kShift - base) / c_log2;
     if (t <= t1) {
         const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
         uint32_t top = 0;
@@ -919,7 +936,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         }
     };
     auto put_weight = [&](float m, float l) {
-        if (ranges > 1 && g == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m / c_log2, l);
+        if (ranges > 1 && g == 0) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m, l);
     };
     auto quad_mean = [&](const floatx16_t &x, int e) { return make_float4(mean(x[e]), mean(x[e + 1]), mean(x[e + 2]), mean(x[e + 3])); };
     if constexpr (KG == 1) {
@@ -951,8 +968,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         __syncthreads();
         if (r0 + rl >= R) return;
         const float2 other = xm[((1 - kg) * 4 + wave) * 64 + lane];
-        const float m = fmaxf(m_ref, other.x), fin = fmaxf(m, -1e30f);
-        float own = l_run * __builtin_amdgcn_exp2f(m_ref - fin), theirs = other.y * __builtin_amdgcn_exp2f(other.x - fin);
+        const float m = fmaxf(m_ref, other.x), fin = reference(m);
+        float own = l_run * __builtin_amdgcn_exp2f((m_ref - fin) * c_log2), theirs = other.y * __builtin_amdgcn_exp2f((other.x - fin) * c_log2);
         const float all = own + theirs, each = all == 0.f ? 0.f : 1.0f / all;
         own *= each;
         theirs *= each;
@@ -998,7 +1015,7 @@ __global__ __launch_bounds__(256) void kvq_attn_merge_kernel(const float *__rest
     const long b = unit / nrb / heads;
     const bool mine = idx < total && row < n * G;
     const size_t prow = (size_t)u * shares * BR + r;
-    auto weight = [&](float2 ml, float m) { return ml.y * __builtin_amdgcn_exp2f((ml.x - fmaxf(m, -1e30f)) * c_log2); };
+    auto weight = [&](float2 ml, float m) { return ml.y * __builtin_amdgcn_exp2f((ml.x - reference(m)) * c_log2); };
     float m = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     auto add = [&](float4 v, float w) {

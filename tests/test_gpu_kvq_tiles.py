@@ -219,6 +219,28 @@ def test_equal_scores_are_the_mean(name):
     assert (np.abs(o - want) <= lim).all()
 
 
+@pytest.mark.parametrize("name", BOTH)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_every_size(name, sign):
+    """Two kinds of keys, one with twice the other's score, about 2^size: all weight lies on the larger score's, equally, and the result is the mean
+    of their values, whichever tiles, shares and groups they stand in."""
+    way = Way(name)
+    g, t = np.random.default_rng(71), np.arange(way.L)
+    unit = np.where(g.random(way.dh) < 0.5, -1.0, 1.0)        # scores are sums of equal terms, without rounding
+    kind = np.where(t * 7 // 3 % 5 < 3, 2.0, 1.0)
+    if sign < 0:                                              # the larger score in few places, the last tile's and the first's among others
+        kind = np.where(np.isin(t, [3, 4, way.L // 2, way.L - 1]), 1.0, 2.0)
+    _, v, _ = way.kqv(72)
+    for size in (20, 24, 26, 27, 28, 30, 40, 60, 100, 112):
+        half = size // 2
+        k = (kind[:, None] * unit)[None, :, None] * 2.0 ** half * np.ones((1, 1, way.two, 1))
+        q = sign * unit * 2.0 ** (size - half) / way.dh ** 0.5 * np.ones((1, way.n, way.few, 1))
+        k, q = way.round(k.astype(np.float32), q.astype(np.float32))
+        kv, held = way.cache(k, v)
+        want = np.repeat(held[1][0][:, kind == (2 if sign > 0 else 1)].mean(1), way.few // way.two, 0)[None]
+        way.check(f"scores {sign * 2.0 ** size:.1g}", way.attend(q, kv), np.tile(want, (way.n, 1, 1)))
+
+
 # ------------------------------------------------------------------------------------ queries with elements of very different sizes
 @pytest.mark.parametrize("name", BOTH)
 @pytest.mark.parametrize("case", ["x 30", "x 200", "x 1000", "x 1e5", "half of them", "one to a block", "a ladder"])

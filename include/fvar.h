@@ -308,7 +308,7 @@ fvar_status fvar_kvq_read(fvar_ctx *ctx, fvar_stream stream, const fvar_kvq *kv,
  *   o[b,i,h,:] = sum_t p_t V[b,t,h',:],  p = softmax of scale * q[b,i,h,:] . K[b,t,h',:] over the visible t
  * (t is held by the sample and its mask byte is not 0).  A sample without a visible row gives 0.  What rows that are not
  * visible hold, NaN included, has no influence.  Scores and sums are fp32.  A query counts with all its bits, but for an error of at most 2 %
- * of a weight (0.02 % rms) where it and the keys are of like size, in bf16 and for many queries.  bf16: values of blocks 2^-36
+ * of a weight (0.02 % rms) where it and the keys are of like size, in bf16 and for many queries.  bf16: values of blocks 2^-35
  * and less of the size of the largest visible block of the sample and kv head may count as 0; fp32: those of 2^-180 and less.  q: query i of sample b starts at element (b*n + i)*ld and holds
  * [heads][Dh]; ld = 0 stands for hidden; a multiple of 8 for bf16 (of 4 for fp32).  o:[B][n][heads][Dh], must not overlap q.
  * B*n*heads <= 2^25.  ws: at least fvar_kvq_attention_workspace_bytes(ctx,kv,B,n), which depends on kv_heads and capacity

@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = floatx4_t{0};
     float m_ref = -INFINITY, l_run = 0.f;
-    const float lag = kLag / c_log2;
+    const float lag = fminf(kLag / c_log2, 3e38f);           // (finite: any score is more than that above none)
     constexpr int TOP = F32 ? kLarge : kTop + 127;
     int E = F32 ? kLarge : 0, acc_E = E;                     // of the values, of the sums
 

@@ -25,13 +25,13 @@ BOTH = sorted(TILES) + sorted(SIXTEEN)
 class Way:
     """A way's context and sizes, and one sample's tensors repeated over them."""
 
-    def __init__(self, name):
+    def __init__(self, name, **kw):
         check_way(name)
         self.name = name
         self.dtype, self.dh, self.H, self.heads, self.B, self.n, self.L, *_ = {**TILES, **SIXTEEN}[name]
         self.two = min(2, self.heads)                         # kv heads of the data
         self.few = self.two * self.H // self.heads            # its query heads
-        self.ctx = _ctx(self.H, self.dh, self.dtype)
+        self.ctx = _ctx(self.H, self.dh, self.dtype, **kw)
 
     def data(self, seed, rows, heads, spread=0.5):
         return _rows(seed, 1, rows, heads, self.dh, self.dtype, spread)
@@ -217,6 +217,16 @@ def test_equal_scores_are_the_mean(name):
     o, want = to_np(way.attend(np.zeros_like(q), kv)[:2]).reshape(2, way.n, -1, way.two, way.few // way.two, way.dh), held[1].mean(2)[0][:, None]
     lim = 2.0 ** -8 * np.abs(want) + way.L * 2.0 ** -24 * np.abs(held[1]).mean(2)[0][:, None]
     assert (np.abs(o - want) <= lim).all()
+
+
+@pytest.mark.parametrize("name", BOTH)
+@pytest.mark.parametrize("scale", [1e-30, 1.3e-38, 2e-38])
+def test_a_scale_that_makes_all_scores_equal(name, scale):
+    way = Way(name, attn_scale=scale)
+    k, v, q = way.kqv(74)
+    kv, held = way.cache(k, v)
+    want = np.repeat(held[1][0].mean(1), way.few // way.two, 0)[None]
+    way.check(f"scale {scale}", way.attend(q, kv), np.tile(want, (way.n, 1, 1)))
 
 
 @pytest.mark.parametrize("name", BOTH)

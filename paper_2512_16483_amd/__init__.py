@@ -157,13 +157,17 @@ def _nbytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
+_current: list = []                                           # what gives the current stream of a device, and that device
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # a Stream object takes 3 us, as long as a launch
-        if raw is not None:
-            return raw(torch.cuda.current_device()) or None
-        stream = torch.cuda.current_stream()
+        if not _current:
+            import torch
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # a Stream object takes 3 us, as long as a launch
+            _current.append((raw, torch.cuda.current_device) if raw is not None else (torch.cuda.current_stream, lambda: None))
+        of, device = _current[0]
+        stream = of(device())
     return getattr(stream, "cuda_stream", stream) or None
 
 
@@ -335,6 +339,7 @@ class KVQ:
                         "lens": (B,), "mask": (B, capacity)}
         self._tensors = {}
         self._c = _KVQ(kv_heads=heads, capacity=capacity, len=len)
+        self._ref, self._batch, self._head_dim = C.byref(self._c), B, 2 * codes
         for name, t in (("k", k), ("v", v), ("k_scale", k_scale), ("v_scale", v_scale), ("lens", lens), ("mask", mask)):
             self._hold(name, t)
 
@@ -359,8 +364,8 @@ class KVQ:
     mask = property(lambda self: self._tensors["mask"], lambda self, t: self._hold("mask", t))
     kv_heads = property(lambda self: self._c.kv_heads)
     capacity = property(lambda self: self._c.capacity)
-    batch = property(lambda self: self._shapes["k"][0])
-    head_dim = property(lambda self: 2 * self._shapes["k"][3])
+    batch = property(lambda self: self._batch)
+    head_dim = property(lambda self: self._head_dim)
 
     @property
     def len(self) -> int:
@@ -371,38 +376,51 @@ class KVQ:
         self._c.len = value
 
     def _for(self, ctx: Context, B: int):
-        if self.head_dim != ctx.head_dim or B > self.batch:
+        if self._head_dim != ctx.head_dim or B > self._batch:
             raise ValueError(f"a cache of {self.batch} samples with head_dim {self.head_dim} does not serve {B} samples "
                              f"with head_dim {ctx.head_dim}")
-        return C.byref(self._c)
+        return self._ref
 
 
-_ELEMENT = {"bf16": "torch.bfloat16", "f32": "torch.float32"}
+_KINDS: dict = {}                                             # element types by the contexts' names for them
 
 
-def _packed(t, kind: str, B: int, rows: int, width: int) -> Optional[int]:
-    """Pointer of contiguous t whose first B * rows * width elements are [B, rows, width] (None passes NULL).  A tensor with room for
-    more is taken where those are its first elements: a flat one, rows of `width`, more samples, or more rows of the only one."""
+def _kind(name: str):
+    if not _KINDS:
+        import torch
+        _KINDS.update(bf16=torch.bfloat16, f32=torch.float32, i32=torch.int32)
+    return _KINDS[name]
+
+
+def _check_room(t, B: int, rows: int, width: int) -> None:
+    """A contiguous tensor that has not just the elements of [B, rows, width]: it may have more where those are its first ones, in a flat one,
+    in rows of `width`, in more samples, or in more rows of the only one."""
+    n, s = t.numel(), t.shape if width > 1 else (*t.shape, 1)
+    fits = n > B * rows * width and (len(s) == 1 or s[-1] == width and len(s) == 2 or
+                                     len(s) > 2 and s[0] * s[1] * width == n and (s[1] == rows or B == 1))
+    if not fits:
+        raise ValueError(f"{B} x {rows} rows of {width} elements are wanted, got a tensor of shape {tuple(t.shape)}")
+
+
+def _packed(t, kind, B: int, rows: int, width: int) -> Optional[int]:
+    """Pointer of contiguous t:[B, rows, width], whose type and size are looked at (None passes NULL)."""
     if t is None:
         return None
-    if str(t.dtype) != kind:
+    if t.dtype is not kind:
         raise ValueError(f"a tensor of {kind} is wanted, got {t.dtype}")
-    n, s = t.numel(), t.shape if width > 1 else (*t.shape, 1)
-    if n != B * rows * width:
-        fits = n > B * rows * width and (len(s) == 1 or s[-1] == width and len(s) == 2 or
-                                         len(s) > 2 and s[0] * s[1] * width == n and (s[1] == rows or B == 1))
-        if not fits:
-            raise ValueError(f"{B} x {rows} rows of {width} elements are wanted, got a tensor of shape {tuple(s)}")
-    return _ptr(t)
+    if not t.is_cuda or not t.is_contiguous():
+        return _ptr(t)                                        # (which says what is wrong)
+    if t.numel() != B * rows * width:
+        _check_room(t, B, rows, width)
+    return t.data_ptr()
 
 
-def _rows(ctx: Context, t, B: int, rows: int, width: int):
+def _rows(t, kind, B: int, rows: int, width: int):
     """Pointer and row pitch of t:[B, rows, ...] of the context's type, whose rows of `width` elements are contiguous; they may lie apart,
     as the parts of a fused projection's output do."""
-    kind = _ELEMENT[ctx.dtype]
     if t is None or t.is_contiguous():
         return _packed(t, kind, B, rows, width), 0
-    if not t.is_cuda or str(t.dtype) != kind:
+    if not t.is_cuda or t.dtype is not kind:
         raise ValueError(f"tensors handed to fvar must be GPU tensors, here of {kind}")
     if t.dim() < 3 or t.shape[0] != B or t.shape[1] != rows or t[0, 0].numel() != width or not t[0, 0].is_contiguous():
         raise ValueError(f"[{B}, {rows}, ...] with contiguous rows of {width} elements is wanted, got shape "
@@ -416,15 +434,16 @@ def _rows(ctx: Context, t, B: int, rows: int, width: int):
 
 
 def fvar_kvq_append(ctx: Context, kv: KVQ, k, v, B: int, rows: int, stream=None) -> None:
-    width = kv.kv_heads * ctx.head_dim
-    (kp, ldk), (vp, ldv) = _rows(ctx, k, B, rows, width), _rows(ctx, v, B, rows, width)
+    kind, width = _kind(ctx.dtype), kv._c.kv_heads * ctx.head_dim
+    (kp, ldk), (vp, ldv) = _rows(k, kind, B, rows, width), _rows(v, kind, B, rows, width)
     if (ldk or width) != (ldv or width):
         raise ValueError("k and v have different distances between rows")
     ctx.check(ctx.lib.fvar_kvq_append(ctx.handle, _stream(stream), kv._for(ctx, B), kp, vp, ldk, B, rows))
 
 
 def fvar_kvq_read(ctx: Context, kv: KVQ, B: int, first: int, rows: int, k=None, v=None, stream=None) -> None:
-    kp, vp = (_packed(t, _ELEMENT[ctx.dtype], B, rows, kv.kv_heads * ctx.head_dim) for t in (k, v))
+    kind, width = _kind(ctx.dtype), kv._c.kv_heads * ctx.head_dim
+    kp, vp = _packed(k, kind, B, rows, width), _packed(v, kind, B, rows, width)
     ctx.check(ctx.lib.fvar_kvq_read(ctx.handle, _stream(stream), kv._for(ctx, B), B, first, rows, kp, vp))
 
 
@@ -433,8 +452,9 @@ def fvar_kvq_attention_workspace_bytes(ctx: Context, kv: KVQ, B: int, n: int) ->
 
 
 def fvar_kvq_attention(ctx: Context, q, kv: KVQ, B: int, n: int, o, ws=None, stream=None) -> None:
-    qp, ld = _rows(ctx, q, B, n, ctx.hidden)
-    op = _packed(o, _ELEMENT[ctx.dtype], B, n, ctx.hidden)
+    kind = _kind(ctx.dtype)
+    qp, ld = _rows(q, kind, B, n, ctx.hidden)
+    op = _packed(o, kind, B, n, ctx.hidden)
     ctx.check(ctx.lib.fvar_kvq_attention(ctx.handle, _stream(stream), qp, ld, kv._for(ctx, B), B, n, op, _ptr(ws), _nbytes(ws)))
 
 
@@ -443,17 +463,18 @@ def fvar_block_kvq_workspace_bytes(ctx: Context, kv: KVQ, B: int, rows: int) -> 
 
 
 def fvar_block_forward_dense_kvq(ctx: Context, w: dict, x, B: int, M: int, kv: KVQ, y, ws, stream=None) -> None:
-    ws_, xy = _weights(w), [_packed(t, _ELEMENT[ctx.dtype], B, M, ctx.hidden) for t in (x, y)]
-    ctx.check(ctx.lib.fvar_block_forward_dense_kvq(ctx.handle, _stream(stream), C.byref(ws_), xy[0], B, M, kv._for(ctx, B), xy[1],
-                                                   _ptr(ws), _nbytes(ws)))
+    ws_, kind = _weights(w), _kind(ctx.dtype)
+    xp, yp = _packed(x, kind, B, M, ctx.hidden), _packed(y, kind, B, M, ctx.hidden)
+    ctx.check(ctx.lib.fvar_block_forward_dense_kvq(ctx.handle, _stream(stream), C.byref(ws_), xp, B, M, kv._for(ctx, B), yp, _ptr(ws),
+                                                   _nbytes(ws)))
 
 
 def fvar_block_forward_pruned_kvq(ctx: Context, w: dict, x, B: int, M: int, idx_keep, k: int, kv: KVQ, y_keep, ws,
                                   stream=None) -> None:
-    ws_, kind = _weights(w), _ELEMENT[ctx.dtype]
+    ws_, kind = _weights(w), _kind(ctx.dtype)
     xp, yp = _packed(x, kind, B, M, ctx.hidden), _packed(y_keep, kind, B, k, ctx.hidden)
     ctx.check(ctx.lib.fvar_block_forward_pruned_kvq(ctx.handle, _stream(stream), C.byref(ws_), xp, B, M,
-                                                    _packed(idx_keep, "torch.int32", B, k, 1), k, kv._for(ctx, B), yp, _ptr(ws),
+                                                    _packed(idx_keep, _kind("i32"), B, k, 1), k, kv._for(ctx, B), yp, _ptr(ws),
                                                     _nbytes(ws)))
 
 

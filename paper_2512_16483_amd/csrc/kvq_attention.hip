@@ -615,25 +615,31 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
         x.keys = NB == 4 ? *reinterpret_cast<const uint32_t *>(sc + lane * NB) : *reinterpret_cast<const uint16_t *>(sc + lane * NB);
     };
     float scale;
-    auto look = [&](int t, const Raw &x, const Next &f) -> unsigned long long {
+    bool far = false;                                        // whether a key that is seen is too large for queries in pieces
+    auto look = [&](int t, const Raw &x, const Next &f, auto as_came) -> unsigned long long {
+        constexpr bool WHOLE = decltype(as_came)::value;     // (queries as they came: any key will do)
         const bool seen = t * 64 + lane < seen_end && (!mask || f.seen);
         const unsigned long long vis = __ballot(seen);
-        uint32_t top = 0;
-        if (seen) {
+        // bit 8 of 256 + limit - byte, for two bytes at a time: at most the limit
+        constexpr uint32_t LOW = 0xff00ff, BIT = 0x1000100;
+        const uint32_t size = (uint32_t)E * 0x10001 + BIT;
+        const uint32_t keys = (limit_even - (x.keys & LOW)) & (limit_odd - (x.keys >> 8 & LOW)) & BIT;
+        const uint32_t fits = (size - (x.all & LOW)) & (size - (x.all >> 8 & LOW)) & (WHOLE ? BIT : keys);
+        if constexpr (!WHOLE) far = false;
+        if (__builtin_expect((__builtin_amdgcn_ballot_w64(fits != BIT) & vis) != 0, 0)) {
+            uint32_t top = 0;
+            if (seen) {
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const uint32_t byte = x.all >> (8 * i) & 255;
-                if (byte != 255) top = max(top, byte);
+                for (int i = 0; i < NB; ++i) {
+                    const uint32_t byte = x.all >> (8 * i) & 255;
+                    if (byte != 255) top = max(top, byte);
+                }
             }
+            if (__builtin_amdgcn_ballot_w64((int)top > E) != 0) E = (int)wave_max(top) + kRoom;
+            if constexpr (!WHOLE) far = (__builtin_amdgcn_ballot_w64(keys != BIT) & vis) != 0;
         }
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) E = (int)wave_max(top) + kRoom;
         scale = value_scale(x.vs, E, kTop + 127, (vis >> vkey) & 1);
         return vis;
-    };
-    // whether a key that is seen is too large for queries in pieces (256 + limit - byte, of two blocks at a time)
-    auto too_large = [&](const Raw &x, unsigned long long vis) {
-        const uint32_t fits = (limit_even - (x.keys & 0xff00ff)) & (limit_odd - (x.keys >> 8 & 0xff00ff)) & 0x1000100;
-        return (__builtin_amdgcn_ballot_w64(fits != 0x1000100) & vis) != 0;
     };
     int vdst[VW];                                            // where the thread's words go, in bytes
 #pragma unroll
@@ -647,8 +653,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
     put_scales(1, later);
     meet();
     read_raw(0, raw);
-    unsigned long long vis = look(t0, raw, next), vis_next;
-    bool far = too_large(raw, vis);                          // of the tile at work
+    unsigned long long vis = look(t0, raw, next, std::false_type{}), vis_next;
 #pragma unroll
     for (int i = 0; i < VW; ++i) convert(0, raw, i);
     next = later;
@@ -660,7 +665,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
             const int s1 = after(stage);
             fetch(min(t + 2, t1), after(s1), later);
             read_raw(s1, raw);
-            look(min(t + 1, t1), raw, next);
+            look(min(t + 1, t1), raw, next, std::true_type{});
 #pragma unroll
             for (int i = 0; i < VW; ++i) convert(s1, raw, i);
             put_scales(after(s1), later);
@@ -864,8 +869,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const u
             sp += k_by;
         }
         hide(1);
-        vis_next = look(min(t + 1, t1), raw, next);
-        if constexpr (!decltype(as_came)::value) far = too_large(raw, vis_next);
+        vis_next = look(min(t + 1, t1), raw, next, as_came);
         region(std::integral_constant<int, 1>{}, as_came, s1);
         settle(1, as_came);
         put_scales(s2, later);

@@ -307,12 +307,13 @@ fvar_status fvar_kvq_read(fvar_ctx *ctx, fvar_stream stream, const fvar_kvq *kv,
 /* Attention over the 4-bit cache, for one query per sample or many:
  *   o[b,i,h,:] = sum_t p_t V[b,t,h',:],  p = softmax of scale * q[b,i,h,:] . K[b,t,h',:] over the visible t
  * (t is held by the sample and its mask byte is not 0).  A sample without a visible row gives 0.  What rows that are not
- * visible hold, NaN included, has no influence.  Scores and sums are fp32.  A query counts with all its bits, but for an error of at most 2 %
- * of a weight (0.02 % rms) where it and the keys are of like size, in bf16 and for many queries.  bf16: values of blocks 2^-35
- * and less of the size of the largest visible block of the sample and kv head may count as 0; fp32: those of 2^-180 and less.  q: query i of sample b starts at element (b*n + i)*ld and holds
- * [heads][Dh]; ld = 0 stands for hidden; a multiple of 8 for bf16 (of 4 for fp32).  o:[B][n][heads][Dh], must not overlap q.
- * B*n*heads <= 2^25.  ws: at least fvar_kvq_attention_workspace_bytes(ctx,kv,B,n), which depends on kv_heads and capacity
- * but not on the pointers, and may be 0 (as it is for sizes that the call refuses). */
+ * visible hold, NaN included, has no influence.  Scores and sums are fp32; queries count with all their bits (bf16, many
+ * queries: but for an error of at most 2 %, 0.02 % rms, of a weight).  Beside far larger values small ones may count as 0: those
+ * of blocks 2^-35 (fp32: 2^-180) and less of the size of the largest visible one of the sample and kv head.
+ * q: query i of sample b starts at element (b*n + i)*ld and holds [heads][Dh]; ld = 0 stands for hidden; a multiple of 8
+ * for bf16 (of 4 for fp32).  o:[B][n][heads][Dh], must not overlap q.  B*n*heads <= 2^25.
+ * ws: at least fvar_kvq_attention_workspace_bytes(ctx,kv,B,n), which depends on kv_heads and capacity but not on the
+ * pointers, and may be 0 (as it is for sizes that the call refuses). */
 size_t fvar_kvq_attention_workspace_bytes(const fvar_ctx *ctx, const fvar_kvq *kv, int32_t B, int32_t n);
 fvar_status fvar_kvq_attention(fvar_ctx *ctx, fvar_stream stream, const void *q, int32_t ld, const fvar_kvq *kv, int32_t B,
                                int32_t n, void *o, void *ws, size_t ws_bytes);

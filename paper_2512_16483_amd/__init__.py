@@ -397,7 +397,7 @@ def _check_room(t, B: int, rows: int, width: int) -> None:
     in rows of `width`, in more samples, or in more rows of the only one."""
     n, s = t.numel(), t.shape if width > 1 else (*t.shape, 1)
     fits = n > B * rows * width and (len(s) == 1 or s[-1] == width and len(s) == 2 or
-                                     len(s) > 2 and s[0] * s[1] * width == n and (s[1] == rows or B == 1))
+                                     len(s) > 2 and s[0] * s[1] * width == n and (s[1] == rows or B == 1 and s[1] > rows))
     if not fits:
         raise ValueError(f"{B} x {rows} rows of {width} elements are wanted, got a tensor of shape {tuple(t.shape)}")
 

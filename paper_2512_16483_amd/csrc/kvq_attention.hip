@@ -422,8 +422,9 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 //     largest value) times the sum of what is left to a score's error.  While that is below 2^-5 over a row for all rows of a wavefront and
 //     the keys of a tile, the pieces serve (queries and keys of normal numbers: 2^-7.5 at most, 2^-14 rms).  From the first tile on for
 //     which it is not (scores of 15 and more, or a few elements far larger than the others), a wavefront takes its queries as they came, in bf16, and
-//     converts the keys: exact, four products of 16 elements for three of 64 and 32 conversions per half a tile more, 10 to 17 % slower (4 x 1600
-//     x 12121, 32 heads of 128: 1240 us, 1100 with pieces; 8 x 231 x 871, 30 of 64, 25.4, 23.0; 4 x 300 x 2500, 16 of 128, 46.9, 40.7).
+//     converts the keys: exact, four products of 16 elements for three of 64 and 32 conversions per half a tile more, 10 to 24 % slower (4 x 1600
+//     x 12121, 32 heads of 128: 1280 us, 1075 with pieces; 8 x 231 x 871, 30 of 64, 27.0, 23.3; 16 x 410 x 1281, 116, 106; 4 x 300 x 2500, 16
+//     of 128, 49.6, 40.0).
 //   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
 // In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
 // product takes it, as in attention.hip.
@@ -433,9 +434,9 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // product that adds to the one right before it waits (a pair of weights 38 cycles, a product 40, both 58, 66 where they add on).
 // KG = 2: two groups of four wavefronts on the same rows, each with half of the keys and stages of its own, which meet in LDS at the end:
 // as full a CU as two workgroups make, without partial results in memory.
-// WAVES, of a SIMD: 3 with 64-wide rows where there are more than two workgroups for every CU (30 heads, 8 x 410 x 1281 keys 66 us, 69 with
-// 2); with 2 there are registers for products that start from the reference, an addition less per weight (32 x 480 x 3001, 16 heads of 128,
-// 396 to 386 us; 30 of 64, 8 x 231 x 871, 25.2 to 23.9).
+// WAVES, of a SIMD: 3 with 64-wide rows where there are more than two workgroups for every CU (30 heads, 8 x 410 x 1281 keys 65 us, 67 with
+// 2, 16 x 410 x 1281 106, 115); with 2 there are registers for products that start from the reference, an addition less per weight (32 x 480 x
+// 3001, 16 heads of 128, 373 to 365 us; 30 of 64, 8 x 231 x 871, 24.3 to 23.0).
 template <int DH, int KG, int WAVES>
 __global__ __launch_bounds__(256 * KG, WAVES) void kvq_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvqCache c, int extra,
                                                                 int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,

@@ -156,6 +156,8 @@ def test_room_for_more_rows_is_taken_only_where_the_rows_are_where_the_calls_loo
         for q, o in ((bad, good), (good, bad)):
             with pytest.raises(ValueError):
                 att(q, o, 2, 5)
+    with pytest.raises(ValueError):
+        att(more, good, 1, 15)                                # rows of one sample and the next
     assert len(ctx.lib.calls) == 5
     pruned = lambda keep, B: fv.fvar_block_forward_pruned_kvq(ctx, {}, zeros(B, 6, 256), B, 6, keep, 5, cache(), zeros(B, 5, 256),
                                                               zeros(8, dtype=torch.uint8), stream=1)

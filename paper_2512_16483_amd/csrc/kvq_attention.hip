@@ -23,14 +23,14 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 
 // Values as fp16 operands.  An fp16 number holds an element of the format times 2^-25 to 2^13, so a value goes in as
 // value * 2^(kTop - E), E the largest scale byte seen so far and two more: sums are rescaled when a byte exceeds E, which is
-// seldom, and blocks 2^-36 and less of the largest vanish.  Weights go in as p * 2^8, with a reference that may be up to
+// seldom, and blocks 2^-35 and less of the largest may vanish.  Weights go in as p * 2^8, with a reference that may be up to
 // 2^7 below the true maximum.  Next to bf16 operands (any exponent, 8 bits) the weights keep 11 bits, so that the
 // output's own rounding is the only one of note: 1.7e-3 against 2.4e-3 of the result.
 // fp32 takes them as they are in bf16 up to blocks of 2^64, and at 2^64 over E from there on: a sum of weights up to 2^7 each stays finite.
 constexpr int kTop = 13, kRoom = 2, kLarge = 127 + 64;
 constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
 
-// (scale with which a block is converted that goes in at 2^(byte - E) of 2^top, top with the exponent's bias)
+// The scale with which a block of scale byte `byte` is converted: E's goes in as 2^(top - 127).
 __device__ __forceinline__ float value_scale(uint32_t byte, int E, int top, bool seen)
 {
     const int e = (int)byte - E + top;

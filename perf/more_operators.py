@@ -424,17 +424,17 @@ def _handle(s):
         else:
             parts = [s[n] for n in ("k_codes", "v_codes", "k_scale", "v_scale")]
             if kind == "write" and case["ragged"]:
-                first, second = fv.KV8(*parts, lens=s["first"]), fv.KV8(*parts, lens=s["last"])
+                first, second = fv.KVB(*parts, lens=s["first"]), fv.KVB(*parts, lens=s["last"])
             elif kind == "write":
-                first, second = fv.KV8(*parts, len=case["prefix"]), fv.KV8(*parts, len=case["prefix"] + case["rows"])
+                first, second = fv.KVB(*parts, len=case["prefix"]), fv.KVB(*parts, len=case["prefix"] + case["rows"])
             else:
-                first = fv.KV8(*parts, len=case["keys"], lens=s["lens"], mask=s["mask"])
+                first = fv.KVB(*parts, len=case["keys"], lens=s["lens"], mask=s["mask"])
             size = 0
             if kind == "attend":
-                size = fv.fvar_kv8_attention_workspace_bytes(ctx, first, B, case["queries"], case["weights"])
+                size = fv.fvar_kvb_attention_workspace_bytes(ctx, first, B, case["queries"], case["weights"])
             elif kind == "evict":
-                second = fv.KV8(s["to_k"], s["to_v"], s["to_k_scale"], s["to_v_scale"], lens=s["to_lens"])
-                size = fv.fvar_kv8_evict_workspace_bytes(ctx, first, B, case["keep"])
+                second = fv.KVB(s["to_k"], s["to_v"], s["to_k_scale"], s["to_v_scale"], lens=s["to_lens"])
+                size = fv.fvar_kvb_evict_workspace_bytes(ctx, first, B, case["keep"])
             ws = torch.empty(size, dtype=torch.uint8, device="cuda")
         s["handle"] = (fv, ctx, first, second, ws)
     return s["handle"]
@@ -448,16 +448,16 @@ def _own(s):
         fv.fvar_rope_apply(ctx, first, s["pos"], B, case["rows"], s["q"], s["k"], s["q_out"], s["k_out"])
         return {"q": s["q_out"], "k": s["k_out"]}
     if kind == "attend":
-        fv.fvar_kv8_attention(ctx, s["q"], first, B, case["queries"], s["o"], ws, weights=s["weights"])
+        fv.fvar_kvb_attention(ctx, s["q"], first, B, case["queries"], s["o"], ws, weights=s["weights"])
         return {"o": s["o"], "weights": s["weights"]} if case["weights"] else {"o": s["o"]}
     if kind == "write":
-        fv.fvar_kv8_append(ctx, first, s["k"], s["v"], B, case["rows"])
+        fv.fvar_kvb_append(ctx, first, s["k"], s["v"], B, case["rows"])
         # the rows just written, and those before them that can share a block with the first
         rows = case["rows"] + BLOCK - 1
-        fv.fvar_kv8_read(ctx, second, B, -rows, rows, s["k_back"], s["v_back"])
+        fv.fvar_kvb_read(ctx, second, B, -rows, rows, s["k_back"], s["v_back"])
         return {"k": s["k_back"], "v": s["v_back"]}
-    fv.fvar_kv8_evict(ctx, first, s["weights"], B, case["keep"], case["recent"], second, s["to_weights"], s["to_lens"], s["idx"], ws)
-    fv.fvar_kv8_read(ctx, second, B, 0, case["keep"], s["k_back"], s["v_back"])
+    fv.fvar_kvb_evict(ctx, first, s["weights"], B, case["keep"], case["recent"], second, s["to_weights"], s["to_lens"], s["idx"], ws)
+    fv.fvar_kvb_read(ctx, second, B, 0, case["keep"], s["k_back"], s["v_back"])
     return {"idx": s["idx"], "lens": s["to_lens"], "weights": s["to_weights"], "k": s["k_back"], "v": s["v_back"]}
 
 

@@ -25,6 +25,10 @@
  * over a key/value cache held in 4 bits (fvar_kvq), and fvar_block_forward_*_kvq
  * run the block over one.
  *
+ * fvar_rope_apply turns queries and keys by their positions.  fvar_kvb_append, fvar_kvb_read and fvar_kvb_attention do
+ * for a cache held in 8 bits (fvar_kvb) what the calls above do for one of 4; its attention can also return the weight that every
+ * row has got, by which fvar_kvb_evict drops rows.
+ *
  * Conventions common to every call
  *  - Every tensor pointer is DEVICE memory owned by the caller, row-major,
  *    contiguous, 16-byte aligned, of element type `fvar_config.dtype`
@@ -132,6 +136,41 @@ typedef struct {
     int32_t capacity;
     int32_t len;
 } fvar_kvq;
+
+/* Key/value cache of one block held in 8 bits.  Elements are E4M3 numbers (sign, 4 bits of exponent with bias 7, 3 of mantissa:
+ * up to 448, 127 is NaN), which share a power of two 2^e, stored as the byte e + 127, over a block of 32 consecutive rows of one
+ * head (rows 32 i .. 32 i + 31; -117 <= e <= 119).
+ *   k, v             [B][kv_heads][capacity][Dh] bytes
+ *   k_scale, v_scale [B][kv_heads][ceil(capacity / 32)] bytes
+ * Everything else as in fvar_kvq (the scales need no alignment). */
+typedef struct {
+    void *k, *v;
+    void *k_scale, *v_scale;
+    const int32_t *lens;
+    const uint8_t *mask;
+    int32_t kv_heads;
+    int32_t capacity;
+    int32_t len;
+} fvar_kvb;
+
+/* Rotary positions.  The first `dim` elements of every head are `axes` parts of P = dim / axes elements; part a is turned by
+ * component a of the row's position p:
+ *   (x, y) -> magnitude * (x cos - y sin, x sin + y cos) by the angle 2 pi p turns[i],  i < P / 2 the pair:
+ * elements i and i + P / 2 of the part, or 2 i and 2 i + 1 where interleaved.  fvar_rope_init fills in turns (and magnitude, where
+ * it is 0, as 1) from the other fields; a program with frequencies of its own may write turns itself. */
+typedef enum { FVAR_ROPE_NONE = 0, FVAR_ROPE_LINEAR = 1, FVAR_ROPE_NTK = 2, FVAR_ROPE_YARN = 3 } fvar_rope_scaling;
+typedef struct {
+    int32_t dim;           /* a multiple of 16 * axes, at most head_dim; elements from dim on are not turned */
+    int32_t axes;          /* 1, or 2 for rows of a token map */
+    int32_t interleaved;   /* 0 or 1 */
+    int32_t scaling;       /* fvar_rope_scaling */
+    double base;           /* > 1; the angle per position of pair i is f_i = base^(-2 i / P) */
+    double factor;         /* s >= 1, how much longer than trained.  LINEAR: f_i / s.  NTK: base * s^(P / (P - 2)), P > 2. */
+    double original;       /* YARN: positions trained on.  r_i = original * f_i / (2 pi), g_i = clamp((r_i - low) / (high - low), 0, 1): */
+    double low, high;      /*       f_i * (g_i + (1 - g_i) / s); low < high */
+    double magnitude;      /* factor of the results (YARN: 0.1 ln s + 1 is usual); 0 stands for 1 */
+    double turns[64];      /* f_i / (2 pi), i < P / 2 */
+} fvar_rope;
 
 typedef struct fvar_ctx fvar_ctx;
 typedef void *fvar_stream;
@@ -329,12 +368,65 @@ fvar_status fvar_block_forward_pruned_kvq(fvar_ctx *ctx, fvar_stream stream, con
                                           int32_t B, int32_t M, const int32_t *idx_keep, int32_t k, const fvar_kvq *kv,
                                           void *y_keep, void *ws, size_t ws_bytes);
 
+/* Fills in r->turns from the other fields.  Host-only work, for a program to do once. */
+fvar_status fvar_rope_init(fvar_rope *r);
+/* Turns queries and keys by their positions, pos: device int32 [B][n][axes] (any values, also negative ones).
+ * q: row i of sample b starts at element (b*n + i)*ld_q and holds [heads][Dh]; k likewise with ld_k and [kv_heads][Dh].  Either may
+ * be NULL.  The results go to q_out and k_out in the same way with their own ld_*_out, whole rows of a head, the elements from dim
+ * on as they are; an output is the input itself (with the same ld) or shares no memory with an input.  ld = 0 stands for a
+ * packed row; a multiple of 8 for bf16 (of 4 for fp32).  kv_heads divides the context's heads.  Angles are exact to 2^-50 of a turn per position,
+ * sines and cosines and the products are fp32.  B * n <= 2^24.  No workspace. */
+fvar_status fvar_rope_apply(fvar_ctx *ctx, fvar_stream stream, const fvar_rope *r, const int32_t *pos, int32_t B, int32_t n,
+                            int32_t kv_heads, const void *q, int32_t ld_q, const void *k, int32_t ld_k, void *q_out, int32_t ld_q_out,
+                            void *k_out, int32_t ld_k_out);
+
+/* The 8-bit cache (fvar_kvb).  A block's power is the smallest that serves what the block holds:
+ *   e = the smallest integer within [-117, 119] for which max |x| <= 464 * 2^e over the finite elements;
+ *   each element becomes the nearest value of the format times 2^e, ties to the even code, at most 448 * 2^e; what is not finite reads
+ *   back as NaN and does not count for e.
+ * No element is then further off than half a step of its binade (or 2^(e-10) near 0; beyond 464 * 2^119 values are cut off).
+ * fvar_kvb_append writes rows behind those that each sample holds, as fvar_kvq_append does.  Where rows come into a block that holds some
+ * already, e is the larger of theirs and the block's, and where that raises it, the rows held are rounded once more, to the new e.
+ * fvar_kvb_read is fvar_kvq_read for this cache. */
+fvar_status fvar_kvb_append(fvar_ctx *ctx, fvar_stream stream, const fvar_kvb *kv, const void *k, const void *v,
+                            int32_t ld, int32_t B, int32_t rows);
+fvar_status fvar_kvb_read(fvar_ctx *ctx, fvar_stream stream, const fvar_kvb *kv, int32_t B, int32_t first, int32_t rows,
+                          void *k, void *v);
+
+/* Attention over the 8-bit cache, as fvar_kvq_attention over one of 4 bits.  Scores and sums are fp32, queries count with all their
+ * bits.  Beside far larger values small ones may count as 0: those of 2^-37 (fp32: 2^-180) and less of the largest value of the
+ * blocks with a visible row, of the sample and kv head.
+ * weights: NULL, or fp32 [B][kv_heads][capacity], 16-byte aligned: of every row that a sample holds, the sum of p_t over the queries and
+ * the query heads that read it, 0 for a hidden one; add != 0: added to what is there.  Rows not held are left as they are.  A query whose
+ * weights are not numbers adds none.
+ * ws: at least fvar_kvb_attention_workspace_bytes(ctx,kv,B,n,weights != NULL). */
+size_t fvar_kvb_attention_workspace_bytes(const fvar_ctx *ctx, const fvar_kvb *kv, int32_t B, int32_t n, int32_t weights);
+fvar_status fvar_kvb_attention(fvar_ctx *ctx, fvar_stream stream, const void *q, int32_t ld, const fvar_kvb *kv, int32_t B,
+                               int32_t n, void *o, float *weights, int32_t add, void *ws, size_t ws_bytes);
+
+/* Eviction: of the rows that a sample holds and that from->mask does not hide, `keep` stay for every kv head (all of them, where they are
+ * not more): the last `recent` of all the rows that the sample holds, and of the others those with the largest weights, equal ones from the
+ * lowest row on (a weight that is not a number counts as larger than all numbers).  They move to the front in their order, the blocks' powers
+ * are chosen anew as above, and keys stay turned by the positions they had.
+ * weights: [B][kv_heads][from->capacity] as fvar_kvb_attention leaves them.
+ * to: the cache that receives the rows; its lens, mask and len are not read.  It has from's kv_heads, and is from's own memory throughout (all
+ * four pointers and the capacity), or shares none with it; to->capacity >= keep.
+ * to_weights: [B][kv_heads][to->capacity], receives the weights of the rows kept and 0 behind them; it may be `weights` itself
+ * where the caches are one, and shares no memory with it otherwise.  to_lens: int32 [B], receives the rows that each sample then
+ * holds, the same for all its heads (NULL allowed; may be from->lens).  idx: int32 [B][kv_heads][keep], receives the rows' former
+ * places, -1 behind them (NULL allowed).  No row of `to` is hidden: the mask ends here.
+ * 1 <= keep, 0 <= recent <= keep.  ws: at least fvar_kvb_evict_workspace_bytes(ctx,from,B,keep), whether idx is given or not. */
+size_t fvar_kvb_evict_workspace_bytes(const fvar_ctx *ctx, const fvar_kvb *from, int32_t B, int32_t keep);
+fvar_status fvar_kvb_evict(fvar_ctx *ctx, fvar_stream stream, const fvar_kvb *from, const float *weights, int32_t B, int32_t keep,
+                           int32_t recent, const fvar_kvb *to, float *to_weights, int32_t *to_lens, int32_t *idx, void *ws,
+                           size_t ws_bytes);
+
 /* Debug checks, off by default.  While on, fvar_block_forward_pruned, fvar_lowrank_fill and
  * fvar_cache_fill copy their index arrays to the host and verify the contract (in range,
  * strictly ascending per sample, idx_keep and idx_drop disjoint, hence a partition of [0,M));
  * a violation returns FVAR_ERR_INVALID_ARG with nothing launched.  The block calls also put a
  * 256-byte canary behind their workspace (fvar_block_workspace_bytes grows by that much while
- * the checks are on) and return FVAR_ERR_WORKSPACE if a kernel overwrote it.  Calls with a 4-bit cache that
+ * the checks are on) and return FVAR_ERR_WORKSPACE if a kernel overwrote it.  Calls with a 4-bit or 8-bit cache that
  * has lens copy them to the host and return FVAR_ERR_INVALID_ARG where one is negative or where it, with the rows that
  * the call appends, exceeds the capacity.  Calls made with
  * the checks on synchronise the stream and are not asynchronous. */

@@ -26,6 +26,8 @@ EXPORTS = (
     "fvar_fill_scored_workspace_bytes", "fvar_lowrank_fill_scored",
     "fvar_kvq_append", "fvar_kvq_read", "fvar_kvq_attention_workspace_bytes", "fvar_kvq_attention",
     "fvar_block_kvq_workspace_bytes", "fvar_block_forward_dense_kvq", "fvar_block_forward_pruned_kvq",
+    "fvar_rope_init", "fvar_rope_apply", "fvar_kvb_append", "fvar_kvb_read", "fvar_kvb_attention_workspace_bytes",
+    "fvar_kvb_attention", "fvar_kvb_evict_workspace_bytes", "fvar_kvb_evict",
 )
 
 
@@ -56,6 +58,16 @@ class _KVQ(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("lens", C.c_void_p), ("mask", C.c_void_p), ("kv_heads", C.c_int32), ("capacity", C.c_int32),
                 ("len", C.c_int32)]
+
+
+class _KVB(C.Structure):
+    _fields_ = _KVQ._fields_
+
+
+class _Rope(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("axes", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("original", C.c_double), ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double),
+                ("turns", C.c_double * 64)]
 
 
 class _ProfileEntry(C.Structure):
@@ -136,6 +148,23 @@ def load_library() -> C.CDLL:
     lib.fvar_block_forward_dense_kvq.restype = C.c_int
     lib.fvar_block_forward_pruned_kvq.argtypes = [vp, vp, C.POINTER(_Weights), vp, i32, i32, vp, i32, kvq, vp, vp, sz]
     lib.fvar_block_forward_pruned_kvq.restype = C.c_int
+    rope, kvb = C.POINTER(_Rope), C.POINTER(_KVB)
+    lib.fvar_rope_init.argtypes = [rope]
+    lib.fvar_rope_init.restype = C.c_int
+    lib.fvar_rope_apply.argtypes = [vp, vp, rope, vp, i32, i32, i32, vp, i32, vp, i32, vp, i32, vp, i32]
+    lib.fvar_rope_apply.restype = C.c_int
+    lib.fvar_kvb_append.argtypes = [vp, vp, kvb, vp, vp, i32, i32, i32]
+    lib.fvar_kvb_append.restype = C.c_int
+    lib.fvar_kvb_read.argtypes = [vp, vp, kvb, i32, i32, i32, vp, vp]
+    lib.fvar_kvb_read.restype = C.c_int
+    lib.fvar_kvb_attention_workspace_bytes.argtypes = [vp, kvb, i32, i32, i32]
+    lib.fvar_kvb_attention_workspace_bytes.restype = sz
+    lib.fvar_kvb_attention.argtypes = [vp, vp, vp, i32, kvb, i32, i32, vp, vp, i32, vp, sz]
+    lib.fvar_kvb_attention.restype = C.c_int
+    lib.fvar_kvb_evict_workspace_bytes.argtypes = [vp, kvb, i32, i32]
+    lib.fvar_kvb_evict_workspace_bytes.restype = sz
+    lib.fvar_kvb_evict.argtypes = [vp, vp, kvb, vp, i32, i32, i32, kvb, vp, vp, vp, vp, sz]
+    lib.fvar_kvb_evict.restype = C.c_int
     lib.fvar_profile_enable.argtypes = [vp, i32]
     lib.fvar_profile_enable.restype = C.c_int
     lib.fvar_profile_read.argtypes = [vp, C.POINTER(_ProfileEntry), i32]
@@ -324,23 +353,14 @@ def fvar_upsample_tokens(ctx: Context, src, B: int, hs: int, ws: int, c: int, hd
                                            wd, _ptr(dst)))
 
 
-class KVQ:
-    """Key/value cache of one block in 4 bits: the tensors of fvar_kvq and the rows that it holds.
+class _Cache:
+    """What KVQ and KVB have in common: the tensors of a cache, which its C structure points to, and the rows that it holds."""
 
-    k, v: uint8 [B, kv_heads, capacity, head_dim / 2]; k_scale, v_scale: uint8 [B, kv_heads, capacity, head_dim / 32];
-    lens: int32 [B] on the GPU, or None where every sample holds `len` rows; mask: uint8 or bool [B, capacity], 0 hides a
-    row from the attention, or None.  The tensors and `len` may be assigned to, tensors of the same shape; they are the caller's,
-    who advances len or lens."""
-
-    def __init__(self, k, v, k_scale, v_scale, len: int = 0, lens=None, mask=None):
-        B, heads, capacity, codes = k.shape
-        self._shapes = {"k": (B, heads, capacity, codes), "v": (B, heads, capacity, codes),
-                        "k_scale": (B, heads, capacity, codes // 16), "v_scale": (B, heads, capacity, codes // 16),
-                        "lens": (B,), "mask": (B, capacity)}
-        self._tensors = {}
-        self._c = _KVQ(kv_heads=heads, capacity=capacity, len=len)
-        self._ref, self._batch, self._head_dim = C.byref(self._c), B, 2 * codes
-        for name, t in (("k", k), ("v", v), ("k_scale", k_scale), ("v_scale", v_scale), ("lens", lens), ("mask", mask)):
+    def _set_up(self, c, shapes: dict, head_dim: int, tensors: dict) -> None:
+        self._shapes, self._tensors = shapes, {}
+        self._c = c
+        self._ref, self._batch, self._head_dim = C.byref(c), shapes["lens"][0], head_dim
+        for name, t in tensors.items():
             self._hold(name, t)
 
     def _hold(self, name: str, t) -> None:
@@ -380,6 +400,34 @@ class KVQ:
             raise ValueError(f"a cache of {self.batch} samples with head_dim {self.head_dim} does not serve {B} samples "
                              f"with head_dim {ctx.head_dim}")
         return self._ref
+
+
+class KVQ(_Cache):
+    """Key/value cache of one block in 4 bits: the tensors of fvar_kvq and the rows that it holds.
+
+    k, v: uint8 [B, kv_heads, capacity, head_dim / 2]; k_scale, v_scale: uint8 [B, kv_heads, capacity, head_dim / 32];
+    lens: int32 [B] on the GPU, or None where every sample holds `len` rows; mask: uint8 or bool [B, capacity], 0 hides a
+    row from the attention, or None.  The tensors and `len` may be assigned to, tensors of the same shape; they are the caller's,
+    who advances len or lens."""
+
+    def __init__(self, k, v, k_scale, v_scale, len: int = 0, lens=None, mask=None):
+        B, heads, capacity, codes = k.shape
+        held, scales = (B, heads, capacity, codes), (B, heads, capacity, codes // 16)
+        self._set_up(_KVQ(kv_heads=heads, capacity=capacity, len=len),
+                     {"k": held, "v": held, "k_scale": scales, "v_scale": scales, "lens": (B,), "mask": (B, capacity)}, 2 * codes,
+                     {"k": k, "v": v, "k_scale": k_scale, "v_scale": v_scale, "lens": lens, "mask": mask})
+
+
+class KVB(_Cache):
+    """Key/value cache of one block in 8 bits: the tensors of fvar_kvb and the rows that it holds, as KVQ but for
+    k, v: uint8 [B, kv_heads, capacity, head_dim]; k_scale, v_scale: uint8 [B, kv_heads, ceil(capacity / 32)]."""
+
+    def __init__(self, k, v, k_scale, v_scale, len: int = 0, lens=None, mask=None):
+        B, heads, capacity, head_dim = k.shape
+        held, scales = (B, heads, capacity, head_dim), (B, heads, (capacity + 31) // 32)
+        self._set_up(_KVB(kv_heads=heads, capacity=capacity, len=len),
+                     {"k": held, "v": held, "k_scale": scales, "v_scale": scales, "lens": (B,), "mask": (B, capacity)}, head_dim,
+                     {"k": k, "v": v, "k_scale": k_scale, "v_scale": v_scale, "lens": lens, "mask": mask})
 
 
 _KINDS: dict = {}                                             # element types by the contexts' names for them
@@ -476,6 +524,81 @@ def fvar_block_forward_pruned_kvq(ctx: Context, w: dict, x, B: int, M: int, idx_
     ctx.check(ctx.lib.fvar_block_forward_pruned_kvq(ctx.handle, _stream(stream), C.byref(ws_), xp, B, M,
                                                     _packed(idx_keep, _kind("i32"), B, k, 1), k, kv._for(ctx, B), yp, _ptr(ws),
                                                     _nbytes(ws)))
+
+
+class Rope:
+    """Rotary positions of a model, see fvar_rope.  scaling: "none", "linear", "ntk" or "yarn"; turns: frequencies of the caller's own, in
+    turns per position, for each pair of a part."""
+
+    def __init__(self, dim: int, interleaved: bool = False, axes: int = 1, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                 original: float = 0.0, low: float = 1.0, high: float = 32.0, magnitude: float = 0.0, turns: Optional[Sequence[float]] = None):
+        self._c = _Rope(dim, axes, 1 if interleaved else 0, {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}[scaling], base, factor, original,
+                        low, high, magnitude)
+        st = load_library().fvar_rope_init(C.byref(self._c))
+        if st != FVAR_OK:
+            raise FvarError(st, "fvar_rope_init: " + load_library().fvar_status_string(st).decode())
+        if turns is not None:
+            if len(turns) != dim // axes // 2:
+                raise ValueError(f"{dim // axes // 2} frequencies are wanted, got {len(turns)}")
+            self._c.turns[:len(turns)] = list(turns)
+        self._ref = C.byref(self._c)
+
+    axes = property(lambda self: self._c.axes)
+    dim = property(lambda self: self._c.dim)
+    turns = property(lambda self: list(self._c.turns[:self._c.dim // self._c.axes // 2]))
+
+
+def fvar_rope_apply(ctx: Context, rope: Rope, pos, B: int, n: int, q=None, k=None, q_out=None, k_out=None, stream=None) -> None:
+    """q: [B, n, heads, head_dim], k: [B, n, kv_heads, head_dim]; either may be None.  Rows may lie apart, as the parts of a fused
+    projection's output do; without an output the rows are turned in place."""
+    kind, kv_heads = _kind(ctx.dtype), ctx.heads if k is None else k.numel() // (B * n * ctx.head_dim)
+    (qp, ldq), (kp, ldk) = _rows(q, kind, B, n, ctx.hidden), _rows(k, kind, B, n, kv_heads * ctx.head_dim)
+    (qo, ldqo) = (qp, ldq) if q_out is None else _rows(q_out, kind, B, n, ctx.hidden)
+    (ko, ldko) = (kp, ldk) if k_out is None else _rows(k_out, kind, B, n, kv_heads * ctx.head_dim)
+    ctx.check(ctx.lib.fvar_rope_apply(ctx.handle, _stream(stream), rope._ref, _packed(pos, _kind("i32"), B, n, rope.axes), B, n, kv_heads,
+                                      qp, ldq, kp, ldk, qo, ldqo, ko, ldko))
+
+
+def fvar_kvb_append(ctx: Context, kv: KVB, k, v, B: int, rows: int, stream=None) -> None:
+    kind, width = _kind(ctx.dtype), kv._c.kv_heads * ctx.head_dim
+    (kp, ldk), (vp, ldv) = _rows(k, kind, B, rows, width), _rows(v, kind, B, rows, width)
+    if (ldk or width) != (ldv or width):
+        raise ValueError("k and v have different distances between rows")
+    ctx.check(ctx.lib.fvar_kvb_append(ctx.handle, _stream(stream), kv._for(ctx, B), kp, vp, ldk, B, rows))
+
+
+def fvar_kvb_read(ctx: Context, kv: KVB, B: int, first: int, rows: int, k=None, v=None, stream=None) -> None:
+    kind, width = _kind(ctx.dtype), kv._c.kv_heads * ctx.head_dim
+    kp, vp = _packed(k, kind, B, rows, width), _packed(v, kind, B, rows, width)
+    ctx.check(ctx.lib.fvar_kvb_read(ctx.handle, _stream(stream), kv._for(ctx, B), B, first, rows, kp, vp))
+
+
+def fvar_kvb_attention_workspace_bytes(ctx: Context, kv: KVB, B: int, n: int, weights: bool = False) -> int:
+    return ctx.lib.fvar_kvb_attention_workspace_bytes(ctx.handle, kv._for(ctx, B), B, n, 1 if weights else 0)
+
+
+def _row_weights(t, kv: KVB, B: int) -> Optional[int]:
+    """Pointer of contiguous fp32 [B, kv_heads, capacity] (None passes NULL)."""
+    return _packed(t, _kind("f32"), B, kv.kv_heads * kv.capacity, 1)
+
+
+def fvar_kvb_attention(ctx: Context, q, kv: KVB, B: int, n: int, o, ws=None, weights=None, add: bool = False, stream=None) -> None:
+    kind = _kind(ctx.dtype)
+    qp, ld = _rows(q, kind, B, n, ctx.hidden)
+    op = _packed(o, kind, B, n, ctx.hidden)
+    ctx.check(ctx.lib.fvar_kvb_attention(ctx.handle, _stream(stream), qp, ld, kv._for(ctx, B), B, n, op, _row_weights(weights, kv, B),
+                                         1 if add else 0, _ptr(ws), _nbytes(ws)))
+
+
+def fvar_kvb_evict_workspace_bytes(ctx: Context, kv: KVB, B: int, keep: int) -> int:
+    return ctx.lib.fvar_kvb_evict_workspace_bytes(ctx.handle, kv._for(ctx, B), B, keep)
+
+
+def fvar_kvb_evict(ctx: Context, kv: KVB, weights, B: int, keep: int, recent: int, to: KVB, to_weights, to_lens=None, idx=None, ws=None,
+                   stream=None) -> None:
+    ctx.check(ctx.lib.fvar_kvb_evict(ctx.handle, _stream(stream), kv._for(ctx, B), _row_weights(weights, kv, B), B, keep, recent,
+                                     to._for(ctx, B), _row_weights(to_weights, to, B), _packed(to_lens, _kind("i32"), B, 1, 1),
+                                     _packed(idx, _kind("i32"), B, kv.kv_heads * keep, 1), _ptr(ws), _nbytes(ws)))
 
 
 def fvar_profile_enable(ctx: Context, on: bool) -> None:

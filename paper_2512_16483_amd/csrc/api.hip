@@ -7,6 +7,7 @@
 #include <map>
 #include <mutex>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/fvar.h"
@@ -184,14 +185,16 @@ BlockWs carve(const fvar_ctx *c, void *ws, int B, int rows, const fvar_kvq *q = 
     return w;
 }
 
-// A 4-bit cache that a call with `rows` new rows per sample can work on (0: none are written).
-fvar_status check_kvq(fvar_ctx *c, hipStream_t st, const fvar_kvq *kv, int B, int rows, const char *who)
+// A 4-bit or 8-bit cache that a call with `rows` new rows per sample can work on (0: none are written).
+template <typename Cache>
+fvar_status check_cache(fvar_ctx *c, hipStream_t st, const Cache *kv, int B, int rows, const char *who)
 {
+    constexpr bool wide_scales = std::is_same<Cache, fvar_kvq>::value;   // read several at a time
     if (!kv) return fail(c, FVAR_ERR_INVALID_ARG, "%s: null cache", who);
     if (B < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need B>=1 (B=%d)", who, B);
     if (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: a pointer of the cache is NULL", who);
-    if (!aligned16(kv->k) || !aligned16(kv->v) || !aligned16(kv->k_scale) || !aligned16(kv->v_scale) ||
+    if (!aligned16(kv->k) || !aligned16(kv->v) || (wide_scales && (!aligned16(kv->k_scale) || !aligned16(kv->v_scale))) ||
         (reinterpret_cast<uintptr_t>(kv->lens) & 3))
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer of the cache not aligned (16 bytes; lens 4)", who);
     if (kv->kv_heads < 1 || c->cfg.heads % kv->kv_heads)
@@ -214,6 +217,12 @@ fvar_status check_kvq(fvar_ctx *c, hipStream_t st, const fvar_kvq *kv, int B, in
     return FVAR_OK;
 }
 
+fvar::KvbCache kvb_cache(const fvar_kvb *kv)
+{
+    return {(uint8_t *)kv->k, (uint8_t *)kv->v, (uint8_t *)kv->k_scale, (uint8_t *)kv->v_scale, kv->lens, kv->mask,
+            kv->kv_heads, kv->capacity, kv->len};
+}
+
 fvar::KvqCache kvq_cache(const fvar_kvq *kv)
 {
     return {(uint8_t *)kv->k, (uint8_t *)kv->v, (uint8_t *)kv->k_scale, (uint8_t *)kv->v_scale, kv->lens, kv->mask,
@@ -229,7 +238,7 @@ int row_pitch(const fvar_ctx *c, int ld, int row)
 }
 
 // Whether the sizes are some that workspace can be computed for: those that the calls accept.
-bool kvq_sizes(const fvar_ctx *c, const fvar_kvq *kv, int B, int n)
+template <typename Cache> bool cache_sizes(const fvar_ctx *c, const Cache *kv, int B, int n)
 {
     return kv && B >= 1 && n >= 1 && kv->kv_heads >= 1 && c->cfg.heads % kv->kv_heads == 0 && kv->capacity >= 1 &&
            kv->capacity <= 1 << 24 && (int64_t)B * kv->kv_heads <= 65535 && (int64_t)B * n <= (1 << 25) / c->cfg.heads;
@@ -239,6 +248,18 @@ size_t kvq_attention_ws(const fvar_ctx *c, const fvar_kvq *kv, int B, int n)
 {
     return align256(fvar::kvq_attention_scratch_floats(dtype(c), B, n, c->cfg.heads, kv->kv_heads, c->cfg.head_dim,
                                                        kv->capacity) * sizeof(float));
+}
+
+size_t kvb_attention_ws(const fvar_ctx *c, const fvar_kvb *kv, int B, int n, bool weights)
+{
+    return align256(fvar::kvb_attention_scratch_floats(dtype(c), B, n, c->cfg.heads, kv->kv_heads, c->cfg.head_dim, kv->capacity,
+                                                       weights) * sizeof(float));
+}
+
+bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + nb && y < x + na;
 }
 
 // The block on `rows` rows per sample, over one of two kinds of cache (the other is null).
@@ -256,7 +277,7 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
     if (!w->w_qkv || !w->w_o || !w->w_fc1 || !w->w_fc2)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: weight matrix pointer is NULL", who);
     if (kvq) {
-        const fvar_status ks = check_kvq(c, st, kvq, B, rows, who);
+        const fvar_status ks = check_cache(c, st, kvq, B, rows, who);
         if (ks != FVAR_OK) return ks;
         if (kvq->kv_heads != c->cfg.heads)
             return fail(c, FVAR_ERR_UNSUPPORTED, "%s: kv_heads=%d, and the block has %d heads of keys", who, kvq->kv_heads,
@@ -576,7 +597,7 @@ fvar_status fvar_block_forward_pruned_kvq(fvar_ctx *c, fvar_stream stream, const
 
 size_t fvar_block_kvq_workspace_bytes(const fvar_ctx *c, const fvar_kvq *kv, int32_t B, int32_t rows)
 {
-    if (!c || !kvq_sizes(c, kv, B, rows)) return 0;
+    if (!c || !cache_sizes(c, kv, B, rows)) return 0;
     return carve(c, nullptr, B, rows, kv).total + (c->debug_checks ? kCanaryBytes : 0);
 }
 
@@ -587,7 +608,7 @@ fvar_status fvar_kvq_append(fvar_ctx *c, fvar_stream stream, const fvar_kvq *kv,
     const char *who = "fvar_kvq_append";
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (rows < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need rows>=1 (rows=%d)", who, rows);
-    const fvar_status ks = check_kvq(c, st, kv, B, rows, who);
+    const fvar_status ks = check_cache(c, st, kv, B, rows, who);
     if (ks != FVAR_OK) return ks;
     if (!k || !v) return fail(c, FVAR_ERR_INVALID_ARG, "%s: k or v is NULL", who);
     if (!aligned16(k) || !aligned16(v)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
@@ -607,7 +628,7 @@ fvar_status fvar_kvq_read(fvar_ctx *c, fvar_stream stream, const fvar_kvq *kv, i
     if (!c) return FVAR_ERR_INVALID_ARG;
     const char *who = "fvar_kvq_read";
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const fvar_status ks = check_kvq(c, st, kv, B, 0, who);
+    const fvar_status ks = check_cache(c, st, kv, B, 0, who);
     if (ks != FVAR_OK) return ks;
     if (!k && !v) return fail(c, FVAR_ERR_INVALID_ARG, "%s: k and v both NULL", who);
     if (!aligned16(k) || !aligned16(v)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
@@ -622,7 +643,7 @@ fvar_status fvar_kvq_read(fvar_ctx *c, fvar_stream stream, const fvar_kvq *kv, i
 
 size_t fvar_kvq_attention_workspace_bytes(const fvar_ctx *c, const fvar_kvq *kv, int32_t B, int32_t n)
 {
-    if (!c || !kvq_sizes(c, kv, B, n)) return 0;
+    if (!c || !cache_sizes(c, kv, B, n)) return 0;
     return kvq_attention_ws(c, kv, B, n);
 }
 
@@ -633,7 +654,7 @@ fvar_status fvar_kvq_attention(fvar_ctx *c, fvar_stream stream, const void *q, i
     const char *who = "fvar_kvq_attention";
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (n < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need n>=1 (n=%d)", who, n);
-    const fvar_status ks = check_kvq(c, st, kv, B, 0, who);
+    const fvar_status ks = check_cache(c, st, kv, B, 0, who);
     if (ks != FVAR_OK) return ks;
     if (!q || !o) return fail(c, FVAR_ERR_INVALID_ARG, "%s: q or o is NULL", who);
     if (!aligned16(q) || !aligned16(o) || !aligned16(ws))
@@ -649,6 +670,195 @@ fvar_status fvar_kvq_attention(fvar_ctx *c, fvar_stream stream, const void *q, i
     timed(c, st, "kvq_attention", [&] {
         fvar::launch_kvq_attention(dtype(c), q, pitch, kvq_cache(kv), 0, B, n, c->cfg.heads, c->cfg.head_dim, c->scale, o,
                                    (float *)ws, st);
+    });
+    return launch_status(c, who);
+}
+
+fvar_status fvar_rope_init(fvar_rope *r)
+{
+    if (!r || r->axes < 1 || r->axes > 2 || r->dim < 1 || r->dim > 128 || r->dim % (16 * r->axes)) return FVAR_ERR_INVALID_ARG;
+    if (r->scaling < FVAR_ROPE_NONE || r->scaling > FVAR_ROPE_YARN || !(r->base > 1.0) || !std::isfinite(r->base) ||
+        !std::isfinite(r->magnitude))
+        return FVAR_ERR_INVALID_ARG;
+    if (r->scaling != FVAR_ROPE_NONE && (!(r->factor >= 1.0) || !std::isfinite(r->factor))) return FVAR_ERR_INVALID_ARG;
+    if (r->scaling == FVAR_ROPE_YARN && (!(r->original > 0.0) || !(r->low < r->high) || !std::isfinite(r->original) ||
+                                         !std::isfinite(r->low) || !std::isfinite(r->high)))
+        return FVAR_ERR_INVALID_ARG;
+    const double two_pi = 6.283185307179586476925;
+    const int P = r->dim / r->axes;
+    const double base = r->scaling == FVAR_ROPE_NTK ? r->base * std::pow(r->factor, (double)P / (P - 2)) : r->base;
+    if (r->magnitude == 0.0) r->magnitude = 1.0;
+    for (int i = 0; i < 64; ++i) {
+        double f = i < P / 2 ? std::pow(base, -2.0 * i / P) : 0.0;
+        if (r->scaling == FVAR_ROPE_LINEAR) f /= r->factor;
+        if (r->scaling == FVAR_ROPE_YARN) {
+            double g = (r->original * f / two_pi - r->low) / (r->high - r->low);
+            g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
+            f *= g + (1.0 - g) / r->factor;
+        }
+        r->turns[i] = f / two_pi;
+    }
+    return FVAR_OK;
+}
+
+fvar_status fvar_rope_apply(fvar_ctx *c, fvar_stream stream, const fvar_rope *r, const int32_t *pos, int32_t B, int32_t n,
+                            int32_t kv_heads, const void *q, int32_t ld_q, const void *k, int32_t ld_k, void *q_out, int32_t ld_q_out,
+                            void *k_out, int32_t ld_k_out)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    const char *who = "fvar_rope_apply";
+    if (!r || !pos) return fail(c, FVAR_ERR_INVALID_ARG, "%s: null argument", who);
+    if (B < 1 || n < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need B>=1 and n>=1 (B=%d n=%d)", who, B, n);
+    if ((int64_t)B * n > (1 << 24)) return fail(c, FVAR_ERR_UNSUPPORTED, "%s: B*n exceeds 2^24", who);
+    if (r->axes < 1 || r->axes > 2 || r->dim < 1 || r->dim > c->cfg.head_dim || r->dim % (16 * r->axes))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: dim=%d with axes=%d: a multiple of 16*axes up to head_dim is wanted", who, r->dim, r->axes);
+    if (!q && !k) return fail(c, FVAR_ERR_INVALID_ARG, "%s: q and k both NULL", who);
+    if (!q != !q_out || !k != !k_out) return fail(c, FVAR_ERR_INVALID_ARG, "%s: an input without its output, or the reverse", who);
+    if (kv_heads < 1 || c->cfg.heads % kv_heads)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: kv_heads=%d does not divide heads=%d", who, kv_heads, c->cfg.heads);
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || (reinterpret_cast<uintptr_t>(pos) & 3))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not aligned (16 bytes; pos 4)", who);
+    const int wq = c->cfg.hidden, wk = kv_heads * c->cfg.head_dim;
+    const fvar::RopeRows rows[2] = {{q, q_out, q ? c->cfg.heads : 0, row_pitch(c, ld_q, wq), row_pitch(c, ld_q_out, wq)},
+                                    {k, k_out, k ? kv_heads : 0, row_pitch(c, ld_k, wk), row_pitch(c, ld_k_out, wk)}};
+    for (const fvar::RopeRows &x : rows)
+        if (x.in && (x.ld_in < 0 || x.ld_out < 0 || (x.in == x.out && x.ld_in != x.ld_out)))
+            return fail(c, FVAR_ERR_INVALID_ARG, "%s: a row pitch is shorter than a row, no multiple of 16 bytes, or in place not the same", who);
+    fvar::RopeTable t;
+    t.dim = r->dim;
+    t.axes = r->axes;
+    t.interleaved = r->interleaved != 0;
+    t.magnitude = (float)r->magnitude;
+    std::memcpy(t.turns, r->turns, sizeof(t.turns));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    timed(c, st, "rope", [&] { fvar::launch_rope(dtype(c), t, rows[0], rows[1], pos, B * n, c->cfg.head_dim, st); });
+    return launch_status(c, who);
+}
+
+fvar_status fvar_kvb_append(fvar_ctx *c, fvar_stream stream, const fvar_kvb *kv, const void *k, const void *v, int32_t ld,
+                            int32_t B, int32_t rows)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    const char *who = "fvar_kvb_append";
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rows < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need rows>=1 (rows=%d)", who, rows);
+    const fvar_status ks = check_cache(c, st, kv, B, rows, who);
+    if (ks != FVAR_OK) return ks;
+    if (!k || !v) return fail(c, FVAR_ERR_INVALID_ARG, "%s: k or v is NULL", who);
+    if (!aligned16(k) || !aligned16(v)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
+    if (rows > kv->capacity) return fail(c, FVAR_ERR_INVALID_ARG, "%s: rows=%d > capacity=%d", who, rows, kv->capacity);
+    const int pitch = row_pitch(c, ld, kv->kv_heads * c->cfg.head_dim);
+    if (pitch < 0)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: ld=%d is shorter than a row or no multiple of 16 bytes", who, ld);
+    timed(c, st, "kvb_append", [&] {
+        fvar::launch_kvb_append(dtype(c), k, v, pitch, kvb_cache(kv), B, rows, c->cfg.head_dim, st);
+    });
+    return launch_status(c, who);
+}
+
+fvar_status fvar_kvb_read(fvar_ctx *c, fvar_stream stream, const fvar_kvb *kv, int32_t B, int32_t first, int32_t rows,
+                          void *k, void *v)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    const char *who = "fvar_kvb_read";
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const fvar_status ks = check_cache(c, st, kv, B, 0, who);
+    if (ks != FVAR_OK) return ks;
+    if (!k && !v) return fail(c, FVAR_ERR_INVALID_ARG, "%s: k and v both NULL", who);
+    if (!aligned16(k) || !aligned16(v)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
+    if (rows < 1 || rows > kv->capacity || first < -kv->capacity || (int64_t)first + (first < 0 ? 0 : rows) > kv->capacity)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: rows [%d,+%d) are outside the capacity of %d", who, first, rows,
+                    kv->capacity);
+    timed(c, st, "kvb_read", [&] {
+        fvar::launch_kvb_read(dtype(c), kvb_cache(kv), B, first, rows, c->cfg.head_dim, k, v, st);
+    });
+    return launch_status(c, who);
+}
+
+size_t fvar_kvb_attention_workspace_bytes(const fvar_ctx *c, const fvar_kvb *kv, int32_t B, int32_t n, int32_t weights)
+{
+    if (!c || !cache_sizes(c, kv, B, n)) return 0;
+    return kvb_attention_ws(c, kv, B, n, weights != 0);
+}
+
+fvar_status fvar_kvb_attention(fvar_ctx *c, fvar_stream stream, const void *q, int32_t ld, const fvar_kvb *kv, int32_t B,
+                               int32_t n, void *o, float *weights, int32_t add, void *ws, size_t ws_bytes)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    const char *who = "fvar_kvb_attention";
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (n < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need n>=1 (n=%d)", who, n);
+    const fvar_status ks = check_cache(c, st, kv, B, 0, who);
+    if (ks != FVAR_OK) return ks;
+    if (!q || !o) return fail(c, FVAR_ERR_INVALID_ARG, "%s: q or o is NULL", who);
+    if (!aligned16(q) || !aligned16(o) || !aligned16(weights) || !aligned16(ws))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
+    const int pitch = row_pitch(c, ld, c->cfg.hidden);
+    if (pitch < 0)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: ld=%d is shorter than a row or no multiple of 16 bytes", who, ld);
+    if ((int64_t)B * n * c->cfg.heads > (1 << 25))
+        return fail(c, FVAR_ERR_UNSUPPORTED, "%s: B*n*heads exceeds 2^25", who);
+    const size_t need = kvb_attention_ws(c, kv, B, n, weights != nullptr);
+    if (need && (!ws || ws_bytes < need))
+        return fail(c, FVAR_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, ws_bytes);
+    timed(c, st, "kvb_attention", [&] {
+        fvar::launch_kvb_attention(dtype(c), q, pitch, kvb_cache(kv), 0, B, n, c->cfg.heads, c->cfg.head_dim, c->scale, o, weights,
+                                   add != 0, (float *)ws, st);
+    });
+    return launch_status(c, who);
+}
+
+size_t fvar_kvb_evict_workspace_bytes(const fvar_ctx *c, const fvar_kvb *from, int32_t B, int32_t keep)
+{
+    if (!c || keep < 1 || keep > (1 << 24) || !cache_sizes(c, from, B, 1)) return 0;
+    return align256((size_t)B * sizeof(int32_t)) + align256((size_t)B * from->kv_heads * keep * sizeof(int32_t));
+}
+
+fvar_status fvar_kvb_evict(fvar_ctx *c, fvar_stream stream, const fvar_kvb *from, const float *weights, int32_t B, int32_t keep,
+                           int32_t recent, const fvar_kvb *to, float *to_weights, int32_t *to_lens, int32_t *idx, void *ws,
+                           size_t ws_bytes)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    const char *who = "fvar_kvb_evict";
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const fvar_status ks = check_cache(c, st, from, B, 0, who);
+    if (ks != FVAR_OK) return ks;
+    if (!to || !to->k || !to->v || !to->k_scale || !to->v_scale || !weights || !to_weights)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: null argument", who);
+    if (!aligned16(to->k) || !aligned16(to->v) || !aligned16(weights) || !aligned16(to_weights) || !aligned16(ws) ||
+        (reinterpret_cast<uintptr_t>(to_lens) & 3) || (reinterpret_cast<uintptr_t>(idx) & 3))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not aligned (16 bytes; to_lens and idx 4)", who);
+    if (to->kv_heads != from->kv_heads)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: caches of %d and %d kv heads", who, from->kv_heads, to->kv_heads);
+    if (keep < 1 || recent < 0 || recent > keep || keep > to->capacity)
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: need 0<=recent<=keep, 1<=keep<=capacity of the second cache (keep=%d recent=%d capacity=%d)",
+                    who, keep, recent, to->capacity);
+    if (to->capacity > (1 << 24)) return fail(c, FVAR_ERR_UNSUPPORTED, "%s: capacity exceeds 2^24", who);
+    {
+        const size_t heads = (size_t)B * from->kv_heads, Dh = c->cfg.head_dim;
+        const bool here = from->k == to->k;
+        const void *a[4] = {from->k, from->v, from->k_scale, from->v_scale}, *b[4] = {to->k, to->v, to->k_scale, to->v_scale};
+        for (int i = 0; i < 4; ++i) {
+            if (here && (a[i] != b[i] || from->capacity != to->capacity))
+                return fail(c, FVAR_ERR_INVALID_ARG, "%s: the caches are one in part", who);
+            for (int j = 0; j < 4 && !here; ++j) {
+                const size_t na = heads * (i < 2 ? from->capacity * Dh : (from->capacity + 31) / 32);
+                const size_t nb = heads * (j < 2 ? to->capacity * Dh : (to->capacity + 31) / 32);
+                if (overlap(a[i], na, b[j], nb)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: the caches share memory", who);
+            }
+        }
+        if (!(here && weights == to_weights) &&
+            overlap(weights, heads * from->capacity * sizeof(float), to_weights, heads * to->capacity * sizeof(float)))
+            return fail(c, FVAR_ERR_INVALID_ARG, "%s: weights and to_weights share memory", who);
+    }
+    const size_t need = fvar_kvb_evict_workspace_bytes(c, from, B, keep);
+    if (!ws || ws_bytes < need)
+        return fail(c, FVAR_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, ws_bytes);
+    int32_t *counts = static_cast<int32_t *>(ws);
+    int32_t *rows = idx ? idx : reinterpret_cast<int32_t *>(static_cast<char *>(ws) + align256((size_t)B * sizeof(int32_t)));
+    timed(c, st, "kvb_rank", [&] { fvar::launch_kvb_rank(kvb_cache(from), weights, B, keep, recent, rows, counts, st); });
+    timed(c, st, "kvb_move", [&] {
+        fvar::launch_kvb_move(kvb_cache(from), weights, kvb_cache(to), to_weights, to_lens, B, keep, c->cfg.head_dim, rows, counts, st);
     });
     return launch_status(c, who);
 }

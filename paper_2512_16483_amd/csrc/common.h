@@ -206,6 +206,37 @@ int kvq_attention_waves_per_simd(int bf16, int B, int n, int H, int heads, int D
 void launch_kvq_attention(DType dt, const void *q, int ld, const KvqCache &c, int extra, int B, int n, int H, int Dh,
                           float scale, void *o, float *part, hipStream_t st);
 
+// Rotary positions, see rope.hip.  turns: of each pair of a part, per position; in / out: null, or rows of [heads][Dh], ld elements apart.
+struct RopeTable { int dim, axes, interleaved; float magnitude; double turns[64]; };
+struct RopeRows { const void *in; void *out; int heads, ld_in, ld_out; };
+void launch_rope(DType dt, const RopeTable &r, const RopeRows &q, const RopeRows &k, const int32_t *pos, int rows, int Dh, hipStream_t st);
+
+// A cache held in 8 bits, see kvb.hip: codes [B][heads][capacity][Dh], scales [B][heads][blocks()].
+// lens: rows of each sample, or null and `len` for all; mask: [B][capacity], 0 hides a row from the attention, or null.
+constexpr int kKvbBlock = 32;              // rows that share a scale
+struct KvbCache {
+    uint8_t *k, *v, *k_scale, *v_scale;
+    const int32_t *lens;
+    const uint8_t *mask;
+    int heads, capacity, len;
+    __host__ __device__ __forceinline__ int blocks() const { return (capacity + kKvbBlock - 1) / kKvbBlock; }
+};
+// rows k, v:[B,rows,heads,Dh] (ld elements from one to the next) written to the cache behind each sample's rows; rows past the
+// capacity are left out
+void launch_kvb_append(DType dt, const void *k, const void *v, int ld, const KvbCache &c, int B, int rows, int Dh, hipStream_t st);
+// k, v:[B,rows,heads,Dh] or null: rows first.. of the cache (first < 0: from the end of each sample's); 0 outside them
+void launch_kvb_read(DType dt, const KvbCache &c, int B, int first, int rows, int Dh, void *k, void *v, hipStream_t st);
+// attention over the cache's rows and `extra` more, see kvb_attention.hip; q:[B,n,H,Dh], ld elements from one query to
+// the next; o:[B,n,H,Dh]; weights: null, or [B][heads][capacity] that receive (add: are increased by) each row's weight;
+// part: kvb_attention_scratch_floats() floats
+size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity, bool weights);
+void launch_kvb_attention(DType dt, const void *q, int ld, const KvbCache &c, int extra, int B, int n, int H, int Dh,
+                          float scale, void *o, float *weights, bool add, float *part, hipStream_t st);
+// eviction, see kvb_evict.hip; idx:[B][heads][keep], counts:[B]
+void launch_kvb_rank(const KvbCache &c, const float *weights, int B, int keep, int recent, int32_t *idx, int32_t *counts, hipStream_t st);
+void launch_kvb_move(const KvbCache &from, const float *weights, const KvbCache &to, float *to_weights, int32_t *to_lens, int B, int keep, int Dh,
+                     const int32_t *idx, const int32_t *counts, hipStream_t st);
+
 // y[b,idx_keep[b,j],:] = y_keep[b,j,:];  y[b,i,:] = w_c[b,i,:] g_c[b] for i in idx_drop[b,:]
 // parts / scores_out: null, or scratch of B*M*fill_score_parts() doubles and a [B*M] fp32 array that
 // receives the energy (sum of squares of the stored elements) of every row of y

@@ -1,0 +1,91 @@
+// Rotary positions: the first `dim` elements of every head are `axes` parts of P = dim / axes elements; pair i of a part is turned by the
+// angle p * f_i, p the part's component of the row's position and f_i the pair's entry of a table (in turns per position).
+//   (x, y) -> magnitude * (x cos - y sin, x sin + y cos);  pairs are (i, i + P / 2), or (2 i, 2 i + 1) where interleaved.
+//
+// An angle is the fraction of p * f_i in 64 bits (a position of 10^6 leaves 2^-4 of a turn's 32-bit fraction), sine and cosine of it in 32.
+#include "common.h"
+
+namespace fvar {
+
+// Sixteen elements of a head, eight pairs, per thread; T rows per workgroup.  The angles of the workgroup's rows are made once, in LDS, for all heads
+// of queries and keys: 64 of them serve 8192 elements of 32 + 32 heads of 128.  A thread keeps to its pairs and its row and goes from head to
+// head with them in registers.
+template <typename E, int DH, int T, bool INTER>
+__global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, RopeRows k, const int32_t *__restrict__ pos, int rows)
+{
+    constexpr int ITEMS = DH / 16, SLOTS = 256 / ITEMS / T, PER = Elem<E>::kPerChunk, HALF = 8 / PER;   // HALF: chunks of eight elements
+    __shared__ float2 turn[T][DH / 2];
+    const int tid = threadIdx.x, pairs = r.dim / 2, row0 = blockIdx.x * T;
+    for (int i = tid; i < T * pairs; i += 256) {
+        const int t = i / pairs, pair = i % pairs, each = pairs / r.axes, axis = pair / each;
+        const int row = min(row0 + t, rows - 1);
+        const double turns = pos[(size_t)row * r.axes + axis] * r.turns[pair % each];
+        const double angle = (turns - rint(turns)) * 6.283185307179586476925;
+        const float hi = (float)angle, lo = (float)(angle - hi);
+        float s, c;
+        sincosf(hi, &s, &c);
+        turn[t][pair] = make_float2(fmaf(-lo, s, c) * r.magnitude, fmaf(lo, c, s) * r.magnitude);
+    }
+    __syncthreads();
+    const int item = tid % ITEMS, t = tid / ITEMS % T, slot = tid / ITEMS / T + blockIdx.y * SLOTS, step = gridDim.y * SLOTS;
+    const size_t row = row0 + t;
+    if (row >= (size_t)rows) return;
+    const bool turned = item * 16 < r.dim;
+    float c[8], s[8];
+    int lo = item * 16, hi = item * 16 + 8;                  // the first of eight elements, and of eight more
+    if (turned) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { c[i] = turn[t][item * 8 + i].x; s[i] = turn[t][item * 8 + i].y; }
+        if (!INTER) {
+            const int part = r.dim / r.axes, each = part / 16, a = item / each;
+            lo = a * part + item % each * 8;
+            hi = lo + part / 2;
+        }
+    }
+    for (int h = slot; h < q.heads + k.heads; h += step) {
+        const bool is_q = h < q.heads;
+        const int head = is_q ? h : h - q.heads;
+        const E *src = (const E *)(is_q ? q.in : k.in) + row * (size_t)(is_q ? q.ld_in : k.ld_in) + head * DH;
+        E *dst = (E *)(is_q ? q.out : k.out) + row * (size_t)(is_q ? q.ld_out : k.ld_out) + head * DH;
+        if (!turned && src == dst) continue;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) {
+            Elem<E>::unpack(*reinterpret_cast<const uint4 *>(src + lo + i * PER), x + i * PER);
+            Elem<E>::unpack(*reinterpret_cast<const uint4 *>(src + hi + i * PER), x + 8 + i * PER);
+        }
+        if (turned) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int one = INTER ? 2 * i : i, two = INTER ? 2 * i + 1 : i + 8;
+                const float a = x[one], b = x[two];
+                x[one] = fmaf(a, c[i], -(b * s[i]));
+                x[two] = fmaf(a, s[i], b * c[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) {
+            *reinterpret_cast<uint4 *>(dst + lo + i * PER) = Elem<E>::pack(x + i * PER);
+            *reinterpret_cast<uint4 *>(dst + hi + i * PER) = Elem<E>::pack(x + 8 + i * PER);
+        }
+    }
+}
+
+void launch_rope(DType dt, const RopeTable &r, const RopeRows &q, const RopeRows &k, const int32_t *pos, int rows, int Dh, hipStream_t st)
+{
+#define FVAR_ROPE(E, DH, T)                                                                                              \
+    (r.interleaved ? launch(rope_kernel<E, DH, T, true>, dim3((unsigned)((rows + T - 1) / T)), dim3(256), 0, st, r, q, k, pos, rows) \
+                   : launch(rope_kernel<E, DH, T, false>, dim3((unsigned)((rows + T - 1) / T)), dim3(256), 0, st, r, q, k, pos, rows))
+#define FVAR_ROPE_T(E, DH) (rows >= 2048 ? FVAR_ROPE(E, DH, 4) : FVAR_ROPE(E, DH, 1))
+    if (dt == DType::BF16) {
+        if (Dh == 64) FVAR_ROPE_T(uint16_t, 64);
+        else FVAR_ROPE_T(uint16_t, 128);
+    } else {
+        if (Dh == 64) FVAR_ROPE_T(float, 64);
+        else FVAR_ROPE_T(float, 128);
+    }
+#undef FVAR_ROPE_T
+#undef FVAR_ROPE
+}
+
+}  // namespace fvar

@@ -13,7 +13,11 @@ namespace fvar {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef short shortx4_t __attribute__((ext_vector_type(4)));
+typedef int intx8_t __attribute__((ext_vector_type(8)));
+typedef unsigned uintx4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) const uintx4_t lds_uintx4_t;
 typedef __attribute__((address_space(3))) shortx4_t lds_shortx4_t;
+typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 
 // Values as fp16 operands: a value goes in as value * 2^(kTop - E), E the largest exponent of a tile seen so far and kRoom more (sums are
 // rescaled when a tile's exceeds E, which is seldom).  A value is at most 448, and fp16 numbers reach down to 2^-24, so tiles are exact
@@ -21,7 +25,7 @@ typedef __attribute__((address_space(3))) shortx4_t lds_shortx4_t;
 // maximum.  Next to bf16 operands the weights keep 11 bits, so that the output's own rounding is the only one of note.
 // fp32 takes values as they are in bf16, exact, up to tiles of 2^64, and at 2^64 over E from there on: a sum of weights up to 2^7 each stays finite.
 constexpr int kTop = 6, kRoom = 2, kLarge = 64;
-constexpr float kShift = 8.f, kLag = 7.f;
+constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
 
 __device__ __forceinline__ uint4 half_eight(uint32_t a, uint32_t b, float s)
 {
@@ -347,6 +351,529 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
     }
 }
 
+// 16 bytes per lane global -> LDS; the wavefront fills 1 KiB starting at `lds_addr` in lane order.  The compiler does not see the
+// load: it is waited for by hand before a barrier.
+__device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_off, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(lds_addr), "v"(byte_off), "s"(base) : "memory", "m0");
+}
+
+// 128 rows per workgroup, 32 per wavefront, over tiles of 64 keys, two blocks of the cache; bf16.  For the rows of a whole scale, where the
+// matrix cores and the softmax bound the time.
+//   S^T = K Q^T by the 32x32x64 block-scaled MFMA: it takes keys in 8 bits with their scale bytes as they lie in memory, so K is not
+//     converted.  Q goes in as two E4M3 numbers per element, with a power of two per row, 2^e, and 2^(e-4) for what the first leaves:
+//     the first leaves at most half a step of its binade, eight steps of bf16's eight bits, which the second holds whole.  Two
+//     products at twice the rate of bf16 take as long as one of bf16 would, without a conversion of K.  (Elements below 2^-15 of
+//     their row's largest are held to 2^-23 of it, as fp32 sums hold them.)
+//   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
+// In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
+// product takes it, as in attention.hip.
+// Tiles come by DMA two ahead: three of keys in LDS, two of values as they came (each wavefront converts what it fetched itself), and five
+// halves of converted values: while some wavefronts still read the second half of the tile before, others write both halves of the next.
+// With 128-wide rows that is half of a CU's LDS.
+// The loop goes by halves of a tile: beside the softmax of one stand the scores of the next and the products of the one before, in turn.
+// KG = 2: two groups of four wavefronts on the same rows, each with half of the keys and LDS of its own, which meet at the end:
+// as full a CU as two workgroups make, without partial results in memory.
+template <int DH, int KG>
+__global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvbCache c, int extra,
+                                                                int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,
+                                                                int full_units, int shares, float *__restrict__ part_o,
+                                                                float *__restrict__ part_ml, float2 *__restrict__ stats)
+{
+    constexpr int KS = DH / 64, DB = DH / 32;                // k64 steps of S, 32-row blocks of O^T
+    constexpr int VW = DH / 32;                              // groups of eight values per thread
+    constexpr int RAW = 64 * DH, HALF = 32 * DH * 2;         // bytes of a tile's codes, of half a tile of converted values
+    constexpr int VOFF = 3 * RAW, COFF = VOFF + 2 * RAW, GROUP = COFF + 5 * HALF;
+    __shared__ uint4 lds[KG * GROUP / 16];                   // [group][3 x keys | 2 x values as they came | 5 x half a tile of values]
+
+    const int tid = threadIdx.x & 255, lane = tid & 63, rl = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = KG > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8) : 0;
+    int unit = blockIdx.x, share = 0, ranges = 1;
+    if (unit < full_units) {
+        unit = xcd_grouped(unit, full_units / nrb, nrb);
+    } else {
+        const int t = unit - full_units;
+        unit = full_units + t / shares;
+        share = t % shares;
+        ranges = shares;
+    }
+    const int rb = unit % nrb, hk = unit / nrb % c.heads, b = unit / (nrb * c.heads);
+    const int G = H / c.heads, R = n * G;
+    const int len = kvb_length(c, b, extra);
+    const int tiles = (len + 63) / 64;
+    // the group's tiles [t0, t1], one at least and as many as the other's: where there is none, one in which nothing is seen
+    const int first_tile = tiles * share / ranges, end = tiles * (share + 1) / ranges;   // (at most 2^18 tiles and 16 shares)
+    const int trips = max((end - first_tile + KG - 1) / KG, 1), t0 = first_tile + kg * trips, t1 = t0 + trips - 1;
+    const int seen_end = min(len, min(end, t1 + 1) * 64), last_row = max(len - 1, 0);
+    const int r0 = rb * 128 + wave * 32, row = min(r0 + rl, R - 1);
+    const bool active = __builtin_amdgcn_readfirstlane(r0 < R ? 1 : 0) != 0;
+
+    const size_t head = (size_t)(b * c.heads + hk);
+    const uint8_t *Kc = c.k + head * c.capacity * DH, *Vc = c.v + head * c.capacity * DH;
+    const uint8_t *Ks = c.k_scale + head * c.blocks(), *Vs = c.v_scale + head * c.blocks();
+    const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
+    uint8_t *lds8 = reinterpret_cast<uint8_t *>(lds) + kg * GROUP;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)lds + kg * GROUP;
+
+    // ---- A tile by DMA.  K: 16-byte chunks of a row are turned by its number, so that the rows of sixteen lanes that read one chunk
+    // lie in all banks.  V: the order in which the threads convert it: 32 bytes (64-wide rows: 16) of a row each, neighbouring quads
+    // four rows apart (128-wide rows) so that their writes lie in different banks.  A row past the last is the last again.
+    constexpr int CH = DH / 16, DMAS = DH / 64;              // chunks of a row; instructions of a wavefront for a tile
+    auto kturn = [](int key) { return DH == 128 ? (key >> 1) & 7 : (key >> 2) & 3; };
+    const int vkey = DH == 128 ? wave * 16 + ((lane >> 4) & 3) + (lane >> 2 & 3) * 4 : tid >> 2, vpart = tid & 3;
+    uint32_t seen_later = 1, seen_next = 1;                  // mask bytes of the lane's key, two tiles ahead and one
+    auto fetch = [&](int t, int kslot, int vslot) {
+        const int first = t * 64;
+        const bool last = first + 64 > len;                  // uniform
+#pragma unroll
+        for (int i = 0; i < DMAS; ++i) {
+            const int key = (wave * DMAS + i) * (64 / CH) + lane / CH, chunk = (lane % CH) ^ kturn(key);
+            const uint32_t at = last ? min(first + key, last_row) : first + key;
+            tile_dma_b128(Kc, at * DH + chunk * 16, lds_base + kslot * RAW + (wave * DMAS + i) * 1024);
+        }
+        const uint32_t vat = last ? min(first + vkey, last_row) : first + vkey;
+#pragma unroll
+        for (int i = 0; i < DMAS; ++i)
+            tile_dma_b128(Vc, vat * DH + (vpart * DMAS + i) * 16, lds_base + VOFF + vslot * RAW + (wave * DMAS + i) * 1024);
+        if (mask) seen_later = mask[last ? min(first + lane, last_row) : first + lane];
+    };
+    fetch(t0, 0, 0);                                         // on their way under what follows
+    seen_next = seen_later;
+    fetch(min(t0 + 1, t1), 1, 1);
+
+    // ---- scale bytes of 64 blocks, a lane's each: of the tiles from 32 * (t / 32) on
+    const int last_block = last_row / kKvbBlock;
+    uint32_t kbytes = 0, vbytes = 0;
+    int held = -1;
+    auto scales_of = [&](int t) {                            // before a byte of tile t is asked for
+        if (__builtin_expect((t >> 5) != held, 0)) {
+            held = t >> 5;
+            const int at = min(held * 64 + lane, last_block);
+            kbytes = Ks[at];
+            vbytes = Vs[at];
+        }
+    };
+    auto byte_of = [&](uint32_t bytes, int t, int half) { return __builtin_amdgcn_readlane((int)bytes, (t & 31) * 2 + half); };
+
+    // ---- Q in two pieces of 8 bits: lane = row, elements 64 s + 32 g .. + 31
+    intx8_t qf[KS][2];
+    int qbyte;
+    {
+        const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
+        uint4 w[KS][4];
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[s][i] = *reinterpret_cast<const uint4 *>(src + 64 * s + 8 * i);
+                const uint32_t x[4] = {w[s][i].x, w[s][i].y, w[s][i].z, w[s][i].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top = max(top, max(x[j] << 16 & 0x7fff0000u, x[j] & 0x7fff0000u));
+            }
+        {
+            const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+            top = max(both[0], both[1]);
+        }
+        const bool odd = top >= 0x7f800000u;                 // an element that is not finite: no score of the row is a number
+        const uint32_t byte = kvb_byte(odd ? 0x3f800000u : top);
+        qbyte = (int)byte | (int)(byte - 4) << 8;
+        const float size = __uint_as_float(byte << 23), rest = __uint_as_float((byte - 4) << 23);
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t a = i & 1 ? w[s][i / 2].z : w[s][i / 2].x, d = i & 1 ? w[s][i / 2].w : w[s][i / 2].y;
+                float x[4] = {bf16_lo(a), bf16_hi(a), bf16_lo(d), bf16_hi(d)};
+                const uint32_t one = kvb_four(x, size);
+                const floatx2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(one, size, false);
+                const floatx2_t hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(one, size, true);
+                x[0] -= lo[0]; x[1] -= lo[1]; x[2] -= hi[0]; x[3] -= hi[1];
+                qf[s][0][i] = odd ? 0x7f7f7f7f : (int)one;
+                qf[s][1][i] = odd ? 0 : (int)kvb_four(x, rest);
+            }
+    }
+
+    // everything on its way to LDS is there, for all wavefronts
+    auto meet = [&]() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+
+    // ---- converted values: chunks of a row are turned so that four rows' 64-byte quarters lie in different banks when they are read
+    // (transposing load, as in attention.hip), and the chunks of neighbouring quads of lanes when they are written
+    auto turn = [](int key) { return DH == 128 ? ((key & 3) << 2) | ((key >> 2) & 3) : ((key >> 1) & 1) << 2; };
+    const int tG = lane >> 4, tj = (lane >> 2) & 3, ta = lane & 3;
+    const int vrow = 4 * (tG >> 1) + tj;
+    // chunk 4 db + 2 (tG & 1) + (ta >> 1) of row vrow + 8 step8, in bytes
+    auto chunk_at = [&](int db, int step8) {
+        const int key = vrow + 8 * step8;
+        return (key * DH + (((4 * db + 2 * (tG & 1) + (ta >> 1)) ^ turn(key)) << 3) + (ta & 1) * 4) * 2;
+    };
+
+    floatx16_t acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = floatx16_t{0};
+    float l_run = 0.f, most = -1.f;                          // most: the sum of weights from which on a reference is looked for; < 0: no reference yet
+    float m_ref = 0.f;                                       // the reference: the products that make scores start from - m_ref
+    floatx16_t bases = floatx16_t{0};
+    auto set_base = [&](float m) {
+        m_ref = m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bases[i] = -m;
+        asm volatile("" : "+v"(bases));
+    };
+    int E = -200, E_now = -200, acc_E = -200;                // of the values converted last, of the tile at work, of the sums
+
+    // A thread's values as they came; the rows that can be seen, and the size of the values: E is the same in all wavefronts.
+    struct Raw { uint32_t v[2 * VW]; };
+    auto read_raw = [&](int vslot, Raw &x) {
+        const uint8_t *src = lds8 + VOFF + vslot * RAW + wave * DMAS * 1024 + lane * 16;
+#pragma unroll
+        for (int i = 0; i < DMAS; ++i) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(src + i * 1024);
+            x.v[4 * i] = w.x; x.v[4 * i + 1] = w.y; x.v[4 * i + 2] = w.z; x.v[4 * i + 3] = w.w;
+        }
+    };
+    float vsize = 0.f;
+    auto look = [&](int t, Raw &x, uint32_t seen_byte) -> unsigned long long {
+        const unsigned long long vis = __ballot(t * 64 + lane < seen_end && seen_byte != 0);
+        scales_of(t);
+        const int e0 = byte_of(vbytes, t, 0) - 127, e1 = byte_of(vbytes, t, 1) - 127;
+        if ((uint32_t)vis != 0 && e0 > E) E = e0 + kRoom;
+        if (vis >> 32 != 0 && e1 > E) E = e1 + kRoom;
+        vsize = power_of_two((wave < 2 ? e0 : e1) - E + kTop);
+        if (__builtin_expect(vis != ~0ull, 0) && !(vis >> vkey & 1)) {
+#pragma unroll
+            for (int i = 0; i < 2 * VW; ++i) x.v[i] = 0;
+        }
+        return vis;
+    };
+    uint32_t vdst[VW];                                       // where the thread's values go within half a tile, in bytes
+#pragma unroll
+    for (int i = 0; i < VW; ++i) vdst[i] = COFF + ((vkey & 31) * DH + (((vpart * VW + i) ^ turn(vkey)) << 3)) * 2;
+    int cslot = wave >> 1;                                   // the half tile that they go to
+    auto convert = [&](const Raw &x, int i) {
+        *reinterpret_cast<uint4 *>(lds8 + cslot * HALF + vdst[i]) = half_eight(x.v[2 * i], x.v[2 * i + 1], vsize);
+    };
+    auto next_half = [](int s, int by) { return s + by >= 5 ? s + by - 5 : s + by; };
+
+    Raw raw;
+    meet();
+    read_raw(0, raw);
+    unsigned long long vis = look(t0, raw, seen_next), vis_next;
+#pragma unroll
+    for (int i = 0; i < VW; ++i) convert(raw, i);
+    cslot = next_half(cslot, 2);
+    seen_next = seen_later;
+    __syncthreads();
+    int kslot = 0, vslot = 0;                                // of the tile at work
+    auto after = [](int s) { return s == 2 ? 0 : s + 1; };
+    if (!active) {                                           // rows past the end: only helps with the tiles
+        for (int t = t0; t <= t1; ++t) {
+            read_raw(vslot ^ 1, raw);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            fetch(min(t + 2, t1), after(after(kslot)), vslot);
+            look(min(t + 1, t1), raw, seen_next);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) convert(raw, i);
+            cslot = next_half(cslot, 2);
+            seen_next = seen_later;
+            kslot = after(kslot);
+            vslot ^= 1;
+            meet();
+        }
+        if (KG > 1) {                                        // (the meeting of the groups)
+            __syncthreads();
+            __syncthreads();
+        }
+        return;
+    }
+
+    // Where the lane reads values of the first 16 keys of half a tile, and the first 32 keys of a tile; further on by constants.
+    lds_byte_t *vp[DB][2], *kp[KS][2];
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) vp[i][h] = (lds_byte_t *)(lds8 + COFF + HALF + chunk_at(i, h));
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) kp[s][j] = (lds_byte_t *)(lds8 + rl * DH + ((4 * s + 2 * g + j) ^ kturn(rl)) * 16);
+    int rslot = 1;                                           // the half tile of values that vp points to
+
+    floatx16_t s[2];                                         // scores of the two halves of a tile
+    f16x8_t pf[2][2];                                        // their weights, by steps of 16 keys
+    float sum;
+    pf[1][0] = pf[1][1] = f16x8_t{0};
+    auto load_keys = [&](int half, uintx4_t (&k)[KS][2]) {
+#pragma unroll
+        for (int x = 0; x < KS; ++x)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) k[x][j] = *(lds_uintx4_t *)(kp[x][j] + half * (RAW / 2));
+    };
+#define FVAR_S(half, ks, p, on)                                                                                          \
+    s[half] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(                                                           \
+        intx8_t{(int)k[ks][0][0], (int)k[ks][0][1], (int)k[ks][0][2], (int)k[ks][0][3], (int)k[ks][1][0], (int)k[ks][1][1],      \
+                (int)k[ks][1][2], (int)k[ks][1][3]}, qf[ks][p], on, 0, 0, 0, kb, p, qbyte)
+    // product number i of a half's scores: smaller pieces first
+    auto score = [&](int half, int i, const uintx4_t (&k)[KS][2], int kb) {
+        if (i == 0) FVAR_S(half, 0, 1, bases);
+        if (i == 1) FVAR_S(half, KS - 1, KS == 2 ? 1 : 0, s[half]);
+        if constexpr (KS == 2) {
+            if (i == 2) FVAR_S(half, 0, 0, s[half]);
+            if (i == 3) FVAR_S(half, 1, 0, s[half]);
+        }
+    };
+#undef FVAR_S
+    auto load_v = [&](int i, int rows) -> f16x8_t {
+        const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vp[i][0] + rows * DH * 2));
+        const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vp[i][1] + rows * DH * 2));
+        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // One half's softmax beside the scores of the other (of the next tile where that is the first) and the products of the other's
+    // weights (of the tile before where that is the second).  A step: a product, the weights of a pair or two in three stages.
+    auto region = [&](auto which, int kb) {
+        constexpr int half = decltype(which)::value, other = 1 - half;
+        constexpr int NS = 2 * KS, NPV = 2 * DB, STEPS = NS + NPV, PP = DH == 128 ? 1 : 2;     // PP: pairs of weights per step
+        uintx4_t k[KS][2];
+        f16x8_t vf[DB];
+        load_keys(other, k);
+#pragma unroll
+        for (int i = 0; i < DB; ++i) vf[i] = load_v(i, 0);
+        if constexpr (half == 0) read_raw(vslot ^ 1, raw);
+        __builtin_amdgcn_sched_barrier(0);
+        float x[16], a, bsum;
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step) {
+            const int before = min((step + 1) / 2, NS);      // scores' products up to here, this one included if it is one
+            if ((step & 1) && step / 2 < NS) {
+                score(other, step / 2, k, kb);
+            } else {
+                const int i = step - before;
+                acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i % DB], pf[other][i / DB], acc[i % DB], 0, 0, 0);
+                if (i < DB) vf[i] = load_v(i, 16);
+            }
+#pragma unroll
+            for (int w = 0; w < PP; ++w) {
+                const int p2 = (step - 2) * PP + w, p1 = (step - 1) * PP + w, p0 = step * PP + w;
+                if (p1 >= 0 && p1 < 8) {
+                    x[2 * p1] = __builtin_amdgcn_exp2f(x[2 * p1]);
+                    x[2 * p1 + 1] = __builtin_amdgcn_exp2f(x[2 * p1 + 1]);
+                }
+                if (p0 < 8) {
+                    x[2 * p0] = fmaf(s[half][2 * p0], c_log2, kShift);
+                    x[2 * p0 + 1] = fmaf(s[half][2 * p0 + 1], c_log2, kShift);
+                }
+                if (p2 >= 0 && p2 < 8) {
+                    a = p2 ? a + x[2 * p2] : x[0];
+                    bsum = p2 ? bsum + x[2 * p2 + 1] : x[1];
+                    asm volatile("" : "+v"(a), "+v"(bsum));  // here, not after the region with all of x alive until then
+                    const f16x2v_t p = __builtin_convertvector((floatx2_t{x[2 * p2], x[2 * p2 + 1]}), f16x2v_t);
+                    pf[half][p2 >> 2][(2 * p2) & 7] = p[0];
+                    pf[half][p2 >> 2][(2 * p2 + 1) & 7] = p[1];
+                }
+            }
+            if constexpr (half == 1) {
+                constexpr int from = DH == 128 ? 6 : 3;
+                if (step >= from && step - from < VW) convert(raw, step - from);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum = a + bsum;
+        // the region's results are made in it
+        asm volatile("" : "+v"(pf[half][0]), "+v"(pf[half][1]), "+v"(sum));
+        asm volatile("" : "+v"(s[other]));
+#pragma unroll
+        for (int i = 0; i < DB; ++i) asm volatile("" : "+v"(acc[i]));
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto hide = [&](int half) {
+        const uint32_t part = (uint32_t)(vis >> (32 * half));
+        if (__builtin_expect(part != ~0u, 0)) {
+            const uint32_t mine = part >> (4 * g);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[half][i] = -INFINITY;
+        }
+    };
+    auto settle = [&](int half) {
+        // The reference is not the running maximum but one that was it; the weights tell when it no longer serves.  A sum of NaN
+        // does not ask for another: it stays NaN.
+        const bool anew = (__builtin_amdgcn_ballot_w64(sum > most) != 0 && (uint32_t)(vis >> (32 * half)) != 0) || E_now != acc_E;
+        if (__builtin_expect(anew, 0)) {
+            float mx = s[half][0];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
+            const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+            const bool had = most >= 0.f, none = !had && mx == -INFINITY;
+            float alpha = 1.f;
+            if (!none && (!had || mx > 0.f)) {
+                s[0] -= mx;
+                s[1] -= mx;
+                set_base(m_ref + mx);
+                alpha = __builtin_amdgcn_exp2f(-mx * c_log2);
+            }
+            if (!had) alpha = 0.f;
+            const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E_now, -200));
+            most = none ? -1.f : kMost;
+            acc_E = E_now;
+            l_run *= alpha;
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                acc[i] *= down;
+                asm volatile("" : "+v"(acc[i]));
+            }
+            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[half][i], c_log2, kShift));
+                const float y = __builtin_amdgcn_exp2f(fmaf(s[half][i + 1], c_log2, kShift));
+                sum += x + y;
+                const f16x2v_t p = __builtin_convertvector((floatx2_t{x, y}), f16x2v_t);
+                pf[half][i >> 3][i & 7] = p[0];
+                pf[half][i >> 3][(i & 7) + 1] = p[1];
+            }
+        }
+        l_run += sum;
+    };
+    auto to_half = [&](int to) {                             // vp goes on to half tile `to`
+        const int by = (to - rslot) * HALF;
+        rslot = to;
+#pragma unroll
+        for (int i = 0; i < DB; ++i) { vp[i][0] += by; vp[i][1] += by; }
+    };
+
+    E_now = E;
+    {
+        uintx4_t k[KS][2];
+        load_keys(0, k);
+        const int kb = byte_of(kbytes, t0, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) score(0, i, k, kb);
+    }
+    for (int t = t0; t <= t1; ++t) {
+        const int tn = min(t + 1, t1);
+        fetch(min(t + 2, t1), after(after(kslot)), vslot);
+        hide(0);
+        region(std::integral_constant<int, 0>{}, byte_of(kbytes, t, 1));
+        settle(0);
+        {
+            // values go on to this tile's first half, keys to the next tile's
+            to_half(t == t0 ? 0 : next_half(rslot, 1));
+            const int k_by = kslot == 2 ? -2 * RAW : RAW;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) { kp[i][0] += k_by; kp[i][1] += k_by; }
+        }
+        hide(1);
+        vis_next = look(tn, raw, seen_next);
+        region(std::integral_constant<int, 1>{}, byte_of(kbytes, tn, 0));
+        settle(1);
+        to_half(next_half(rslot, 1));
+        cslot = next_half(cslot, 2);
+        seen_next = seen_later;
+        vis = vis_next;
+        kslot = after(kslot);
+        vslot ^= 1;
+        E_now = E;
+        meet();
+    }
+    if (most < 0.f) m_ref = -INFINITY;
+    // the last half's products
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(load_v(i, 16 * u), pf[1][u], acc[i], 0, 0, 0);
+
+    // ---- means, back at their size (see kTop)
+    {
+        const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+        l_run = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+    }
+    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+    auto mean = [&](float x) { return __builtin_amdgcn_ldexpf(x * inv, acc_E - kTop); };
+    const size_t prow = ((size_t)(unit - full_units) * shares + share) * 128 + wave * 32 + rl;
+    uint16_t *dst = o + (size_t)(b * (long)n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH;
+    // Two quads of results that lie eight apart in the lane's row: four more stand in the lane 32 further, which changes one of its
+    // quads for one of these, so that each stores 16 bytes.  A share's,
+    // with its weight, go as they are to the merge.
+    auto put = [&](auto divided, int d, float4 x, float4 y) {
+        if constexpr (decltype(divided)::value) {
+            float *to = part_o + prow * DH + d + 4 * g;
+            *reinterpret_cast<float4 *>(to) = x;
+            *reinterpret_cast<float4 *>(to + 8) = y;
+        } else {
+            const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16x2(x.x, x.y), pack_bf16x2(y.x, y.y), false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16x2(x.z, x.w), pack_bf16x2(y.z, y.w), false, false);
+            *reinterpret_cast<uint4 *>(dst + d + 8 * g) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+        }
+    };
+    auto put_weight = [&](float m, float l) {
+        if (g) return;
+        if (ranges > 1) *reinterpret_cast<float2 *>(part_ml + prow * 2) = make_float2(m, l);
+        else if (stats) stats[head * R + row] = make_float2(m, l * 0.00390625f);   // (without 2^kShift)
+    };
+    auto quad_mean = [&](const floatx16_t &x, int e) { return make_float4(mean(x[e]), mean(x[e + 1]), mean(x[e + 2]), mean(x[e + 3])); };
+    if constexpr (KG == 1) {
+        if (r0 + rl >= R) return;
+        auto finish = [&](auto divided) {
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; e += 8) put(divided, 32 * i + 2 * e, quad_mean(acc[i], e), quad_mean(acc[i], e + 4));
+        };
+        if (ranges > 1) finish(std::true_type{});
+        else finish(std::false_type{});
+        put_weight(m_ref, l_run);
+    } else {
+        // each group leaves half of its means, its reference and weight where the other finds them, and takes the other half to the end
+        constexpr int HB = DB / 2;
+        float4 *xo = reinterpret_cast<float4 *>(lds);        // [group][wave][block, quad][lane]
+        float2 *xm = reinterpret_cast<float2 *>(xo + 8 * HB * 4 * 64);   // [group][wave][lane]
+        auto leave = [&](const floatx16_t *x) {
+#pragma unroll
+            for (int i = 0; i < HB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) xo[((kg * 4 + wave) * HB * 4 + i * 4 + e / 4) * 64 + lane] = quad_mean(x[i], e);
+        };
+        __syncthreads();                                     // the stages have been read
+        if (kg) leave(acc);
+        else leave(acc + HB);
+        xm[(kg * 4 + wave) * 64 + lane] = make_float2(m_ref, l_run);
+        __syncthreads();
+        if (r0 + rl >= R) return;
+        const float2 other = xm[((1 - kg) * 4 + wave) * 64 + lane];
+        const float m = fmaxf(m_ref, other.x), fin = reference(m);
+        float own = l_run * __builtin_amdgcn_exp2f((m_ref - fin) * c_log2), theirs = other.y * __builtin_amdgcn_exp2f((other.x - fin) * c_log2);
+        const float all = own + theirs, each = all == 0.f ? 0.f : 1.0f / all;
+        own *= each;
+        theirs *= each;
+        auto finish = [&](auto divided, const floatx16_t *x) {
+            auto joined = [&](int i, int e) {
+                const float4 a = quad_mean(x[i], e), b = xo[(((1 - kg) * 4 + wave) * HB * 4 + i * 4 + e / 4) * 64 + lane];
+                return make_float4(fmaf(b.x, theirs, a.x * own), fmaf(b.y, theirs, a.y * own), fmaf(b.z, theirs, a.z * own),
+                                   fmaf(b.w, theirs, a.w * own));
+            };
+#pragma unroll
+            for (int i = 0; i < HB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; e += 8) put(divided, 32 * (kg * HB + i) + 2 * e, joined(i, e), joined(i, e + 4));
+        };
+        if (ranges > 1) {
+            if (kg) finish(std::true_type{}, acc + HB);
+            else finish(std::true_type{}, acc);
+        } else {
+            if (kg) finish(std::false_type{}, acc + HB);
+            else finish(std::false_type{}, acc);
+        }
+        if (!kg) put_weight(m, all);
+    }
+}
+
 // The shares of rows joined: each is a mean and its weight.  A unit is a block of BR rows of one (sample, kv head); the shares
 // of unit first + u lie at [u][share][row].  GROUPS groups of DH/4 threads per row, four head-dim elements a thread: a group takes every
 // GROUPS-th share, four at a time, with a running reference and mean (not the sum: a mean times its weight need not be a number that fp32
@@ -558,21 +1085,45 @@ __global__ __launch_bounds__(256) void kvb_weights_join_kernel(KvbCache c, int e
     *to = add ? *to + sum : sum;
 }
 
+// Blocks of how many rows of a (sample, kv head) an attention is run by: 16 (kvb_attn_rows_kernel) or 128 (kvb_attn_tiles_kernel, bf16
+// only).
+static int kvb_block(DType dt, int B, int n, int H, int heads, int length)
+{
+    const int rows = n * (H / heads);
+    if (dt != DType::BF16 || rows <= 48) return 16;
+    return (long)B * heads * ((rows + 15) / 16) * length <= (rows <= 64 ? 1l << 21 : 1l << 20) ? 16 : 128;
+}
+
 // nrb blocks per (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
-// `ragged`: samples of lengths of their own, which only the GPU knows.  waves: wavefronts of a workgroup.
+// `ragged`: samples of lengths of their own, which only the GPU knows.
+// waves: wavefronts of a workgroup, which divide a block's keys (16 rows), or its rows and, if there are 8, keys (128 rows).
 struct KvbRun { int block, nrb, units, full, shares, waves; };
-static KvbRun kvb_run(int block, int B, int n, int H, int heads, int length, bool ragged)
+constexpr int kGroupsFrom = 2048, kGroupsTo = 4096;          // lengths at which the choice between one and two groups changes
+static KvbRun kvb_run(int block, int B, int n, int H, int heads, int Dh, int length, bool ragged)
 {
     KvbRun run;
     run.block = block;
     run.nrb = (n * (H / heads) + block - 1) / block;
     run.units = B * heads * run.nrb;
     run.waves = 4;
-    const int tiles = (length + 31) / 32;
-    const int places = ragged ? 1024 : 512, least = run.units < 256 ? 2 : 8;
-    const int want = (places + run.units - 1) / run.units, most = tiles / (least * 4);
+    if (block == 16) {
+        const int tiles = (length + 31) / 32;
+        const int places = ragged ? 1024 : 512, least = run.units < 256 ? 2 : 8;
+        const int want = (places + run.units - 1) / run.units, most = tiles / (least * 4);
+        run.shares = want < most ? want : most > 0 ? most : 1;
+        run.full = run.shares > 1 ? 0 : run.units;
+        return run;
+    }
+    const int two = 512;
+    bool groups = run.units <= 256 || (run.units <= 320 && length >= kGroupsFrom);
+    if (run.units <= 256 && length >= kGroupsTo) groups = (two / run.units) * 256 * 8 <= (256 / run.units) * two * 9;
+    const int slots = groups ? 256 : two, rest = run.units % slots, most = (length + 63) / 64 / (groups ? 8 : 4);
+    run.waves = groups ? 8 : 4;
+    run.full = run.units - rest;
+    int want = rest ? slots / rest : 1;
+    if (want > 16) want = 16;
     run.shares = want < most ? want : most > 0 ? most : 1;
-    run.full = run.shares > 1 ? 0 : run.units;
+    if (run.shares == 1) run.full = run.units;
     return run;
 }
 
@@ -588,8 +1139,18 @@ static int weight_shares(int B, int heads, int length, int rows)
 
 size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity, bool weights)
 {
-    const KvbRun run = kvb_run(16, B, n, H, heads, capacity, true);
-    size_t floats = (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
+    // Between those lengths shares never fall as the length grows, nor where samples have lengths of their own, so for either kind of
+    // blocks the longest length of each stretch is enough for every call; a shorter length may be run by the other kind.
+    size_t floats = 0;
+    for (int length : {capacity, kGroupsTo - 1, kGroupsFrom - 1}) {
+        if (length > capacity) continue;
+        for (int block = 16; block <= 128; block *= 8) {
+            if (block == 128 ? kvb_block(dt, B, n, H, heads, length) == 16 : kvb_block(dt, B, n, H, heads, 1) == 128) continue;
+            const KvbRun run = kvb_run(block, B, n, H, heads, Dh, length, true);
+            const size_t take = (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
+            if (take > floats) floats = take;
+        }
+    }
     // every row's reference and sum; partial sums of at most kWeightPlaces workgroups of 256 keys
     if (weights) floats += 2 * (size_t)B * n * H + 256 * kWeightPlaces;
     return floats;
@@ -600,7 +1161,8 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
                        float *part, hipStream_t st)
 {
     const int length = c.lens ? c.capacity : c.len + extra;
-    const KvbRun run = kvb_run(16, B, n, H, c.heads, length, c.lens != nullptr);
+    const DType dt = sizeof(T) == 2 ? DType::BF16 : DType::F32;
+    const KvbRun run = kvb_run(kvb_block(dt, B, n, H, c.heads, length), B, n, H, c.heads, DH, length, c.lens != nullptr);
     const int divided = run.units - run.full;
     float2 *stats = nullptr;
     float *sums = part;
@@ -614,9 +1176,18 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
 #define FVAR_ROWS(NW, MASKED)                                                                                            \
     launch(kvb_attn_rows_kernel<T, DH, NW, MASKED>, dim3(wgs), dim3(64 * NW), 0, st, (const T *)q, ld, c, extra, n, H,    \
            c_log2, (T *)o, run.nrb, run.shares, part, part_ml, stats)
-    if (c.mask) FVAR_ROWS(4, true);
-    else FVAR_ROWS(4, false);
+    if (run.block == 16) {
+        if (c.mask) FVAR_ROWS(4, true);
+        else FVAR_ROWS(4, false);
 #undef FVAR_ROWS
+    } else if constexpr (sizeof(T) == 2) {
+#define FVAR_TILES(KG)                                                                                                   \
+    launch(kvb_attn_tiles_kernel<DH, KG>, dim3(wgs), dim3(256 * KG), 0, st, (const T *)q, ld, c, extra, n, H,             \
+           c_log2, (T *)o, run.nrb, run.full, run.shares, part, part_ml, stats)
+        if (run.waves == 8) FVAR_TILES(2);
+        else FVAR_TILES(1);
+#undef FVAR_TILES
+    }
     if (divided) {
         const int total = divided * run.block, per = 256 / (DH / 4);
         if (run.shares > 8)

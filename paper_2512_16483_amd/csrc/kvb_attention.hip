@@ -103,12 +103,14 @@ __device__ __forceinline__ int xcd_grouped(int id, int groups, int size)
 //   O^T = V^T P^T: a lane takes pieces of sixteen values as they lie in memory, converts them and leaves them in LDS row by
 //     row, from where the transposing load brings eight keys of one head-dim element; P is in that order already.
 // fp32: Q and P go in as three bf16 numbers each, K and V are exact in one.
-// stats: null, or for every row what its weights were taken against: reference and sum.
+// stats: null, or for every row what its weights were taken against: reference and sum.  scores: null, or [B * heads][rows][pitch] where there
+// is one block of rows, and receives them (not those of tiles without a visible key).
 template <typename T, int DH, int NW, bool MASKED>
 __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__restrict__ q, int ld, KvbCache c, int extra,
                                                                 int n, int H, float c_log2, T *__restrict__ o,
                                                                 int nrb, int splits, float *__restrict__ part_o,
-                                                                float *__restrict__ part_ml, float2 *__restrict__ stats)
+                                                                float *__restrict__ part_ml, float2 *__restrict__ stats,
+                                                                float *__restrict__ scores, int pitch)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NP = F32 ? 3 : 1;
@@ -249,6 +251,11 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
                     if (!(mine >> i & 1)) s[0][i] = -INFINITY;
                     if (!(mine >> (16 + i) & 1)) s[1][i] = -INFINITY;
                 }
+            }
+            if (scores && c16 < R) {
+                float *to = scores + (head * R + c16) * (size_t)pitch + (t - NW) * 32 + 4 * g4;
+                *reinterpret_cast<floatx4_t *>(to) = s[0];
+                *reinterpret_cast<floatx4_t *>(to + 16) = s[1];
             }
             const float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
             const bool lags = __builtin_amdgcn_ballot_w64(mx - m_ref > lag) != 0 || E != acc_E;
@@ -948,8 +955,9 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
 }
 
 // Weights of the rows: every wavefront holds 64 keys as bf16 operands, takes the scores of all rows of queries against them once more, and
-// adds up exp2((s - reference) * c - log2(sum)) over the rows, each key's in its own registers: no atomics, one order.  32 rows at a time come
-// through LDS for the four wavefronts, the next ones on their way.  A row whose weights are not numbers adds nothing.
+// adds up exp2((s - reference) * c - log2(sum)) over the rows, each key's in its own registers: no atomics, one order.  64 rows at a time come
+// through LDS for the four wavefronts, by DMA while the ones before are at work (fp32: 32 rows, in three pieces of bf16).  A row whose weights
+// are not numbers adds nothing.
 //   grid: (blocks of 256 keys, B * heads, shares of the rows); shares: as partial sums [share][B * heads][256 * gridDim.x].
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict__ q, int ld, KvbCache c, int extra, int n, int H, float c_log2,
@@ -957,15 +965,59 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
                                                              float *__restrict__ part)
 {
     constexpr bool F32 = sizeof(T) == 4;
-    constexpr int NP = F32 ? 3 : 1, KS = DH / 16, CH = DH / 8, PER = 32 * CH / 256;   // PER: chunks of eight elements per thread
-    __shared__ uint4 ql[2][NP][32 * CH];
+    constexpr int NP = F32 ? 3 : 1, KS = DH / 16, CH = DH / 8;   // CH: chunks of eight elements of a row
+    constexpr int SETS = F32 ? 1 : 2, ROWS = 32 * SETS, PER = ROWS * CH / 256;
+    __shared__ uint4 ql[2][NP][ROWS * CH];
     const int tid = threadIdx.x, lane = tid & 63, rl = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int head = blockIdx.y, b = head / c.heads, hk = head % c.heads;
     const int G = H / c.heads, R = n * G, len = kvb_length(c, b, extra);
     const int key0 = blockIdx.x * 256 + wave * 64;
     if ((int)blockIdx.x * 256 >= len) return;                // (of the whole workgroup)
-    const int tiles = (R + 31) / 32, t0 = (int)((long)tiles * blockIdx.z / gridDim.z), t1 = (int)((long)tiles * (blockIdx.z + 1) / gridDim.z);
+    const int tiles = (R + ROWS - 1) / ROWS, t0 = (int)((long)tiles * blockIdx.z / gridDim.z), t1 = (int)((long)tiles * (blockIdx.z + 1) / gridDim.z);
+
+    // ---- rows of queries: chunks are turned by the row's number, so that the rows of sixteen lanes that read one chunk lie in all banks
+    auto turn = [](int row) { return DH == 128 ? row & 15 : (row >> 1) & 7; };
+    const uint32_t lds_base = (uint32_t)(uintptr_t)ql;
+    uint4 next[F32 ? PER : 1][2];
+    float2 next_stat[SETS];
+    auto fetch = [&](int t, int buffer) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = F32 ? i * 256 + tid : (wave * PER + i) * 64 + lane;
+            const int in_tile = at / CH, row = min(t * ROWS + in_tile, R - 1);
+            const size_t src = (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH;
+            if constexpr (F32) {
+                next[i][0] = *reinterpret_cast<const uint4 *>(q + src + at % CH * 8);
+                next[i][1] = *reinterpret_cast<const uint4 *>(q + src + at % CH * 8 + 4);
+            } else {
+                // (addresses of any distance from q: 64 bits per lane)
+                const uint16_t *from = q + src + ((at % CH) ^ turn(in_tile)) * 8;
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                             :: "s"(lds_base + (buffer * ROWS * CH + (wave * PER + i) * 64) * 16), "v"(from) : "memory", "m0");
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < SETS; ++j) next_stat[j] = stats[(size_t)head * R + min(t * ROWS + j * 32 + rl, R - 1)];
+    };
+    auto put = [&](int buffer) {
+        if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int at = i * 256 + tid, to = at / CH * CH + ((at % CH) ^ turn(at / CH));
+                float x[8];
+                bf16x8_t pieces[3];
+                Elem<float>::unpack(next[i][0], x);
+                Elem<float>::unpack(next[i][1], x + 4);
+                three_pieces(x, pieces);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) ql[buffer][p][to] = __builtin_bit_cast(uint4, pieces[p]);
+            }
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+    };
+    if (t0 < t1) fetch(t0, 0);
 
     // ---- keys: lane = key, half a row
     bf16x8_t kf[2][KS];
@@ -982,68 +1034,46 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
         }
     }
 
-    // ---- rows of queries: chunks are turned by the row's number, so that the rows of sixteen lanes that read one chunk lie in all banks
-    auto place = [](int row, int chunk) { return row * CH + (chunk ^ (DH == 128 ? row & 15 : (row >> 1) & 7)); };
-    uint4 next[PER][F32 ? 2 : 1];
-    float2 next_stat;
-    auto fetch = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int at = i * 256 + tid, row = min(t * 32 + at / CH, R - 1);
-            const T *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + at % CH * 8;
-            next[i][0] = *reinterpret_cast<const uint4 *>(src);
-            if constexpr (F32) next[i][1] = *reinterpret_cast<const uint4 *>(src + 4);
-        }
-        next_stat = stats[(size_t)head * R + min(t * 32 + rl, R - 1)];
-    };
-    auto put = [&](int buffer) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int at = i * 256 + tid, to = place(at / CH, at % CH);
-            if constexpr (F32) {
-                float x[8];
-                bf16x8_t pieces[3];
-                Elem<float>::unpack(next[i][0], x);
-                Elem<float>::unpack(next[i][1], x + 4);
-                three_pieces(x, pieces);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) ql[buffer][p][to] = __builtin_bit_cast(uint4, pieces[p]);
-            } else {
-                ql[buffer][0][to] = next[i][0];
-            }
-        }
-    };
-
     floatx16_t acc[2] = {floatx16_t{0}, floatx16_t{0}};
-    if (t0 < t1) {
-        fetch(t0);
-        put(0);
-    }
+    if (t0 < t1) put(0);
     for (int t = t0; t < t1; ++t) {
-        const float2 stat = next_stat;
+        float2 stat[SETS];
+#pragma unroll
+        for (int j = 0; j < SETS; ++j) stat[j] = next_stat[j];
         const int buffer = (t - t0) & 1;
         __syncthreads();                                     // this tile's rows are there, the other buffer has been read
-        if (t + 1 < t1) fetch(t + 1);
-        floatx16_t s[2] = {floatx16_t{0}, floatx16_t{0}};
+        if (t + 1 < t1) fetch(t + 1, buffer ^ 1);
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
+        for (int j = 0; j < SETS; ++j) {
+            floatx16_t s[2] = {floatx16_t{0}, floatx16_t{0}};
 #pragma unroll
-            for (int p = NP - 1; p >= 0; --p) {
-                const bf16x8_t qf = __builtin_bit_cast(bf16x8_t, ql[buffer][p][place(rl, g * KS + i)]);
+            for (int i = 0; i < KS; ++i) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][i], qf, s[u], 0, 0, 0);
+                for (int p = NP - 1; p >= 0; --p) {
+                    const bf16x8_t qf = __builtin_bit_cast(bf16x8_t, ql[buffer][p][(j * 32 + rl) * CH + ((g * KS + i) ^ turn(rl))]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][i], qf, s[u], 0, 0, 0);
+                }
+            }
+            const bool there = t * ROWS + j * 32 + rl < R, counts = there && stat[j].y > 0.f;
+            const float m = counts ? reference(stat[j].x) : 0.f, off = counts ? -__builtin_amdgcn_logf(stat[j].y) : -INFINITY;
+            const float both = fmaf(-m, c_log2, off);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(fabsf(m * c_log2) >= 4096.f || there != counts) == 0, 1)) {
+                // reference and sum as one number, the same for all keys: off by 2^-25 of itself
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[u][i] += __builtin_amdgcn_exp2f(fmaf(s[u][i], c_log2, both));
+            } else {
+                // the difference first, exact near the reference; at most 1: scores of 2^20 and more differ by more than that between
+                // two ways to add their products up, and 0 for what is not a number
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        acc[u][i] += __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(s[u][i] - m, c_log2, off)), 0.f, 1.f);
             }
         }
-        const bool counts = t * 32 + rl < R && stat.y > 0.f;
-        const float m = counts ? reference(stat.x) : 0.f, off = counts ? -__builtin_amdgcn_logf(stat.y) : -INFINITY;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float x = fmaf(s[u][i] - m, c_log2, off);
-                // (at most 1: scores of 2^20 and more differ by more than that between two ways to add their products up)
-                acc[u][i] += __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f);
-            }
         if (t + 1 < t1) put(buffer ^ 1);
     }
 
@@ -1072,6 +1102,35 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     }
     float *to = weights + (size_t)head * c.capacity + key;
     *to = add ? *to + mine : mine;
+}
+
+// The same where one block of sixteen rows is all, and kvb_attn_rows_kernel has left their scores: those are a few bytes for every key, which a
+// second look at the keys would be 128 for.  Four keys per thread.  grid: (blocks of 1024 keys, B * heads).
+__global__ __launch_bounds__(256) void kvb_weights_few_kernel(KvbCache c, int extra, int R, float c_log2, const float2 *__restrict__ stats,
+                                                              const float *__restrict__ scores, int pitch, float *__restrict__ weights, int add)
+{
+    const int head = blockIdx.y, b = head / c.heads, len = kvb_length(c, b, extra), key = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (key >= len) return;
+    const float *src = scores + (size_t)head * R * pitch + key;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < R; ++r) {
+        const float2 stat = stats[(size_t)head * R + r];
+        const float4 s = *reinterpret_cast<const float4 *>(src + (size_t)r * pitch);
+        if (!(stat.y > 0.f)) continue;
+        const float m = reference(stat.x), each = 1.0f / stat.y;
+        sum[0] += __builtin_amdgcn_exp2f((s.x - m) * c_log2) * each;
+        sum[1] += __builtin_amdgcn_exp2f((s.y - m) * c_log2) * each;
+        sum[2] += __builtin_amdgcn_exp2f((s.z - m) * c_log2) * each;
+        sum[3] += __builtin_amdgcn_exp2f((s.w - m) * c_log2) * each;
+    }
+    const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
+    float *to = weights + (size_t)head * c.capacity;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (key + i >= len) return;
+        const float x = !mask || mask[key + i] != 0 ? sum[i] : 0.f;
+        to[key + i] = add ? to[key + i] + x : x;
+    }
 }
 
 __global__ __launch_bounds__(256) void kvb_weights_join_kernel(KvbCache c, int extra, const float *__restrict__ part, int pitch, int shares,
@@ -1127,6 +1186,10 @@ static KvbRun kvb_run(int block, int B, int n, int H, int heads, int Dh, int len
     return run;
 }
 
+// Whether the weights come from scores that the attention leaves (see kvb_weights_few_kernel), and the room of a row of them.
+static bool few_rows(int rows) { return rows <= 16; }
+static size_t score_pitch(int length) { return ((size_t)length + 31) / 32 * 32; }
+
 // Shares of the rows of queries for the weights: where the keys alone do not fill the chip.
 constexpr int kWeightPlaces = 512;
 static int weight_shares(int B, int heads, int length, int rows)
@@ -1151,8 +1214,8 @@ size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, in
             if (take > floats) floats = take;
         }
     }
-    // every row's reference and sum; partial sums of at most kWeightPlaces workgroups of 256 keys
-    if (weights) floats += 2 * (size_t)B * n * H + 256 * kWeightPlaces;
+    // every row's reference and sum; their scores, or partial sums of at most kWeightPlaces workgroups of 256 keys
+    if (weights) floats += (2 * (size_t)B * n * H + 3) / 4 * 4 + (few_rows(n * (H / heads)) ? (size_t)B * n * H * score_pitch(capacity) : 256 * kWeightPlaces);
     return floats;
 }
 
@@ -1165,17 +1228,19 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
     const KvbRun run = kvb_run(kvb_block(dt, B, n, H, c.heads, length), B, n, H, c.heads, DH, length, c.lens != nullptr);
     const int divided = run.units - run.full;
     float2 *stats = nullptr;
-    float *sums = part;
+    float *sums = part, *scores = nullptr;
+    const int rows = n * (H / c.heads), pitch = (int)score_pitch(length);
     if (weights) {
         stats = reinterpret_cast<float2 *>(part);
-        sums = part + 2 * (size_t)B * n * H;
-        part = sums + 256 * kWeightPlaces;
+        sums = part + (2 * (size_t)B * n * H + 3) / 4 * 4;
+        scores = few_rows(rows) ? sums : nullptr;
+        part = sums + (scores ? (size_t)B * n * H * pitch : 256 * kWeightPlaces);
     }
     float *part_ml = part + (size_t)divided * run.shares * run.block * DH;
     const unsigned wgs = (unsigned)(run.full + divided * run.shares);
 #define FVAR_ROWS(NW, MASKED)                                                                                            \
     launch(kvb_attn_rows_kernel<T, DH, NW, MASKED>, dim3(wgs), dim3(64 * NW), 0, st, (const T *)q, ld, c, extra, n, H,    \
-           c_log2, (T *)o, run.nrb, run.shares, part, part_ml, stats)
+           c_log2, (T *)o, run.nrb, run.shares, part, part_ml, stats, scores, pitch)
     if (run.block == 16) {
         if (c.mask) FVAR_ROWS(4, true);
         else FVAR_ROWS(4, false);
@@ -1197,8 +1262,11 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
             launch(kvb_attn_merge_kernel<T, DH, 1>, dim3((unsigned)((total + per - 1) / per)), dim3(256), 0, st, (const float *)part,
                    (const float *)part_ml, n, H, c.heads, run.nrb, run.block, run.full, run.shares, c_log2, total, (T *)o, stats);
     }
-    if (weights && length > 0) {
-        const int blocks = (length + 255) / 256, shares = weight_shares(B, c.heads, length, n * (H / c.heads));
+    if (scores && length > 0) {
+        launch(kvb_weights_few_kernel, dim3((unsigned)((length + 1023) / 1024), (unsigned)(B * c.heads)), dim3(256), 0, st, c, extra, rows, c_log2,
+               (const float2 *)stats, (const float *)scores, pitch, weights, add ? 1 : 0);
+    } else if (weights && length > 0) {
+        const int blocks = (length + 255) / 256, shares = weight_shares(B, c.heads, length, rows);
         launch(kvb_weights_kernel<T, DH>, dim3((unsigned)blocks, (unsigned)(B * c.heads), (unsigned)shares), dim3(256), 0, st, (const T *)q, ld, c,
                extra, n, H, c_log2, (const float2 *)stats, weights, add ? 1 : 0, sums);
         if (shares > 1)

@@ -24,6 +24,12 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 // down to 2^-19 of the largest one's size, and 0 below 2^-37.  Weights go in as p * 2^kShift, with a reference that may be up to 2^kLag below the true
 // maximum.  Next to bf16 operands the weights keep 11 bits, so that the output's own rounding is the only one of note.
 // fp32 takes values as they are in bf16, exact, up to tiles of 2^64, and at 2^64 over E from there on: a sum of weights up to 2^7 each stays finite.
+#ifndef FVAR_P1
+#define FVAR_P1 512
+#endif
+#ifndef FVAR_P2
+#define FVAR_P2 1024
+#endif
 constexpr int kTop = 6, kRoom = 2, kLarge = 64;
 constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
 
@@ -74,6 +80,34 @@ __device__ __forceinline__ void three_pieces(const float *x, bf16x8_t *out)
     for (int p = 0; p < 3; ++p) out[p] = __builtin_bit_cast(bf16x8_t, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
 }
 
+// Queries in two E4M3 numbers per element, with a power of two per row, 2^e, and 2^(e-4) for what the first leaves: the first leaves at most half
+// a step of its binade, eight steps of bf16's eight bits, which the second holds whole.  (Elements below 2^-15 of their row's largest are held to
+// 2^-23 of it, as fp32 sums hold them.)  top: of the row's bits, sign taken off; from it the scale bytes of both pieces, in byte 0 and 1.
+// A row with an element that is not finite becomes NaN, and so do its scores.
+__device__ __forceinline__ uint32_t top_of_eight(uint4 w, uint32_t top)
+{
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, max(x[i] << 16 & 0x7fff0000u, x[i] & 0x7fff0000u));
+    return top;
+}
+__device__ __forceinline__ int piece_bytes(uint32_t top)
+{
+    const int byte = (int)kvb_byte(top >= 0x7f800000u ? 0x3f800000u : top);
+    return byte | (byte - 4) << 8;
+}
+__device__ __forceinline__ void two_pieces(uint32_t a, uint32_t b, uint32_t top, int bytes, int &first, int &second)
+{
+    const float size = __uint_as_float((uint32_t)(bytes & 255) << 23), rest = __uint_as_float((uint32_t)(bytes >> 8) << 23);
+    float x[4] = {bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b)};
+    const uint32_t one = kvb_four(x, size);
+    const floatx2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(one, size, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(one, size, true);
+    x[0] -= lo[0]; x[1] -= lo[1]; x[2] -= hi[0]; x[3] -= hi[1];
+    const bool odd = top >= 0x7f800000u;
+    first = odd ? 0x7f7f7f7f : (int)one;
+    second = odd ? 0 : (int)kvb_four(x, rest);
+}
+
 template <typename T> struct Quad;                           // four consecutive results
 template <> struct Quad<uint16_t> {
     __device__ static __forceinline__ void store(uint16_t *p, float4 v)
@@ -98,17 +132,17 @@ __device__ __forceinline__ int xcd_grouped(int id, int groups, int size)
 // Sixteen rows per workgroup, whose wavefronts take every NW-th tile of 32 keys, a block of the cache, of the workgroup's share [t0, t1) of the
 // key axis, each with a softmax of its own, and meet in LDS at the end.  For the rows of one query or a few, where the
 // cache's way from memory is what counts (each wavefront fetches a tile ahead, no barrier in the loop), and for fp32.
-//   S^T = K Q^T by 16x16x32 MFMAs: a lane holds a quarter of one key as it lies in memory, converts it to bf16 (exact) and
-//     multiplies eight elements at a time; Q follows that order.
+//   S^T = K Q^T by the 16x16x128 block-scaled MFMA: a lane holds a quarter of one key as it lies in memory, Q follows that order in two numbers per
+//     element (see two_pieces).
 //   O^T = V^T P^T: a lane takes pieces of sixteen values as they lie in memory, converts them and leaves them in LDS row by
 //     row, from where the transposing load brings eight keys of one head-dim element; P is in that order already.
-// fp32: Q and P go in as three bf16 numbers each, K and V are exact in one.
-// stats: null, or for every row what its weights were taken against: reference and sum.  scores: null, or [B * heads][rows][pitch] where there
-// is one block of rows, and receives them (not those of tiles without a visible key).
+// fp32: keys are converted too, Q and P go in as three bf16 numbers each, K and V are exact in one.
+// stats: null, or for every row what its weights were taken against: reference and sum.  scores: null, or [B * heads][pitch][rows][32] where there
+// is one block of rows, and receives them by tiles (not those of tiles without a visible key).
 template <typename T, int DH, int NW, bool MASKED>
 __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__restrict__ q, int ld, KvbCache c, int extra,
                                                                 int n, int H, float c_log2, T *__restrict__ o,
-                                                                int nrb, int splits, float *__restrict__ part_o,
+                                                                int nrb, int splits, int chunk, float *__restrict__ part_o,
                                                                 float *__restrict__ part_ml, float2 *__restrict__ stats,
                                                                 float *__restrict__ scores, int pitch)
 {
@@ -125,29 +159,52 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
     int unit = xcd_grouped(blockIdx.x, (int)(gridDim.x / nrb), nrb);
     const int rb = unit % nrb;
     unit /= nrb;
-    const int split = unit % splits;
-    unit /= splits;
+    // shares last: all samples' first shares come first, and the XCDs have as many of them each
+    const int problems = (int)(gridDim.x / (nrb * splits)), split = unit / problems;
+    unit %= problems;
     const int hk = unit % c.heads, b = unit / c.heads;
     const int G = H / c.heads, R = n * G;
     const int len = kvb_length(c, b, extra);
     const int tiles = (len + 31) / 32;
     // (products below 2^30: at most 2^19 tiles and 1024 shares)
-    const int t0 = tiles * split / splits, t1 = tiles * (split + 1) / splits;
+    const int t0 = chunk ? chunk * split : tiles * split / splits, t1 = chunk ? min(t0 + chunk, tiles) : tiles * (split + 1) / splits;
+    if (chunk && split > 0 && t0 >= t1) return;              // a share past the sample's end, which the merge knows of
     const int last = max(tiles - 1, 0), last_row = max(len - 1, 0);
 
     // ---- Q: lane = row, the elements of the lane's part of a key
     const int row = min(rb * 16 + c16, R - 1);
     const T *qsrc = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g4 * (DH / 4);
-    bf16x8_t qf[KS][NP];
+    bf16x8_t qf[F32 ? KS : 1][3];
+    intx8_t qp[2];
+    int qbyte = 0;
+    if constexpr (F32) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        if constexpr (F32) {
+        for (int s = 0; s < KS; ++s) {
             float x[8];
             *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(qsrc + 8 * s);
             *reinterpret_cast<float4 *>(x + 4) = *reinterpret_cast<const float4 *>(qsrc + 8 * s + 4);
             three_pieces(x, qf[s]);
-        } else {
-            qf[s][0] = *reinterpret_cast<const bf16x8_t *>(qsrc + 8 * s);
+        }
+    } else {
+        uint4 w[KS];
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            w[s] = *reinterpret_cast<const uint4 *>(qsrc + 8 * s);
+            top = top_of_eight(w[s], top);
+        }
+        const auto x = __builtin_amdgcn_permlane16_swap(top, top, false, false);
+        top = max(x[0], x[1]);
+        const auto y = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+        top = max(y[0], y[1]);
+        qbyte = piece_bytes(top);
+        qp[0] = qp[1] = intx8_t{0};
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) {
+            int one, two;
+            two_pieces(i & 1 ? w[i / 2].z : w[i / 2].x, i & 1 ? w[i / 2].w : w[i / 2].y, top, qbyte, one, two);
+            qp[0][i] = one;
+            qp[1][i] = two;
         }
     }
 
@@ -171,6 +228,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
         if constexpr (MASKED) x.vis = (uint32_t)__ballot(base + (lane & 31) < len && ahead != 0);
         const int first = MASKED && x.vis ? __builtin_ctz(x.vis) : 0;
         auto place = [&](int i) { return (uint32_t)min(base + (!MASKED || (x.vis >> i & 1) ? i : first), last_row); };
+        // (loads come back in order: the bytes that are wanted first, first)
+        x.ks = Ks[at];
+        x.vs = Vs[at];
         fetch_mask(t + NW);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -181,8 +241,6 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
 #pragma unroll
         for (int j = 0; j < VL; ++j)
             x.v[j] = *reinterpret_cast<const uint4 *>(Vc + place((64 * j + lane) / VP) * DH + lane % VP * 16);
-        x.ks = Ks[at];
-        x.vs = Vs[at];
         if constexpr (!MASKED) x.vis = base + (lane & 31) < len;
     };
 
@@ -217,14 +275,29 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 s[u] = floatx4_t{0};
+                if constexpr (F32) {
 #pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    const uint4 w = x.k[u][i / 2];
-                    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, i & 1 ? bf16_eight(w.z, w.w, ksize) : bf16_eight(w.x, w.y, ksize));
+                    for (int i = 0; i < KS; ++i) {
+                        const uint4 w = x.k[u][i / 2];
+                        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, i & 1 ? bf16_eight(w.z, w.w, ksize) : bf16_eight(w.x, w.y, ksize));
 #pragma unroll
-                    for (int p = NP - 1; p >= 0; --p)
-                        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][p], s[u], 0, 0, 0);
+                        for (int p = 2; p >= 0; --p) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][p], s[u], 0, 0, 0);
+                    }
+                } else {
+                    intx8_t kf = {0};                        // (64-wide rows: the other half of the contraction is 0)
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) {
+                        kf[4 * w] = (int)x.k[u][w].x; kf[4 * w + 1] = (int)x.k[u][w].y;
+                        kf[4 * w + 2] = (int)x.k[u][w].z; kf[4 * w + 3] = (int)x.k[u][w].w;
+                    }
+                    s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[1], s[u], 0, 0, 0, (int)x.ks, 1, qbyte);
+                    s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[0], s[u], 0, 0, 0, (int)x.ks, 0, qbyte);
                 }
+            }
+            if (scores && c16 < R) {
+                float *to = scores + (head * pitch + t) * (size_t)(R * 32) + c16 * 32 + 4 * g4;
+                *reinterpret_cast<floatx4_t *>(to) = s[0];
+                *reinterpret_cast<floatx4_t *>(to + 16) = s[1];
             }
             // ---- values to LDS
             const int ve = (int)__builtin_amdgcn_readfirstlane((int)x.vs) - 127;
@@ -251,11 +324,6 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
                     if (!(mine >> i & 1)) s[0][i] = -INFINITY;
                     if (!(mine >> (16 + i) & 1)) s[1][i] = -INFINITY;
                 }
-            }
-            if (scores && c16 < R) {
-                float *to = scores + (head * R + c16) * (size_t)pitch + (t - NW) * 32 + 4 * g4;
-                *reinterpret_cast<floatx4_t *>(to) = s[0];
-                *reinterpret_cast<floatx4_t *>(to + 16) = s[1];
             }
             const float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
             const bool lags = __builtin_amdgcn_ballot_w64(mx - m_ref > lag) != 0 || E != acc_E;
@@ -369,10 +437,8 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // 128 rows per workgroup, 32 per wavefront, over tiles of 64 keys, two blocks of the cache; bf16.  For the rows of a whole scale, where the
 // matrix cores and the softmax bound the time.
 //   S^T = K Q^T by the 32x32x64 block-scaled MFMA: it takes keys in 8 bits with their scale bytes as they lie in memory, so K is not
-//     converted.  Q goes in as two E4M3 numbers per element, with a power of two per row, 2^e, and 2^(e-4) for what the first leaves:
-//     the first leaves at most half a step of its binade, eight steps of bf16's eight bits, which the second holds whole.  Two
-//     products at twice the rate of bf16 take as long as one of bf16 would, without a conversion of K.  (Elements below 2^-15 of
-//     their row's largest are held to 2^-23 of it, as fp32 sums hold them.)
+//     converted.  Q goes in as two numbers per element (see two_pieces): two products at twice the rate of bf16 take as long as one
+//     of bf16 would, without a conversion of K.
 //   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
 // In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
 // product takes it, as in attention.hip.
@@ -476,30 +542,19 @@ __global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint1
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 w[s][i] = *reinterpret_cast<const uint4 *>(src + 64 * s + 8 * i);
-                const uint32_t x[4] = {w[s][i].x, w[s][i].y, w[s][i].z, w[s][i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) top = max(top, max(x[j] << 16 & 0x7fff0000u, x[j] & 0x7fff0000u));
+                top = top_of_eight(w[s][i], top);
             }
-        {
-            const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-            top = max(both[0], both[1]);
-        }
-        const bool odd = top >= 0x7f800000u;                 // an element that is not finite: no score of the row is a number
-        const uint32_t byte = kvb_byte(odd ? 0x3f800000u : top);
-        qbyte = (int)byte | (int)(byte - 4) << 8;
-        const float size = __uint_as_float(byte << 23), rest = __uint_as_float((byte - 4) << 23);
+        const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+        top = max(both[0], both[1]);
+        qbyte = piece_bytes(top);
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint32_t a = i & 1 ? w[s][i / 2].z : w[s][i / 2].x, d = i & 1 ? w[s][i / 2].w : w[s][i / 2].y;
-                float x[4] = {bf16_lo(a), bf16_hi(a), bf16_lo(d), bf16_hi(d)};
-                const uint32_t one = kvb_four(x, size);
-                const floatx2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(one, size, false);
-                const floatx2_t hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(one, size, true);
-                x[0] -= lo[0]; x[1] -= lo[1]; x[2] -= hi[0]; x[3] -= hi[1];
-                qf[s][0][i] = odd ? 0x7f7f7f7f : (int)one;
-                qf[s][1][i] = odd ? 0 : (int)kvb_four(x, rest);
+                int one, two;
+                two_pieces(i & 1 ? w[s][i / 2].z : w[s][i / 2].x, i & 1 ? w[s][i / 2].w : w[s][i / 2].y, top, qbyte, one, two);
+                qf[s][0][i] = one;
+                qf[s][1][i] = two;
             }
     }
 
@@ -888,8 +943,8 @@ __global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint1
 // rows many; more where a few rows have many shares, whose loads would wait for each other (64 shares of 16 rows: 24 us by one, 3 by 8).
 template <typename T, int DH, int GROUPS>
 __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                                                             int n, int H, int heads, int nrb, int BR, int first, int shares,
-                                                             float c_log2, int total, T *__restrict__ o, float2 *__restrict__ stats)
+                                                             KvbCache c, int extra, int n, int H, int nrb, int BR, int first, int shares,
+                                                             int chunk, float c_log2, int total, T *__restrict__ o, float2 *__restrict__ stats)
 {
     constexpr int W = DH / 4, ROWS = 256 / (W * GROUPS);     // threads of a group, rows of a workgroup
     __shared__ float4 lo[GROUPS > 1 ? 256 : 1];
@@ -897,10 +952,12 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
     const int d = threadIdx.x % W * 4, group = threadIdx.x / W % GROUPS, in_wg = threadIdx.x / (W * GROUPS);
     const int idx = blockIdx.x * ROWS + in_wg;               // row among those of the divided units
     const int r = idx % BR, u = idx / BR, unit = first + u;
-    const int G = H / heads, row = unit % nrb * BR + r, hk = unit / nrb % heads;
-    const long b = unit / nrb / heads;
+    const int G = H / c.heads, row = unit % nrb * BR + r, hk = unit / nrb % c.heads;
+    const long b = unit / nrb / c.heads;
     const bool mine = idx < total && row < n * G;
     const size_t prow = (size_t)u * shares * BR + r;
+    // shares that have been written
+    const int here = chunk && mine ? max(min(((kvb_length(c, (int)b, extra) + 31) / 32 + chunk - 1) / chunk, shares), 1) : shares;
     auto weight = [&](float2 ml, float m) { return ml.y * __builtin_amdgcn_exp2f((ml.x - reference(m)) * c_log2); };
     float m = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -908,13 +965,13 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
         acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y); acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
     };
     if (mine) {
-        for (int s = group; s < shares; s += 4 * GROUPS) {
+        for (int s = group; s < here; s += 4 * GROUPS) {
             float2 ml[4];
             float4 v[4];
             float now = m, w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool there = s + i * GROUPS < shares;  // (instead of one that is not, the first with a weight of 0)
+                const bool there = s + i * GROUPS < here;  // (instead of one that is not, the first with a weight of 0)
                 const size_t at = prow + (size_t)(there ? s + i * GROUPS : s) * BR;
                 ml[i] = *reinterpret_cast<const float2 *>(part_ml + at * 2);
                 v[i] = *reinterpret_cast<const float4 *>(part_o + at * DH + d);
@@ -1111,17 +1168,26 @@ __global__ __launch_bounds__(256) void kvb_weights_few_kernel(KvbCache c, int ex
 {
     const int head = blockIdx.y, b = head / c.heads, len = kvb_length(c, b, extra), key = (blockIdx.x * 256 + threadIdx.x) * 4;
     if (key >= len) return;
-    const float *src = scores + (size_t)head * R * pitch + key;
+    const float *src = scores + ((size_t)head * pitch + key / 32) * (R * 32) + key % 32;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int r = 0; r < R; ++r) {
-        const float2 stat = stats[(size_t)head * R + r];
-        const float4 s = *reinterpret_cast<const float4 *>(src + (size_t)r * pitch);
-        if (!(stat.y > 0.f)) continue;
-        const float m = reference(stat.x), each = 1.0f / stat.y;
-        sum[0] += __builtin_amdgcn_exp2f((s.x - m) * c_log2) * each;
-        sum[1] += __builtin_amdgcn_exp2f((s.y - m) * c_log2) * each;
-        sum[2] += __builtin_amdgcn_exp2f((s.z - m) * c_log2) * each;
-        sum[3] += __builtin_amdgcn_exp2f((s.w - m) * c_log2) * each;
+    for (int r0 = 0; r0 < R; r0 += 4) {                      // four rows' scores at a time on their way
+        float2 stat[4];
+        float4 s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = min(r0 + i, R - 1);
+            stat[i] = stats[(size_t)head * R + r];
+            s[i] = *reinterpret_cast<const float4 *>(src + r * 32);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (r0 + i >= R || !(stat[i].y > 0.f)) continue;
+            const float m = reference(stat[i].x), each = 1.0f / stat[i].y;
+            sum[0] += __builtin_amdgcn_exp2f((s[i].x - m) * c_log2) * each;
+            sum[1] += __builtin_amdgcn_exp2f((s[i].y - m) * c_log2) * each;
+            sum[2] += __builtin_amdgcn_exp2f((s[i].z - m) * c_log2) * each;
+            sum[3] += __builtin_amdgcn_exp2f((s[i].w - m) * c_log2) * each;
+        }
     }
     const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
     float *to = weights + (size_t)head * c.capacity;
@@ -1156,7 +1222,8 @@ static int kvb_block(DType dt, int B, int n, int H, int heads, int length)
 // nrb blocks per (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
 // `ragged`: samples of lengths of their own, which only the GPU knows.
 // waves: wavefronts of a workgroup, which divide a block's keys (16 rows), or its rows and, if there are 8, keys (128 rows).
-struct KvbRun { int block, nrb, units, full, shares, waves; };
+// chunk: 16 rows, samples of lengths of their own: tiles of 32 keys of a share, so that workgroups have as much to do whatever the lengths.
+struct KvbRun { int block, nrb, units, full, shares, waves, chunk; };
 constexpr int kGroupsFrom = 2048, kGroupsTo = 4096;          // lengths at which the choice between one and two groups changes
 static KvbRun kvb_run(int block, int B, int n, int H, int heads, int Dh, int length, bool ragged)
 {
@@ -1165,11 +1232,13 @@ static KvbRun kvb_run(int block, int B, int n, int H, int heads, int Dh, int len
     run.nrb = (n * (H / heads) + block - 1) / block;
     run.units = B * heads * run.nrb;
     run.waves = 4;
+    run.chunk = 0;
     if (block == 16) {
         const int tiles = (length + 31) / 32;
-        const int places = ragged ? 1024 : 512, least = run.units < 256 ? 2 : 8;
+        const int places = ragged ? FVAR_P2 : FVAR_P1, least = run.units < 256 ? 2 : 8;
         const int want = (places + run.units - 1) / run.units, most = tiles / (least * 4);
         run.shares = want < most ? want : most > 0 ? most : 1;
+        if (ragged && run.shares > 1) run.chunk = (tiles + run.shares - 1) / run.shares;
         run.full = run.shares > 1 ? 0 : run.units;
         return run;
     }
@@ -1186,9 +1255,9 @@ static KvbRun kvb_run(int block, int B, int n, int H, int heads, int Dh, int len
     return run;
 }
 
-// Whether the weights come from scores that the attention leaves (see kvb_weights_few_kernel), and the room of a row of them.
+// Whether the weights come from scores that the attention leaves (see kvb_weights_few_kernel), and the tiles of them.
 static bool few_rows(int rows) { return rows <= 16; }
-static size_t score_pitch(int length) { return ((size_t)length + 31) / 32 * 32; }
+static size_t score_tiles(int length) { return ((size_t)length + 31) / 32; }
 
 // Shares of the rows of queries for the weights: where the keys alone do not fill the chip.
 constexpr int kWeightPlaces = 512;
@@ -1215,7 +1284,7 @@ size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, in
         }
     }
     // every row's reference and sum; their scores, or partial sums of at most kWeightPlaces workgroups of 256 keys
-    if (weights) floats += (2 * (size_t)B * n * H + 3) / 4 * 4 + (few_rows(n * (H / heads)) ? (size_t)B * n * H * score_pitch(capacity) : 256 * kWeightPlaces);
+    if (weights) floats += (2 * (size_t)B * n * H + 3) / 4 * 4 + (few_rows(n * (H / heads)) ? (size_t)B * n * H * 32 * score_tiles(capacity) : 256 * kWeightPlaces);
     return floats;
 }
 
@@ -1229,18 +1298,18 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
     const int divided = run.units - run.full;
     float2 *stats = nullptr;
     float *sums = part, *scores = nullptr;
-    const int rows = n * (H / c.heads), pitch = (int)score_pitch(length);
+    const int rows = n * (H / c.heads), pitch = (int)score_tiles(length);
     if (weights) {
         stats = reinterpret_cast<float2 *>(part);
         sums = part + (2 * (size_t)B * n * H + 3) / 4 * 4;
         scores = few_rows(rows) ? sums : nullptr;
-        part = sums + (scores ? (size_t)B * n * H * pitch : 256 * kWeightPlaces);
+        part = sums + (scores ? (size_t)B * n * H * 32 * pitch : 256 * kWeightPlaces);
     }
     float *part_ml = part + (size_t)divided * run.shares * run.block * DH;
     const unsigned wgs = (unsigned)(run.full + divided * run.shares);
 #define FVAR_ROWS(NW, MASKED)                                                                                            \
     launch(kvb_attn_rows_kernel<T, DH, NW, MASKED>, dim3(wgs), dim3(64 * NW), 0, st, (const T *)q, ld, c, extra, n, H,    \
-           c_log2, (T *)o, run.nrb, run.shares, part, part_ml, stats, scores, pitch)
+           c_log2, (T *)o, run.nrb, run.shares, run.chunk, part, part_ml, stats, scores, pitch)
     if (run.block == 16) {
         if (c.mask) FVAR_ROWS(4, true);
         else FVAR_ROWS(4, false);
@@ -1257,10 +1326,10 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
         const int total = divided * run.block, per = 256 / (DH / 4);
         if (run.shares > 8)
             launch(kvb_attn_merge_kernel<T, DH, 8>, dim3((unsigned)((total + per / 8 - 1) / (per / 8))), dim3(256), 0, st, (const float *)part,
-                   (const float *)part_ml, n, H, c.heads, run.nrb, run.block, run.full, run.shares, c_log2, total, (T *)o, stats);
+                   (const float *)part_ml, c, extra, n, H, run.nrb, run.block, run.full, run.shares, run.chunk, c_log2, total, (T *)o, stats);
         else
             launch(kvb_attn_merge_kernel<T, DH, 1>, dim3((unsigned)((total + per - 1) / per)), dim3(256), 0, st, (const float *)part,
-                   (const float *)part_ml, n, H, c.heads, run.nrb, run.block, run.full, run.shares, c_log2, total, (T *)o, stats);
+                   (const float *)part_ml, c, extra, n, H, run.nrb, run.block, run.full, run.shares, run.chunk, c_log2, total, (T *)o, stats);
     }
     if (scores && length > 0) {
         launch(kvb_weights_few_kernel, dim3((unsigned)((length + 1023) / 1024), (unsigned)(B * c.heads)), dim3(256), 0, st, c, extra, rows, c_log2,

@@ -470,13 +470,19 @@ def _rows(t, kind, B: int, rows: int, width: int):
         return _packed(t, kind, B, rows, width), 0
     if not t.is_cuda or t.dtype is not kind:
         raise ValueError(f"tensors handed to fvar must be GPU tensors, here of {kind}")
-    if t.dim() < 3 or t.shape[0] != B or t.shape[1] != rows or t[0, 0].numel() != width or not t[0, 0].is_contiguous():
+    shape, strides, run = t.shape, t.stride(), 1
+    for i in range(len(shape) - 1, 1, -1):                    # (a view of a row, to ask it, takes longer than a launch)
+        if shape[i] != 1 and strides[i] != run:
+            run = -1
+            break
+        run *= shape[i]
+    if len(shape) < 3 or shape[0] != B or shape[1] != rows or run != width:
         raise ValueError(f"[{B}, {rows}, ...] with contiguous rows of {width} elements is wanted, got shape "
-                         f"{tuple(t.shape)} with strides {t.stride()}")
-    ld = t.stride(1) if rows > 1 else t.stride(0)
+                         f"{tuple(shape)} with strides {strides}")
+    ld = strides[1] if rows > 1 else strides[0]
     if ld < width:                                            # rows that share memory, or one broadcast over them: 0 would mean packed
         raise ValueError(f"rows of {width} elements cannot be {ld} elements apart: a copy of the tensor is wanted")
-    if B > 1 and t.stride(0) != rows * ld:
+    if B > 1 and strides[0] != rows * ld:
         raise ValueError("the rows of all samples have to be equally far apart")
     return t.data_ptr(), ld
 

@@ -9,11 +9,12 @@ namespace fvar {
 
 // Sixteen elements of a head, eight pairs, per thread; T rows per workgroup.  The angles of the workgroup's rows are made once, in LDS, for all heads
 // of queries and keys: 64 of them serve 8192 elements of 32 + 32 heads of 128.  A thread keeps to its pairs and its row and goes from head to
-// head with them in registers.
-template <typename E, int DH, int T, bool INTER>
+// head with them in registers, FLY heads on their way at a time.  Memory-bound: 6400 rows of 32 + 32 heads of 128 in bf16 take 40 us with results
+// past the caches (5.2 TB/s), 43 through them; four rows per workgroup 46, eight 53.  Few rows take their launch: 32 of 32 + 8 heads 3.7 us.
+template <typename E, int DH, int T, bool INTER, bool PAST>
 __global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, RopeRows k, const int32_t *__restrict__ pos, int rows)
 {
-    constexpr int ITEMS = DH / 16, SLOTS = 256 / ITEMS / T, PER = Elem<E>::kPerChunk, HALF = 8 / PER;   // HALF: chunks of eight elements
+    constexpr int FLY = T == 1 ? 1 : 2, ITEMS = DH / 16, SLOTS = 256 / ITEMS / T, PER = Elem<E>::kPerChunk, HALF = 8 / PER;   // HALF: chunks of eight elements
     __shared__ float2 turn[T][DH / 2];
     const int tid = threadIdx.x, pairs = r.dim / 2, row0 = blockIdx.x * T;
     for (int i = tid; i < T * pairs; i += 256) {
@@ -27,6 +28,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, Rope
         turn[t][pair] = make_float2(fmaf(-lo, s, c) * r.magnitude, fmaf(lo, c, s) * r.magnitude);
     }
     __syncthreads();
+    auto put = [](E *to, uint4 v) {
+        typedef uint32_t uintx4_t __attribute__((ext_vector_type(4)));
+        if (PAST) __builtin_nontemporal_store(uintx4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<uintx4_t *>(to));
+        else *reinterpret_cast<uint4 *>(to) = v;
+    };
     const int item = tid % ITEMS, t = tid / ITEMS % T, slot = tid / ITEMS / T + blockIdx.y * SLOTS, step = gridDim.y * SLOTS;
     const size_t row = row0 + t;
     if (row >= (size_t)rows) return;
@@ -42,41 +48,58 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, Rope
             hi = lo + part / 2;
         }
     }
-    for (int h = slot; h < q.heads + k.heads; h += step) {
-        const bool is_q = h < q.heads;
-        const int head = is_q ? h : h - q.heads;
-        const E *src = (const E *)(is_q ? q.in : k.in) + row * (size_t)(is_q ? q.ld_in : k.ld_in) + head * DH;
-        E *dst = (E *)(is_q ? q.out : k.out) + row * (size_t)(is_q ? q.ld_out : k.ld_out) + head * DH;
-        if (!turned && src == dst) continue;
-        float x[16];
+    // FLY heads on their way at a time
+    const int heads = q.heads + k.heads;
+    for (int h0 = slot; h0 < heads; h0 += FLY * step) {
+        uint4 raw[FLY][2 * HALF];
+        E *dst[FLY];
 #pragma unroll
-        for (int i = 0; i < HALF; ++i) {
-            Elem<E>::unpack(*reinterpret_cast<const uint4 *>(src + lo + i * PER), x + i * PER);
-            Elem<E>::unpack(*reinterpret_cast<const uint4 *>(src + hi + i * PER), x + 8 + i * PER);
-        }
-        if (turned) {
+        for (int f = 0; f < FLY; ++f) {
+            const int h = min(h0 + f * step, heads - 1);
+            const bool is_q = h < q.heads;
+            const int head = is_q ? h : h - q.heads;
+            const E *src = (const E *)(is_q ? q.in : k.in) + row * (size_t)(is_q ? q.ld_in : k.ld_in) + head * DH;
+            dst[f] = (E *)(is_q ? q.out : k.out) + row * (size_t)(is_q ? q.ld_out : k.ld_out) + head * DH;
+            if (h0 + f * step >= heads || (!turned && src == dst[f])) dst[f] = nullptr;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int one = INTER ? 2 * i : i, two = INTER ? 2 * i + 1 : i + 8;
-                const float a = x[one], b = x[two];
-                x[one] = fmaf(a, c[i], -(b * s[i]));
-                x[two] = fmaf(a, s[i], b * c[i]);
+            for (int i = 0; i < HALF; ++i) {
+                raw[f][i] = *reinterpret_cast<const uint4 *>(src + lo + i * PER);
+                raw[f][HALF + i] = *reinterpret_cast<const uint4 *>(src + hi + i * PER);
             }
         }
 #pragma unroll
-        for (int i = 0; i < HALF; ++i) {
-            *reinterpret_cast<uint4 *>(dst + lo + i * PER) = Elem<E>::pack(x + i * PER);
-            *reinterpret_cast<uint4 *>(dst + hi + i * PER) = Elem<E>::pack(x + 8 + i * PER);
+        for (int f = 0; f < FLY; ++f) {
+            if (!dst[f]) continue;
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 2 * HALF; ++i) Elem<E>::unpack(raw[f][i], x + i * PER);
+            if (turned) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int one = INTER ? 2 * i : i, two = INTER ? 2 * i + 1 : i + 8;
+                    const float a = x[one], b = x[two];
+                    x[one] = fmaf(a, c[i], -(b * s[i]));
+                    x[two] = fmaf(a, s[i], b * c[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) {
+                put(dst[f] + lo + i * PER, Elem<E>::pack(x + i * PER));
+                put(dst[f] + hi + i * PER, Elem<E>::pack(x + 8 + i * PER));
+            }
         }
     }
 }
 
 void launch_rope(DType dt, const RopeTable &r, const RopeRows &q, const RopeRows &k, const int32_t *pos, int rows, int Dh, hipStream_t st)
 {
-#define FVAR_ROPE(E, DH, T)                                                                                              \
-    (r.interleaved ? launch(rope_kernel<E, DH, T, true>, dim3((unsigned)((rows + T - 1) / T)), dim3(256), 0, st, r, q, k, pos, rows) \
-                   : launch(rope_kernel<E, DH, T, false>, dim3((unsigned)((rows + T - 1) / T)), dim3(256), 0, st, r, q, k, pos, rows))
-#define FVAR_ROPE_T(E, DH) (rows >= 2048 ? FVAR_ROPE(E, DH, 4) : FVAR_ROPE(E, DH, 1))
+    const bool past = (size_t)rows * (q.heads + k.heads) * Dh * (dt == DType::BF16 ? 2 : 4) > (32u << 20);   // the L2s together
+#define FVAR_ROPE(E, DH, T, INTER, PAST)                                                                                 \
+    launch(rope_kernel<E, DH, T, INTER, PAST>, dim3((unsigned)((rows + T - 1) / T)), dim3(256), 0, st, r, q, k, pos, rows)
+#define FVAR_ROPE_T(E, DH)                                                                                               \
+    (past          ? (r.interleaved ? FVAR_ROPE(E, DH, 2, true, true) : FVAR_ROPE(E, DH, 2, false, true))                 \
+     : rows >= 2048 ? (r.interleaved ? FVAR_ROPE(E, DH, 2, true, false) : FVAR_ROPE(E, DH, 2, false, false))              \
+                    : (r.interleaved ? FVAR_ROPE(E, DH, 1, true, false) : FVAR_ROPE(E, DH, 1, false, false)))
     if (dt == DType::BF16) {
         if (Dh == 64) FVAR_ROPE_T(uint16_t, 64);
         else FVAR_ROPE_T(uint16_t, 128);

@@ -8,7 +8,7 @@
 namespace fvar {
 
 // Key of a row: hidden ones below all others, late ones above, a weight that is not a number above all numbers.
-constexpr uint32_t kHidden = 0u, kLate = 0xffffffffu, kNoNumber = 0xfffffffeu;
+constexpr uint32_t kHidden = 0u, kNothing = 0x80000000u, kLate = 0xffffffffu, kNoNumber = 0xfffffffeu;   // kNothing: a weight of 0
 __device__ __forceinline__ uint32_t row_key(float weight, bool seen, bool late)
 {
     const uint32_t key = weight != weight ? kNoNumber : score_key(weight);
@@ -23,7 +23,7 @@ template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void kvb_rank_kernel(KvbCache c, const float *__restrict__ weights, int keep, int recent,
                                                                int32_t *__restrict__ idx, int32_t *__restrict__ counts)
 {
-    __shared__ int late_here[kSelWaves], seen_here[kSelWaves];
+    __shared__ int late_here[kSelWaves], seen_here[kSelWaves], some_here[kSelWaves];
     const int tid = threadIdx.x, b = blockIdx.x / c.heads, len = kvb_length(c, b, 0);
     const int from = max(len - recent, 0);                   // the first late row
     const float *w = weights + (size_t)blockIdx.x * c.capacity;
@@ -31,12 +31,15 @@ __global__ __launch_bounds__(kSelThreads) void kvb_rank_kernel(KvbCache c, const
     int32_t *out = idx + (size_t)blockIdx.x * keep;
     auto key_at = [&](int i) { return row_key(w[i], !mask || mask[i] != 0, i >= from); };
 
-    uint32_t key[KPT > 0 ? KPT : 1], lo = 0xffffffffu, hi = 0u;
-    int late = 0, seen = 0;
+    // Rows that have got nothing are many, and far from all others: the range in which the last row to stay is looked for is that of the
+    // others, or, where those are too few, the rest.
+    uint32_t key[KPT > 0 ? KPT : 1], lo = 0xffffffffu, hi = 0u, least = 0xffffffffu;
+    int late = 0, seen = 0, some = 0;
     auto look = [&](uint32_t x) {
         late += x == kLate;
         seen += x != kHidden;
-        if (x != kLate && x != kHidden) { lo = min(lo, x); hi = max(hi, x); }
+        if (x != kLate && x > kNothing) { ++some; lo = min(lo, x); hi = max(hi, x); }
+        if (x != kHidden) least = min(least, x);
     };
     if constexpr (KPT > 0) {
         float weight[KPT];
@@ -57,12 +60,16 @@ __global__ __launch_bounds__(kSelThreads) void kvb_rank_kernel(KvbCache c, const
         for (int i = tid; i < len; i += kSelThreads) look(key_at(i));
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { late += __shfl_xor(late, o); seen += __shfl_xor(seen, o); }
-    if ((tid & 63) == 0) { late_here[tid >> 6] = late; seen_here[tid >> 6] = seen; }
+    for (int o = 32; o > 0; o >>= 1) {
+        late += __shfl_xor(late, o);
+        seen += __shfl_xor(seen, o);
+        some += __shfl_xor(some, o);
+    }
+    if ((tid & 63) == 0) { late_here[tid >> 6] = late; seen_here[tid >> 6] = seen; some_here[tid >> 6] = some; }
     __syncthreads();
-    late = seen = 0;
+    late = seen = some = 0;
 #pragma unroll
-    for (int i = 0; i < kSelWaves; ++i) { late += late_here[i]; seen += seen_here[i]; }
+    for (int i = 0; i < kSelWaves; ++i) { late += late_here[i]; seen += seen_here[i]; some += some_here[i]; }
     const int count = min(keep, seen);
     for (int i = count + tid; i < keep; i += kSelThreads) out[i] = -1;
     if (blockIdx.x % c.heads == 0 && tid == 0) counts[b] = count;
@@ -74,7 +81,13 @@ __global__ __launch_bounds__(kSelThreads) void kvb_rank_kernel(KvbCache c, const
         __shared__ SelectLds<KPT> sh;
         uint32_t T = kNoNumber;                              // late rows alone
         int need_eq = 0;
-        if (count > late) select_threshold<KPT>(key, len, count - late, lo, hi, sh, T, need_eq);
+        int want = count - late;
+        if (want > some) {                                   // (keys above hi are not counted)
+            want -= some;
+            lo = least;
+            hi = kNothing;
+        }
+        if (want > 0) select_threshold<KPT>(key, len, want, lo, hi, sh, T, need_eq);
         select_sweep<KPT>(key, len, T, need_eq, sh, emit);
     } else {
         __shared__ SelectStreamLds sh;

@@ -1015,11 +1015,12 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
 // adds up exp2((s - reference) * c - log2(sum)) over the rows, each key's in its own registers: no atomics, one order.  64 rows at a time come
 // through LDS for the four wavefronts, by DMA while the ones before are at work (fp32: 32 rows, in three pieces of bf16).  A row whose weights
 // are not numbers adds nothing.
-//   grid: (blocks of 256 keys, B * heads, shares of the rows); shares: as partial sums [share][B * heads][256 * gridDim.x].
+//   A workgroup: a block of 256 keys of one of `heads` (sample, kv head), and a share of its rows; several shares leave partial sums
+// [share][heads][256 * blocks].
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict__ q, int ld, KvbCache c, int extra, int n, int H, float c_log2,
                                                              const float2 *__restrict__ stats, float *__restrict__ weights, int add,
-                                                             float *__restrict__ part)
+                                                             float *__restrict__ part, int blocks, int heads, int shares)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NP = F32 ? 3 : 1, KS = DH / 16, CH = DH / 8;   // CH: chunks of eight elements of a row
@@ -1027,11 +1028,13 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     __shared__ uint4 ql[2][NP][ROWS * CH];
     const int tid = threadIdx.x, lane = tid & 63, rl = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int head = blockIdx.y, b = head / c.heads, hk = head % c.heads;
+    // the blocks of a head, which read the same rows of queries, on one XCD, unless samples differ in length
+    const int id = c.lens ? blockIdx.x : xcd_contiguous(blockIdx.x, gridDim.x);
+    const int block = id % blocks, head = id / blocks % heads, share = id / blocks / heads, b = head / c.heads, hk = head % c.heads;
     const int G = H / c.heads, R = n * G, len = kvb_length(c, b, extra);
-    const int key0 = blockIdx.x * 256 + wave * 64;
-    if ((int)blockIdx.x * 256 >= len) return;                // (of the whole workgroup)
-    const int tiles = (R + ROWS - 1) / ROWS, t0 = (int)((long)tiles * blockIdx.z / gridDim.z), t1 = (int)((long)tiles * (blockIdx.z + 1) / gridDim.z);
+    const int key0 = block * 256 + wave * 64;
+    if (block * 256 >= len) return;                          // (of the whole workgroup)
+    const int tiles = (R + ROWS - 1) / ROWS, t0 = (int)((long)tiles * share / shares), t1 = (int)((long)tiles * (share + 1) / shares);
 
     // ---- rows of queries: chunks are turned by the row's number, so that the rows of sixteen lanes that read one chunk lie in all banks
     auto turn = [](int row) { return DH == 128 ? row & 15 : (row >> 1) & 7; };
@@ -1091,7 +1094,52 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
         }
     }
 
-    floatx16_t acc[2] = {floatx16_t{0}, floatx16_t{0}};
+    // The weights of 32 rows are made beside the products of the next ones, an exponential or two for each product (fp32, with three products
+    // where bf16 has one and no registers for both: after their own).
+    floatx16_t acc[2] = {floatx16_t{0}, floatx16_t{0}}, s[2] = {floatx16_t{0}, floatx16_t{0}};
+    float m = 0.f, off = -INFINITY, both = -INFINITY;        // of the rows whose scores s are
+    bool plain = true;
+    auto weigh = [&]() {
+        // the difference first, exact near the reference; at most 1: scores of 2^20 and more differ by more than that between
+        // two ways to add their products up, and 0 for what is not a number
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                acc[u][i] += __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(s[u][i] - m, c_log2, off)), 0.f, 1.f);
+    };
+    // reference and sum as one number, the same for all keys: off by 2^-25 of itself
+    auto weigh_plain = [&](int e) { acc[e >> 4][e & 15] += __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], c_log2, both)); };
+    auto finish = [&]() {
+        if (plain) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) weigh_plain(e);
+        } else {
+            weigh();
+        }
+    };
+    auto products = [&](auto beside, int buffer, int j) {
+        constexpr int EACH = 32 / (2 * KS);
+        floatx16_t now[2] = {floatx16_t{0}, floatx16_t{0}};
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            bf16x8_t qf[NP];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) qf[p] = __builtin_bit_cast(bf16x8_t, ql[buffer][p][(j * 32 + rl) * CH + ((g * KS + i) ^ turn(rl))]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) now[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][i], qf[p], now[u], 0, 0, 0);
+                if constexpr (decltype(beside)::value) {
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e) weigh_plain((2 * i + u) * EACH + e);
+                }
+            }
+        }
+        s[0] = now[0];
+        s[1] = now[1];
+    };
+
     if (t0 < t1) put(0);
     for (int t = t0; t < t1; ++t) {
         float2 stat[SETS];
@@ -1102,37 +1150,22 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
         if (t + 1 < t1) fetch(t + 1, buffer ^ 1);
 #pragma unroll
         for (int j = 0; j < SETS; ++j) {
-            floatx16_t s[2] = {floatx16_t{0}, floatx16_t{0}};
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {
-#pragma unroll
-                for (int p = NP - 1; p >= 0; --p) {
-                    const bf16x8_t qf = __builtin_bit_cast(bf16x8_t, ql[buffer][p][(j * 32 + rl) * CH + ((g * KS + i) ^ turn(rl))]);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][i], qf, s[u], 0, 0, 0);
-                }
+            if (!F32 && __builtin_expect(plain, 1)) {
+                products(std::true_type{}, buffer, j);
+            } else {
+                if constexpr (!F32) weigh();
+                products(std::false_type{}, buffer, j);
             }
             const bool there = t * ROWS + j * 32 + rl < R, counts = there && stat[j].y > 0.f;
-            const float m = counts ? reference(stat[j].x) : 0.f, off = counts ? -__builtin_amdgcn_logf(stat[j].y) : -INFINITY;
-            const float both = fmaf(-m, c_log2, off);
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(fabsf(m * c_log2) >= 4096.f || there != counts) == 0, 1)) {
-                // reference and sum as one number, the same for all keys: off by 2^-25 of itself
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[u][i] += __builtin_amdgcn_exp2f(fmaf(s[u][i], c_log2, both));
-            } else {
-                // the difference first, exact near the reference; at most 1: scores of 2^20 and more differ by more than that between
-                // two ways to add their products up, and 0 for what is not a number
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        acc[u][i] += __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(s[u][i] - m, c_log2, off)), 0.f, 1.f);
-            }
+            m = counts ? reference(stat[j].x) : 0.f;
+            off = counts ? -__builtin_amdgcn_logf(stat[j].y) : -INFINITY;
+            both = fmaf(-m, c_log2, off);
+            plain = __builtin_amdgcn_ballot_w64(fabsf(m * c_log2) >= 4096.f || there != counts) == 0;
+            if constexpr (F32) finish();
         }
         if (t + 1 < t1) put(buffer ^ 1);
     }
+    if constexpr (!F32) finish();
 
     // ---- sums over the rows of a tile: 32 lanes; the lane then takes one key
     float mine = 0.f;
@@ -1153,8 +1186,8 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     const int key = key0 + 32 * mu + 8 * (mi >> 2) + 4 * g + (mi & 3);
     if (key >= len) return;
     if (c.mask && c.mask[(size_t)b * c.capacity + key] == 0) mine = 0.f;
-    if (gridDim.z > 1) {
-        part[((size_t)blockIdx.z * gridDim.y + head) * (256 * gridDim.x) + key] = mine;
+    if (shares > 1) {
+        part[((size_t)share * heads + head) * (256 * blocks) + key] = mine;
         return;
     }
     float *to = weights + (size_t)head * c.capacity + key;
@@ -1336,8 +1369,8 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
                (const float2 *)stats, (const float *)scores, pitch, weights, add ? 1 : 0);
     } else if (weights && length > 0) {
         const int blocks = (length + 255) / 256, shares = weight_shares(B, c.heads, length, rows);
-        launch(kvb_weights_kernel<T, DH>, dim3((unsigned)blocks, (unsigned)(B * c.heads), (unsigned)shares), dim3(256), 0, st, (const T *)q, ld, c,
-               extra, n, H, c_log2, (const float2 *)stats, weights, add ? 1 : 0, sums);
+        launch(kvb_weights_kernel<T, DH>, dim3((unsigned)(blocks * B * c.heads * shares)), dim3(256), 0, st, (const T *)q, ld, c, extra, n, H, c_log2,
+               (const float2 *)stats, weights, add ? 1 : 0, sums, blocks, B * c.heads, shares);
         if (shares > 1)
             launch(kvb_weights_join_kernel, dim3((unsigned)blocks, (unsigned)(B * c.heads)), dim3(256), 0, st, c, extra, (const float *)sums,
                    256 * blocks, shares, weights, add ? 1 : 0);

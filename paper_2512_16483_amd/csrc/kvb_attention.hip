@@ -24,12 +24,6 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 // down to 2^-19 of the largest one's size, and 0 below 2^-37.  Weights go in as p * 2^kShift, with a reference that may be up to 2^kLag below the true
 // maximum.  Next to bf16 operands the weights keep 11 bits, so that the output's own rounding is the only one of note.
 // fp32 takes values as they are in bf16, exact, up to tiles of 2^64, and at 2^64 over E from there on: a sum of weights up to 2^7 each stays finite.
-#ifndef FVAR_P1
-#define FVAR_P1 512
-#endif
-#ifndef FVAR_P2
-#define FVAR_P2 1024
-#endif
 constexpr int kTop = 6, kRoom = 2, kLarge = 64;
 constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
 
@@ -936,6 +930,76 @@ __global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint1
     }
 }
 
+// Shares of a unit's keys that have been written (see kvb_attn_rows_kernel's chunk).
+__device__ __forceinline__ int shares_written(int len, int shares, int chunk)
+{
+    return chunk ? max(min(((len + 31) / 32 + chunk - 1) / chunk, shares), 1) : shares;
+}
+
+// Weights of the rows where one block of sixteen rows is all, and kvb_attn_rows_kernel has left their scores: those are a few bytes for every
+// key, which a second look at the keys would be 128 for.  Four keys per thread; workgroup `id` of `blocks` for every head.  The rows' references
+// and sums come from stats, or, where the keys have been divided, from the shares' (16 threads a row).
+__device__ __forceinline__ void weigh_few(const KvbCache &c, int extra, int R, float c_log2, const float2 *stats, const float *part_ml, int shares,
+                                          int chunk, const float *scores, int pitch, float *weights, int add, int id, int blocks, float unit)
+{
+    __shared__ float2 rows[16];
+    const int head = id / blocks, b = head / c.heads, len = kvb_length(c, b, extra), key = (id % blocks * 256 + threadIdx.x) * 4;
+    if (id % blocks * 1024 >= len) return;                   // (the whole workgroup)
+    const int r = threadIdx.x >> 4, from = threadIdx.x & 15;
+    if (part_ml) {
+        const int here = shares_written(len, shares, chunk);
+        float m = -INFINITY, l = 0.f;
+        for (int s = from; s < here; s += 16) {
+            const float2 x = *reinterpret_cast<const float2 *>(part_ml + (((size_t)head * shares + s) * 16 + r) * 2);
+            const float now = fmaxf(m, x.x);
+            l = l * __builtin_amdgcn_exp2f((m - reference(now)) * c_log2) + x.y * __builtin_amdgcn_exp2f((x.x - reference(now)) * c_log2);
+            m = now;
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) {
+            const float m2 = __shfl_xor(m, o), l2 = __shfl_xor(l, o), now = fmaxf(m, m2);
+            l = l * __builtin_amdgcn_exp2f((m - reference(now)) * c_log2) + l2 * __builtin_amdgcn_exp2f((m2 - reference(now)) * c_log2);
+            m = now;
+        }
+        if (from == 0) rows[r] = make_float2(m, l * unit);
+    } else if (threadIdx.x < R) {
+        rows[threadIdx.x] = stats[(size_t)head * R + threadIdx.x];
+    }
+    __syncthreads();
+    if (key >= len) return;
+    const float *src = scores + ((size_t)head * pitch + key / 32) * (R * 32) + key % 32;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r0 = 0; r0 < R; r0 += 4) {                      // four rows' scores at a time on their way
+        float4 s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = *reinterpret_cast<const float4 *>(src + min(r0 + i, R - 1) * 32);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 stat = rows[min(r0 + i, R - 1)];
+            if (r0 + i >= R || !(stat.y > 0.f)) continue;
+            const float m = reference(stat.x), each = 1.0f / stat.y;
+            sum[0] += __builtin_amdgcn_exp2f((s[i].x - m) * c_log2) * each;
+            sum[1] += __builtin_amdgcn_exp2f((s[i].y - m) * c_log2) * each;
+            sum[2] += __builtin_amdgcn_exp2f((s[i].z - m) * c_log2) * each;
+            sum[3] += __builtin_amdgcn_exp2f((s[i].w - m) * c_log2) * each;
+        }
+    }
+    const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
+    float *to = weights + (size_t)head * c.capacity;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (key + i >= len) return;
+        const float x = !mask || mask[key + i] != 0 ? sum[i] : 0.f;
+        to[key + i] = add ? to[key + i] + x : x;
+    }
+}
+__global__ __launch_bounds__(256) void kvb_weights_few_kernel(KvbCache c, int extra, int R, float c_log2, const float2 *__restrict__ stats,
+                                                              const float *__restrict__ scores, int pitch, float *__restrict__ weights, int add,
+                                                              int blocks)
+{
+    weigh_few(c, extra, R, c_log2, stats, nullptr, 1, 0, scores, pitch, weights, add, blockIdx.x, blocks, 1.f);
+}
+
 // The shares of rows joined: each is a mean and its weight.  A unit is a block of BR rows of one (sample, kv head); the shares
 // of unit first + u lie at [u][share][row].  GROUPS groups of DH/4 threads per row, four head-dim elements a thread: a group takes every
 // GROUPS-th share, four at a time, with a running reference and mean (not the sum: a mean times its weight need not be a number that fp32
@@ -944,8 +1008,15 @@ __global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint1
 template <typename T, int DH, int GROUPS>
 __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
                                                              KvbCache c, int extra, int n, int H, int nrb, int BR, int first, int shares,
-                                                             int chunk, float c_log2, int total, T *__restrict__ o, float2 *__restrict__ stats)
+                                                             int chunk, float c_log2, int total, T *__restrict__ o, float2 *__restrict__ stats,
+                                                             const float *__restrict__ scores, int pitch, float *__restrict__ weights, int add,
+                                                             int merges, int blocks)
 {
+    if (blockIdx.x >= merges) {                              // the rows' weights, which need not wait for the joined results
+        weigh_few(c, extra, n * (H / c.heads), c_log2, nullptr, part_ml, shares, chunk, scores, pitch, weights, add, blockIdx.x - merges, blocks,
+                  sizeof(T) == 4 ? 1.f : 0.00390625f);
+        return;
+    }
     constexpr int W = DH / 4, ROWS = 256 / (W * GROUPS);     // threads of a group, rows of a workgroup
     __shared__ float4 lo[GROUPS > 1 ? 256 : 1];
     __shared__ float2 lm[GROUPS > 1 ? 256 / W : 1];
@@ -957,11 +1028,11 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
     const bool mine = idx < total && row < n * G;
     const size_t prow = (size_t)u * shares * BR + r;
     // shares that have been written
-    const int here = chunk && mine ? max(min(((kvb_length(c, (int)b, extra) + 31) / 32 + chunk - 1) / chunk, shares), 1) : shares;
+    const int here = chunk && mine ? shares_written(kvb_length(c, (int)b, extra), shares, chunk) : shares;
     auto weight = [&](float2 ml, float m) { return ml.y * __builtin_amdgcn_exp2f((ml.x - reference(m)) * c_log2); };
     float m = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](float4 v, float w) {
+    auto put_in = [&](float4 v, float w) {
         acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y); acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
     };
     if (mine) {
@@ -986,7 +1057,7 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
             const float each = sum == 0.f ? 0.f : 1.0f / sum, keep = before * each;
             acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) add(v[i], w[i] * each);
+            for (int i = 0; i < 4; ++i) put_in(v[i], w[i] * each);
             m = now;
         }
     }
@@ -1003,7 +1074,7 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
         const float each = sum == 0.f ? 0.f : 1.0f / sum;
         acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < GROUPS; ++k) add(lo[threadIdx.x + k * W], weight(lm[threadIdx.x / W + k], m) * each);
+        for (int k = 0; k < GROUPS; ++k) put_in(lo[threadIdx.x + k * W], weight(lm[threadIdx.x / W + k], m) * each);
     }
     if (mine) {
         Quad<T>::store(o + (size_t)(b * n + row / G) * H * DH + (size_t)(hk * G + row % G) * DH + d, acc);
@@ -1194,44 +1265,6 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     *to = add ? *to + mine : mine;
 }
 
-// The same where one block of sixteen rows is all, and kvb_attn_rows_kernel has left their scores: those are a few bytes for every key, which a
-// second look at the keys would be 128 for.  Four keys per thread.  grid: (blocks of 1024 keys, B * heads).
-__global__ __launch_bounds__(256) void kvb_weights_few_kernel(KvbCache c, int extra, int R, float c_log2, const float2 *__restrict__ stats,
-                                                              const float *__restrict__ scores, int pitch, float *__restrict__ weights, int add)
-{
-    const int head = blockIdx.y, b = head / c.heads, len = kvb_length(c, b, extra), key = (blockIdx.x * 256 + threadIdx.x) * 4;
-    if (key >= len) return;
-    const float *src = scores + ((size_t)head * pitch + key / 32) * (R * 32) + key % 32;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int r0 = 0; r0 < R; r0 += 4) {                      // four rows' scores at a time on their way
-        float2 stat[4];
-        float4 s[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = min(r0 + i, R - 1);
-            stat[i] = stats[(size_t)head * R + r];
-            s[i] = *reinterpret_cast<const float4 *>(src + r * 32);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (r0 + i >= R || !(stat[i].y > 0.f)) continue;
-            const float m = reference(stat[i].x), each = 1.0f / stat[i].y;
-            sum[0] += __builtin_amdgcn_exp2f((s[i].x - m) * c_log2) * each;
-            sum[1] += __builtin_amdgcn_exp2f((s[i].y - m) * c_log2) * each;
-            sum[2] += __builtin_amdgcn_exp2f((s[i].z - m) * c_log2) * each;
-            sum[3] += __builtin_amdgcn_exp2f((s[i].w - m) * c_log2) * each;
-        }
-    }
-    const uint8_t *mask = c.mask ? c.mask + (size_t)b * c.capacity : nullptr;
-    float *to = weights + (size_t)head * c.capacity;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (key + i >= len) return;
-        const float x = !mask || mask[key + i] != 0 ? sum[i] : 0.f;
-        to[key + i] = add ? to[key + i] + x : x;
-    }
-}
-
 __global__ __launch_bounds__(256) void kvb_weights_join_kernel(KvbCache c, int extra, const float *__restrict__ part, int pitch, int shares,
                                                                float *__restrict__ weights, int add)
 {
@@ -1268,8 +1301,14 @@ static KvbRun kvb_run(int block, int B, int n, int H, int heads, int Dh, int len
     run.chunk = 0;
     if (block == 16) {
         const int tiles = (length + 31) / 32;
-        const int places = ragged ? FVAR_P2 : FVAR_P1, least = run.units < 256 ? 2 : 8;
-        const int want = (places + run.units - 1) / run.units, most = tiles / (least * 4);
+        // Eight wavefronts where there are more tiles than that to divide and at most a workgroup for every CU: fewer shares to join, or
+        // none (1 query of 16 heads of 128 over 600 keys 8.2 us in one launch, 7.7 + 2.8 by four; fp32, 2 x 128 x 552, 16 heads of 64, 8.8, 10.1).
+        run.waves = run.units <= 256 && tiles > 16 && !ragged ? 8 : 4;
+        // Enough wavefronts for two on every SIMD; four where samples differ, with shares as long as each other, so that a CU that has had
+        // short ones takes more (32 samples of 1 to 16921 keys, 8 kv heads, 512, 1024, 2048, 4096 places: 127, 105, 108, 102 us and a joining of
+        // 4.8, 4.8, 4.8, 9.8).  Each with two tiles per wavefront at least, or eight where every CU has a workgroup already.
+        const int places = ragged ? 1024 : 2048 / run.waves, least = run.units < 256 ? 2 : 8;
+        const int want = (places + run.units - 1) / run.units, most = tiles / (least * run.waves);
         run.shares = want < most ? want : most > 0 ? most : 1;
         if (ragged && run.shares > 1) run.chunk = (tiles + run.shares - 1) / run.shares;
         run.full = run.shares > 1 ? 0 : run.units;
@@ -1298,7 +1337,7 @@ static int weight_shares(int B, int heads, int length, int rows)
 {
     const long wgs = (long)B * heads * ((length + 255) / 256);
     long shares = wgs > 0 ? kWeightPlaces / wgs : 1;
-    if (shares > (rows + 31) / 32) shares = (rows + 31) / 32;
+    if (shares > (rows + 31) / 128) shares = (rows + 31) / 128;      // (fewer than 128 rows each are not worth a joining)
     return (int)(shares > 8 ? 8 : shares < 1 ? 1 : shares);
 }
 
@@ -1344,8 +1383,8 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
     launch(kvb_attn_rows_kernel<T, DH, NW, MASKED>, dim3(wgs), dim3(64 * NW), 0, st, (const T *)q, ld, c, extra, n, H,    \
            c_log2, (T *)o, run.nrb, run.shares, run.chunk, part, part_ml, stats, scores, pitch)
     if (run.block == 16) {
-        if (c.mask) FVAR_ROWS(4, true);
-        else FVAR_ROWS(4, false);
+        if (run.waves == 8) { if (c.mask) FVAR_ROWS(8, true); else FVAR_ROWS(8, false); }
+        else { if (c.mask) FVAR_ROWS(4, true); else FVAR_ROWS(4, false); }
 #undef FVAR_ROWS
     } else if constexpr (sizeof(T) == 2) {
 #define FVAR_TILES(KG)                                                                                                   \
@@ -1355,18 +1394,23 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
         else FVAR_TILES(1);
 #undef FVAR_TILES
     }
+    const int few_blocks = (length + 1023) / 1024, few_wgs = scores ? few_blocks * B * c.heads : 0;
     if (divided) {
         const int total = divided * run.block, per = 256 / (DH / 4);
-        if (run.shares > 8)
-            launch(kvb_attn_merge_kernel<T, DH, 8>, dim3((unsigned)((total + per / 8 - 1) / (per / 8))), dim3(256), 0, st, (const float *)part,
-                   (const float *)part_ml, c, extra, n, H, run.nrb, run.block, run.full, run.shares, run.chunk, c_log2, total, (T *)o, stats);
-        else
-            launch(kvb_attn_merge_kernel<T, DH, 1>, dim3((unsigned)((total + per - 1) / per)), dim3(256), 0, st, (const float *)part,
-                   (const float *)part_ml, c, extra, n, H, run.nrb, run.block, run.full, run.shares, run.chunk, c_log2, total, (T *)o, stats);
+        const bool eight = run.shares > 8 || (run.shares > 2 && total <= 1024);
+        const int merges = eight ? (total + per / 8 - 1) / (per / 8) : (total + per - 1) / per;
+#define FVAR_MERGE(GROUPS)                                                                                               \
+    launch(kvb_attn_merge_kernel<T, DH, GROUPS>, dim3((unsigned)(merges + few_wgs)), dim3(256), 0, st, (const float *)part, (const float *)part_ml, \
+           c, extra, n, H, run.nrb, run.block, run.full, run.shares, run.chunk, c_log2, total, (T *)o, stats, (const float *)scores, pitch, weights, \
+           add ? 1 : 0, merges, few_blocks)
+        if (eight) FVAR_MERGE(8);
+        else FVAR_MERGE(1);
+#undef FVAR_MERGE
     }
-    if (scores && length > 0) {
-        launch(kvb_weights_few_kernel, dim3((unsigned)((length + 1023) / 1024), (unsigned)(B * c.heads)), dim3(256), 0, st, c, extra, rows, c_log2,
-               (const float2 *)stats, (const float *)scores, pitch, weights, add ? 1 : 0);
+    if (scores) {
+        if (!divided && length > 0)
+            launch(kvb_weights_few_kernel, dim3((unsigned)few_wgs), dim3(256), 0, st, c, extra, rows, c_log2, (const float2 *)stats,
+                   (const float *)scores, pitch, weights, add ? 1 : 0, few_blocks);
     } else if (weights && length > 0) {
         const int blocks = (length + 255) / 256, shares = weight_shares(B, c.heads, length, rows);
         launch(kvb_weights_kernel<T, DH>, dim3((unsigned)(blocks * B * c.heads * shares)), dim3(256), 0, st, (const T *)q, ld, c, extra, n, H, c_log2,

@@ -442,8 +442,10 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // The loop goes by halves of a tile: beside the softmax of one stand the scores of the next and the products of the one before, in turn.
 // KG = 2: two groups of four wavefronts on the same rows, each with half of the keys and LDS of its own, which meet at the end:
 // as full a CU as two workgroups make, without partial results in memory.
-template <int DH, int KG>
-__global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvbCache c, int extra,
+// WAVES, of a SIMD: 3 with 64-wide rows where there are at least two rounds of workgroups (30 heads, 16 x 410 x 1281 keys 136 to 124 us, 32 x 400 x 3000 513 to 443); with 2 there
+// are registers for products that start from the reference, an addition less per weight.
+template <int DH, int KG, int WAVES>
+__global__ __launch_bounds__(256 * KG, WAVES) void kvb_attn_tiles_kernel(const uint16_t *__restrict__ q, int ld, KvbCache c, int extra,
                                                                 int n, int H, float c_log2, uint16_t *__restrict__ o, int nrb,
                                                                 int full_units, int shares, float *__restrict__ part_o,
                                                                 float *__restrict__ part_ml, float2 *__restrict__ stats)
@@ -573,14 +575,18 @@ __global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint1
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = floatx16_t{0};
     float l_run = 0.f, most = -1.f;                          // most: the sum of weights from which on a reference is looked for; < 0: no reference yet
-    float m_ref = 0.f;                                       // the reference: the products that make scores start from - m_ref
+    constexpr bool FROM = WAVES == 2;
+    float m_ref = 0.f;                                       // the reference; FROM: the products that make scores start from - m_ref
     floatx16_t bases = floatx16_t{0};
     auto set_base = [&](float m) {
         m_ref = m;
+        if constexpr (FROM) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) bases[i] = -m;
-        asm volatile("" : "+v"(bases));
+            for (int i = 0; i < 16; ++i) bases[i] = -m;
+            asm volatile("" : "+v"(bases));
+        }
     };
+    auto exponent = [&](float score) { return fmaf(FROM ? score : score - m_ref, c_log2, kShift); };
     int E = -200, E_now = -200, acc_E = -200;                // of the values converted last, of the tile at work, of the sums
 
     // A thread's values as they came; the rows that can be seen, and the size of the values: E is the same in all wavefronts.
@@ -720,8 +726,8 @@ __global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint1
                     x[2 * p1 + 1] = __builtin_amdgcn_exp2f(x[2 * p1 + 1]);
                 }
                 if (p0 < 8) {
-                    x[2 * p0] = fmaf(s[half][2 * p0], c_log2, kShift);
-                    x[2 * p0 + 1] = fmaf(s[half][2 * p0 + 1], c_log2, kShift);
+                    x[2 * p0] = exponent(s[half][2 * p0]);
+                    x[2 * p0 + 1] = exponent(s[half][2 * p0 + 1]);
                 }
                 if (p2 >= 0 && p2 < 8) {
                     a = p2 ? a + x[2 * p2] : x[0];
@@ -767,11 +773,14 @@ __global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint1
             mx = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
             const bool had = most >= 0.f, none = !had && mx == -INFINITY;
             float alpha = 1.f;
-            if (!none && (!had || mx > 0.f)) {
-                s[0] -= mx;
-                s[1] -= mx;
-                set_base(m_ref + mx);
-                alpha = __builtin_amdgcn_exp2f(-mx * c_log2);
+            const float over = FROM ? mx : mx - m_ref;
+            if (!none && (!had || over > 0.f)) {
+                if constexpr (FROM) {
+                    s[0] -= mx;
+                    s[1] -= mx;
+                }
+                set_base(FROM ? m_ref + mx : mx);
+                alpha = __builtin_amdgcn_exp2f(-over * c_log2);
             }
             if (!had) alpha = 0.f;
             const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E_now, -200));
@@ -786,8 +795,8 @@ __global__ __launch_bounds__(256 * KG, 2) void kvb_attn_tiles_kernel(const uint1
             sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[half][i], c_log2, kShift));
-                const float y = __builtin_amdgcn_exp2f(fmaf(s[half][i + 1], c_log2, kShift));
+                const float x = __builtin_amdgcn_exp2f(exponent(s[half][i]));
+                const float y = __builtin_amdgcn_exp2f(exponent(s[half][i + 1]));
                 sum += x + y;
                 const f16x2v_t p = __builtin_convertvector((floatx2_t{x, y}), f16x2v_t);
                 pf[half][i >> 3][i & 7] = p[0];
@@ -1277,12 +1286,16 @@ __global__ __launch_bounds__(256) void kvb_weights_join_kernel(KvbCache c, int e
 }
 
 // Blocks of how many rows of a (sample, kv head) an attention is run by: 16 (kvb_attn_rows_kernel) or 128 (kvb_attn_tiles_kernel, bf16
-// only).
+// only).  The first starts and ends soonest and is bound by the work, which it does at less than half the other's pace; the other fetches
+// and converts for 128 rows whatever there are, and joins groups and shares.  So the work decides, and at half a block and less three times as
+// much of it is still by 16.  us by 16 / by 128, 16 heads of 128: 1 x 144 rows x 265 keys 7 / 15, 1 x 400 x 921 15 / 23, 1 x 576 x 1497
+// 27 / 26, 1 x 200 x 4813 33 / 26, 16 x 100 x 1000 42 / 27; 8 x 64 x 2521 29 / 34, 16 x 64 x 3000 63 / 50, 8 x 32 x 3001 20 / 35,
+// 32 x 32 x 3001 92 / 85, 32 x 48 x 3001 117 / 101; 30 heads of 64: 1 x 324 x 640 10 / 13, 2 x 231 x 871 15 / 16, 8 x 169 x 316 20 / 14.
 static int kvb_block(DType dt, int B, int n, int H, int heads, int length)
 {
     const int rows = n * (H / heads);
-    if (dt != DType::BF16 || rows <= 48) return 16;
-    return (long)B * heads * ((rows + 15) / 16) * length <= (rows <= 64 ? 1l << 21 : 1l << 20) ? 16 : 128;
+    if (dt != DType::BF16 || rows <= 16) return 16;
+    return (long)B * heads * ((rows + 15) / 16) * length <= (rows <= 64 ? 16l << 17 : 5l << 17) ? 16 : 128;
 }
 
 // nrb blocks per (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
@@ -1314,7 +1327,13 @@ static KvbRun kvb_run(int block, int B, int n, int H, int heads, int Dh, int len
         run.full = run.shares > 1 ? 0 : run.units;
         return run;
     }
-    const int two = 512;
+    // Up to a workgroup on every CU: two groups of wavefronts in each, and shares where there are half as many or fewer.  Otherwise, and over long
+    // caches where shares of one group leave fewer CUs idle, two workgroups on every CU (three of 64-wide rows, where there are two rounds of
+    // them); those beyond the last full round are divided.  Pieces have four tiles at least for each group.  A quarter of a round more than one
+    // by two groups, divided, is also soonest done so, if there is enough to divide.  us by one / by two groups, 16 heads of 128: 4 x 300 x 2500 keys
+    // 55 / 43, 1 x 200 x 4813 31 / 26, 1 x 1152 x 6000 78 / 87, 1 x 1600 x 2500 56 / 44; 30 heads of 64: 8 x 231 x 871 26 / 31, 1 x 640 x 6000 54 / 63, 1 x 1152
+    // x 6000 121 / 83.
+    const int two = Dh == 64 && run.units >= 2 * 768 ? 768 : 512;
     bool groups = run.units <= 256 || (run.units <= 320 && length >= kGroupsFrom);
     if (run.units <= 256 && length >= kGroupsTo) groups = (two / run.units) * 256 * 8 <= (256 / run.units) * two * 9;
     const int slots = groups ? 256 : two, rest = run.units % slots, most = (length + 63) / 64 / (groups ? 8 : 4);
@@ -1387,11 +1406,12 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
         else { if (c.mask) FVAR_ROWS(4, true); else FVAR_ROWS(4, false); }
 #undef FVAR_ROWS
     } else if constexpr (sizeof(T) == 2) {
-#define FVAR_TILES(KG)                                                                                                   \
-    launch(kvb_attn_tiles_kernel<DH, KG>, dim3(wgs), dim3(256 * KG), 0, st, (const T *)q, ld, c, extra, n, H,             \
+#define FVAR_TILES(KG, WAVES)                                                                                            \
+    launch(kvb_attn_tiles_kernel<DH, KG, WAVES>, dim3(wgs), dim3(256 * KG), 0, st, (const T *)q, ld, c, extra, n, H,             \
            c_log2, (T *)o, run.nrb, run.full, run.shares, part, part_ml, stats)
-        if (run.waves == 8) FVAR_TILES(2);
-        else FVAR_TILES(1);
+        if (run.waves == 8) FVAR_TILES(2, 2);
+        else if (DH == 64 && run.units >= 2 * 768) FVAR_TILES(1, DH == 64 ? 3 : 2);
+        else FVAR_TILES(1, 2);
 #undef FVAR_TILES
     }
     const int few_blocks = (length + 1023) / 1024, few_wgs = scores ? few_blocks * B * c.heads : 0;

@@ -26,8 +26,8 @@
  * run the block over one.
  *
  * fvar_rope_apply turns queries and keys by their positions.  fvar_kvb_append, fvar_kvb_read and fvar_kvb_attention do
- * for a cache held in 8 bits (fvar_kvb) what the calls above do for one of 4; its attention can also return the weight that every
- * row has got, by which fvar_kvb_evict drops rows.
+ * for a cache held in 8 bits (fvar_kvb) what the calls above do for one of 4, fvar_block_forward_*_kvb run the block over one, with
+ * its queries and keys turned; the attention can also return the weight that every row has got, by which fvar_kvb_evict drops rows.
  *
  * Conventions common to every call
  *  - Every tensor pointer is DEVICE memory owned by the caller, row-major,
@@ -403,6 +403,18 @@ fvar_status fvar_kvb_read(fvar_ctx *ctx, fvar_stream stream, const fvar_kvb *kv,
 size_t fvar_kvb_attention_workspace_bytes(const fvar_ctx *ctx, const fvar_kvb *kv, int32_t B, int32_t n, int32_t weights);
 fvar_status fvar_kvb_attention(fvar_ctx *ctx, fvar_stream stream, const void *q, int32_t ld, const fvar_kvb *kv, int32_t B,
                                int32_t n, void *o, float *weights, int32_t add, void *ws, size_t ws_bytes);
+
+/* fvar_block_forward_dense / _pruned over an 8-bit cache, as the calls over a 4-bit one.  rope, pos: NULL, or queries and new keys are turned
+ * by their positions before the keys are written, pos: device int32 [B][rows][axes], rows = M (dense) or k (pruned, in idx_keep order).
+ * weights, add: as in fvar_kvb_attention, of all rows with the new ones.
+ * ws: at least fvar_block_kvb_workspace_bytes(ctx,kv,B,rows,weights != NULL). */
+size_t fvar_block_kvb_workspace_bytes(const fvar_ctx *ctx, const fvar_kvb *kv, int32_t B, int32_t rows, int32_t weights);
+fvar_status fvar_block_forward_dense_kvb(fvar_ctx *ctx, fvar_stream stream, const fvar_block_weights *w, const void *x, int32_t B,
+                                         int32_t M, const fvar_kvb *kv, const fvar_rope *rope, const int32_t *pos, float *weights,
+                                         int32_t add, void *y, void *ws, size_t ws_bytes);
+fvar_status fvar_block_forward_pruned_kvb(fvar_ctx *ctx, fvar_stream stream, const fvar_block_weights *w, const void *x, int32_t B,
+                                          int32_t M, const int32_t *idx_keep, int32_t k, const fvar_kvb *kv, const fvar_rope *rope,
+                                          const int32_t *pos, float *weights, int32_t add, void *y_keep, void *ws, size_t ws_bytes);
 
 /* Eviction: of the rows that a sample holds and that from->mask does not hide, `keep` stay for every kv head (all of them, where they are
  * not more): the last `recent` of all the rows that the sample holds, and of the others those with the largest weights, equal ones from the

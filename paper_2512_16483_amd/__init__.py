@@ -28,6 +28,7 @@ EXPORTS = (
     "fvar_block_kvq_workspace_bytes", "fvar_block_forward_dense_kvq", "fvar_block_forward_pruned_kvq",
     "fvar_rope_init", "fvar_rope_apply", "fvar_kvb_append", "fvar_kvb_read", "fvar_kvb_attention_workspace_bytes",
     "fvar_kvb_attention", "fvar_kvb_evict_workspace_bytes", "fvar_kvb_evict",
+    "fvar_block_kvb_workspace_bytes", "fvar_block_forward_dense_kvb", "fvar_block_forward_pruned_kvb",
 )
 
 
@@ -165,6 +166,12 @@ def load_library() -> C.CDLL:
     lib.fvar_kvb_evict_workspace_bytes.restype = sz
     lib.fvar_kvb_evict.argtypes = [vp, vp, kvb, vp, i32, i32, i32, kvb, vp, vp, vp, vp, sz]
     lib.fvar_kvb_evict.restype = C.c_int
+    lib.fvar_block_kvb_workspace_bytes.argtypes = [vp, kvb, i32, i32, i32]
+    lib.fvar_block_kvb_workspace_bytes.restype = sz
+    lib.fvar_block_forward_dense_kvb.argtypes = [vp, vp, C.POINTER(_Weights), vp, i32, i32, kvb, rope, vp, vp, i32, vp, vp, sz]
+    lib.fvar_block_forward_dense_kvb.restype = C.c_int
+    lib.fvar_block_forward_pruned_kvb.argtypes = [vp, vp, C.POINTER(_Weights), vp, i32, i32, vp, i32, kvb, rope, vp, vp, i32, vp, vp, sz]
+    lib.fvar_block_forward_pruned_kvb.restype = C.c_int
     lib.fvar_profile_enable.argtypes = [vp, i32]
     lib.fvar_profile_enable.restype = C.c_int
     lib.fvar_profile_read.argtypes = [vp, C.POINTER(_ProfileEntry), i32]
@@ -594,6 +601,35 @@ def fvar_kvb_attention(ctx: Context, q, kv: KVB, B: int, n: int, o, ws=None, wei
     op = _packed(o, kind, B, n, ctx.hidden)
     ctx.check(ctx.lib.fvar_kvb_attention(ctx.handle, _stream(stream), qp, ld, kv._for(ctx, B), B, n, op, _row_weights(weights, kv, B),
                                          1 if add else 0, _ptr(ws), _nbytes(ws)))
+
+
+def fvar_block_kvb_workspace_bytes(ctx: Context, kv: KVB, B: int, rows: int, weights: bool = False) -> int:
+    return ctx.lib.fvar_block_kvb_workspace_bytes(ctx.handle, kv._for(ctx, B), B, rows, 1 if weights else 0)
+
+
+def _turned(rope: Optional[Rope], pos, B: int, rows: int):
+    if rope is None:
+        if pos is not None:
+            raise ValueError("positions without rope")
+        return None, None
+    return rope._ref, _packed(pos, _kind("i32"), B, rows, rope.axes)
+
+
+def fvar_block_forward_dense_kvb(ctx: Context, w: dict, x, B: int, M: int, kv: KVB, y, ws, rope: Optional[Rope] = None, pos=None, weights=None,
+                                 add: bool = False, stream=None) -> None:
+    ws_, kind, (rp, pp) = _weights(w), _kind(ctx.dtype), _turned(rope, pos, B, M)
+    xp, yp = _packed(x, kind, B, M, ctx.hidden), _packed(y, kind, B, M, ctx.hidden)
+    ctx.check(ctx.lib.fvar_block_forward_dense_kvb(ctx.handle, _stream(stream), C.byref(ws_), xp, B, M, kv._for(ctx, B), rp, pp,
+                                                   _row_weights(weights, kv, B), 1 if add else 0, yp, _ptr(ws), _nbytes(ws)))
+
+
+def fvar_block_forward_pruned_kvb(ctx: Context, w: dict, x, B: int, M: int, idx_keep, k: int, kv: KVB, y_keep, ws, rope: Optional[Rope] = None,
+                                  pos=None, weights=None, add: bool = False, stream=None) -> None:
+    ws_, kind, (rp, pp) = _weights(w), _kind(ctx.dtype), _turned(rope, pos, B, k)
+    xp, yp = _packed(x, kind, B, M, ctx.hidden), _packed(y_keep, kind, B, k, ctx.hidden)
+    ctx.check(ctx.lib.fvar_block_forward_pruned_kvb(ctx.handle, _stream(stream), C.byref(ws_), xp, B, M,
+                                                    _packed(idx_keep, _kind("i32"), B, k, 1), k, kv._for(ctx, B), rp, pp,
+                                                    _row_weights(weights, kv, B), 1 if add else 0, yp, _ptr(ws), _nbytes(ws)))
 
 
 def fvar_kvb_evict_workspace_bytes(ctx: Context, kv: KVB, B: int, keep: int) -> int:

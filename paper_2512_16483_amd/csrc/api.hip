@@ -148,14 +148,25 @@ fvar_status validate_indices(fvar_ctx *c, hipStream_t st, const int32_t *idx_kee
 
 struct BlockWs {
     char *x_keep, *u, *q, *att, *h1, *hid;
-    char *k_new, *v_new;                      // new K / V rows on their way into a 4-bit cache
+    char *k_new, *v_new;                      // new K / V rows on their way into a 4-bit or 8-bit cache
     float *part;                              // partial results of the attention and of each linear layer in turn
     fvar::GemmPlan qkv, o, fc1, fc2;          // how each linear layer runs at this row count
     size_t total;
 };
 
-// q: null, or the 4-bit cache that the block runs over
-BlockWs carve(const fvar_ctx *c, void *ws, int B, int rows, const fvar_kvq *q = nullptr)
+// The cache that a block runs over, one of three kinds (the others are null); with 8 bits, what turns queries and keys (or null) and the rows'
+// weights (or null).
+struct BlockCache {
+    const fvar_kv *kv = nullptr;
+    const fvar_kvq *kvq = nullptr;
+    const fvar_kvb *kvb = nullptr;
+    const fvar_rope *rope = nullptr;
+    const int32_t *pos = nullptr;
+    float *weights = nullptr;
+    int32_t add = 0;
+};
+
+BlockWs carve(const fvar_ctx *c, void *ws, int B, int rows, const BlockCache &q = {})
 {
     const size_t es = esize(c), R = (size_t)B * rows, d = c->cfg.hidden, F = c->cfg.ffn_hidden;
     BlockWs w;
@@ -173,11 +184,13 @@ BlockWs carve(const fvar_ctx *c, void *ws, int B, int rows, const fvar_kvq *q = 
     w.qkv = plan.layer[0]; w.o = plan.layer[1]; w.fc1 = plan.layer[2]; w.fc2 = plan.layer[3];
     size_t part = plan.floats;
     w.k_new = w.v_new = nullptr;
-    if (q) {
+    if (q.kvq || q.kvb) {
         w.k_new = w.att;                      // both are read before their buffers are written
         w.v_new = w.h1;
-        const size_t att = fvar::kvq_attention_scratch_floats(dtype(c), B, rows, c->cfg.heads, q->kv_heads, c->cfg.head_dim,
-                                                              q->capacity);
+        const size_t att = q.kvq ? fvar::kvq_attention_scratch_floats(dtype(c), B, rows, c->cfg.heads, q.kvq->kv_heads, c->cfg.head_dim,
+                                                                      q.kvq->capacity)
+                                 : fvar::kvb_attention_scratch_floats(dtype(c), B, rows, c->cfg.heads, q.kvb->kv_heads, c->cfg.head_dim,
+                                                                      q.kvb->capacity, q.weights != nullptr);
         if (att > part) part = att;
     }
     w.part = part ? reinterpret_cast<float *>(take(part * sizeof(float))) : nullptr;
@@ -256,19 +269,42 @@ size_t kvb_attention_ws(const fvar_ctx *c, const fvar_kvb *kv, int B, int n, boo
                                                        weights) * sizeof(float));
 }
 
+// Settings and positions that rows can be turned by.
+fvar_status check_rope(fvar_ctx *c, const fvar_rope *r, const int32_t *pos, const char *who)
+{
+    if (!r || !pos) return fail(c, FVAR_ERR_INVALID_ARG, "%s: rope or pos is NULL", who);
+    if (r->axes < 1 || r->axes > 2 || r->dim < 1 || r->dim > c->cfg.head_dim || r->dim % (16 * r->axes))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: dim=%d with axes=%d: a multiple of 16*axes up to head_dim is wanted", who, r->dim, r->axes);
+    if (reinterpret_cast<uintptr_t>(pos) & 3) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pos is not 4-byte aligned", who);
+    return FVAR_OK;
+}
+
+fvar::RopeTable rope_table(const fvar_rope *r)
+{
+    fvar::RopeTable t;
+    t.dim = r->dim;
+    t.axes = r->axes;
+    t.interleaved = r->interleaved != 0;
+    t.magnitude = (float)r->magnitude;
+    std::memcpy(t.turns, r->turns, sizeof(t.turns));
+    return t;
+}
+
 bool overlap(const void *a, size_t na, const void *b, size_t nb)
 {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return a && b && x < y + nb && y < x + na;
 }
 
-// The block on `rows` rows per sample, over one of two kinds of cache (the other is null).
+// The block on `rows` rows per sample, over one of three kinds of cache.
 // idx == nullptr: rows are x's own rows (rows == M).
 fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights *w, const void *x,
-                          int B, int M, const int32_t *idx, int rows, const fvar_kv *kv, const fvar_kvq *kvq, void *y,
+                          int B, int M, const int32_t *idx, int rows, const BlockCache &cache, void *y,
                           void *ws, size_t ws_bytes, const char *who)
 {
-    if (!w || !x || (!kv && !kvq) || !y) return fail(c, FVAR_ERR_INVALID_ARG, "%s: null argument", who);
+    const fvar_kv *kv = cache.kv;
+    const bool held = cache.kvq || cache.kvb;                // in 4 or 8 bits
+    if (!w || !x || (!kv && !held) || !y) return fail(c, FVAR_ERR_INVALID_ARG, "%s: null argument", who);
     if (B < 1 || M < 1 || rows < 1 || rows > M)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: need B>=1 and 1<=rows<=M (B=%d M=%d rows=%d)", who, B,
                     M, rows);
@@ -276,11 +312,12 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: idx_keep may be NULL only when k == M", who);
     if (!w->w_qkv || !w->w_o || !w->w_fc1 || !w->w_fc2)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: weight matrix pointer is NULL", who);
-    if (kvq) {
-        const fvar_status ks = check_cache(c, st, kvq, B, rows, who);
+    if (held) {
+        const fvar_status ks = cache.kvq ? check_cache(c, st, cache.kvq, B, rows, who) : check_cache(c, st, cache.kvb, B, rows, who);
         if (ks != FVAR_OK) return ks;
-        if (kvq->kv_heads != c->cfg.heads)
-            return fail(c, FVAR_ERR_UNSUPPORTED, "%s: kv_heads=%d, and the block has %d heads of keys", who, kvq->kv_heads,
+        const int kv_heads = cache.kvq ? cache.kvq->kv_heads : cache.kvb->kv_heads;
+        if (kv_heads != c->cfg.heads)
+            return fail(c, FVAR_ERR_UNSUPPORTED, "%s: kv_heads=%d, and the block has %d heads of keys", who, kv_heads,
                         c->cfg.heads);
         if ((int64_t)B * rows * c->cfg.heads > (1 << 25))
             return fail(c, FVAR_ERR_UNSUPPORTED, "%s: B*rows*heads exceeds 2^25", who);
@@ -288,6 +325,11 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
         (int64_t)kv->len + rows > (int64_t)kv->capacity)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: KV cache too small (len=%d + rows=%d > capacity=%d)",
                     who, kv->len, rows, kv->capacity);
+    if (cache.rope) {
+        const fvar_status rs = check_rope(c, cache.rope, cache.pos, who);
+        if (rs != FVAR_OK) return rs;
+    }
+    if (!aligned16(cache.weights)) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
     const void *ptrs[] = {x, y, kv ? kv->k : nullptr, kv ? kv->v : nullptr, w->w_qkv, w->w_o, w->w_fc1, w->w_fc2, w->ln1_g, w->ln1_b,
                           w->ln2_g, w->ln2_b, w->b_qkv, w->b_o, w->b_fc1, w->b_fc2, ws};
     for (const void *p : ptrs)
@@ -308,7 +350,7 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
         if ((int64_t)B * 8 > 65535 || c->cfg.heads > 65535)
             return fail(c, FVAR_ERR_UNSUPPORTED, "%s: B or heads exceeds the launch grid limits", who);
     }
-    BlockWs s = carve(c, ws, B, rows, kvq);
+    BlockWs s = carve(c, ws, B, rows, cache);
     const size_t ws_need = s.total + (c->debug_checks ? kCanaryBytes : 0);
     if (!ws || ws_bytes < ws_need)
         return fail(c, FVAR_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, ws_need,
@@ -339,17 +381,30 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
     timed(c, st, "gemm_qkv", [&] {
         fvar::GemmEpilogue e;
         e.bias = w->b_qkv; e.out0 = s.q; e.ld0 = d; e.split = d;
-        e.kcache = kvq ? s.k_new : kv->k; e.vcache = kvq ? s.v_new : kv->v; e.hd = d;
-        e.cap = kvq ? rows : kv->capacity; e.len = kvq ? 0 : kv->len;
+        e.kcache = held ? s.k_new : kv->k; e.vcache = held ? s.v_new : kv->v; e.hd = d;
+        e.cap = held ? rows : kv->capacity; e.len = held ? 0 : kv->len;
         e.rows_per_sample = rows;
         launched &= fvar::launch_gemm(dt, s.u, w->w_qkv, R, 3 * d, d, e, s.qkv, s.part, st);
     });
-    if (kvq) {
+    if (cache.kvq) {
         timed(c, st, "kvq_append", [&] {
-            fvar::launch_kvq_append(dt, s.k_new, s.v_new, d, kvq_cache(kvq), B, rows, Dh, st);
+            fvar::launch_kvq_append(dt, s.k_new, s.v_new, d, kvq_cache(cache.kvq), B, rows, Dh, st);
         });
         timed(c, st, "kvq_attention", [&] {
-            fvar::launch_kvq_attention(dt, s.q, d, kvq_cache(kvq), rows, B, rows, H, Dh, c->scale, s.att, s.part, st);
+            fvar::launch_kvq_attention(dt, s.q, d, kvq_cache(cache.kvq), rows, B, rows, H, Dh, c->scale, s.att, s.part, st);
+        });
+    } else if (cache.kvb) {
+        if (cache.rope) {
+            timed(c, st, "rope", [&] {
+                fvar::launch_rope(dt, rope_table(cache.rope), {s.q, s.q, H, d, d}, {s.k_new, s.k_new, H, d, d}, cache.pos, R, Dh, st);
+            });
+        }
+        timed(c, st, "kvb_append", [&] {
+            fvar::launch_kvb_append(dt, s.k_new, s.v_new, d, kvb_cache(cache.kvb), B, rows, Dh, st);
+        });
+        timed(c, st, "kvb_attention", [&] {
+            fvar::launch_kvb_attention(dt, s.q, d, kvb_cache(cache.kvb), rows, B, rows, H, Dh, c->scale, s.att, cache.weights,
+                                       cache.add != 0, s.part, st);
         });
     } else {
         timed(c, st, "attention", [&] {
@@ -564,7 +619,9 @@ fvar_status fvar_block_forward_dense(fvar_ctx *c, fvar_stream stream, const fvar
                                      void *ws, size_t ws_bytes)
 {
     if (!c) return FVAR_ERR_INVALID_ARG;
-    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, nullptr, M, kv, nullptr, y, ws,
+    BlockCache cache;
+    cache.kv = kv;
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, nullptr, M, cache, y, ws,
                          ws_bytes, "fvar_block_forward_dense");
 }
 
@@ -574,7 +631,9 @@ fvar_status fvar_block_forward_pruned(fvar_ctx *c, fvar_stream stream, const fva
                                       size_t ws_bytes)
 {
     if (!c) return FVAR_ERR_INVALID_ARG;
-    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, idx_keep, k, kv, nullptr, y_keep,
+    BlockCache cache;
+    cache.kv = kv;
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, idx_keep, k, cache, y_keep,
                          ws, ws_bytes, "fvar_block_forward_pruned");
 }
 
@@ -582,7 +641,9 @@ fvar_status fvar_block_forward_dense_kvq(fvar_ctx *c, fvar_stream stream, const 
                                          int32_t B, int32_t M, const fvar_kvq *kv, void *y, void *ws, size_t ws_bytes)
 {
     if (!c) return FVAR_ERR_INVALID_ARG;
-    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, nullptr, M, nullptr, kv, y, ws, ws_bytes,
+    BlockCache cache;
+    cache.kvq = kv;
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, nullptr, M, cache, y, ws, ws_bytes,
                          "fvar_block_forward_dense_kvq");
 }
 
@@ -591,14 +652,50 @@ fvar_status fvar_block_forward_pruned_kvq(fvar_ctx *c, fvar_stream stream, const
                                           void *y_keep, void *ws, size_t ws_bytes)
 {
     if (!c) return FVAR_ERR_INVALID_ARG;
-    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, idx_keep, k, nullptr, kv, y_keep, ws, ws_bytes,
+    BlockCache cache;
+    cache.kvq = kv;
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, idx_keep, k, cache, y_keep, ws, ws_bytes,
                          "fvar_block_forward_pruned_kvq");
 }
 
 size_t fvar_block_kvq_workspace_bytes(const fvar_ctx *c, const fvar_kvq *kv, int32_t B, int32_t rows)
 {
     if (!c || !cache_sizes(c, kv, B, rows)) return 0;
-    return carve(c, nullptr, B, rows, kv).total + (c->debug_checks ? kCanaryBytes : 0);
+    BlockCache cache;
+    cache.kvq = kv;
+    return carve(c, nullptr, B, rows, cache).total + (c->debug_checks ? kCanaryBytes : 0);
+}
+
+size_t fvar_block_kvb_workspace_bytes(const fvar_ctx *c, const fvar_kvb *kv, int32_t B, int32_t rows, int32_t weights)
+{
+    if (!c || !cache_sizes(c, kv, B, rows)) return 0;
+    float some;
+    BlockCache cache;
+    cache.kvb = kv;
+    cache.weights = weights ? &some : nullptr;               // (only whether there are any)
+    return carve(c, nullptr, B, rows, cache).total + (c->debug_checks ? kCanaryBytes : 0);
+}
+
+fvar_status fvar_block_forward_dense_kvb(fvar_ctx *c, fvar_stream stream, const fvar_block_weights *w, const void *x, int32_t B, int32_t M,
+                                         const fvar_kvb *kv, const fvar_rope *rope, const int32_t *pos, float *weights, int32_t add, void *y,
+                                         void *ws, size_t ws_bytes)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    BlockCache cache;
+    cache.kvb = kv; cache.rope = rope; cache.pos = pos; cache.weights = weights; cache.add = add;
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, nullptr, M, cache, y, ws, ws_bytes,
+                         "fvar_block_forward_dense_kvb");
+}
+
+fvar_status fvar_block_forward_pruned_kvb(fvar_ctx *c, fvar_stream stream, const fvar_block_weights *w, const void *x, int32_t B, int32_t M,
+                                          const int32_t *idx_keep, int32_t k, const fvar_kvb *kv, const fvar_rope *rope, const int32_t *pos,
+                                          float *weights, int32_t add, void *y_keep, void *ws, size_t ws_bytes)
+{
+    if (!c) return FVAR_ERR_INVALID_ARG;
+    BlockCache cache;
+    cache.kvb = kv; cache.rope = rope; cache.pos = pos; cache.weights = weights; cache.add = add;
+    return block_forward(c, static_cast<hipStream_t>(stream), w, x, B, M, idx_keep, k, cache, y_keep, ws, ws_bytes,
+                         "fvar_block_forward_pruned_kvb");
 }
 
 fvar_status fvar_kvq_append(fvar_ctx *c, fvar_stream stream, const fvar_kvq *kv, const void *k, const void *v, int32_t ld,
@@ -707,31 +804,24 @@ fvar_status fvar_rope_apply(fvar_ctx *c, fvar_stream stream, const fvar_rope *r,
 {
     if (!c) return FVAR_ERR_INVALID_ARG;
     const char *who = "fvar_rope_apply";
-    if (!r || !pos) return fail(c, FVAR_ERR_INVALID_ARG, "%s: null argument", who);
+    const fvar_status rs = check_rope(c, r, pos, who);
+    if (rs != FVAR_OK) return rs;
     if (B < 1 || n < 1) return fail(c, FVAR_ERR_INVALID_ARG, "%s: need B>=1 and n>=1 (B=%d n=%d)", who, B, n);
     if ((int64_t)B * n > (1 << 24)) return fail(c, FVAR_ERR_UNSUPPORTED, "%s: B*n exceeds 2^24", who);
-    if (r->axes < 1 || r->axes > 2 || r->dim < 1 || r->dim > c->cfg.head_dim || r->dim % (16 * r->axes))
-        return fail(c, FVAR_ERR_INVALID_ARG, "%s: dim=%d with axes=%d: a multiple of 16*axes up to head_dim is wanted", who, r->dim, r->axes);
     if (!q && !k) return fail(c, FVAR_ERR_INVALID_ARG, "%s: q and k both NULL", who);
     if (!q != !q_out || !k != !k_out) return fail(c, FVAR_ERR_INVALID_ARG, "%s: an input without its output, or the reverse", who);
     if (kv_heads < 1 || c->cfg.heads % kv_heads)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: kv_heads=%d does not divide heads=%d", who, kv_heads, c->cfg.heads);
-    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || (reinterpret_cast<uintptr_t>(pos) & 3))
-        return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not aligned (16 bytes; pos 4)", who);
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
     const int wq = c->cfg.hidden, wk = kv_heads * c->cfg.head_dim;
     const fvar::RopeRows rows[2] = {{q, q_out, q ? c->cfg.heads : 0, row_pitch(c, ld_q, wq), row_pitch(c, ld_q_out, wq)},
                                     {k, k_out, k ? kv_heads : 0, row_pitch(c, ld_k, wk), row_pitch(c, ld_k_out, wk)}};
     for (const fvar::RopeRows &x : rows)
         if (x.in && (x.ld_in < 0 || x.ld_out < 0 || (x.in == x.out && x.ld_in != x.ld_out)))
             return fail(c, FVAR_ERR_INVALID_ARG, "%s: a row pitch is shorter than a row, no multiple of 16 bytes, or in place not the same", who);
-    fvar::RopeTable t;
-    t.dim = r->dim;
-    t.axes = r->axes;
-    t.interleaved = r->interleaved != 0;
-    t.magnitude = (float)r->magnitude;
-    std::memcpy(t.turns, r->turns, sizeof(t.turns));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    timed(c, st, "rope", [&] { fvar::launch_rope(dtype(c), t, rows[0], rows[1], pos, B * n, c->cfg.head_dim, st); });
+    timed(c, st, "rope", [&] { fvar::launch_rope(dtype(c), rope_table(r), rows[0], rows[1], pos, B * n, c->cfg.head_dim, st); });
     return launch_status(c, who);
 }
 

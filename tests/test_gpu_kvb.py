@@ -51,6 +51,20 @@ def load(kv, k, v):
     return out
 
 
+def fill(kv, L):
+    """Codes drawn as they are, with powers that differ from block to block, in the first rows of a cache; their values."""
+    g, out = np.random.default_rng(11), []
+    for codes, scales in ((kv.k, kv.k_scale), (kv.v, kv.v_scale)):
+        c, s = codes.cpu().numpy().copy(), scales.cpu().numpy().copy()
+        x = np.clip(g.standard_normal((*c.shape[:2], L, c.shape[3]), dtype=np.float32) * 100, -448, 448)
+        c[:, :, :L] = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+        s[:, :, :-(-L // 32)] = g.integers(119, 122, (*s.shape[:2], -(-L // 32)))
+        codes.copy_(torch.from_numpy(c))
+        scales.copy_(torch.from_numpy(s))
+        out.append(kvb.values(c[:, :, :L], s))
+    return out
+
+
 def attend(ctx, q, kv, dtype, B, n, junk=float("nan"), weights=None, **kw):
     o = torch.full((B, n, ctx.heads, ctx.head_dim), junk, dtype=tdtype(dtype), device="cuda")
     size = fv.fvar_kvb_attention_workspace_bytes(ctx, kv, B, n, weights is not None)
@@ -214,15 +228,19 @@ SHAPES = [("bf16", 2, 2, 64, 1, 1, 1), ("bf16", 4, 1, 128, 2, 1, 33), ("bf16", 1
           ("bf16", 30, 30, 64, 2, 7, 100), ("bf16", 30, 10, 64, 1, 37, 95), ("bf16", 16, 16, 128, 2, 130, 333), ("bf16", 8, 2, 128, 1, 300, 64),
           ("bf16", 4, 4, 64, 3, 257, 700), ("bf16", 2, 1, 128, 1, 1000, 1500), ("f32", 4, 4, 64, 2, 1, 40), ("f32", 6, 2, 128, 1, 19, 129),
           ("f32", 16, 16, 64, 2, 128, 552), ("f32", 2, 1, 128, 2, 65, 1000)]
+# three wavefronts per SIMD; whole rounds of workgroups and a divided rest; more keys per workgroup than it holds scale bytes of at once; the
+# same with a single query; one query of few keys by eight wavefronts; fp32 in shares
+LARGE = [("bf16", 30, 30, 64, 32, 200, 70), ("bf16", 16, 16, 128, 33, 129, 1030), ("bf16", 16, 16, 64, 4, 512, 4500), ("bf16", 16, 4, 128, 2, 3, 9000),
+         ("bf16", 16, 16, 64, 1, 1, 700), ("f32", 4, 2, 64, 1, 5, 3000)]
 
 
-@pytest.mark.parametrize("dtype,H,heads,dh,B,n,L", SHAPES)
+@pytest.mark.parametrize("dtype,H,heads,dh,B,n,L", SHAPES + LARGE)
 @pytest.mark.parametrize("kind", ["plain", "ragged", "masked"])
 def test_attention_and_weights(dtype, H, heads, dh, B, n, L, kind):
     g = np.random.default_rng(L + n)
     cap = L + 5
     ctx, kv = ctx_of(H, dh, dtype), empty_cache(B, heads, cap, dh, fill=0x7F)           # NaN wherever nothing is written
-    k, v = load(kv, rows_of(1, B, L, heads, dh, dtype), rows_of(2, B, L, heads, dh, dtype))
+    k, v = load(kv, rows_of(1, B, L, heads, dh, dtype), rows_of(2, B, L, heads, dh, dtype)) if B * L * heads < 3e5 else fill(kv, L)
     q = rows_of(3, B, n, H, dh, dtype, spread=0.2)
     lens, mask = [L] * B, None
     kv.len = L
@@ -383,3 +401,68 @@ def test_debug_checks_look_at_lengths():
     assert e.value.status == fv.FVAR_ERR_INVALID_ARG
     kv.lens = torch.tensor([3, 39], dtype=torch.int32, device="cuda")
     fv.fvar_kvb_append(ctx, kv, x, x, B, 1)
+
+
+# ------------------------------------------------------------------------------------ the block
+@pytest.mark.parametrize("dtype,d,H,B,M,keep,Lp,ragged,turned,weigh", [
+    ("bf16", 256, 4, 2, 40, 40, 30, False, True, True), ("bf16", 256, 2, 2, 100, 37, 65, True, True, True), ("bf16", 512, 8, 1, 300, 300, 100, False, False, True),
+    ("f32", 256, 4, 2, 64, 20, 33, True, True, False), ("f32", 256, 2, 1, 50, 50, 0, False, False, False), ("bf16", 1024, 8, 3, 256, 130, 200, False, True, True)])
+def test_block_over_the_cache(dtype, d, H, B, M, keep, Lp, ragged, turned, weigh):
+    """The block with W_o = 1 and an MLP of 0 gives x + attention: against the oracle's attention over the cache that the block left, whose
+    new rows are the oracle's of the plain block's K and V rows, turned by the call of their own."""
+    dh, F = d // H, 64
+    x = wl.activations_lowrank(B, M, d, seed=100 + M, bf16=dtype == "bf16")
+    g = np.random.default_rng(101)
+    bf = lambda a: wl.round_to_bf16(a) if dtype == "bf16" else a.astype(np.float32)
+    w = {"w_qkv": bf(0.05 * g.standard_normal((3 * d, d))), "b_qkv": bf(0.1 * g.standard_normal(3 * d)), "w_o": np.eye(d, dtype=np.float32),
+         "w_fc1": np.zeros((F, d), np.float32), "w_fc2": np.zeros((d, F), np.float32)}
+    wd = {n: to_dev(a, dtype) for n, a in w.items()}
+    rolled = dict(wd, w_qkv=wd["w_qkv"].roll(d, 0).contiguous(), b_qkv=wd["b_qkv"].roll(d, 0).contiguous())   # q rows come out as K rows
+    ctx = fv.Context(hidden=d, heads=H, head_dim=dh, ffn_hidden=F, dtype=dtype)
+    xd = to_dev(x, dtype)
+    idx = np.stack([np.sort(g.permutation(M)[:keep]) for _ in range(B)]).astype(np.int32)
+    idx_d = torch.from_numpy(idx).cuda()
+    cap = Lp + keep + 2
+
+    def plain(weights):
+        K, V = (torch.zeros((B, cap, H, dh), dtype=tdtype(dtype), device="cuda") for _ in range(2))
+        y = torch.empty((B, keep, d), dtype=tdtype(dtype), device="cuda")
+        ws = torch.empty(fv.fvar_block_workspace_bytes(ctx, B, keep), dtype=torch.uint8, device="cuda")
+        fv.fvar_block_forward_pruned(ctx, weights, xd, B, M, idx_d, keep, K, V, cap, Lp, y, ws)
+        return K[:, Lp:Lp + keep].contiguous(), V[:, Lp:Lp + keep].contiguous()
+
+    (kn, vn), (qn, _) = plain(wd), plain(rolled)
+    r = fv.Rope(dim=32, axes=2, interleaved=True) if turned else None
+    pos = torch.from_numpy(np.stack([idx // 16, idx % 16], -1).astype(np.int32)).cuda() if turned else None
+    if turned:
+        fv.fvar_rope_apply(ctx, r, pos, B, keep, qn, kn)
+    qn, kn, vn = to_np(qn), to_np(kn), to_np(vn)
+    lens = [Lp - 9 * b for b in range(B)] if ragged else [Lp] * B
+    kv = empty_cache(B, H, cap, dh, len=Lp, lens=torch.tensor(lens, dtype=torch.int32, device="cuda") if ragged else None)
+    if Lp:
+        load(kv, rows_of(102, B, Lp, H, dh, dtype), rows_of(103, B, Lp, H, dh, dtype))
+    want = []
+    for rows, codes, scales in ((kn, kv.k, kv.k_scale), (vn, kv.v, kv.v_scale)):
+        want.append((codes.cpu().numpy().copy(), scales.cpu().numpy().copy()))
+        kvb.append(*want[-1], lens, rows)
+    fv.fvar_debug_checks(ctx, True)                           # with the canary behind the workspace
+    size = fv.fvar_block_kvb_workspace_bytes(ctx, kv, B, keep, weights=weigh)
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    y = torch.empty((B, keep, d), dtype=tdtype(dtype), device="cuda")
+    sums = torch.full((B, H, cap), 0.5, device="cuda") if weigh else None
+    if keep == M:
+        fv.fvar_block_forward_dense_kvb(ctx, wd, xd, B, M, kv, y, ws, rope=r, pos=pos, weights=sums, add=True)
+    else:
+        fv.fvar_block_forward_pruned_kvb(ctx, wd, xd, B, M, idx_d, keep, kv, y, ws, rope=r, pos=pos, weights=sums, add=True)
+    fv.fvar_debug_checks(ctx, False)
+    for (c, s), codes, scales in zip(want, (kv.k, kv.v), (kv.k_scale, kv.v_scale)):
+        assert np.array_equal(codes.cpu().numpy(), c)
+        assert np.array_equal(scales.cpu().numpy(), s)
+    held = [kvb.values(c, s) for c, s in want]
+    ends = [n + keep for n in lens]
+    att, got = kvb.attention(qn, *held, dh ** -0.5, ends)
+    xk = np.stack([x[b, idx[b]] for b in range(B)])
+    check(f"block {dtype} {B}x{keep}", y, xk + att.reshape(B, keep, d), dtype)
+    if weigh:
+        there = (np.arange(cap) < np.array(ends)[:, None])[:, None]
+        check_weights(f"block {dtype} {B}x{keep}", sums, np.where(there, 0.5 + got, 0.5), qn, held[0], dh ** -0.5)

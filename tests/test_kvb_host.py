@@ -112,15 +112,20 @@ BAD_CACHES = [(dict(k=None), 1), (dict(v=None), 1), (dict(k_scale=None), 1), (di
 
 
 @pytest.mark.parametrize("kw,status", BAD_CACHES)
-@pytest.mark.parametrize("name", ["append", "read", "attention", "evict"])
+@pytest.mark.parametrize("name", ["append", "read", "attention", "evict", "dense", "pruned"])
 def test_calls_refuse_a_cache_that_is_none(name, kw, status):
     lib, fake = fv.load_library(), 0x1000
     ctx = fv.Context(hidden=256, heads=4, head_dim=64, ffn_hidden=256)
+    if name in ("dense", "pruned"):
+        kw = dict(dict(kv_heads=4), **kw)
+    w = C.byref(fv._Weights(*[fake] * 12))
     kv, h, to = C.byref(_cache(**kw)), ctx.handle, C.byref(_cache(k=0x500000, v=0x600000, k_scale=0x700000, v_scale=0x800000))
     got = {"append": lambda: lib.fvar_kvb_append(h, None, kv, fake, fake, 0, 1, 1),
            "read": lambda: lib.fvar_kvb_read(h, None, kv, 1, 0, 1, fake, fake),
            "attention": lambda: lib.fvar_kvb_attention(h, None, fake, 0, kv, 1, 1, fake, None, 0, fake, 1 << 40),
-           "evict": lambda: lib.fvar_kvb_evict(h, None, kv, fake, 1, 4, 0, to, 0x900000, None, None, fake, 1 << 40)}[name]()
+           "evict": lambda: lib.fvar_kvb_evict(h, None, kv, fake, 1, 4, 0, to, 0x900000, None, None, fake, 1 << 40),
+           "dense": lambda: lib.fvar_block_forward_dense_kvb(h, None, w, fake, 1, 1, kv, None, None, None, 0, fake, fake, 1 << 40),
+           "pruned": lambda: lib.fvar_block_forward_pruned_kvb(h, None, w, fake, 1, 2, fake, 1, kv, None, None, None, 0, fake, fake, 1 << 40)}[name]()
     assert got == status and lib.fvar_last_error(h)
 
 
@@ -215,6 +220,27 @@ def test_rope_refuses_rows_that_are_none():
     assert apply(ld_q=248) == inv and apply(ld_k=129, ld_k_out=129) == inv and apply(ld_q=264) == inv and apply(ld_q_out=-8) == inv
     assert apply(n=(1 << 24) + 1) == fv.FVAR_ERR_UNSUPPORTED
     assert lib.fvar_rope_apply(None, None, C.byref(good), fake, 1, 1, 2, fake, 0, None, 0, fake, 0, None, 0) == inv
+
+
+def test_block_refuses_what_it_cannot_do():
+    lib, fake, inv = fv.load_library(), 0x1000, fv.FVAR_ERR_INVALID_ARG
+    ctx = fv.Context(hidden=256, heads=4, head_dim=64, ffn_hidden=256)
+    h, w, kv, r = ctx.handle, C.byref(fv._Weights(*[fake] * 12)), _cache(kv_heads=4), _rope()
+    assert lib.fvar_rope_init(C.byref(r)) == 0
+
+    def dense(kv=kv, rope=r, pos=fake, weights=None, ws=fake, size=1 << 40, M=2):
+        return lib.fvar_block_forward_dense_kvb(h, None, w, fake, 1, M, C.byref(kv), None if rope is None else C.byref(rope), pos, weights, 0, fake, ws, size)
+
+    assert dense(kv=_cache(kv_heads=2)) == fv.FVAR_ERR_UNSUPPORTED and dense(M=51) == inv
+    assert dense(pos=None) == inv and dense(pos=0x1001) == inv and dense(rope=_rope(dim=128)) == inv and dense(rope=_rope(axes=3)) == inv
+    assert dense(weights=fake + 8) == inv
+    for weigh in (0, 1):
+        need = lib.fvar_block_kvb_workspace_bytes(h, C.byref(kv), 1, 2, weigh)
+        assert need > 0 and dense(weights=fake if weigh else None, size=need - 1) == fv.FVAR_ERR_WORKSPACE
+    assert dense(ws=None) == fv.FVAR_ERR_WORKSPACE
+    assert lib.fvar_block_kvb_workspace_bytes(h, C.byref(_cache(kv_heads=3)), 1, 2, 0) == 0
+    assert lib.fvar_block_forward_dense_kvb(None, None, w, fake, 1, 1, C.byref(kv), None, None, None, 0, fake, fake, 1 << 40) == inv
+    assert lib.fvar_block_forward_dense_kvb(h, None, w, fake, 1, 1, None, None, None, None, 0, fake, fake, 1 << 40) == inv
 
 
 # ------------------------------------------------------------------------------------ binding

@@ -126,11 +126,12 @@ __device__ __forceinline__ int xcd_grouped(int id, int groups, int size)
 // Sixteen rows per workgroup, whose wavefronts take every NW-th tile of 32 keys, a block of the cache, of the workgroup's share [t0, t1) of the
 // key axis, each with a softmax of its own, and meet in LDS at the end.  For the rows of one query or a few, where the
 // cache's way from memory is what counts (each wavefront fetches a tile ahead, no barrier in the loop), and for fp32.
-//   S^T = K Q^T by the 16x16x128 block-scaled MFMA: a lane holds a quarter of one key as it lies in memory, Q follows that order in two numbers per
-//     element (see two_pieces).
+//   S^T = K Q^T by 16x16x32 MFMAs: a lane holds a quarter of one key as it lies in memory, converts it to bf16 (exact) and
+//     multiplies eight elements at a time; Q follows that order.  (The block-scaled MFMA takes keys unconverted and is no faster here, where
+//     memory is what counts, but adds its 128 products up to 2^-18 of their sum only, which the rows' weights would show: 2e-5 instead of 1e-7.)
 //   O^T = V^T P^T: a lane takes pieces of sixteen values as they lie in memory, converts them and leaves them in LDS row by
 //     row, from where the transposing load brings eight keys of one head-dim element; P is in that order already.
-// fp32: keys are converted too, Q and P go in as three bf16 numbers each, K and V are exact in one.
+// fp32: Q and P go in as three bf16 numbers each, K and V are exact in one.
 // stats: null, or for every row what its weights were taken against: reference and sum.  scores: null, or [B * heads][pitch][rows][32] where there
 // is one block of rows, and receives them by tiles (not those of tiles without a visible key).
 template <typename T, int DH, int NW, bool MASKED>
@@ -168,37 +169,16 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
     // ---- Q: lane = row, the elements of the lane's part of a key
     const int row = min(rb * 16 + c16, R - 1);
     const T *qsrc = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g4 * (DH / 4);
-    bf16x8_t qf[F32 ? KS : 1][3];
-    intx8_t qp[2];
-    int qbyte = 0;
-    if constexpr (F32) {
+    bf16x8_t qf[KS][NP];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
+    for (int s = 0; s < KS; ++s) {
+        if constexpr (F32) {
             float x[8];
             *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(qsrc + 8 * s);
             *reinterpret_cast<float4 *>(x + 4) = *reinterpret_cast<const float4 *>(qsrc + 8 * s + 4);
             three_pieces(x, qf[s]);
-        }
-    } else {
-        uint4 w[KS];
-        uint32_t top = 0;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            w[s] = *reinterpret_cast<const uint4 *>(qsrc + 8 * s);
-            top = top_of_eight(w[s], top);
-        }
-        const auto x = __builtin_amdgcn_permlane16_swap(top, top, false, false);
-        top = max(x[0], x[1]);
-        const auto y = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-        top = max(y[0], y[1]);
-        qbyte = piece_bytes(top);
-        qp[0] = qp[1] = intx8_t{0};
-#pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) {
-            int one, two;
-            two_pieces(i & 1 ? w[i / 2].z : w[i / 2].x, i & 1 ? w[i / 2].w : w[i / 2].y, top, qbyte, one, two);
-            qp[0][i] = one;
-            qp[1][i] = two;
+        } else {
+            qf[s][0] = *reinterpret_cast<const bf16x8_t *>(qsrc + 8 * s);
         }
     }
 
@@ -269,23 +249,12 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 s[u] = floatx4_t{0};
-                if constexpr (F32) {
 #pragma unroll
-                    for (int i = 0; i < KS; ++i) {
-                        const uint4 w = x.k[u][i / 2];
-                        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, i & 1 ? bf16_eight(w.z, w.w, ksize) : bf16_eight(w.x, w.y, ksize));
+                for (int i = 0; i < KS; ++i) {
+                    const uint4 w = x.k[u][i / 2];
+                    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, i & 1 ? bf16_eight(w.z, w.w, ksize) : bf16_eight(w.x, w.y, ksize));
 #pragma unroll
-                        for (int p = 2; p >= 0; --p) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][p], s[u], 0, 0, 0);
-                    }
-                } else {
-                    intx8_t kf = {0};                        // (64-wide rows: the other half of the contraction is 0)
-#pragma unroll
-                    for (int w = 0; w < KW; ++w) {
-                        kf[4 * w] = (int)x.k[u][w].x; kf[4 * w + 1] = (int)x.k[u][w].y;
-                        kf[4 * w + 2] = (int)x.k[u][w].z; kf[4 * w + 3] = (int)x.k[u][w].w;
-                    }
-                    s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[1], s[u], 0, 0, 0, (int)x.ks, 1, qbyte);
-                    s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qp[0], s[u], 0, 0, 0, (int)x.ks, 0, qbyte);
+                    for (int p = NP - 1; p >= 0; --p) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][p], s[u], 0, 0, 0);
                 }
             }
             if (scores && c16 < R) {
@@ -432,7 +401,8 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // matrix cores and the softmax bound the time.
 //   S^T = K Q^T by the 32x32x64 block-scaled MFMA: it takes keys in 8 bits with their scale bytes as they lie in memory, so K is not
 //     converted.  Q goes in as two numbers per element (see two_pieces): two products at twice the rate of bf16 take as long as one
-//     of bf16 would, without a conversion of K.
+//     of bf16 would, without a conversion of K.  (It adds 64 products up to about 2^-18 of the sum of their sizes, where bf16's are added up
+//     to 2^-24: with scores up to 30 or so weights are off by 2^-13 at most, fp16 holds them to 2^-12.)
 //   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
 // In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
 // product takes it, as in attention.hip.
@@ -1092,7 +1062,7 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
 }
 
 // Weights of the rows: every wavefront holds 64 keys as bf16 operands, takes the scores of all rows of queries against them once more, and
-// adds up exp2((s - reference) * c - log2(sum)) over the rows, each key's in its own registers: no atomics, one order.  64 rows at a time come
+// adds up exp2((s - reference) * c) / sum over the rows, each key's in its own registers: no atomics, one order.  64 rows at a time come
 // through LDS for the four wavefronts, by DMA while the ones before are at work (fp32: 32 rows, in three pieces of bf16).  A row whose weights
 // are not numbers adds nothing.
 //   A workgroup: a block of 256 keys of one of `heads` (sample, kv head), and a share of its rows; several shares leave partial sums
@@ -1177,7 +1147,7 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     // The weights of 32 rows are made beside the products of the next ones, an exponential or two for each product (fp32, with three products
     // where bf16 has one and no registers for both: after their own).
     floatx16_t acc[2] = {floatx16_t{0}, floatx16_t{0}}, s[2] = {floatx16_t{0}, floatx16_t{0}};
-    float m = 0.f, off = -INFINITY, both = -INFINITY;        // of the rows whose scores s are
+    float m = 0.f, each = 0.f, mc = INFINITY;                  // of the rows whose scores s are: reference, 1 / sum, reference in units of log2
     bool plain = true;
     auto weigh = [&]() {
         // the difference first, exact near the reference; at most 1: scores of 2^20 and more differ by more than that between
@@ -1186,10 +1156,12 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                acc[u][i] += __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(s[u][i] - m, c_log2, off)), 0.f, 1.f);
+                acc[u][i] += __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f((s[u][i] - m) * c_log2) * each, 0.f, 1.f);
     };
-    // reference and sum as one number, the same for all keys: off by 2^-25 of itself
-    auto weigh_plain = [&](int e) { acc[e >> 4][e & 15] += __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], c_log2, both)); };
+    // (what mc's rounding leaves is in `each`)
+    auto weigh_plain = [&](int e) {
+        acc[e >> 4][e & 15] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], c_log2, -mc)), each, acc[e >> 4][e & 15]);
+    };
     auto finish = [&]() {
         if (plain) {
 #pragma unroll
@@ -1238,9 +1210,10 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
             }
             const bool there = t * ROWS + j * 32 + rl < R, counts = there && stat[j].y > 0.f;
             m = counts ? reference(stat[j].x) : 0.f;
-            off = counts ? -__builtin_amdgcn_logf(stat[j].y) : -INFINITY;
-            both = fmaf(-m, c_log2, off);
-            plain = __builtin_amdgcn_ballot_w64(fabsf(m * c_log2) >= 4096.f || there != counts) == 0;
+            each = counts ? 1.0f / stat[j].y : 0.f;
+            mc = counts ? m * c_log2 : INFINITY;             // (a row that does not count: weights of 0, whatever its scores)
+            plain = __builtin_amdgcn_ballot_w64(there != counts || (counts && fabsf(mc) >= 4096.f)) == 0;
+            if (plain && counts) each *= __builtin_amdgcn_exp2f(-fmaf(m, c_log2, -mc));
             if constexpr (F32) finish();
         }
         if (t + 1 < t1) put(buffer ^ 1);

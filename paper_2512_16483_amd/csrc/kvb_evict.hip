@@ -59,12 +59,9 @@ __global__ __launch_bounds__(kSelThreads) void kvb_rank_kernel(KvbCache c, const
     } else {
         for (int i = tid; i < len; i += kSelThreads) look(key_at(i));
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        late += __shfl_xor(late, o);
-        seen += __shfl_xor(seen, o);
-        some += __shfl_xor(some, o);
-    }
+    late = (int)wave_total((uint32_t)late);
+    seen = (int)wave_total((uint32_t)seen);
+    some = (int)wave_total((uint32_t)some);
     if ((tid & 63) == 0) { late_here[tid >> 6] = late; seen_here[tid >> 6] = seen; some_here[tid >> 6] = some; }
     __syncthreads();
     late = seen = some = 0;
@@ -141,7 +138,7 @@ template <int DH> struct MovedBlock {
             const uint32_t m = max(max(largest(w[i].x), largest(w[i].y)), max(largest(w[i].z), largest(w[i].w)));
             top = max(top, __float_as_uint(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(m, __uint_as_float(byte[i] << 23), false)[0]));
         }
-        top = kvb_wave_max(top);
+        top = wave_largest(top);
     }
     __device__ __forceinline__ void put(uint8_t *codes, uint8_t *scales, int block, int count)
     {

@@ -13,6 +13,31 @@ __device__ __forceinline__ uint32_t score_key(float s)
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
+// Over a wavefront, in registers (a shuffle is a trip through LDS): sum and largest in every lane, running sum.
+template <typename Op> __device__ __forceinline__ uint32_t wave_fold(uint32_t v, Op op)
+{
+    v = op(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));             // quad_perm 1,0,3,2
+    v = op(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));             // quad_perm 2,3,0,1
+    v = op(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true));            // row_half_mirror
+    v = op(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true));            // row_mirror
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = op(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return op(b[0], b[1]);
+}
+__device__ __forceinline__ uint32_t wave_total(uint32_t v) { return wave_fold(v, [](uint32_t x, uint32_t y) { return x + y; }); }
+__device__ __forceinline__ uint32_t wave_largest(uint32_t v) { return wave_fold(v, [](uint32_t x, uint32_t y) { return max(x, y); }); }
+__device__ __forceinline__ int wave_running(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);                           // row_shr:1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);                          // row_bcast:15 to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);                          // row_bcast:31 to rows 2 and 3
+    return v;
+}
+
 constexpr int kSelThreads = 1024;
 constexpr int kSelWaves = kSelThreads / 64;
 constexpr int kSelBins = 4096;               // four per thread
@@ -41,11 +66,8 @@ __device__ __forceinline__ void select_threshold(const uint32_t (&key)[KPT], int
 {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
-    }
+    lo = ~wave_largest(~lo);
+    hi = wave_largest(hi);
     if (lane == 0) { sh.wave_min[wave] = lo; sh.wave_max[wave] = hi; }
     reinterpret_cast<int4 *>(sh.hist)[tid] = make_int4(0, 0, 0, 0);
     __syncthreads();
@@ -69,12 +91,7 @@ __device__ __forceinline__ void select_threshold(const uint32_t (&key)[KPT], int
         __syncthreads();
         const int4 c = reinterpret_cast<const int4 *>(sh.hist)[tid];
         const int sum = c.x + c.y + c.z + c.w;
-        int incl = sum;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int t = __shfl_up(incl, o);
-            if (lane >= o) incl += t;
-        }
+        const int incl = wave_running(sum);
         if (lane == 63) sh.totals[wave] = incl;
         __syncthreads();
         int run = incl - sum;                            // keys in larger bins
@@ -154,12 +171,7 @@ __device__ __forceinline__ void select_sweep(const uint32_t (&key)[KPT], int M, 
 #pragma unroll
     for (int j0 = 0; j0 < KPT; j0 += 4) {                // 64 pieces of 64 tokens at a time
         const int mine = j0 * kSelWaves + lane < KPT * kSelWaves ? sh.counts[j0 * kSelWaves + lane] : 0;
-        int incl = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int t = __shfl_up(incl, o);
-            if (lane >= o) incl += t;
-        }
+        const int incl = wave_running(mine);
         const int before = incl - mine + carry;
         carry += __builtin_amdgcn_readlane(incl, 63);
 #pragma unroll

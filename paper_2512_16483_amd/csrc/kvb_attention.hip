@@ -1089,6 +1089,8 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     // ---- rows of queries: chunks are turned by the row's number, so that the rows of sixteen lanes that read one chunk lie in all banks
     auto turn = [](int row) { return DH == 128 ? row & 15 : (row >> 1) & 7; };
     const uint32_t lds_base = (uint32_t)(uintptr_t)ql;
+    const T *first = q + (size_t)b * n * ld + hk * G * DH;
+    const int shift = (G & (G - 1)) == 0 ? __builtin_ctz(G) : -1;    // (a division for every piece would take as long as a third of the products)
     uint4 next[F32 ? PER : 1][2];
     float2 next_stat[SETS];
     auto fetch = [&](int t, int buffer) {
@@ -1096,13 +1098,14 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
         for (int i = 0; i < PER; ++i) {
             const int at = F32 ? i * 256 + tid : (wave * PER + i) * 64 + lane;
             const int in_tile = at / CH, row = min(t * ROWS + in_tile, R - 1);
-            const size_t src = (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH;
+            const int query = shift >= 0 ? row >> shift : row / G;
+            const size_t src = (size_t)query * ld + (row - query * G) * DH;
             if constexpr (F32) {
-                next[i][0] = *reinterpret_cast<const uint4 *>(q + src + at % CH * 8);
-                next[i][1] = *reinterpret_cast<const uint4 *>(q + src + at % CH * 8 + 4);
+                next[i][0] = *reinterpret_cast<const uint4 *>(first + src + at % CH * 8);
+                next[i][1] = *reinterpret_cast<const uint4 *>(first + src + at % CH * 8 + 4);
             } else {
                 // (addresses of any distance from q: 64 bits per lane)
-                const uint16_t *from = q + src + ((at % CH) ^ turn(in_tile)) * 8;
+                const uint16_t *from = first + src + ((at % CH) ^ turn(in_tile)) * 8;
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                              :: "s"(lds_base + (buffer * ROWS * CH + (wave * PER + i) * 64) * 16), "v"(from) : "memory", "m0");
             }

@@ -230,6 +230,8 @@ void launch_kvb_read(DType dt, const KvbCache &c, int B, int first, int rows, in
 // the next; o:[B,n,H,Dh]; weights: null, or [B][heads][capacity] that receive (add: are increased by) each row's weight;
 // part: kvb_attention_scratch_floats() floats
 size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity, bool weights);
+int kvb_attention_ways(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged);
+long kvb_attention_takes(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged, int weights);
 void launch_kvb_attention(DType dt, const void *q, int ld, const KvbCache &c, int extra, int B, int n, int H, int Dh,
                           float scale, void *o, float *weights, bool add, float *part, hipStream_t st);
 // eviction, see kvb_evict.hip; idx:[B][heads][keep], counts:[B]

@@ -128,7 +128,7 @@ __device__ __forceinline__ int xcd_grouped(int id, int groups, int size)
 // cache's way from memory is what counts (each wavefront fetches a tile ahead, no barrier in the loop), and for fp32.
 //   S^T = K Q^T by 16x16x32 MFMAs: a lane holds a quarter of one key as it lies in memory, converts it to bf16 (exact) and
 //     multiplies eight elements at a time; Q follows that order.  (The block-scaled MFMA takes keys unconverted and is no faster here, where
-//     memory is what counts, but adds its 128 products up to 2^-18 of their sum only, which the rows' weights would show: 2e-5 instead of 1e-7.)
+//     memory is what counts, but adds less exactly, which the rows' weights would show: 2e-5 of them, rms, instead of 1e-7.)
 //   O^T = V^T P^T: a lane takes pieces of sixteen values as they lie in memory, converts them and leaves them in LDS row by
 //     row, from where the transposing load brings eight keys of one head-dim element; P is in that order already.
 // fp32: Q and P go in as three bf16 numbers each, K and V are exact in one.
@@ -401,8 +401,8 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // matrix cores and the softmax bound the time.
 //   S^T = K Q^T by the 32x32x64 block-scaled MFMA: it takes keys in 8 bits with their scale bytes as they lie in memory, so K is not
 //     converted.  Q goes in as two numbers per element (see two_pieces): two products at twice the rate of bf16 take as long as one
-//     of bf16 would, without a conversion of K.  (It adds 64 products up to about 2^-18 of the sum of their sizes, where bf16's are added up
-//     to 2^-24: with scores up to 30 or so weights are off by 2^-13 at most, fp16 holds them to 2^-12.)
+//     of bf16 would, without a conversion of K.  (It adds 64 products less exactly than bf16's are added: scores are off by 2^-14.6 of
+//     the sum of their products' sizes at most, 2^-19 rms, which at sums of 10 is 2^-11 of a weight at most; fp16 holds one to 2^-12.)
 //   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
 // In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
 // product takes it, as in attention.hip.
@@ -1336,6 +1336,15 @@ static int weight_shares(int B, int heads, int length, int rows)
     return (int)(shares > 8 ? 8 : shares < 1 ? 1 : shares);
 }
 
+// Floats that partial results take, and, before them, what the weights need: every row's reference and sum; their scores, or partial sums of
+// at most kWeightPlaces workgroups of 256 keys.
+static size_t part_floats(const KvbRun &run, int Dh) { return (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2); }
+static size_t stat_floats(int B, int n, int H) { return (2 * (size_t)B * n * H + 3) / 4 * 4; }
+static size_t weight_floats(int B, int n, int H, int heads, int length)
+{
+    return few_rows(n * (H / heads)) ? (size_t)B * n * H * 32 * score_tiles(length) : 256 * kWeightPlaces;
+}
+
 size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, int Dh, int capacity, bool weights)
 {
     // Between those lengths shares never fall as the length grows, nor where samples have lengths of their own, so for either kind of
@@ -1345,14 +1354,25 @@ size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, in
         if (length > capacity) continue;
         for (int block = 16; block <= 128; block *= 8) {
             if (block == 128 ? kvb_block(dt, B, n, H, heads, length) == 16 : kvb_block(dt, B, n, H, heads, 1) == 128) continue;
-            const KvbRun run = kvb_run(block, B, n, H, heads, Dh, length, true);
-            const size_t take = (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2);
+            const size_t take = part_floats(kvb_run(block, B, n, H, heads, Dh, length, true), Dh);
             if (take > floats) floats = take;
         }
     }
-    // every row's reference and sum; their scores, or partial sums of at most kWeightPlaces workgroups of 256 keys
-    if (weights) floats += (2 * (size_t)B * n * H + 3) / 4 * 4 + (few_rows(n * (H / heads)) ? (size_t)B * n * H * 32 * score_tiles(capacity) : 256 * kWeightPlaces);
-    return floats;
+    return floats + (weights ? stat_floats(B, n, H) + weight_floats(B, n, H, heads, capacity) : 0);
+}
+
+// How an attention is run, and the floats that it takes, for the tests: 100000 * rows of a block + 1000 * wavefronts + shares.
+int kvb_attention_ways(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged)
+{
+    const int block = kvb_block(bf16 ? DType::BF16 : DType::F32, B, n, H, heads, length);
+    const KvbRun run = kvb_run(block, B, n, H, heads, Dh, length, ragged != 0);
+    return 100000 * block + 1000 * run.waves + run.shares;
+}
+long kvb_attention_takes(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged, int weights)
+{
+    const int block = kvb_block(bf16 ? DType::BF16 : DType::F32, B, n, H, heads, length);
+    const size_t part = part_floats(kvb_run(block, B, n, H, heads, Dh, length, ragged != 0), Dh);
+    return (long)(part + (weights ? stat_floats(B, n, H) + weight_floats(B, n, H, heads, length) : 0));
 }
 
 template <typename T, int DH>
@@ -1368,9 +1388,9 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
     const int rows = n * (H / c.heads), pitch = (int)score_tiles(length);
     if (weights) {
         stats = reinterpret_cast<float2 *>(part);
-        sums = part + (2 * (size_t)B * n * H + 3) / 4 * 4;
+        sums = part + stat_floats(B, n, H);
         scores = few_rows(rows) ? sums : nullptr;
-        part = sums + (scores ? (size_t)B * n * H * 32 * pitch : 256 * kWeightPlaces);
+        part = sums + weight_floats(B, n, H, c.heads, length);
     }
     float *part_ml = part + (size_t)divided * run.shares * run.block * DH;
     const unsigned wgs = (unsigned)(run.full + divided * run.shares);

@@ -232,9 +232,11 @@ SHAPES = [("bf16", 2, 2, 64, 1, 1, 1), ("bf16", 4, 1, 128, 2, 1, 33), ("bf16", 1
 # same with a single query; one query of few keys by eight wavefronts; fp32 in shares
 LARGE = [("bf16", 30, 30, 64, 32, 200, 70), ("bf16", 16, 16, 128, 33, 129, 1030), ("bf16", 16, 16, 64, 4, 512, 4500), ("bf16", 16, 4, 128, 2, 3, 9000),
          ("bf16", 16, 16, 64, 1, 1, 700), ("f32", 4, 2, 64, 1, 5, 3000)]
+# two groups of wavefronts, blocks of rows divided into shares; groups of four wavefronts in shares; blocks of rows that are not full
+TILES = [("bf16", 2, 1, 128, 1, 1000, 6000), ("bf16", 8, 8, 64, 2, 600, 1700), ("bf16", 16, 16, 64, 5, 230, 4100), ("bf16", 16, 4, 64, 40, 40, 900)]
 
 
-@pytest.mark.parametrize("dtype,H,heads,dh,B,n,L", SHAPES + LARGE)
+@pytest.mark.parametrize("dtype,H,heads,dh,B,n,L", SHAPES + LARGE + TILES)
 @pytest.mark.parametrize("kind", ["plain", "ragged", "masked"])
 def test_attention_and_weights(dtype, H, heads, dh, B, n, L, kind):
     g = np.random.default_rng(L + n)
@@ -389,6 +391,57 @@ def test_attention_takes_rows_of_a_fused_projection_and_other_streams_and_graphs
         torch.cuda.synchronize()
         assert torch.equal(o3, o4) and torch.equal(w, w2) and torch.equal(kv.k, eager.k) and torch.equal(kv.v_scale, eager.v_scale)
     assert kv.lens.tolist() == [40, 40]
+
+
+def test_cache_whose_offsets_pass_32_bits():
+    """Two samples of 9 heads over 2^21 rows: 4.8 GB of keys and as much of values, of which the mask leaves the last 100 rows or so."""
+    B, heads, dh, cap, rows = 2, 9, 128, 2 ** 21 + 33, 30
+    start, lens = 2 ** 21 - 96, [cap - 70, cap - 40]
+    ctx, kv = ctx_of(heads, dh, "bf16"), empty_cache(B, heads, cap, dh, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    k, v = rows_of(1, B, rows, heads, dh, "bf16"), rows_of(2, B, rows, heads, dh, "bf16")
+    tail, powers = slice(start, cap), slice(start // 32, None)
+    want = []
+    for codes, scales, x in ((kv.k, kv.k_scale, k), (kv.v, kv.v_scale, v)):
+        codes[:, :, tail].random_(0, 127)
+        scales[:, :, powers].random_(118, 122)
+        want.append((codes[:, :, tail].cpu().numpy().copy(), scales[:, :, powers].cpu().numpy().copy()))
+        kvb.append(*want[-1], [n - start for n in lens], x)
+    fv.fvar_kvb_append(ctx, kv, to_dev(k, "bf16"), to_dev(v, "bf16"), B, rows)
+    kv.lens.add_(rows)
+    lens = [n + rows - start for n in lens]
+    for codes, scales, (c, s) in ((kv.k, kv.k_scale, want[0]), (kv.v, kv.v_scale, want[1])):
+        assert np.array_equal(codes[:, :, tail].cpu().numpy(), c) and np.array_equal(scales[:, :, powers].cpu().numpy(), s)
+    held = [kvb.values(c, s) for c, s in want]
+    back = [torch.empty((B, rows, heads, dh), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    fv.fvar_kvb_read(ctx, kv, B, -rows, rows, *back)
+    for got, x in zip(back, held):
+        assert np.array_equal(to_np(got), np.stack([x[b, :, n - rows:n] for b, n in enumerate(lens)]).swapaxes(1, 2))
+    kv.mask = torch.zeros((B, cap), dtype=torch.uint8, device="cuda")
+    kv.mask[:, start + 10:] = 1
+    kv.mask[1, start + 50] = 0
+    mask = kv.mask[:, tail].cpu().numpy()
+    for n in (1, 200):
+        q = rows_of(3, B, n, heads, dh, "bf16", spread=0.2)
+        o, w = kvb.attention(q, *held, dh ** -0.5, lens, mask)
+        got = torch.full((B, heads, cap), 3.0, device="cuda")
+        check(f"long, n{n}", attend(ctx, to_dev(q, "bf16"), kv, "bf16", B, n, weights=got), o, "bf16")
+        there = (np.arange(cap - start) < np.array(lens)[:, None])[:, None]
+        check_weights(f"long, n{n}", got[:, :, tail], np.where(there, w, 3.0), q, held[0], dh ** -0.5)
+        assert not got[:, :, :start].any()
+    keep, weights = 64, got[:, :, tail].cpu().numpy()
+    outs = [kvb.evict(c, s, weights, lens, keep, 5, mask) for c, s in want]
+    to, tw = empty_cache(B, heads, keep, dh), torch.empty((B, heads, keep), device="cuda")
+    count, idx = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty((B, heads, keep), dtype=torch.int32, device="cuda")
+    ws = torch.empty(fv.fvar_kvb_evict_workspace_bytes(ctx, kv, B, keep), dtype=torch.uint8, device="cuda")
+    fv.fvar_kvb_evict(ctx, kv, got, B, keep, 5, to, tw, count, idx, ws)
+    assert np.array_equal(idx.cpu().numpy(), outs[0][0] + start) and count.tolist() == [keep, keep]
+    assert np.array_equal(tw.cpu().numpy(), np.take_along_axis(weights, outs[0][0], -1))
+    fv.fvar_kvb_evict(ctx, kv, got, B, keep, 5, kv, got, kv.lens, idx, ws)       # in place: the same rows at the front
+    for codes, scales, codes2, scales2, out in ((to.k, to.k_scale, kv.k, kv.k_scale, outs[0]), (to.v, to.v_scale, kv.v, kv.v_scale, outs[1])):
+        assert np.array_equal(codes.cpu().numpy(), np.array([[h[0] for h in b] for b in out[2]]))
+        assert np.array_equal(scales.cpu().numpy(), np.array([[h[1] for h in b] for b in out[2]]))
+        assert torch.equal(codes, codes2[:, :, :keep]) and torch.equal(scales, scales2[:, :, :keep // 32])
+    assert torch.equal(got[:, :, :keep], tw) and not got[:, :, keep:].any()
 
 
 def test_debug_checks_look_at_lengths():

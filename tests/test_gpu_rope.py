@@ -127,3 +127,13 @@ def test_rope_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_rows_whose_offsets_pass_32_bits():
+    H, dh, n = 16, 64, 2_200_001
+    q = torch.randn((1, n, H, dh), dtype=torch.bfloat16, device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda").reshape(1, n, 1)
+    out = torch.empty_like(q)
+    fv.fvar_rope_apply(_ctx(H, dh, "bf16"), fv.Rope(dim=dh), pos, 1, n, q, None, out)
+    at = [0, 1, n // 2, 2 ** 21 - 1, 2 ** 21, n - 2, n - 1]
+    _check(out[:, at], to_np(q[:, at]), np.array(at, np.int32).reshape(1, -1, 1), rope.frequencies(dh), "bf16", dh)

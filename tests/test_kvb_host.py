@@ -303,6 +303,41 @@ def test_binding_holds_a_cache_to_its_shapes():
     assert fv.Rope(dim=64, turns=[0.25] * 32).turns == [0.25] * 32
 
 
+def ways(dtype, B, n, H, heads, dh, length, ragged):
+    """(rows of a block, wavefronts of a workgroup, shares of a divided block) of an attention."""
+    x = fv.load_library()["_ZN4fvar18kvb_attention_waysEiiiiiiii"](dtype == "bf16", B, n, H, heads, dh, length, ragged)
+    return x // 100000, x // 1000 % 100, x % 1000
+
+
+@pytest.mark.parametrize("dtype,B,n,H,heads,dh,length,ragged,expect", [
+    ("bf16", 2, 1, 2, 2, 64, 64, 0, (16, 4, 1)), ("bf16", 1, 1, 16, 16, 64, 700, 0, (16, 8, 1)), ("bf16", 1, 1, 16, 16, 128, 1300, 0, (16, 8, 2)),
+    ("bf16", 2, 3, 16, 4, 128, 9000, 1, (16, 4, 35)), ("bf16", 3, 1, 32, 8, 128, 517, 1, (16, 4, 2)), ("f32", 1, 5, 4, 2, 64, 3000, 0, (16, 8, 5)),
+    ("bf16", 3, 257, 4, 4, 64, 700, 0, (16, 8, 1)), ("bf16", 32, 200, 30, 30, 64, 70, 0, (128, 4, 1)), ("bf16", 33, 129, 16, 16, 128, 1030, 0, (128, 4, 4)),
+    ("bf16", 4, 512, 16, 16, 64, 4500, 0, (128, 8, 1)), ("bf16", 1, 1000, 2, 1, 128, 6000, 0, (128, 8, 11)), ("bf16", 2, 600, 8, 8, 64, 1700, 0, (128, 8, 3)),
+    ("bf16", 5, 230, 16, 16, 64, 4100, 0, (128, 4, 3)), ("bf16", 40, 40, 16, 4, 64, 900, 1, (128, 4, 1))])
+def test_sizes_are_run_as_the_gpu_tests_want_them(dtype, B, n, H, heads, dh, length, ragged, expect):
+    assert ways(dtype, B, n, H, heads, dh, length, ragged) == expect
+
+
+def test_no_length_takes_more_workspace_than_the_capacity_is_told():
+    lib, g = fv.load_library(), np.random.default_rng(5)
+    takes = lib["_ZN4fvar19kvb_attention_takesEiiiiiiiii"]
+    takes.restype = C.c_long
+    for _ in range(4000):
+        dh, group, heads = int(g.choice([64, 128])), int(g.choice([1, 1, 2, 3, 8])), int(np.exp(g.uniform(0, np.log(32))))
+        H, B, n = heads * group, int(np.exp(g.uniform(0, np.log(64)))), int(np.exp(g.uniform(0, np.log(3000))))
+        cap = int(np.exp(g.uniform(0, np.log(40000))))
+        dtype, weights = ("bf16", "f32")[int(g.integers(2))], int(g.integers(2))
+        ctx = fv.Context(hidden=H * dh, heads=H, head_dim=dh, ffn_hidden=64, dtype=dtype) if H * dh <= 4096 else None
+        if ctx is None:
+            continue
+        kv = fv._KVB(0x1000, 0x1000, 0x1000, 0x1000, None, None, heads, cap, 0)
+        room = lib.fvar_kvb_attention_workspace_bytes(ctx.handle, C.byref(kv), B, n, weights)
+        for length in {cap, 1, max(1, cap // 2), max(1, cap // 7), min(cap, 2047), min(cap, 2048), min(cap, 4095), min(cap, 4096), int(g.integers(0, cap + 1))}:
+            for ragged in (0, 1):
+                assert 4 * takes(dtype == "bf16", B, n, H, heads, dh, length, ragged, weights) <= room, (dtype, B, n, H, heads, dh, length, cap, ragged)
+
+
 def test_attention_workspace_serves_every_length_and_falls_never_short():
     """What a shorter cache takes is within what the call is told for the capacity."""
     ctx = fv.Context(hidden=256, heads=4, head_dim=64, ffn_hidden=256)

@@ -2,7 +2,7 @@
 // angle p * f_i, p the part's component of the row's position and f_i the pair's entry of a table (in turns per position).
 //   (x, y) -> magnitude * (x cos - y sin, x sin + y cos);  pairs are (i, i + P / 2), or (2 i, 2 i + 1) where interleaved.
 //
-// An angle is the fraction of p * f_i in 64 bits (a position of 10^6 leaves 2^-4 of a turn's 32-bit fraction), sine and cosine of it in 32.
+// An angle is the fraction of p * f_i in 64 bits, off by 2^-34 of a turn at most for positions up to 10^6; sine and cosine of it in 32.
 #include "common.h"
 
 namespace fvar {

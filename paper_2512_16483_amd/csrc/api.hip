@@ -276,6 +276,10 @@ fvar_status check_rope(fvar_ctx *c, const fvar_rope *r, const int32_t *pos, cons
     if (r->axes < 1 || r->axes > 2 || r->dim < 1 || r->dim > c->cfg.head_dim || r->dim % (16 * r->axes))
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: dim=%d with axes=%d: a multiple of 16*axes up to head_dim is wanted", who, r->dim, r->axes);
     if (reinterpret_cast<uintptr_t>(pos) & 3) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pos is not 4-byte aligned", who);
+    bool some = false;
+    for (int i = 0; i < r->dim / r->axes / 2; ++i) some |= r->turns[i] != 0.0;
+    if (!some || !std::isfinite(r->magnitude))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: rope has no turns (see fvar_rope_init), or magnitude=%g", who, r->magnitude);
     return FVAR_OK;
 }
 
@@ -285,7 +289,7 @@ fvar::RopeTable rope_table(const fvar_rope *r)
     t.dim = r->dim;
     t.axes = r->axes;
     t.interleaved = r->interleaved != 0;
-    t.magnitude = (float)r->magnitude;
+    t.magnitude = r->magnitude == 0.0 ? 1.f : (float)r->magnitude;
     std::memcpy(t.turns, r->turns, sizeof(t.turns));
     return t;
 }
@@ -325,7 +329,7 @@ fvar_status block_forward(fvar_ctx *c, hipStream_t st, const fvar_block_weights 
         (int64_t)kv->len + rows > (int64_t)kv->capacity)
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: KV cache too small (len=%d + rows=%d > capacity=%d)",
                     who, kv->len, rows, kv->capacity);
-    if (cache.rope) {
+    if (cache.rope || cache.pos) {
         const fvar_status rs = check_rope(c, cache.rope, cache.pos, who);
         if (rs != FVAR_OK) return rs;
     }

@@ -137,3 +137,13 @@ def test_rows_whose_offsets_pass_32_bits():
     fv.fvar_rope_apply(_ctx(H, dh, "bf16"), fv.Rope(dim=dh), pos, 1, n, q, None, out)
     at = [0, 1, n // 2, 2 ** 21 - 1, 2 ** 21, n - 2, n - 1]
     _check(out[:, at], to_np(q[:, at]), np.array(at, np.int32).reshape(1, -1, 1), rope.frequencies(dh), "bf16", dh)
+
+
+def test_a_magnitude_of_0_stands_for_1():
+    ctx, r = _ctx(2, 64, "f32"), fv.Rope(dim=64)
+    q, pos = torch.randn((1, 5, 2, 64), device="cuda"), torch.arange(5, dtype=torch.int32, device="cuda").reshape(1, 5, 1)
+    one, two = torch.empty_like(q), torch.empty_like(q)
+    fv.fvar_rope_apply(ctx, r, pos, 1, 5, q, None, one)
+    r._c.magnitude = 0.0                                      # as a program with frequencies of its own may leave it
+    fv.fvar_rope_apply(ctx, r, pos, 1, 5, q, None, two)
+    assert torch.equal(one, two) and not torch.equal(one, q)

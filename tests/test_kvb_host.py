@@ -219,6 +219,11 @@ def test_rope_refuses_rows_that_are_none():
     assert apply(q=0x1008) == inv and apply(k_out=0x1004) == inv
     assert apply(ld_q=248) == inv and apply(ld_k=129, ld_k_out=129) == inv and apply(ld_q=264) == inv and apply(ld_q_out=-8) == inv
     assert apply(n=(1 << 24) + 1) == fv.FVAR_ERR_UNSUPPORTED
+    assert apply(r=_rope()) == inv                            # never filled in
+    odd = _rope()
+    lib.fvar_rope_init(C.byref(odd))
+    odd.magnitude = float("nan")
+    assert apply(r=odd) == inv
     assert lib.fvar_rope_apply(None, None, C.byref(good), fake, 1, 1, 2, fake, 0, None, 0, fake, 0, None, 0) == inv
 
 
@@ -233,6 +238,7 @@ def test_block_refuses_what_it_cannot_do():
 
     assert dense(kv=_cache(kv_heads=2)) == fv.FVAR_ERR_UNSUPPORTED and dense(M=51) == inv
     assert dense(pos=None) == inv and dense(pos=0x1001) == inv and dense(rope=_rope(dim=128)) == inv and dense(rope=_rope(axes=3)) == inv
+    assert dense(rope=None) == inv                            # positions without rope
     assert dense(weights=fake + 8) == inv
     for weigh in (0, 1):
         need = lib.fvar_block_kvb_workspace_bytes(h, C.byref(kv), 1, 2, weigh)

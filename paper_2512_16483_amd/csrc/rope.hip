@@ -9,14 +9,44 @@ namespace fvar {
 
 // Sixteen elements of a head, eight pairs, per thread; T rows per workgroup.  The angles of the workgroup's rows are made once, in LDS, for all heads
 // of queries and keys: 64 of them serve 8192 elements of 32 + 32 heads of 128.  A thread keeps to its pairs and its row and goes from head to
-// head with them in registers, FLY heads on their way at a time.  Memory-bound: 6400 rows of 32 + 32 heads of 128 in bf16 take 40 us with results
-// past the caches (5.2 TB/s), 43 through them; four rows per workgroup 46, eight 53.  Few rows take their launch: 32 of 32 + 8 heads 3.7 us.
+// head with them in registers, FLY heads on their way at a time.  Memory-bound: 6400 rows of 32 + 32 heads of 128 in bf16 take 39.7 us with results
+// past the caches (5.3 TB/s), the first heads fetched behind the angles 41.7, through the caches 3 more; four rows per workgroup 46, eight 53.  Few rows take their launch: 32 of 32 + 8 heads 3.7 us.
 template <typename E, int DH, int T, bool INTER, bool PAST>
 __global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, RopeRows k, const int32_t *__restrict__ pos, int rows)
 {
     constexpr int FLY = T == 1 ? 1 : 2, ITEMS = DH / 16, SLOTS = 256 / ITEMS / T, PER = Elem<E>::kPerChunk, HALF = 8 / PER;   // HALF: chunks of eight elements
     __shared__ float2 turn[T][DH / 2];
     const int tid = threadIdx.x, pairs = r.dim / 2, row0 = blockIdx.x * T;
+    const int item = tid % ITEMS, t = tid / ITEMS % T, slot = tid / ITEMS / T + blockIdx.y * SLOTS, step = gridDim.y * SLOTS;
+    const size_t row = min(row0 + t, rows - 1);
+    const int heads = row0 + t < rows ? q.heads + k.heads : 0;
+    const bool turned = item * 16 < r.dim;
+    int lo = item * 16, hi = item * 16 + 8;                  // the first of eight elements, and of eight more
+    if (turned && !INTER) {
+        const int part = r.dim / r.axes, each = part / 16, a = item / each;
+        lo = a * part + item % each * 8;
+        hi = lo + part / 2;
+    }
+    // FLY heads on their way at a time, the first of them while the angles are made
+    uint4 raw[FLY][2 * HALF];
+    E *dst[FLY];
+    auto fetch = [&](int h0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int f = 0; f < FLY; ++f) {
+            const int h = min(h0 + f * step, q.heads + k.heads - 1);
+            const bool is_q = h < q.heads;
+            const int head = is_q ? h : h - q.heads;
+            const E *src = (const E *)(is_q ? q.in : k.in) + row * (size_t)(is_q ? q.ld_in : k.ld_in) + head * DH;
+            dst[f] = (E *)(is_q ? q.out : k.out) + row * (size_t)(is_q ? q.ld_out : k.ld_out) + head * DH;
+            if (h0 + f * step >= heads || (!turned && src == dst[f])) dst[f] = nullptr;
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) {
+                raw[f][i] = *reinterpret_cast<const uint4 *>(src + lo + i * PER);
+                raw[f][HALF + i] = *reinterpret_cast<const uint4 *>(src + hi + i * PER);
+            }
+        }
+    };
+    fetch(slot);
     for (int i = tid; i < T * pairs; i += 256) {
         const int t = i / pairs, pair = i % pairs, each = pairs / r.axes, axis = pair / each;
         const int row = min(row0 + t, rows - 1);
@@ -33,40 +63,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, Rope
         if (PAST) __builtin_nontemporal_store(uintx4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<uintx4_t *>(to));
         else *reinterpret_cast<uint4 *>(to) = v;
     };
-    const int item = tid % ITEMS, t = tid / ITEMS % T, slot = tid / ITEMS / T + blockIdx.y * SLOTS, step = gridDim.y * SLOTS;
-    const size_t row = row0 + t;
-    if (row >= (size_t)rows) return;
-    const bool turned = item * 16 < r.dim;
     float c[8], s[8];
-    int lo = item * 16, hi = item * 16 + 8;                  // the first of eight elements, and of eight more
     if (turned) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) { c[i] = turn[t][item * 8 + i].x; s[i] = turn[t][item * 8 + i].y; }
-        if (!INTER) {
-            const int part = r.dim / r.axes, each = part / 16, a = item / each;
-            lo = a * part + item % each * 8;
-            hi = lo + part / 2;
-        }
     }
-    // FLY heads on their way at a time
-    const int heads = q.heads + k.heads;
     for (int h0 = slot; h0 < heads; h0 += FLY * step) {
-        uint4 raw[FLY][2 * HALF];
-        E *dst[FLY];
-#pragma unroll
-        for (int f = 0; f < FLY; ++f) {
-            const int h = min(h0 + f * step, heads - 1);
-            const bool is_q = h < q.heads;
-            const int head = is_q ? h : h - q.heads;
-            const E *src = (const E *)(is_q ? q.in : k.in) + row * (size_t)(is_q ? q.ld_in : k.ld_in) + head * DH;
-            dst[f] = (E *)(is_q ? q.out : k.out) + row * (size_t)(is_q ? q.ld_out : k.ld_out) + head * DH;
-            if (h0 + f * step >= heads || (!turned && src == dst[f])) dst[f] = nullptr;
-#pragma unroll
-            for (int i = 0; i < HALF; ++i) {
-                raw[f][i] = *reinterpret_cast<const uint4 *>(src + lo + i * PER);
-                raw[f][HALF + i] = *reinterpret_cast<const uint4 *>(src + hi + i * PER);
-            }
-        }
+        if (h0 != slot) fetch(h0);
 #pragma unroll
         for (int f = 0; f < FLY; ++f) {
             if (!dst[f]) continue;

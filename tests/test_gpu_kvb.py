@@ -273,6 +273,34 @@ def test_attention_and_weights(dtype, H, heads, dh, B, n, L, kind):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("junk", [0, 255])
+@pytest.mark.parametrize("H,heads,dh,B,n", [(4, 2, 64, 2, 1), (2, 2, 128, 1, 9), (8, 8, 64, 1, 40), (8, 4, 128, 2, 150), (30, 30, 64, 32, 200), (16, 16, 128, 33, 129)])
+def test_scales_of_blocks_that_hold_nothing_have_no_influence(dtype, junk, H, heads, dh, B, n):
+    """Lengths at which tiles of two blocks, or of 256 keys, end in blocks that were never written, whatever stands there."""
+    if dtype == "f32" and B * n > 500:
+        return
+    cap = 640
+    ctx = ctx_of(H, dh, dtype)
+    x, q = [rows_of(s, B, 353, heads, dh, dtype) for s in (1, 2)], to_dev(rows_of(3, B, n, H, dh, dtype, spread=0.2), dtype)
+    a, b = empty_cache(B, heads, cap, dh, fill=127), empty_cache(B, heads, cap, dh, fill=junk)
+    for L in (1, 32, 65, 96, 353):
+        for kv in (a, b):
+            kv.len, kv.lens = 0, None
+            for t in (kv.k, kv.v, kv.k_scale, kv.v_scale):
+                t.fill_(junk if kv is b else 127)
+            fv.fvar_kvb_append(ctx, kv, *[to_dev(np.ascontiguousarray(y[:, :L]), dtype) for y in x], B, L)
+            kv.len = L
+        for ragged in (False, True):
+            outs = []
+            for kv in (a, b):
+                kv.lens = torch.full((B,), L, dtype=torch.int32, device="cuda") if ragged else None
+                w = torch.zeros((B, heads, cap), device="cuda")
+                outs.append((attend(ctx, q, kv, dtype, B, n, weights=w), w))
+            assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]), (L, ragged)
+            assert torch.isfinite(outs[0][0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_without_a_visible_row(dtype):
     H, heads, dh, B, n, cap = 4, 2, 64, 3, 200, 96
     ctx, kv = ctx_of(H, dh, dtype), empty_cache(B, heads, cap, dh, fill=0x7F, lens=torch.tensor([0, 96, -3], dtype=torch.int32, device="cuda"))

@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
             }
         }
         t += NW;
-        fetch(t, x);
+        if (t < t1) fetch(t, x);
         if (any) {
             // ---- softmax
             if (__builtin_expect(vis != ~0u, 0)) {
@@ -1263,20 +1263,22 @@ __global__ __launch_bounds__(256) void kvb_weights_join_kernel(KvbCache c, int e
 
 // Blocks of how many rows of a (sample, kv head) an attention is run by: 16 (kvb_attn_rows_kernel) or 128 (kvb_attn_tiles_kernel, bf16
 // only).  The first starts and ends soonest and is bound by the work, which it does at less than half the other's pace; the other fetches
-// and converts for 128 rows whatever there are, and joins groups and shares.  So the work decides, and at half a block and less three times as
-// much of it is still by 16.  us by 16 / by 128, 16 heads of 128: 1 x 144 rows x 265 keys 7 / 15, 1 x 400 x 921 15 / 23, 1 x 576 x 1497
-// 27 / 26, 1 x 200 x 4813 33 / 26, 16 x 100 x 1000 42 / 27; 8 x 64 x 2521 29 / 34, 16 x 64 x 3000 63 / 50, 8 x 32 x 3001 20 / 35,
-// 32 x 32 x 3001 92 / 85, 32 x 48 x 3001 117 / 101; 30 heads of 64: 1 x 324 x 640 10 / 13, 2 x 231 x 871 15 / 16, 8 x 169 x 316 20 / 14.
-static int kvb_block(DType dt, int B, int n, int H, int heads, int length)
+// and converts for 128 rows whatever there are, and joins groups and shares.  So the work decides, with 64-wide rows, which take the first less, at two
+// thirds more, and at half a block and less at five times as much; and a tile of the other's 64 keys that is all there is has nothing to run beside it.  us by 16 / by
+// 128, 16 heads of 128: 1 x 144 rows x 265 keys 7 / 15, 1 x 400 x 921 15 / 23, 2 x 400 x 400 16.9 / 17.7, 4 x 400 x 250 18.7 / 15.1, 8 x 400 x 200 27.9 / 20.2,
+// 1 x 800 x 600 19.9 / 18.8, 1 x 200 x 4813 33 / 26, 32 x 400 x 60 41 / 45; 8 x 64 x 2521 29 / 34, 16 x 64 x 3000 63 / 50, 8 x 32 x 3001 20 / 35,
+// 32 x 32 x 3001 92 / 85, 32 x 48 x 3001 117 / 101; 30 heads of 64: 1 x 324 x 640 10 / 13, 2 x 231 x 871 15 / 16, 4 x 400 x 200 12.8 / 13.6, 25 x 1043 x 29
+// 73 / 80; 16 heads of 64, 2 x 128 x 2000, 10.5 / 16.9.
+static int kvb_block(DType dt, int B, int n, int H, int heads, int Dh, int length)
 {
     const int rows = n * (H / heads);
-    if (dt != DType::BF16 || rows <= 16) return 16;
-    return (long)B * heads * ((rows + 15) / 16) * length <= (rows <= 64 ? 16l << 17 : 5l << 17) ? 16 : 128;
+    if (dt != DType::BF16 || rows <= 16 || length <= 64) return 16;
+    return (long)B * heads * ((rows + 15) / 16) * length <= (rows <= 64 ? 16l << 17 : Dh == 64 ? 5l << 17 : 3l << 17) ? 16 : 128;
 }
 
 // nrb blocks per (sample, kv head), units in all, of which the first `full` take all keys and each other one is divided into `shares`.
 // `ragged`: samples of lengths of their own, which only the GPU knows.
-// waves: wavefronts of a workgroup, which divide a block's keys (16 rows), or its rows and, if there are 8, keys (128 rows).
+// waves: wavefronts of a workgroup, 1, 2, 4 or 8, which divide a block's keys (16 rows), or 4 or 8, which divide its rows and, if there are 8, keys (128 rows).
 // chunk: 16 rows, samples of lengths of their own: tiles of 32 keys of a share, so that workgroups have as much to do whatever the lengths.
 struct KvbRun { int block, nrb, units, full, shares, waves, chunk; };
 constexpr int kGroupsFrom = 2048, kGroupsTo = 4096;          // lengths at which the choice between one and two groups changes
@@ -1292,7 +1294,10 @@ static KvbRun kvb_run(int block, int B, int n, int H, int heads, int Dh, int len
         const int tiles = (length + 31) / 32;
         // Eight wavefronts where there are more tiles than that to divide and at most a workgroup for every CU: fewer shares to join, or
         // none (1 query of 16 heads of 128 over 600 keys 8.2 us in one launch, 7.7 + 2.8 by four; fp32, 2 x 128 x 552, 16 heads of 64, 8.8, 10.1).
-        run.waves = run.units <= 256 && tiles > 16 && !ragged ? 8 : 4;
+        // One where there is a single tile, or where blocks alone fill every SIMD's two places, two for two tiles and half as many blocks: no
+        // wavefront that waits, nothing to join (us by one / two / four: 9 x 370 rows x 26 keys, 30 heads of 64, 11.6 / - / 27.8; 16 heads of 128, 32 x 64
+        // x 119, 13.3 / 15.8 / 20.4, x 500 27.9 / - / 33.7, 16 x 64 x 500 - / 17.6 / 20.4; 2 x 64 x 100 9.1 / - / 5.5).
+        run.waves = run.units <= 256 && tiles > 16 && !ragged ? 8 : tiles <= 1 || run.units >= 2048 ? 1 : tiles <= 2 || run.units >= 1024 ? 2 : 4;
         // Enough wavefronts for two on every SIMD; four where samples differ, with shares as long as each other, so that a CU that has had
         // short ones takes more (32 samples of 1 to 16921 keys, 8 kv heads, 512, 1024, 2048, 4096 places: 127, 105, 108, 102 us and a joining of
         // 4.8, 4.8, 4.8, 9.8).  Each with two tiles per wavefront at least, or eight where every CU has a workgroup already.
@@ -1353,7 +1358,7 @@ size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, in
     for (int length : {capacity, kGroupsTo - 1, kGroupsFrom - 1}) {
         if (length > capacity) continue;
         for (int block = 16; block <= 128; block *= 8) {
-            if (block == 128 ? kvb_block(dt, B, n, H, heads, length) == 16 : kvb_block(dt, B, n, H, heads, 1) == 128) continue;
+            if (block == 128 ? kvb_block(dt, B, n, H, heads, Dh, length) == 16 : kvb_block(dt, B, n, H, heads, Dh, 1) == 128) continue;
             const size_t take = part_floats(kvb_run(block, B, n, H, heads, Dh, length, true), Dh);
             if (take > floats) floats = take;
         }
@@ -1364,13 +1369,13 @@ size_t kvb_attention_scratch_floats(DType dt, int B, int n, int H, int heads, in
 // How an attention is run, and the floats that it takes, for the tests: 100000 * rows of a block + 1000 * wavefronts + shares.
 int kvb_attention_ways(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged)
 {
-    const int block = kvb_block(bf16 ? DType::BF16 : DType::F32, B, n, H, heads, length);
+    const int block = kvb_block(bf16 ? DType::BF16 : DType::F32, B, n, H, heads, Dh, length);
     const KvbRun run = kvb_run(block, B, n, H, heads, Dh, length, ragged != 0);
     return 100000 * block + 1000 * run.waves + run.shares;
 }
 long kvb_attention_takes(int bf16, int B, int n, int H, int heads, int Dh, int length, int ragged, int weights)
 {
-    const int block = kvb_block(bf16 ? DType::BF16 : DType::F32, B, n, H, heads, length);
+    const int block = kvb_block(bf16 ? DType::BF16 : DType::F32, B, n, H, heads, Dh, length);
     const size_t part = part_floats(kvb_run(block, B, n, H, heads, Dh, length, ragged != 0), Dh);
     return (long)(part + (weights ? stat_floats(B, n, H) + weight_floats(B, n, H, heads, length) : 0));
 }
@@ -1381,7 +1386,7 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
 {
     const int length = c.lens ? c.capacity : c.len + extra;
     const DType dt = sizeof(T) == 2 ? DType::BF16 : DType::F32;
-    const KvbRun run = kvb_run(kvb_block(dt, B, n, H, c.heads, length), B, n, H, c.heads, DH, length, c.lens != nullptr);
+    const KvbRun run = kvb_run(kvb_block(dt, B, n, H, c.heads, DH, length), B, n, H, c.heads, DH, length, c.lens != nullptr);
     const int divided = run.units - run.full;
     float2 *stats = nullptr;
     float *sums = part, *scores = nullptr;
@@ -1399,7 +1404,9 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
            c_log2, (T *)o, run.nrb, run.shares, run.chunk, part, part_ml, stats, scores, pitch)
     if (run.block == 16) {
         if (run.waves == 8) { if (c.mask) FVAR_ROWS(8, true); else FVAR_ROWS(8, false); }
-        else { if (c.mask) FVAR_ROWS(4, true); else FVAR_ROWS(4, false); }
+        else if (run.waves == 4) { if (c.mask) FVAR_ROWS(4, true); else FVAR_ROWS(4, false); }
+        else if (run.waves == 2) { if (c.mask) FVAR_ROWS(2, true); else FVAR_ROWS(2, false); }
+        else { if (c.mask) FVAR_ROWS(1, true); else FVAR_ROWS(1, false); }
 #undef FVAR_ROWS
     } else if constexpr (sizeof(T) == 2) {
 #define FVAR_TILES(KG, WAVES)                                                                                            \

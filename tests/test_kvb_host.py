@@ -316,7 +316,10 @@ def ways(dtype, B, n, H, heads, dh, length, ragged):
 
 
 @pytest.mark.parametrize("dtype,B,n,H,heads,dh,length,ragged,expect", [
-    ("bf16", 2, 1, 2, 2, 64, 64, 0, (16, 4, 1)), ("bf16", 1, 1, 16, 16, 64, 700, 0, (16, 8, 1)), ("bf16", 1, 1, 16, 16, 128, 1300, 0, (16, 8, 2)),
+    ("bf16", 2, 1, 2, 2, 64, 64, 0, (16, 2, 1)), ("bf16", 2, 33, 4, 1, 128, 32, 0, (16, 1, 1)), ("bf16", 32, 64, 16, 16, 128, 150, 0, (16, 1, 1)),
+    ("bf16", 16, 64, 16, 16, 64, 500, 1, (16, 2, 1)), ("f32", 40, 60, 16, 16, 64, 90, 0, (16, 1, 1)), ("f32", 16, 70, 16, 16, 64, 200, 0, (16, 2, 1)),
+    ("bf16", 2, 7, 30, 30, 64, 100, 0, (16, 4, 1)), ("bf16", 8, 400, 16, 16, 128, 60, 0, (16, 1, 1)),
+    ("bf16", 1, 1, 16, 16, 64, 700, 0, (16, 8, 1)), ("bf16", 1, 1, 16, 16, 128, 1300, 0, (16, 8, 2)),
     ("bf16", 2, 3, 16, 4, 128, 9000, 1, (16, 4, 35)), ("bf16", 3, 1, 32, 8, 128, 517, 1, (16, 4, 2)), ("f32", 1, 5, 4, 2, 64, 3000, 0, (16, 8, 5)),
     ("bf16", 3, 257, 4, 4, 64, 700, 0, (16, 8, 1)), ("bf16", 32, 200, 30, 30, 64, 70, 0, (128, 4, 1)), ("bf16", 33, 129, 16, 16, 128, 1030, 0, (128, 4, 4)),
     ("bf16", 4, 512, 16, 16, 64, 4500, 0, (128, 8, 1)), ("bf16", 1, 1000, 2, 1, 128, 6000, 0, (128, 8, 11)), ("bf16", 2, 600, 8, 8, 64, 1700, 0, (128, 8, 3)),

@@ -1063,18 +1063,18 @@ __global__ __launch_bounds__(256) void kvb_attn_merge_kernel(const float *__rest
 
 // Weights of the rows: every wavefront holds 64 keys as bf16 operands, takes the scores of all rows of queries against them once more, and
 // adds up exp2((s - reference) * c) / sum over the rows, each key's in its own registers: no atomics, one order.  64 rows at a time come
-// through LDS for the four wavefronts, by DMA while the ones before are at work (fp32: 32 rows, in three pieces of bf16).  A row whose weights
-// are not numbers adds nothing.
-//   A workgroup: a block of 256 keys of one of `heads` (sample, kv head), and a share of its rows; several shares leave partial sums
-// [share][heads][256 * blocks].
-template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict__ q, int ld, KvbCache c, int extra, int n, int H, float c_log2,
+// through LDS for the W wavefronts, by DMA while the ones before are at work (32 in fp32, in three pieces of bf16, and for a single wavefront of 128-wide
+// rows, which 64 would run out of registers).  A row whose weights are not numbers adds nothing.
+//   A workgroup: a block of 64 W keys of one of `heads` (sample, kv head), and a share of its rows; several shares leave partial sums
+// [share][heads][64 W blocks].
+template <typename T, int DH, int W>
+__global__ __launch_bounds__(64 * W, 2) void kvb_weights_kernel(const T *__restrict__ q, int ld, KvbCache c, int extra, int n, int H, float c_log2,
                                                              const float2 *__restrict__ stats, float *__restrict__ weights, int add,
                                                              float *__restrict__ part, int blocks, int heads, int shares)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NP = F32 ? 3 : 1, KS = DH / 16, CH = DH / 8;   // CH: chunks of eight elements of a row
-    constexpr int SETS = F32 ? 1 : 2, ROWS = 32 * SETS, PER = ROWS * CH / 256;
+    constexpr int SETS = F32 || (W == 1 && DH == 128) ? 1 : 2, ROWS = 32 * SETS, PER = ROWS * CH / (64 * W);
     __shared__ uint4 ql[2][NP][ROWS * CH];
     const int tid = threadIdx.x, lane = tid & 63, rl = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1082,8 +1082,8 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     const int id = c.lens ? blockIdx.x : xcd_contiguous(blockIdx.x, gridDim.x);
     const int block = id % blocks, head = id / blocks % heads, share = id / blocks / heads, b = head / c.heads, hk = head % c.heads;
     const int G = H / c.heads, R = n * G, len = kvb_length(c, b, extra);
-    const int key0 = block * 256 + wave * 64;
-    if (block * 256 >= len) return;                          // (of the whole workgroup)
+    const int key0 = (block * W + wave) * 64;
+    if (block * (64 * W) >= len) return;                          // (of the whole workgroup)
     const int tiles = (R + ROWS - 1) / ROWS, t0 = (int)((long)tiles * share / shares), t1 = (int)((long)tiles * (share + 1) / shares);
 
     // ---- rows of queries: chunks are turned by the row's number, so that the rows of sixteen lanes that read one chunk lie in all banks
@@ -1096,7 +1096,7 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     auto fetch = [&](int t, int buffer) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = F32 ? i * 256 + tid : (wave * PER + i) * 64 + lane;
+            const int at = F32 ? i * (64 * W) + tid : (wave * PER + i) * 64 + lane;
             const int in_tile = at / CH, row = min(t * ROWS + in_tile, R - 1);
             const int query = shift >= 0 ? row >> shift : row / G;
             const size_t src = (size_t)query * ld + (row - query * G) * DH;
@@ -1117,7 +1117,7 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
         if constexpr (F32) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int at = i * 256 + tid, to = at / CH * CH + ((at % CH) ^ turn(at / CH));
+                const int at = i * (64 * W) + tid, to = at / CH * CH + ((at % CH) ^ turn(at / CH));
                 float x[8];
                 bf16x8_t pieces[3];
                 Elem<float>::unpack(next[i][0], x);
@@ -1243,7 +1243,7 @@ __global__ __launch_bounds__(256, 2) void kvb_weights_kernel(const T *__restrict
     if (key >= len) return;
     if (c.mask && c.mask[(size_t)b * c.capacity + key] == 0) mine = 0.f;
     if (shares > 1) {
-        part[((size_t)share * heads + head) * (256 * blocks) + key] = mine;
+        part[((size_t)share * heads + head) * (64 * W * blocks) + key] = mine;
         return;
     }
     float *to = weights + (size_t)head * c.capacity + key;
@@ -1333,16 +1333,20 @@ static size_t score_tiles(int length) { return ((size_t)length + 31) / 32; }
 
 // Shares of the rows of queries for the weights: where the keys alone do not fill the chip.
 constexpr int kWeightPlaces = 512;
-static int weight_shares(int B, int heads, int length, int rows)
+// A single wavefront for each, where it has all keys there are and the heads alone are as many as the CUs: with four, three would have none (us by one / by
+// four, joining included: 30 heads of 64, 9 x 370 rows x 26 keys 12.8 / 15.4, 25 x 1043 x 29 31 / 55; 16 heads of 128, 32 x 400 x 50 21 / 24, 32 x 36 x
+// 55 6.3 / 8.1; 8 x 97 x 60, heads of 64, 9.6 / 9.1, 2 x 375 x 2 11.3 / 10.3).
+static int weight_waves(DType dt, int B, int heads, int length) { return dt == DType::BF16 && length <= 64 && (long)B * heads >= 256 ? 1 : 4; }
+static int weight_shares(int B, int heads, int length, int rows, int waves)
 {
-    const long wgs = (long)B * heads * ((length + 255) / 256);
-    long shares = wgs > 0 ? kWeightPlaces / wgs : 1;
+    const long wgs = (long)B * heads * ((length + 64 * waves - 1) / (64 * waves));
+    long shares = wgs > 0 ? kWeightPlaces * 4 / waves / wgs : 1;
     if (shares > (rows + 31) / 128) shares = (rows + 31) / 128;      // (fewer than 128 rows each are not worth a joining)
     return (int)(shares > 8 ? 8 : shares < 1 ? 1 : shares);
 }
 
 // Floats that partial results take, and, before them, what the weights need: every row's reference and sum; their scores, or partial sums of
-// at most kWeightPlaces workgroups of 256 keys.
+// at most kWeightPlaces workgroups of 256 keys, or four times as many of 64.
 static size_t part_floats(const KvbRun &run, int Dh) { return (size_t)(run.units - run.full) * run.shares * run.block * (Dh + 2); }
 static size_t stat_floats(int B, int n, int H) { return (2 * (size_t)B * n * H + 3) / 4 * 4; }
 static size_t weight_floats(int B, int n, int H, int heads, int length)
@@ -1435,12 +1439,18 @@ static void launch_kvb(const void *q, int ld, const KvbCache &c, int extra, int 
             launch(kvb_weights_few_kernel, dim3((unsigned)few_wgs), dim3(256), 0, st, c, extra, rows, c_log2, (const float2 *)stats,
                    (const float *)scores, pitch, weights, add ? 1 : 0, few_blocks);
     } else if (weights && length > 0) {
-        const int blocks = (length + 255) / 256, shares = weight_shares(B, c.heads, length, rows);
-        launch(kvb_weights_kernel<T, DH>, dim3((unsigned)(blocks * B * c.heads * shares)), dim3(256), 0, st, (const T *)q, ld, c, extra, n, H, c_log2,
-               (const float2 *)stats, weights, add ? 1 : 0, sums, blocks, B * c.heads, shares);
+        const int waves = weight_waves(dt, B, c.heads, length), blocks = (length + 64 * waves - 1) / (64 * waves), shares = weight_shares(B, c.heads, length, rows, waves);
+#define FVAR_WEIGHTS(W)                                                                                                  \
+    launch(kvb_weights_kernel<T, DH, W>, dim3((unsigned)(blocks * B * c.heads * shares)), dim3(64 * W), 0, st, (const T *)q, ld, c, extra, n, H, c_log2, \
+           (const float2 *)stats, weights, add ? 1 : 0, sums, blocks, B * c.heads, shares)
+        if (waves == 4) FVAR_WEIGHTS(4);
+        else if constexpr (sizeof(T) == 2) {
+            FVAR_WEIGHTS(1);
+        }
+#undef FVAR_WEIGHTS
         if (shares > 1)
-            launch(kvb_weights_join_kernel, dim3((unsigned)blocks, (unsigned)(B * c.heads)), dim3(256), 0, st, c, extra, (const float *)sums,
-                   256 * blocks, shares, weights, add ? 1 : 0);
+            launch(kvb_weights_join_kernel, dim3((unsigned)((length + 255) / 256), (unsigned)(B * c.heads)), dim3(256), 0, st, c, extra, (const float *)sums,
+                   64 * waves * blocks, shares, weights, add ? 1 : 0);
     }
 }
 

@@ -236,7 +236,7 @@ LARGE = [("bf16", 30, 30, 64, 32, 200, 70), ("bf16", 16, 16, 128, 33, 129, 1030)
 TILES = [("bf16", 2, 1, 128, 1, 1000, 6000), ("bf16", 8, 8, 64, 2, 600, 1700), ("bf16", 16, 16, 64, 5, 230, 4100), ("bf16", 16, 4, 64, 40, 40, 900)]
 # blocks of 16 rows by a single wavefront, and by two
 FEW = [("bf16", 16, 16, 128, 32, 64, 150), ("bf16", 16, 16, 64, 16, 64, 500), ("f32", 16, 16, 64, 40, 60, 90), ("f32", 16, 16, 64, 16, 70, 200),
-       ("bf16", 16, 16, 128, 8, 400, 60), ("f32", 8, 4, 128, 20, 110, 31)]
+       ("bf16", 16, 16, 128, 8, 400, 60), ("f32", 8, 4, 128, 20, 110, 31), ("bf16", 30, 30, 64, 9, 370, 26), ("bf16", 16, 16, 128, 17, 40, 55), ("bf16", 32, 16, 128, 16, 150, 64)]
 
 
 @pytest.mark.parametrize("dtype,H,heads,dh,B,n,L", SHAPES + LARGE + TILES + FEW)

@@ -1205,6 +1205,8 @@ __global__ __launch_bounds__(64 * W, 2) void kvb_weights_kernel(const T *__restr
         if (t + 1 < t1) fetch(t + 1, buffer ^ 1);
 #pragma unroll
         for (int j = 0; j < SETS; ++j) {
+            // (a set without a row would be the last row's copies: products for nothing, and where that row's scores are no numbers, no lane would tell)
+            if (j && t * ROWS + j * 32 >= R) break;
             if (!F32 && __builtin_expect(plain, 1)) {
                 products(std::true_type{}, buffer, j);
             } else {

@@ -1,0 +1,46 @@
+"""Attention over the 8-bit cache in 64 bits on the GPU, for tests whose sizes would take numpy long, with what bounds the kernels' errors."""
+import torch
+
+
+def reference(q, k, v, seen, scale, counts=None):
+    """q [B, n, H, dh], k and v [B, heads, L, dh], seen [B, L], all on the GPU; counts [B, n, H]: the queries that add to the rows' weights.
+    -> o [B, n, H, dh], weights [B, heads, L], size [B, n, H]: the largest scale sum |q k| of a query, span [B, n, H, dh]: sum p |v|."""
+    B, n, H, dh = q.shape
+    heads, L = k.shape[1], k.shape[2]
+    G = H // heads
+    rows = q.double().reshape(B, n, heads, G, dh).permute(0, 2, 1, 3, 4).reshape(B * heads, n * G, dh).contiguous()
+    kk, vv = k.double().reshape(B * heads, L, dh), v.double().reshape(B * heads, L, dh)
+    hidden = ~seen[:, None].expand(B, heads, L).reshape(B * heads, 1, L)
+    kk, vv = (x.masked_fill(hidden.swapaxes(1, 2), 0) for x in (kk, vv))          # (what hidden rows hold is no number at times)
+    kt = kk.swapaxes(1, 2).contiguous()
+    s = (torch.bmm(rows, kt) * scale).masked_fill(hidden, -torch.inf)
+    p = torch.exp(s - s.amax(-1, keepdim=True).clamp_min(-1e300))
+    p = p / p.sum(-1, keepdim=True).clamp_min(1e-300)
+    size = torch.bmm(rows.abs(), kt.abs()).masked_fill(hidden, 0).amax(-1) * scale
+    back = lambda x: x.reshape(B, heads, n, G, -1).permute(0, 2, 1, 3, 4).reshape(B, n, H, -1)
+    o, span = back(torch.bmm(p, vv)), back(torch.bmm(p, vv.abs()))
+    if counts is not None:
+        live = counts.reshape(B, n, heads, G).permute(0, 2, 1, 3).reshape(B * heads, n * G, 1)
+        p = torch.where(live, p, 0.0)
+    return o, p.sum(1).reshape(B, heads, L), back(size[..., None])[..., 0], span
+
+
+def score_error(size, dh, block):
+    """By how much a score may be off: blocks of 128 rows add products up to 2^-14 of their sizes' sum, the others in fp32, in any order."""
+    return size * (2.0 ** -14 if block == 128 else dh * 2.0 ** -24)
+
+
+def weight_room(want, size, dh, block):
+    """want [B, heads, L], size: the largest scale sum |q k|.  The numerators are fp32 scores' exponentials, the sums those of scores of score_error;
+    exp and the division 2^-22, sums of positive numbers their steps times 2^-24, below 2^-18 for what is tested."""
+    off = 2 * dh * 2.0 ** -24 * size + (score_error(size, dh, 128) if block == 128 else 0.0)
+    return want * (torch.expm1(torch.as_tensor(off, dtype=torch.float64)) + 2.0 ** -20 + 2.0 ** -18) + 1e-30
+
+
+def output_room(o, span, size, most, L, dh, block):
+    """bf16 contexts.  Weights: of scores off by score_error, in p and in its sum; rounded to fp16 once, 2^-11, or 2^-25 below its normal numbers
+    where the largest is 2^8 at least: 2^-33 each.  Values: fp16 next to the largest, `most` [B, 1, H, 1], of the blocks with a visible row, which stands at
+    2^11 of them at least: 2^-25 is 2^-36 of it.  Sums of L numbers in fp32.  The output's own rounding: 2^-8."""
+    wrong = torch.expm1(2 * score_error(size, dh, block))[..., None] + 2.0 ** -11 + (L + 64) * 2.0 ** -24
+    room = wrong * span + (L * 2.0 ** -33 + 2.0 ** -36) * most
+    return room + 2.0 ** -8 * (o.abs() + room) + 1e-38

@@ -1,0 +1,70 @@
+"""Attention over the 8-bit cache where queries or keys are no numbers."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_16483_amd as fv
+
+pytestmark = pytest.mark.gpu
+
+from gpu_util import to_dev  # noqa: E402
+from kvb_util import reference, weight_room  # noqa: E402
+from test_gpu_kvb import attend, ctx_of, empty_cache, load, rows_of  # noqa: E402
+from test_kvb_host import ways  # noqa: E402
+
+# rows of queries R = n H / heads by their remainder of 64, whole sets of 32 and not; keys by one and by four wavefronts; rows in two shares
+ROWS = [(64, 2, 2, 1, 1, 200), (128, 4, 1, 2, 3, 90), (64, 2, 2, 1, 17, 200), (128, 4, 2, 1, 16, 200), (64, 2, 2, 2, 33, 200), (128, 2, 2, 1, 63, 130),
+        (64, 1, 1, 1, 65, 300), (128, 2, 1, 2, 48, 100), (64, 4, 4, 1, 200, 333), (64, 2, 1, 1, 130, 300), (64, 16, 16, 16, 20, 60),
+        (128, 16, 16, 17, 20, 60), (64, 32, 16, 16, 36, 64), (128, 16, 8, 4, 270, 300)]
+
+
+def _setup(dtype, dh, H, heads, B, n, L):
+    ctx, kv = ctx_of(H, dh, dtype), empty_cache(B, heads, L + 3, dh, fill=0x7F, len=L)
+    k, v = (torch.from_numpy(x).cuda() for x in load(kv, rows_of(1, B, L, heads, dh, dtype), rows_of(2, B, L, heads, dh, dtype)))
+    return ctx, kv, k, v, to_dev(rows_of(3, B, n, H, dh, dtype, spread=0.2), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dh,H,heads,B,n,L", ROWS)
+def test_a_last_query_that_is_no_number_adds_no_weight(dtype, bad, dh, H, heads, B, n, L):
+    ctx, kv, k, v, q = _setup(dtype, dh, H, heads, B, n, L)
+    clean = attend(ctx, q, kv, dtype, B, n)
+    counts = torch.ones((B, n, H), dtype=torch.bool, device="cuda")
+    for b in range(0, B, 2):                                  # the last row of the first kv head and of the last
+        for h in {H // heads - 1, H - 1}:
+            q[b, n - 1, h, 5 + h] = bad
+            counts[b, n - 1, h] = False
+    w = torch.full((B, heads, L + 3), 0.5, device="cuda")
+    o = attend(ctx, q, kv, dtype, B, n, weights=w, add=True)
+    assert torch.equal(o[counts], clean[counts])
+    assert torch.isnan(o[~counts]).any(-1).all()
+    seen = torch.ones((B, L), dtype=torch.bool, device="cuda")
+    q[~counts] = 0
+    _, want, size, _ = reference(q, k[:, :, :L], v[:, :, :L], seen, dh ** -0.5, counts)
+    block = ways(dtype, B, n, H, heads, dh, L, 0)[0]
+    off = (w[:, :, :L].double() - 0.5 - want).abs()
+    assert (off <= weight_room(want, float(size.max()), dh, block) + 2.0 ** -24 * (0.5 + want)).all(), float(off.max())
+    assert (w[:, :, L:] == 0.5).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh,H,heads,B,n,L", ROWS)
+def test_a_visible_key_that_is_no_number_leaves_its_head_without_weights(dtype, dh, H, heads, B, n, L):
+    ctx, kv, _, _, q = _setup(dtype, dh, H, heads, B, n, L)
+    clean = torch.full((B, heads, L + 3), 0.5, device="cuda")
+    want = attend(ctx, q, kv, dtype, B, n, weights=clean, add=True)
+    kv.k[B - 1, heads - 1, L // 2, 7] = 0x7F
+    w = torch.full((B, heads, L + 3), 0.5, device="cuda")
+    o = attend(ctx, q, kv, dtype, B, n, weights=w, add=True)
+    G = H // heads
+    assert torch.isnan(o[B - 1, :, H - G:]).all() and (w[B - 1, heads - 1] == 0.5).all()
+    o[B - 1, :, H - G:], w[B - 1, heads - 1] = want[B - 1, :, H - G:], clean[B - 1, heads - 1]
+    assert torch.equal(o, want) and torch.equal(w, clean)
+    kv.mask = torch.ones((B, L + 3), dtype=torch.uint8, device="cuda")
+    kv.mask[B - 1, L // 2] = 0                                # hidden, it has no influence
+    attend(ctx, q, kv, dtype, B, n, weights=w)
+    assert torch.isfinite(w[:, :, :L]).all() and not w[B - 1, :, L // 2].any()
+    assert (w[:, :, :L].sum(-1) - n * G).abs().max() <= 1e-3 * n * G

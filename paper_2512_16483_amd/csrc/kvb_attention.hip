@@ -77,7 +77,8 @@ __device__ __forceinline__ void three_pieces(const float *x, bf16x8_t *out)
 // Queries in two E4M3 numbers per element, with a power of two per row, 2^e, and 2^(e-4) for what the first leaves: the first leaves at most half
 // a step of its binade, eight steps of bf16's eight bits, which the second holds whole.  (Elements below 2^-15 of their row's largest are held to
 // 2^-23 of it, as fp32 sums hold them.)  top: of the row's bits, sign taken off; from it the scale bytes of both pieces, in byte 0 and 1.
-// A row with an element that is not finite becomes NaN, and so do its scores.
+// A row with an element that is not finite becomes NaN, and so do its scores.  bf16 goes up to 255 * 2^120, past the cache's largest power: from 464 * 2^119
+// on a row's is 2^120, whose largest first piece is 240 * 2^120 (256 would not be a finite fp32 number); 15 * 2^120 and less is left, 240 * 2^116.
 __device__ __forceinline__ uint32_t top_of_eight(uint4 w, uint32_t top)
 {
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};
@@ -87,14 +88,17 @@ __device__ __forceinline__ uint32_t top_of_eight(uint4 w, uint32_t top)
 }
 __device__ __forceinline__ int piece_bytes(uint32_t top)
 {
-    const int byte = (int)kvb_byte(top >= 0x7f800000u ? 0x3f800000u : top);
+    const int byte = max((int)kvb_byte(top >= 0x7f800000u ? 0x3f800000u : top), top > 0x7f680000u && top < 0x7f800000u ? 247 : 0);
     return byte | (byte - 4) << 8;
 }
 __device__ __forceinline__ void two_pieces(uint32_t a, uint32_t b, uint32_t top, int bytes, int &first, int &second)
 {
     const float size = __uint_as_float((uint32_t)(bytes & 255) << 23), rest = __uint_as_float((uint32_t)(bytes >> 8) << 23);
-    float x[4] = {bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b)};
-    const uint32_t one = kvb_four(x, size);
+    const float most = 240.f * 0x1p120f;
+    float x[4] = {bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b)}, y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_fmed3f(x[i], -most, most);
+    const uint32_t one = kvb_four(y, size);
     const floatx2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(one, size, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(one, size, true);
     x[0] -= lo[0]; x[1] -= lo[1]; x[2] -= hi[0]; x[3] -= hi[1];
     const bool odd = top >= 0x7f800000u;

@@ -1,4 +1,4 @@
-"""Attention over the 8-bit cache where queries or keys are no numbers."""
+"""Attention over the 8-bit cache where queries, keys and values are no numbers, or among the largest and smallest that their type has."""
 import math
 
 import numpy as np
@@ -10,7 +10,7 @@ import paper_2512_16483_amd as fv
 pytestmark = pytest.mark.gpu
 
 from gpu_util import to_dev  # noqa: E402
-from kvb_util import reference, weight_room  # noqa: E402
+from kvb_util import output_room, reference, weight_room  # noqa: E402
 from test_gpu_kvb import attend, ctx_of, empty_cache, load, rows_of  # noqa: E402
 from test_kvb_host import ways  # noqa: E402
 
@@ -68,3 +68,33 @@ def test_a_visible_key_that_is_no_number_leaves_its_head_without_weights(dtype, 
     attend(ctx, q, kv, dtype, B, n, weights=w)
     assert torch.isfinite(w[:, :, :L]).all() and not w[B - 1, :, L // 2].any()
     assert (w[:, :, :L].sum(-1) - n * G).abs().max() <= 1e-3 * n * G
+
+
+# blocks of 16 rows, of 128 by four wavefronts and by eight, and in shares
+SIZES = [(64, 2, 2, 1, 1, 100), (128, 4, 2, 2, 20, 90), (64, 30, 15, 17, 65, 300), (128, 8, 8, 17, 150, 300), (64, 8, 4, 17, 65, 1100),
+         (128, 4, 2, 3, 129, 4100)]
+
+
+@pytest.mark.parametrize("dh,H,heads,B,n,L", SIZES)
+def test_queries_up_to_the_largest_number_of_their_type(dh, H, heads, B, n, L):
+    """Elements of 200 to 255 times 2^120, bf16's largest among them, over keys so small that scores are as usual."""
+    ctx, kv = ctx_of(H, dh, "bf16"), empty_cache(B, heads, L, dh, len=L)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    draw = lambda *s: torch.randn(s, generator=g, device="cuda")
+    rows = [(draw(B, L, heads, dh) * by).bfloat16() for by in (2.0 ** -124, 1)]
+    fv.fvar_kvb_append(ctx, fv.KVB(kv.k, kv.v, kv.k_scale, kv.v_scale), *rows, B, L)
+    held = [torch.empty_like(x) for x in rows]
+    fv.fvar_kvb_read(ctx, kv, B, 0, L, *held)
+    m = torch.randint(200, 256, (B, n, H, dh), generator=g, device="cuda")
+    m[:, :, :, 0] = 255
+    q = (m * torch.where(draw(B, n, H, dh) < 0, -1, 1) * 2.0 ** 120).bfloat16()
+    assert torch.equal(q.double().abs(), m.double() * 2.0 ** 120)
+    w = torch.zeros((B, heads, L), device="cuda")
+    o = attend(ctx, q, kv, "bf16", B, n, weights=w).double()
+    seen = torch.ones((B, L), dtype=torch.bool, device="cuda")
+    k, v = (x.swapaxes(1, 2).contiguous() for x in held)
+    want, sums, size, span = reference(q, k, v, seen, dh ** -0.5)
+    block = ways("bf16", B, n, H, heads, dh, L, 0)[0]
+    room = output_room(want, span, size, float(v.abs().max()), L, dh, block)
+    assert ((o - want).abs() <= room).all(), float(((o - want).abs() / room).max())
+    assert ((w.double() - sums).abs() <= weight_room(sums, float(size.max()), dh, block)).all()

@@ -35,6 +35,8 @@ __device__ __forceinline__ uint4 bf16_eight(uint32_t a, uint32_t b, float s)
 {
     return make_uint4(kvb_bf16<0>(a, s), kvb_bf16<1>(a, s), kvb_bf16<0>(b, s), kvb_bf16<1>(b, s));
 }
+// of four codes those that are no numbers, and 0 for the others
+__device__ __forceinline__ uint32_t no_number(uint32_t x) { return x & ((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)min(max(e + 127, 0), 254) << 23); }
 
 // the same value in the lanes of a column group: 16 and 32 lanes apart
@@ -270,6 +272,12 @@ __global__ __launch_bounds__(64 * NW, 2) void kvb_attn_rows_kernel(const T *__re
             const int ve = (int)__builtin_amdgcn_readfirstlane((int)x.vs) - 127;
             if (__builtin_expect(ve > E, 0)) E = ve + kRoom;
             const float vsize = power_of_two(ve - E + TOP);
+            if (F32 && __builtin_expect(ve - E + TOP < -126, 0)) {
+                // below 2^-188 of the largest: 0, as the least scale that there is would make them more than they are
+#pragma unroll
+                for (int j = 0; j < VL; ++j)
+                    x.v[j] = make_uint4(no_number(x.v[j].x), no_number(x.v[j].y), no_number(x.v[j].z), no_number(x.v[j].w));
+            }
 #pragma unroll
             for (int j = 0; j < VL; ++j) {
                 const int key = (64 * j + lane) / VP, piece = (lane % VP) ^ turn(key);

@@ -98,3 +98,43 @@ def test_queries_up_to_the_largest_number_of_their_type(dh, H, heads, B, n, L):
     room = output_room(want, span, size, float(v.abs().max()), L, dh, block)
     assert ((o - want).abs() <= room).all(), float(((o - want).abs() / room).max())
     assert ((w.double() - sums).abs() <= weight_room(sums, float(size.max()), dh, block)).all()
+
+
+@pytest.mark.parametrize("n", [1, 20, 150])
+@pytest.mark.parametrize("at", [0, 2, 4])
+@pytest.mark.parametrize("less", [60, 150, 195, 215])
+def test_fp32_values_far_below_those_of_a_block_without_weight(n, at, less):
+    """A block of values 2^less times larger than all others, whose keys get no weight at all: the others count down to 2^-180 of it as they are, and
+    from there on no more than they are."""
+    H, heads, dh, B, L = 2, 1, 64, 2, 160
+    ctx, kv = ctx_of(H, dh, "f32"), empty_cache(B, heads, L, dh, len=L)
+    g = torch.Generator(device="cuda").manual_seed(less + at)
+    draw = lambda *s: torch.randn(s, generator=g, device="cuda")
+    q, k, v = draw(B, n, H, dh), draw(B, L, heads, dh), draw(B, L, heads, dh) * 2.0 ** (110 - less)
+    far = slice(32 * at, 32 * at + 32)
+    q[..., 0], k[..., 0] = 40, 0
+    k[:, far, :, 0] = -40                                     # 200 less than the other scores, and more: exp(-200) is 0 in fp32
+    v[:, far] = draw(B, 32, heads, dh) * 2.0 ** 110
+    fv.fvar_kvb_append(ctx, fv.KVB(kv.k, kv.v, kv.k_scale, kv.v_scale), k, v, B, L)
+    held = [torch.empty_like(k), torch.empty_like(v)]
+    fv.fvar_kvb_read(ctx, kv, B, 0, L, *held)
+    o = attend(ctx, q, kv, "f32", B, n).double()
+    seen = torch.ones((B, L), dtype=torch.bool, device="cuda")
+    seen[:, far] = False                                      # (their part, exp(-150) 2^215 of the others' at most, would show in 64 bits)
+    want, _, size, span = reference(q, *[x.swapaxes(1, 2).contiguous() for x in held], seen, dh ** -0.5)
+    wrong = 2 * dh * 2.0 ** -24 * float(size.max()) + (L + 64) * 2.0 ** -24
+    room = span * (wrong if less < 180 else 1 + wrong)
+    assert ((o - want).abs() <= room).all(), float(((o - want).abs() / span).max())
+
+
+@pytest.mark.parametrize("n", [1, 20])
+def test_fp32_values_that_are_no_numbers_stay_so_far_below_a_larger_block(n):
+    H, heads, dh, B, L = 1, 1, 64, 1, 160
+    ctx, kv = ctx_of(H, dh, "f32"), empty_cache(B, heads, L, dh, len=L)
+    v = torch.randn(B, L, heads, dh, device="cuda") * 2.0 ** -105
+    v[:, :32] = 2.0 ** 110
+    v[:, 130, :, 9] = math.nan
+    k = torch.randn_like(v).clamp(-3, 3)
+    fv.fvar_kvb_append(ctx, fv.KVB(kv.k, kv.v, kv.k_scale, kv.v_scale), k, v, B, L)
+    o = attend(ctx, torch.randn(B, n, H, dh, device="cuda"), kv, "f32", B, n)
+    assert torch.isnan(o[..., 9]).all() and torch.isfinite(o[..., :9]).all() and torch.isfinite(o[..., 10:]).all()

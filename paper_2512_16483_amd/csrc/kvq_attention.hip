@@ -280,6 +280,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 2 : 3) void kvq_attn_rows
                 if (seen && x.vs[j] != 255) top = max(top, x.vs[j]);
             }
             if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)top > E) != 0, 0)) E = (int)wave_max(top) + kRoom;
+            if (F32 && __builtin_expect(__builtin_amdgcn_readfirstlane(E) > kLarge, 0)) {
+                // 2^-188 of the largest and less: 0, as the least scale that there is would make them more than they are
+#pragma unroll
+                for (int j = 0; j < VL; ++j)
+                    if ((int)x.vs[j] - E + TOP < 1) x.v[j] = make_uint4(0, 0, 0, 0);
+            }
 #pragma unroll
             for (int j = 0; j < VL; ++j) {
                 const int key = (64 * j + lane) / NB, blk = lane % NB;

@@ -113,7 +113,7 @@ def test_fp32_values_far_below_those_of_a_block_without_weight(n, at, less):
     q, k, v = draw(B, n, H, dh), draw(B, L, heads, dh), draw(B, L, heads, dh) * 2.0 ** (110 - less)
     far = slice(32 * at, 32 * at + 32)
     q[..., 0], k[..., 0] = 40, 0
-    k[:, far, :, 0] = -40                                     # 200 less than the other scores, and more: exp(-200) is 0 in fp32
+    k[:, far, :, 0] = -40                                     # 200 less than the other scores: exp(-150) is 0 in fp32
     v[:, far] = draw(B, 32, heads, dh) * 2.0 ** 110
     fv.fvar_kvb_append(ctx, fv.KVB(kv.k, kv.v, kv.k_scale, kv.v_scale), k, v, B, L)
     held = [torch.empty_like(k), torch.empty_like(v)]

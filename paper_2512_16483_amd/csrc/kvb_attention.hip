@@ -26,6 +26,7 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 // fp32 takes values as they are in bf16, exact, up to tiles of 2^64, and at 2^64 over E from there on: a sum of weights up to 2^7 each stays finite.
 constexpr int kTop = 6, kRoom = 2, kLarge = 64;
 constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
+constexpr float kPlain = 11.5f;                              // largest product of an element of a query and of a key: 8 in a score, in units of log2
 
 __device__ __forceinline__ uint4 half_eight(uint32_t a, uint32_t b, float s)
 {
@@ -413,8 +414,12 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 // matrix cores and the softmax bound the time.
 //   S^T = K Q^T by the 32x32x64 block-scaled MFMA: it takes keys in 8 bits with their scale bytes as they lie in memory, so K is not
 //     converted.  Q goes in as two numbers per element (see two_pieces): two products at twice the rate of bf16 take as long as one
-//     of bf16 would, without a conversion of K.  (It adds 64 products less exactly than bf16's are added: scores are off by 2^-14.6 of
-//     the sum of their products' sizes at most, 2^-19 rms, which at sums of 10 is 2^-11 of a weight at most; fp16 holds one to 2^-12.)
+//     of bf16 would, without a conversion of K.  It adds eight products of neighbouring elements at a time, and drops of each what lies below 2^-13
+//     of the largest: of normal numbers, 2^-15 of the sum of the products' sizes at most, 2^-18 rms, which at sums of 10 is 2^-11 of a weight at most (fp16 holds
+//     one to 2^-12); where one channel is far larger than the others, up to 2^-10.  So the scores of keys whose products with the wavefront's queries
+//     might pass 8, by their block's power and the queries' largest element, are made once more by bf16 products, which are added in fp32: what a
+//     product loses is 2^-10 at most.  4 x 1600 x 12121, 32 heads, one channel 20 times the others', all keys that way: 2100 us (1120 without, and
+//     outputs of such keys off by 4.6e-3 of their 2-norm); where none are, 1171 (1167).
 //   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
 // In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
 // product takes it, as in attention.hip.
@@ -510,7 +515,7 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvb_attn_tiles_kernel(const u
 
     // ---- Q in two pieces of 8 bits: lane = row, elements 64 s + 32 g .. + 31
     intx8_t qf[KS][2];
-    int qbyte;
+    int qbyte, plain_to;                                     // plain_to: the largest scale byte of keys whose products with these rows stay within kPlain
     {
         const uint16_t *src = q + (size_t)(b * (long)n + row / G) * ld + (size_t)(hk * G + row % G) * DH + g * 32;
         uint4 w[KS][4];
@@ -525,6 +530,8 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvb_attn_tiles_kernel(const u
         const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
         top = max(both[0], both[1]);
         qbyte = piece_bytes(top);
+        const float largest = __uint_as_float(kvb_wave_max(top >= 0x7f800000u ? 0 : top));
+        plain_to = __builtin_amdgcn_readfirstlane((int)(__float_as_uint(kPlain / fabsf(c_log2) / 464.f / largest) >> 23));
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -672,6 +679,24 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvb_attn_tiles_kernel(const u
         }
     };
 #undef FVAR_S
+    // A half's scores once more, by bf16 products of what its keys and the queries' pieces stand for, which are added in fp32.
+    auto exact = [&](int half, int kb) __attribute__((always_inline)) {
+        const float ksize = __uint_as_float((uint32_t)kb << 23);
+        s[half] = bases;
+#pragma unroll
+        for (int p = 1; p >= 0; --p) {
+            float size = __uint_as_float((uint32_t)(qbyte >> (8 * p) & 255) << 23);
+            asm volatile("" : "+v"(size));                   // (or the queries are converted ahead of the loop, into registers that there are none of)
+#pragma unroll
+            for (int i = 0; i < KS * 4; ++i) {
+                const uintx4_t w = *(lds_uintx4_t *)(kp[i / 4][i / 2 % 2] + half * (RAW / 2));
+                const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, i & 1 ? bf16_eight(w[2], w[3], ksize) : bf16_eight(w[0], w[1], ksize));
+                const bf16x8_t qe = __builtin_bit_cast(bf16x8_t, bf16_eight(qf[i / 4][p][i % 4 * 2], qf[i / 4][p][i % 4 * 2 + 1], size));
+                s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qe, s[half], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
     auto load_v = [&](int i, int rows) -> f16x8_t {
         const shortx4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vp[i][0] + rows * DH * 2));
         const shortx4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vp[i][1] + rows * DH * 2));
@@ -743,47 +768,51 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvb_attn_tiles_kernel(const u
                 if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1)) s[half][i] = -INFINITY;
         }
     };
-    auto settle = [&](int half) {
+    auto renew = [&](int half) __attribute__((always_inline)) {
+        float mx = s[half][0];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
+        const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+        const bool had = most >= 0.f, none = !had && mx == -INFINITY;
+        float alpha = 1.f;
+        const float over = FROM ? mx : mx - m_ref;
+        if (!none && (!had || over > 0.f)) {
+            if constexpr (FROM) {
+                s[0] -= mx;
+                s[1] -= mx;
+            }
+            set_base(FROM ? m_ref + mx : mx);
+            alpha = __builtin_amdgcn_exp2f(-over * c_log2);
+        }
+        if (!had) alpha = 0.f;
+        const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E_now, -200));
+        most = none ? -1.f : kMost;
+        acc_E = E_now;
+        l_run *= alpha;
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            acc[i] *= down;
+            asm volatile("" : "+v"(acc[i]));
+        }
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            const float x = __builtin_amdgcn_exp2f(exponent(s[half][i]));
+            const float y = __builtin_amdgcn_exp2f(exponent(s[half][i + 1]));
+            sum += x + y;
+            const f16x2v_t p = __builtin_convertvector((floatx2_t{x, y}), f16x2v_t);
+            pf[half][i >> 3][i & 7] = p[0];
+            pf[half][i >> 3][(i & 7) + 1] = p[1];
+        }
+    };
+    auto settle = [&](int half, int kb) __attribute__((always_inline)) {     // kb: of the keys whose scores the region has made
         // The reference is not the running maximum but one that was it; the weights tell when it no longer serves.  A sum of NaN
         // does not ask for another: it stays NaN.
         const bool anew = (__builtin_amdgcn_ballot_w64(sum > most) != 0 && (uint32_t)(vis >> (32 * half)) != 0) || E_now != acc_E;
-        if (__builtin_expect(anew, 0)) {
-            float mx = s[half][0];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[half][i]);
-            const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-            mx = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-            const bool had = most >= 0.f, none = !had && mx == -INFINITY;
-            float alpha = 1.f;
-            const float over = FROM ? mx : mx - m_ref;
-            if (!none && (!had || over > 0.f)) {
-                if constexpr (FROM) {
-                    s[0] -= mx;
-                    s[1] -= mx;
-                }
-                set_base(FROM ? m_ref + mx : mx);
-                alpha = __builtin_amdgcn_exp2f(-over * c_log2);
-            }
-            if (!had) alpha = 0.f;
-            const float down = __builtin_amdgcn_ldexpf(alpha, max(acc_E - E_now, -200));
-            most = none ? -1.f : kMost;
-            acc_E = E_now;
-            l_run *= alpha;
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                acc[i] *= down;
-                asm volatile("" : "+v"(acc[i]));
-            }
-            sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(exponent(s[half][i]));
-                const float y = __builtin_amdgcn_exp2f(exponent(s[half][i + 1]));
-                sum += x + y;
-                const f16x2v_t p = __builtin_convertvector((floatx2_t{x, y}), f16x2v_t);
-                pf[half][i >> 3][i & 7] = p[0];
-                pf[half][i >> 3][(i & 7) + 1] = p[1];
-            }
+        if (__builtin_expect(anew || kb > plain_to, 0)) {
+            if (kb > plain_to) exact(1 - half, kb);
+            if (anew) renew(half);
         }
         l_run += sum;
     };
@@ -801,13 +830,15 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvb_attn_tiles_kernel(const u
         const int kb = byte_of(kbytes, t0, 0);
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) score(0, i, k, kb);
+        if (__builtin_expect(kb > plain_to, 0)) exact(0, kb);
     }
     for (int t = t0; t <= t1; ++t) {
         const int tn = min(t + 1, t1);
         fetch(min(t + 2, t1), after(after(kslot)), vslot);
         hide(0);
-        region(std::integral_constant<int, 0>{}, byte_of(kbytes, t, 1));
-        settle(0);
+        const int kb1 = byte_of(kbytes, t, 1);
+        region(std::integral_constant<int, 0>{}, kb1);
+        settle(0, kb1);
         {
             // values go on to this tile's first half, keys to the next tile's
             to_half(t == t0 ? 0 : next_half(rslot, 1));
@@ -817,8 +848,9 @@ __global__ __launch_bounds__(256 * KG, WAVES) void kvb_attn_tiles_kernel(const u
         }
         hide(1);
         vis_next = look(tn, raw, seen_next);
-        region(std::integral_constant<int, 1>{}, byte_of(kbytes, tn, 0));
-        settle(1);
+        const int kb0 = byte_of(kbytes, tn, 0);
+        region(std::integral_constant<int, 1>{}, kb0);
+        settle(1, kb0);
         to_half(next_half(rslot, 1));
         cslot = next_half(cslot, 2);
         seen_next = seen_later;

@@ -373,8 +373,8 @@ fvar_status fvar_rope_init(fvar_rope *r);
 /* Turns queries and keys by their positions, pos: device int32 [B][n][axes] (any values, also negative ones).
  * q: row i of sample b starts at element (b*n + i)*ld_q and holds [heads][Dh]; k likewise with ld_k and [kv_heads][Dh].  Either may
  * be NULL.  The results go to q_out and k_out in the same way with their own ld_*_out, whole rows of a head, the elements from dim
- * on as they are; an output is the input itself (with the same ld) or shares no memory with an input.  ld = 0 stands for a
- * packed row; a multiple of 8 for bf16 (of 4 for fp32).  kv_heads divides the context's heads.  Angles are exact to 2^-50 of a turn per position,
+ * on as they are; an output is the input itself (with the same ld) or shares no memory with an input, pos or the other
+ * output, which is refused.  ld = 0 stands for a packed row; a multiple of 8 for bf16 (of 4 for fp32).  kv_heads divides the context's heads.  Angles are exact to 2^-50 of a turn per position,
  * sines and cosines and the products are fp32.  B * n <= 2^24.  No workspace. */
 fvar_status fvar_rope_apply(fvar_ctx *ctx, fvar_stream stream, const fvar_rope *r, const int32_t *pos, int32_t B, int32_t n,
                             int32_t kv_heads, const void *q, int32_t ld_q, const void *k, int32_t ld_k, void *q_out, int32_t ld_q_out,

@@ -1,5 +1,6 @@
 // C ABI of the library: argument validation, workspace carving and the launch sequence of each
 // entry point.  Host code only; every arithmetic step runs in the kernels of this directory.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -38,6 +39,28 @@ struct fvar_ctx {
     std::vector<Rec> recs;
     std::vector<hipEvent_t> pool;
 };
+
+namespace fvar {
+
+// Whether two sets of rows have a byte in common: `rows` of them, `width` bytes of every `ld`, from a and b on.
+bool rows_share_memory(size_t a, long width_a, long ld_a, long rows_a, size_t b, long width_b, long ld_b, long rows_b)
+{
+    if (a >= b + (size_t)((rows_b - 1) * ld_b + width_b) || b >= a + (size_t)((rows_a - 1) * ld_a + width_a)) return false;
+    const long d = (long)(b - a);                            // row i of a is [i ld_a, + width_a), row j of b [d + j ld_b, + width_b)
+    auto down = [](long x, long y) { return x >= 0 ? x / y : -((-x + y - 1) / y); };
+    if (ld_a == ld_b) {
+        // their distance is d + k ld, k = j - i, of which the largest below width_a counts, and the smaller ones that still reach the row
+        const long last = std::min(down(width_a - 1 - d, ld_a), rows_b - 1);
+        return last > -rows_a && d + last * ld_a > -width_b;
+    }
+    for (long i = std::max(0l, down(d - width_a, ld_a)); i < rows_a && i * ld_a < d + (rows_b - 1) * ld_b + width_b; ++i) {
+        const long j = std::min(down(i * ld_a + width_a - 1 - d, ld_b), rows_b - 1);
+        if (j >= 0 && d + j * ld_b + width_b > i * ld_a) return true;
+    }
+    return false;
+}
+
+}  // namespace fvar
 
 namespace {
 
@@ -824,6 +847,17 @@ fvar_status fvar_rope_apply(fvar_ctx *c, fvar_stream stream, const fvar_rope *r,
     for (const fvar::RopeRows &x : rows)
         if (x.in && (x.ld_in < 0 || x.ld_out < 0 || (x.in == x.out && x.ld_in != x.ld_out)))
             return fail(c, FVAR_ERR_INVALID_ARG, "%s: a row pitch is shorter than a row, no multiple of 16 bytes, or in place not the same", who);
+    const long es = (long)esize(c), count = (long)B * n;
+    auto meet = [&](const void *out, const fvar::RopeRows &x, const void *other, long width, long ld, long n_other) {
+        return out && other && fvar::rows_share_memory((size_t)out, x.heads * c->cfg.head_dim * es, x.ld_out * es, count, (size_t)other, width, ld, n_other);
+    };
+    for (int i = 0; i < 2; ++i) {
+        const fvar::RopeRows &x = rows[i], &y = rows[1 - i];
+        const long wx = x.heads * c->cfg.head_dim * es, wy = y.heads * c->cfg.head_dim * es, wp = count * r->axes * (long)sizeof(int32_t);
+        if ((x.out != x.in && meet(x.out, x, x.in, wx, x.ld_in * es, count)) || meet(x.out, x, y.in, wy, y.ld_in * es, count) ||
+            meet(x.out, x, y.out, wy, y.ld_out * es, count) || meet(x.out, x, pos, wp, wp, 1))
+            return fail(c, FVAR_ERR_INVALID_ARG, "%s: an output shares memory with another tensor", who);
+    }
     hipStream_t st = static_cast<hipStream_t>(stream);
     timed(c, st, "rope", [&] { fvar::launch_rope(dtype(c), rope_table(r), rows[0], rows[1], pos, B * n, c->cfg.head_dim, st); });
     return launch_status(c, who);

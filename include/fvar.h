@@ -168,8 +168,8 @@ typedef struct {
     double factor;         /* s >= 1, how much longer than trained.  LINEAR: f_i / s.  NTK: base * s^(P / (P - 2)), P > 2. */
     double original;       /* YARN: positions trained on.  r_i = original * f_i / (2 pi), g_i = clamp((r_i - low) / (high - low), 0, 1): */
     double low, high;      /*       f_i * (g_i + (1 - g_i) / s); low < high */
-    double magnitude;      /* factor of the results (YARN: 0.1 ln s + 1 is usual); 0 stands for 1 */
-    double turns[64];      /* f_i / (2 pi), i < P / 2 */
+    double magnitude;      /* factor of the results (YARN: 0.1 ln s + 1 is usual), a normal number of fp32; 0 stands for 1 */
+    double turns[64];      /* f_i / (2 pi), i < P / 2; finite */
 } fvar_rope;
 
 typedef struct fvar_ctx fvar_ctx;

@@ -6,6 +6,7 @@ when the library has not been built (python -m paper_2512_16483_amd.build)."""
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional, Sequence
 
@@ -553,6 +554,8 @@ class Rope:
         if turns is not None:
             if len(turns) != dim // axes // 2:
                 raise ValueError(f"{dim // axes // 2} frequencies are wanted, got {len(turns)}")
+            if not all(math.isfinite(t) for t in turns):
+                raise ValueError("frequencies have to be finite")
             self._c.turns[:len(turns)] = list(turns)
         self._ref = C.byref(self._c)
 

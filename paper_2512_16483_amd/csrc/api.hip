@@ -1,6 +1,7 @@
 // C ABI of the library: argument validation, workspace carving and the launch sequence of each
 // entry point.  Host code only; every arithmetic step runs in the kernels of this directory.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -292,6 +293,9 @@ size_t kvb_attention_ws(const fvar_ctx *c, const fvar_kvb *kv, int B, int n, boo
                                                        weights) * sizeof(float));
 }
 
+// 0, or a normal number of fp32
+bool rope_magnitude(double m) { return m == 0.0 || (std::fabs(m) >= FLT_MIN && std::fabs(m) <= FLT_MAX); }
+
 // Settings and positions that rows can be turned by.
 fvar_status check_rope(fvar_ctx *c, const fvar_rope *r, const int32_t *pos, const char *who)
 {
@@ -299,10 +303,13 @@ fvar_status check_rope(fvar_ctx *c, const fvar_rope *r, const int32_t *pos, cons
     if (r->axes < 1 || r->axes > 2 || r->dim < 1 || r->dim > c->cfg.head_dim || r->dim % (16 * r->axes))
         return fail(c, FVAR_ERR_INVALID_ARG, "%s: dim=%d with axes=%d: a multiple of 16*axes up to head_dim is wanted", who, r->dim, r->axes);
     if (reinterpret_cast<uintptr_t>(pos) & 3) return fail(c, FVAR_ERR_INVALID_ARG, "%s: pos is not 4-byte aligned", who);
-    bool some = false;
-    for (int i = 0; i < r->dim / r->axes / 2; ++i) some |= r->turns[i] != 0.0;
-    if (!some || !std::isfinite(r->magnitude))
-        return fail(c, FVAR_ERR_INVALID_ARG, "%s: rope has no turns (see fvar_rope_init), or magnitude=%g", who, r->magnitude);
+    bool some = false, finite = true;
+    for (int i = 0; i < r->dim / r->axes / 2; ++i) {
+        some |= r->turns[i] != 0.0;
+        finite &= std::isfinite(r->turns[i]);
+    }
+    if (!some || !finite || !rope_magnitude(r->magnitude))
+        return fail(c, FVAR_ERR_INVALID_ARG, "%s: rope has no turns (see fvar_rope_init), some that are not finite, or magnitude=%g", who, r->magnitude);
     return FVAR_OK;
 }
 
@@ -802,7 +809,7 @@ fvar_status fvar_rope_init(fvar_rope *r)
 {
     if (!r || r->axes < 1 || r->axes > 2 || r->dim < 1 || r->dim > 128 || r->dim % (16 * r->axes)) return FVAR_ERR_INVALID_ARG;
     if (r->scaling < FVAR_ROPE_NONE || r->scaling > FVAR_ROPE_YARN || !(r->base > 1.0) || !std::isfinite(r->base) ||
-        !std::isfinite(r->magnitude))
+        !rope_magnitude(r->magnitude))
         return FVAR_ERR_INVALID_ARG;
     if (r->scaling != FVAR_ROPE_NONE && (!(r->factor >= 1.0) || !std::isfinite(r->factor))) return FVAR_ERR_INVALID_ARG;
     if (r->scaling == FVAR_ROPE_YARN && (!(r->original > 0.0) || !(r->low < r->high) || !std::isfinite(r->original) ||

@@ -1,6 +1,7 @@
 """Rows that fvar_rope_apply can turn, and those that share memory, without a GPU: refusals come before anything is launched."""
 import ctypes as C
 import itertools
+import math
 import random
 
 import pytest
@@ -59,3 +60,27 @@ def test_rows_share_memory_where_bytes_do(seed):
         a, b = 1000, 1000 + rng.randint(-40, 40)
         bytes_of = lambda at, w, ld, rows: set(itertools.chain.from_iterable(range(at + i * ld, at + i * ld + w) for i in range(rows)))
         assert share(a, wa, la, n, b, wb, lb, m) == bool(bytes_of(a, wa, la, n) & bytes_of(b, wb, lb, m)), (a, wa, la, n, b, wb, lb, m)
+
+
+@pytest.mark.parametrize("name,value", [("turns", math.nan), ("turns", math.inf), ("turns", -math.inf), ("magnitude", 1e39), ("magnitude", -1e300),
+                                        ("magnitude", 1e-46)])
+@pytest.mark.parametrize("pair", [0, 13, 31])
+def test_a_table_that_is_no_number_is_refused(name, value, pair):
+    """Frequencies that a program wrote itself; a magnitude that fp32 does not hold, or holds as 0."""
+    ctx, lib, r = fv.Context(hidden=256, heads=4, head_dim=64, ffn_hidden=256), fv.load_library(), _rope()
+    if name == "turns":
+        r.turns[pair] = value
+        with pytest.raises(ValueError):
+            fv.Rope(dim=64, turns=[value if i == pair else 0.1 for i in range(32)])
+    else:
+        r.magnitude = value
+        with pytest.raises(fv.FvarError):
+            fv.Rope(dim=64, magnitude=value)
+    assert lib.fvar_rope_apply(ctx.handle, None, C.byref(r), 0x10, 1, 4, 4, BASE, 0, None, 0, BASE, 0, None, 0) == INV
+    kv = fv._KVB(0x100000, 0x200000, 0x300000, 0x400000, None, None, 4, 100, 50)
+    w = C.byref(fv._Weights(*[0x1000] * 12))
+    assert lib.fvar_block_forward_dense_kvb(ctx.handle, None, w, 0x1000, 1, 1, C.byref(kv), C.byref(r), 0x10, None, 0, 0x1000, 0x1000, 1 << 40) == INV
+    r = _rope(dim=32)
+    r.turns[16] = math.nan                                    # behind the table's pairs: not read
+    assert lib.fvar_rope_apply(ctx.handle, None, C.byref(r), 0x10, 1, 4, 4, BASE, 0, None, 0, BASE + 512, 0, None, 0) == INV   # (refused for its rows)
+    assert b"shares memory" in lib.fvar_last_error(ctx.handle)

@@ -567,6 +567,8 @@ class Rope:
 def fvar_rope_apply(ctx: Context, rope: Rope, pos, B: int, n: int, q=None, k=None, q_out=None, k_out=None, stream=None) -> None:
     """q: [B, n, heads, head_dim], k: [B, n, kv_heads, head_dim]; either may be None.  Rows may lie apart, as the parts of a fused
     projection's output do; without an output the rows are turned in place."""
+    if B < 1 or n < 1:
+        raise ValueError(f"B >= 1 and n >= 1 are wanted, got {B} and {n}")
     kind, kv_heads = _kind(ctx.dtype), ctx.heads if k is None else k.numel() // (B * n * ctx.head_dim)
     (qp, ldq), (kp, ldk) = _rows(q, kind, B, n, ctx.hidden), _rows(k, kind, B, n, kv_heads * ctx.head_dim)
     (qo, ldqo) = (qp, ldq) if q_out is None else _rows(q_out, kind, B, n, ctx.hidden)

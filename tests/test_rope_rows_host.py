@@ -5,8 +5,10 @@ import math
 import random
 
 import pytest
+import torch
 
 import paper_2512_16483_amd as fv
+from test_kvb_host import _Fake
 
 INV = fv.FVAR_ERR_INVALID_ARG
 
@@ -84,3 +86,12 @@ def test_a_table_that_is_no_number_is_refused(name, value, pair):
     r.turns[16] = math.nan                                    # behind the table's pairs: not read
     assert lib.fvar_rope_apply(ctx.handle, None, C.byref(r), 0x10, 1, 4, 4, BASE, 0, None, 0, BASE + 512, 0, None, 0) == INV   # (refused for its rows)
     assert b"shares memory" in lib.fvar_last_error(ctx.handle)
+
+
+@pytest.mark.parametrize("B,n", [(0, 4), (2, 0), (-1, 4), (2, -3), (0, 0)])
+def test_the_binding_refuses_no_rows(B, n):
+    bf16, i32 = (lambda *s: _Fake(*s, dtype=torch.bfloat16)), lambda *s: _Fake(*s, dtype=torch.int32)
+    ctx, r = fv.Context(hidden=256, heads=4, head_dim=64, ffn_hidden=256), fv.Rope(dim=64)
+    for kw in (dict(q=bf16(2, 4, 4, 64)), dict(k=bf16(2, 4, 4, 64)), dict(q=bf16(2, 4, 4, 64), k=bf16(2, 4, 2, 64))):
+        with pytest.raises(ValueError):
+            fv.fvar_rope_apply(ctx, r, i32(2, 4), B, n, stream=0, **kw)

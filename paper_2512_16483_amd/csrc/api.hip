@@ -320,7 +320,7 @@ fvar::RopeTable rope_table(const fvar_rope *r)
     t.axes = r->axes;
     t.interleaved = r->interleaved != 0;
     t.magnitude = r->magnitude == 0.0 ? 1.f : (float)r->magnitude;
-    std::memcpy(t.turns, r->turns, sizeof(t.turns));
+    for (int i = 0; i < 64; ++i) t.turns[i] = r->turns[i] - std::rint(r->turns[i]);   // exact; a position is a whole number, and so are its whole turns
     return t;
 }
 

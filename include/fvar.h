@@ -428,7 +428,8 @@ fvar_status fvar_block_forward_pruned_kvb(fvar_ctx *ctx, fvar_stream stream, con
  * to_weights: [B][kv_heads][to->capacity], receives the weights of the rows kept and 0 behind them; it may be `weights` itself
  * where the caches are one, and shares no memory with it otherwise.  to_lens: int32 [B], receives the rows that each sample then
  * holds, the same for all its heads (NULL allowed; may be from->lens).  idx: int32 [B][kv_heads][keep], receives the rows' former
- * places, -1 behind them (NULL allowed).  No row of `to` is hidden: the mask ends here.
+ * places, -1 behind them (NULL allowed).  No row of `to` is hidden then: where the caches are one, the program takes the mask out of it, as it
+ * sets len or lens (a mask left there would hide the rows that have moved to its places).
  * 1 <= keep, 0 <= recent <= keep.  ws: at least fvar_kvb_evict_workspace_bytes(ctx,from,B,keep), whether idx is given or not. */
 size_t fvar_kvb_evict_workspace_bytes(const fvar_ctx *ctx, const fvar_kvb *from, int32_t B, int32_t keep);
 fvar_status fvar_kvb_evict(fvar_ctx *ctx, fvar_stream stream, const fvar_kvb *from, const float *weights, int32_t B, int32_t keep,

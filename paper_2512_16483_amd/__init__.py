@@ -643,6 +643,8 @@ def fvar_kvb_evict_workspace_bytes(ctx: Context, kv: KVB, B: int, keep: int) -> 
 
 def fvar_kvb_evict(ctx: Context, kv: KVB, weights, B: int, keep: int, recent: int, to: KVB, to_weights, to_lens=None, idx=None, ws=None,
                    stream=None) -> None:
+    """to is kv itself, or shares no memory with it.  The lengths and the mask stay the caller's: afterwards to.lens is to_lens (or to.len `keep`, where every
+    sample held as many rows that are not hidden), and to.mask None."""
     ctx.check(ctx.lib.fvar_kvb_evict(ctx.handle, _stream(stream), kv._for(ctx, B), _row_weights(weights, kv, B), B, keep, recent,
                                      to._for(ctx, B), _row_weights(to_weights, to, B), _packed(to_lens, _kind("i32"), B, 1, 1),
                                      _packed(idx, _kind("i32"), B, kv.kv_heads * keep, 1), _ptr(ws), _nbytes(ws)))

@@ -17,7 +17,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, Rope
     constexpr int FLY = T == 1 ? 1 : 2, ITEMS = DH / 16, SLOTS = 256 / ITEMS / T, PER = Elem<E>::kPerChunk, HALF = 8 / PER;   // HALF: chunks of eight elements
     __shared__ float2 turn[T][DH / 2];
     const int tid = threadIdx.x, pairs = r.dim / 2, row0 = blockIdx.x * T;
-    const int item = tid % ITEMS, t = tid / ITEMS % T, slot = tid / ITEMS / T + blockIdx.y * SLOTS, step = gridDim.y * SLOTS;
+    const int item = tid % ITEMS, t = tid / ITEMS % T, slot = tid / ITEMS / T;
     const size_t row = min(row0 + t, rows - 1);
     const int heads = row0 + t < rows ? q.heads + k.heads : 0;
     const bool turned = item * 16 < r.dim;
@@ -33,12 +33,12 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, Rope
     auto fetch = [&](int h0) __attribute__((always_inline)) {
 #pragma unroll
         for (int f = 0; f < FLY; ++f) {
-            const int h = min(h0 + f * step, q.heads + k.heads - 1);
+            const int h = min(h0 + f * SLOTS, q.heads + k.heads - 1);
             const bool is_q = h < q.heads;
             const int head = is_q ? h : h - q.heads;
             const E *src = (const E *)(is_q ? q.in : k.in) + row * (size_t)(is_q ? q.ld_in : k.ld_in) + head * DH;
             dst[f] = (E *)(is_q ? q.out : k.out) + row * (size_t)(is_q ? q.ld_out : k.ld_out) + head * DH;
-            if (h0 + f * step >= heads || (!turned && src == dst[f])) dst[f] = nullptr;
+            if (h0 + f * SLOTS >= heads || (!turned && src == dst[f])) dst[f] = nullptr;
 #pragma unroll
             for (int i = 0; i < HALF; ++i) {
                 raw[f][i] = *reinterpret_cast<const uint4 *>(src + lo + i * PER);
@@ -68,7 +68,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTable r, RopeRows q, Rope
 #pragma unroll
         for (int i = 0; i < 8; ++i) { c[i] = turn[t][item * 8 + i].x; s[i] = turn[t][item * 8 + i].y; }
     }
-    for (int h0 = slot; h0 < heads; h0 += FLY * step) {
+#pragma unroll 1                                              // (unrolled, 6400 rows of 64 heads take 40.9 us instead of 40.3)
+    for (int h0 = slot; h0 < heads; h0 += FLY * SLOTS) {
         if (h0 != slot) fetch(h0);
 #pragma unroll
         for (int f = 0; f < FLY; ++f) {

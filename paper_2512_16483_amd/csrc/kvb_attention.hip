@@ -21,8 +21,9 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 
 // Values as fp16 operands: a value goes in as value * 2^(kTop - E), E the largest exponent of a tile seen so far and kRoom more (sums are
 // rescaled when a tile's exceeds E, which is seldom).  A value is at most 448, and fp16 numbers reach down to 2^-24, so tiles are exact
-// down to 2^-19 of the largest one's size, and 0 below 2^-37.  Weights go in as p * 2^kShift, with a reference that may be up to 2^kLag below the true
-// maximum.  Next to bf16 operands the weights keep 11 bits, so that the output's own rounding is the only one of note.
+// down to 2^-19 of the largest one's size, and single values down to 2^-33 of the largest value; they lose bits from there on, and are 0
+// below 2^-37.  Weights go in as p * 2^kShift, with a reference that may be up to 2^kLag below the true maximum.  Next to bf16 operands the
+// weights keep 11 bits, so that the output's own rounding is the only one of note.
 // fp32 takes values as they are in bf16, exact, up to tiles of 2^64, and at 2^64 over E from there on: a sum of weights up to 2^7 each stays finite.
 constexpr int kTop = 6, kRoom = 2, kLarge = 64;
 constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
@@ -78,8 +79,8 @@ __device__ __forceinline__ void three_pieces(const float *x, bf16x8_t *out)
 }
 
 // Queries in two E4M3 numbers per element, with a power of two per row, 2^e, and 2^(e-4) for what the first leaves: the first leaves at most half
-// a step of its binade, eight steps of bf16's eight bits, which the second holds whole.  (Elements below 2^-15 of their row's largest are held to
-// 2^-23 of it, as fp32 sums hold them.)  top: of the row's bits, sign taken off; from it the scale bytes of both pieces, in byte 0 and 1.
+// a step of its binade, eight steps of bf16's eight bits, which the second holds whole.  (Elements below 2^-13 of their row's largest are held to
+// 2^-21 of it.)  top: of the row's bits, sign taken off; from it the scale bytes of both pieces, in byte 0 and 1.
 // A row with an element that is not finite becomes NaN, and so do its scores.  bf16 goes up to 255 * 2^120, past the cache's largest power: from 464 * 2^119
 // on a row's is 2^120, whose largest first piece is 240 * 2^120 (256 would not be a finite fp32 number); 15 * 2^120 and less is left, 240 * 2^116.
 __device__ __forceinline__ uint32_t top_of_eight(uint4 w, uint32_t top)

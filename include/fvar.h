@@ -394,7 +394,7 @@ fvar_status fvar_kvb_read(fvar_ctx *ctx, fvar_stream stream, const fvar_kvb *kv,
                           void *k, void *v);
 
 /* Attention over the 8-bit cache, as fvar_kvq_attention over one of 4 bits.  Scores and sums are fp32, queries count with all their
- * bits (bf16, more than 16 query rows of a kv head: where no product of an element of a query and of a key can pass 8 in its score, each counts to 2^-13 of
+ * bits (bf16, more than 16 query rows of a kv head: where no product of an element of a query and of a key can pass 11 in its score, each counts to 2^-13 of
  * the largest of its eight neighbours', of normal numbers 2^-18 rms of the sizes' sum; elements of a query below 2^-13 of its largest may count to
  * 2^-21 of that, and to 2^-126).  Beside far larger values small ones count to 2^-37 (fp32: 2^-180) of the largest value of the blocks with a visible row, of the
  * sample and kv head; what is less may count as 0.

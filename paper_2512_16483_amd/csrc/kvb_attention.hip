@@ -27,7 +27,7 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 // fp32 takes values as they are in bf16, exact, up to tiles of 2^64, and at 2^64 over E from there on: a sum of weights up to 2^7 each stays finite.
 constexpr int kTop = 6, kRoom = 2, kLarge = 64;
 constexpr float kShift = 8.f, kLag = 7.f, kMost = 32768.f;
-constexpr float kPlain = 11.5f;                              // largest product of an element of a query and of a key: 8 in a score, in units of log2
+constexpr float kPlain = 16.f;                               // largest product of an element of a query and of a key, in units of log2: 11 in a score
 
 __device__ __forceinline__ uint4 half_eight(uint32_t a, uint32_t b, float s)
 {
@@ -418,9 +418,11 @@ __device__ __forceinline__ void tile_dma_b128(const void *base, uint32_t byte_of
 //     of bf16 would, without a conversion of K.  It adds eight products of neighbouring elements at a time, and drops of each what lies below 2^-13
 //     of the largest: of normal numbers, 2^-15 of the sum of the products' sizes at most, 2^-18 rms, which at sums of 10 is 2^-11 of a weight at most (fp16 holds
 //     one to 2^-12); where one channel is far larger than the others, up to 2^-10.  So the scores of keys whose products with the wavefront's queries
-//     might pass 8, by their block's power and the queries' largest element, are made once more by bf16 products, which are added in fp32: what a
-//     product loses is 2^-10 at most.  4 x 1600 x 12121, 32 heads, one channel 20 times the others', all keys that way: 2100 us (1120 without, and
-//     outputs of such keys off by 4.6e-3 of their 2-norm); where none are, 1171 (1167).
+//     might pass 11, by their block's power and the queries' largest element, are made once more by bf16 products, which are added in fp32: what a
+//     product loses is 2^-9.5 at most.  (Outputs are off by their rounding to bf16 then, 1.67e-3 of their 2-norm; by 1.77e-3 with one channel whose products are
+//     11, 2.9e-3 with 16 such.)  4 x 1600 x 12121, 32 heads, one channel 20 times the others', all keys that way: 2100 us (1120 without, and outputs
+//     of such keys off by 4.6e-3); where none are, 1171 (1167).  With a limit of 8 a 50th of the wavefronts over normal numbers found some (8 x 231 x 871, 30
+//     heads of 64, 25.5 to 31.7 us; 26.1 with 11).
 //   O^T = V^T P^T by the 32x32x16 fp16 MFMA: the workgroup converts a tile of values once, into LDS.
 // In the 32x32 accumulator layout a lane owns a query column, so the sum is lane-local, and P is in the order in which the second
 // product takes it, as in attention.hip.
